@@ -341,6 +341,118 @@ isoloco_status isoloco_get_timing(isoloco_plan_t plan, isoloco_timing* out);
 
 isoloco_status isoloco_plan_destroy(isoloco_plan_t plan);
 
+/* ---------------------------------------------------------------------------
+ * Operators of the workers' inner training step
+ *
+ * What produces the replicas that the outer step merges: the operators of a
+ * training step around its matrix products.  They share the conventions above:
+ * the caller owns every buffer, a call only enqueues kernel launches on the
+ * caller's stream (it may be captured in a HIP graph), a call that fails
+ * validation enqueues nothing, and no state is kept between calls.  Matrices
+ * are row-major with unit stride along a row; ld_* is the distance of two rows
+ * in elements (at least the row's length).  Device pointers need the alignment
+ * of their elements only; 16-byte aligned rows are faster.  Outputs must not
+ * overlap inputs, the workspace or each other unless a function says so.
+ * Workspaces are 256-byte aligned device memory whose contents need not be
+ * set and do not outlive the call; one may serve any number of calls that do
+ * not overlap in time.  dtypes are isoloco_dtype, sums are held in 32 bits or
+ * more and a result is rounded to its type once.  Results do not depend on
+ * timing: the same call gives the same bits.
+ * ------------------------------------------------------------------------- */
+
+typedef enum { ISOLOCO_I32 = 0, ISOLOCO_I64 = 1 } isoloco_index_type;
+
+/* Gradient clipping over many tensors.
+ *
+ *   norm = sqrt(sum over all tensors and elements of g^2)
+ *   coef = max_norm / norm if max_norm < norm < infinity, else 1;  dst = coef * g
+ *
+ * src, dst, counts, dtypes: HOST arrays of n_tensors entries (read before the
+ * call returns): each tensor's device pointer, its result's, its contiguous
+ * elements (0 is allowed) and its type.  dst[i] may be src[i] (in place;
+ * nothing is then written where coef is 1); a tensor's result must not overlap
+ * another tensor.  dst = NULL: the norm only.  norm: two device floats, which
+ * receive norm and coef.  A norm that is infinite or NaN leaves the gradients
+ * as they are, and tells the caller so.  Squares are summed in 64 bits.
+ * max_norm >= 0 (infinity: never clip). */
+isoloco_status isoloco_clip_workspace_size(int32_t n_tensors, size_t* bytes);
+isoloco_status isoloco_clip_grads(const void* const* src, void* const* dst, const int64_t* counts,
+                                  const int32_t* dtypes, int32_t n_tensors, float max_norm, float* norm,
+                                  void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* out[t] = scale * table[ids[t]] for n tokens; table: vocab x dim, out: n x dim.
+ * An id outside [0, vocab) holds no token: a row of zeros. */
+isoloco_status isoloco_embedding(const void* table, int64_t ld_table, int32_t dtype, int64_t vocab, int64_t dim,
+                                 const void* ids, int32_t id_type, int64_t n, float scale, void* out, int64_t ld_out,
+                                 int32_t out_dtype, void* hip_stream);
+
+/* dtable[v] = scale * sum over the t with ids[t] = v of dout[t], in 32 bits, for
+ * every v (rows without tokens: zeros).  accumulate != 0: added to what dtable
+ * holds (a tied head's gradient, an earlier batch's).  Tokens are grouped by id
+ * first and a row's are added in their order: no atomics. */
+isoloco_status isoloco_embedding_backward_workspace_size(int64_t n, int64_t vocab, int64_t dim, size_t* bytes);
+isoloco_status isoloco_embedding_backward(const void* ids, int32_t id_type, int64_t n, const void* dout,
+                                          int64_t ld_dout, int32_t dtype, int64_t vocab, int64_t dim, float scale,
+                                          int32_t accumulate, void* dtable, int64_t ld_dtable, int32_t dtable_dtype,
+                                          void* workspace, size_t workspace_bytes, void* hip_stream);
+
+#define ISOLOCO_MAX_TOP 32
+
+/* Log probabilities of given tokens.  With z = scale * logits of a row (scale > 0):
+ *
+ *   lse = log sum_j e^z_j,  logprob = z_target - lse,  entropy = -sum_j p_j log p_j
+ *   top_logprob, top_index: the top_k largest log probabilities (rows x top_k, in
+ *   falling order, of equal logits the lower index first; NaN ranks above all)
+ *
+ * top_k <= min(ISOLOCO_MAX_TOP, vocab).  Any of logprob (with targets), entropy
+ * and lse may be NULL.  A target outside [0, vocab) is ignored: logprob 0.
+ * Logits of -infinity are masked (p = 0); a row of nothing else has lse =
+ * logprob = -infinity and entropy 0.  A NaN or +infinity among a row's logits
+ * makes its results NaN. */
+isoloco_status isoloco_token_logprobs_workspace_size(int64_t rows, int64_t vocab, int32_t top_k, size_t* bytes);
+isoloco_status isoloco_token_logprobs(const void* logits, int64_t ld_logits, int32_t dtype, int64_t rows,
+                                      int64_t vocab, const void* targets, int32_t target_type, float scale,
+                                      int32_t top_k, float* logprob, float* entropy, float* lse, float* top_logprob,
+                                      int64_t* top_index, void* workspace, size_t workspace_bytes,
+                                      void* hip_stream);
+
+/* The gradient of the above in the logits, from the lse (and entropy) it gave:
+ *
+ *   dlogits_j = scale * (dlogprob (1[j = target] - p_j) - dentropy p_j (log p_j + entropy))
+ *
+ * dlogprob goes with targets (rows whose target is ignored take none), dentropy
+ * with entropy; either pair may be NULL.  dlogits has the logits' type and may
+ * be the logits themselves (same pointer and ld).  A row whose dlogprob and
+ * dentropy are zero, or whose logits are all -infinity, has a zero gradient. */
+isoloco_status isoloco_token_logprobs_backward(const void* logits, int64_t ld_logits, int32_t dtype, int64_t rows,
+                                               int64_t vocab, const void* targets, int32_t target_type, float scale,
+                                               const float* lse, const float* entropy, const float* dlogprob,
+                                               const float* dentropy, void* dlogits, int64_t ld_dlogits,
+                                               void* hip_stream);
+
+typedef enum {
+  ISOLOCO_ACT_SILU = 0, /* g / (1 + e^-g)                   */
+  ISOLOCO_ACT_GELU = 1  /* g Phi(g), the exact normal CDF   */
+} isoloco_activation;
+
+/* out = act(x w_gate^T) * (x w_up^T); x: tokens x dim, w_gate and w_up: hidden x
+ * dim (both ld_w apart), out: tokens x hidden; one dtype. */
+isoloco_status isoloco_gated_ffn_workspace_size(int64_t tokens, int64_t dim, int64_t hidden, int32_t dtype,
+                                                int32_t backward, size_t* bytes);
+isoloco_status isoloco_gated_ffn(const void* x, int64_t ld_x, const void* w_gate, const void* w_up, int64_t ld_w,
+                                 int32_t dtype, int64_t tokens, int64_t dim, int64_t hidden, int32_t act, void* out,
+                                 int64_t ld_out, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Its gradients from dout (tokens x hidden).  dx, or dw_gate with dw_up, may be
+ * NULL.  The projections are formed again (nothing is kept from the forward
+ * call); in bfloat16 the gradients of their two results, which the three
+ * products read, are rounded to bfloat16 once. */
+isoloco_status isoloco_gated_ffn_backward(const void* x, int64_t ld_x, const void* w_gate, const void* w_up,
+                                          int64_t ld_w, int32_t dtype, int64_t tokens, int64_t dim, int64_t hidden,
+                                          int32_t act, const void* dout, int64_t ld_dout, void* dx, int64_t ld_dx,
+                                          void* dw_gate, void* dw_up, int64_t ld_dw, void* workspace,
+                                          size_t workspace_bytes, void* hip_stream);
+
 const char* isoloco_status_string(isoloco_status s);
 
 /* Message of the last failed call on this thread ("" if none). */

@@ -5,6 +5,10 @@ Thin ctypes binding of ``libisoloco.so`` (C ABI declared in
 order of the C function it marshals; ``IsoLoCoPlan`` bundles them with a
 torch-allocated workspace.  All arithmetic runs in the HIP kernels of the
 library: if the library is missing, importing the binding raises.
+
+The operators of the workers' inner training step (clipping, embedding, token
+log probabilities, gated feed-forward block) are in ``operators.py`` and are
+reached from here under the same names.
 """
 import ctypes
 import os
@@ -18,6 +22,13 @@ __all__ = [
     "isoloco_timing", "isoloco_aggregate_static", "ISOLOCO_STATIC_WORKSPACE_BYTES",
     "isoloco_factored_steps", "isoloco_get_products", "isoloco_products",
     "IsoLoCoPlan", "LIB_PATH", "EXPORTED_SYMBOLS",
+    "clip_grads", "embedding", "embedding_backward", "token_logprobs", "token_logprobs_backward", "TokenLogProbs",
+    "gated_ffn", "gated_ffn_backward",
+    "isoloco_clip_workspace_size", "isoloco_clip_grads", "isoloco_embedding",
+    "isoloco_embedding_backward_workspace_size", "isoloco_embedding_backward",
+    "isoloco_token_logprobs_workspace_size", "isoloco_token_logprobs", "isoloco_token_logprobs_backward",
+    "isoloco_gated_ffn_workspace_size", "isoloco_gated_ffn", "isoloco_gated_ffn_backward",
+    "ISOLOCO_I32", "ISOLOCO_I64", "ISOLOCO_ACT_SILU", "ISOLOCO_ACT_GELU", "ISOLOCO_MAX_TOP",
 ]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libisoloco.so")
@@ -47,12 +58,21 @@ ISOLOCO_FLAG_ZERO = 2
 ISOLOCO_FLAG_NOT_CONVERGED = 4
 ISOLOCO_FLAG_BELOW_RESOLUTION = 8
 ISOLOCO_STATIC_WORKSPACE_BYTES = 128 * 1024 * 1024
+ISOLOCO_I32 = 0
+ISOLOCO_I64 = 1
+ISOLOCO_ACT_SILU = 0
+ISOLOCO_ACT_GELU = 1
+ISOLOCO_MAX_TOP = 32
 
 EXPORTED_SYMBOLS = (
     "isoloco_plan", "isoloco_workspace_size", "isoloco_set_workspace", "isoloco_aggregate",
     "isoloco_get_stats", "isoloco_schedule", "isoloco_schedule_phases", "isoloco_plan_destroy",
     "isoloco_status_string", "isoloco_last_error", "isoloco_enable_timing", "isoloco_get_timing",
     "isoloco_aggregate_static", "isoloco_factored_steps", "isoloco_get_products",
+    "isoloco_clip_workspace_size", "isoloco_clip_grads", "isoloco_embedding",
+    "isoloco_embedding_backward_workspace_size", "isoloco_embedding_backward",
+    "isoloco_token_logprobs_workspace_size", "isoloco_token_logprobs", "isoloco_token_logprobs_backward",
+    "isoloco_gated_ffn_workspace_size", "isoloco_gated_ffn", "isoloco_gated_ffn_backward",
 )
 
 
@@ -102,6 +122,10 @@ if not os.path.exists(LIB_PATH):
 _lib = ctypes.CDLL(LIB_PATH)
 
 _P = ctypes.c_void_p
+_I64 = ctypes.c_int64
+_I32 = ctypes.c_int32
+_F = ctypes.c_float
+_SIZE = ctypes.c_size_t
 _sig = {
     "isoloco_plan": (ctypes.c_int, [ctypes.POINTER(isoloco_tensor), ctypes.c_int32, ctypes.c_int64,
                                     ctypes.c_int32, ctypes.c_int, ctypes.POINTER(isoloco_options),
@@ -122,6 +146,22 @@ _sig = {
     "isoloco_plan_destroy": (ctypes.c_int, [_P]),
     "isoloco_enable_timing": (ctypes.c_int, [_P, ctypes.c_int32]),
     "isoloco_get_timing": (ctypes.c_int, [_P, ctypes.POINTER(isoloco_timing)]),
+    "isoloco_clip_workspace_size": (ctypes.c_int, [_I32, ctypes.POINTER(_SIZE)]),
+    "isoloco_clip_grads": (ctypes.c_int, [_P, _P, _P, _P, _I32, _F, _P, _P, _SIZE, _P]),
+    "isoloco_embedding": (ctypes.c_int, [_P, _I64, _I32, _I64, _I64, _P, _I32, _I64, _F, _P, _I64, _I32, _P]),
+    "isoloco_embedding_backward_workspace_size": (ctypes.c_int, [_I64, _I64, _I64, ctypes.POINTER(_SIZE)]),
+    "isoloco_embedding_backward": (ctypes.c_int, [_P, _I32, _I64, _P, _I64, _I32, _I64, _I64, _F, _I32, _P, _I64,
+                                                  _I32, _P, _SIZE, _P]),
+    "isoloco_token_logprobs_workspace_size": (ctypes.c_int, [_I64, _I64, _I32, ctypes.POINTER(_SIZE)]),
+    "isoloco_token_logprobs": (ctypes.c_int, [_P, _I64, _I32, _I64, _I64, _P, _I32, _F, _I32, _P, _P, _P, _P, _P, _P,
+                                              _SIZE, _P]),
+    "isoloco_token_logprobs_backward": (ctypes.c_int, [_P, _I64, _I32, _I64, _I64, _P, _I32, _F, _P, _P, _P, _P, _P,
+                                                       _I64, _P]),
+    "isoloco_gated_ffn_workspace_size": (ctypes.c_int, [_I64, _I64, _I64, _I32, _I32, ctypes.POINTER(_SIZE)]),
+    "isoloco_gated_ffn": (ctypes.c_int, [_P, _I64, _P, _P, _I64, _I32, _I64, _I64, _I64, _I32, _P, _I64, _P, _SIZE,
+                                         _P]),
+    "isoloco_gated_ffn_backward": (ctypes.c_int, [_P, _I64, _P, _P, _I64, _I32, _I64, _I64, _I64, _I32, _P, _I64, _P,
+                                                  _I64, _P, _P, _I64, _P, _SIZE, _P]),
     "isoloco_status_string": (ctypes.c_char_p, [ctypes.c_int]),
     "isoloco_last_error": (ctypes.c_char_p, []),
 }
@@ -342,3 +382,11 @@ class IsoLoCoPlan:
             self.close()
         except Exception:
             pass
+
+
+from .operators import (  # noqa: E402,F401
+    TokenLogProbs, clip_grads, embedding, embedding_backward, gated_ffn, gated_ffn_backward, isoloco_clip_grads,
+    isoloco_clip_workspace_size, isoloco_embedding, isoloco_embedding_backward,
+    isoloco_embedding_backward_workspace_size, isoloco_gated_ffn, isoloco_gated_ffn_backward,
+    isoloco_gated_ffn_workspace_size, isoloco_token_logprobs, isoloco_token_logprobs_backward,
+    isoloco_token_logprobs_workspace_size, token_logprobs, token_logprobs_backward)

@@ -16,26 +16,15 @@
 #include <vector>
 
 #include "isoloco.h"
+#include "isoloco_error.h"
 #include "isoloco_kernels.h"
 #include "isoloco_types.h"
 
 using namespace isoloco;
 
-static_assert(kFlagNonfinite == ISOLOCO_FLAG_NONFINITE && kFlagZero == ISOLOCO_FLAG_ZERO &&
-                  kFlagNotConverged == ISOLOCO_FLAG_NOT_CONVERGED &&
-                  kFlagBelowResolution == ISOLOCO_FLAG_BELOW_RESOLUTION,
-              "the kernels' flag bits are the ABI's");
+namespace isoloco {
 
-namespace {
-
-thread_local std::string g_last_error;
-
-// Static workspace (isoloco_aggregate_static): the plan whose tables each
-// device's array holds (by uid; 0 = none), and the source of plan uids.
-constexpr int kStaticMaxDevices = 64;
-std::mutex g_static_mu;
-uint64_t g_static_owner[kStaticMaxDevices] = {};
-std::atomic<uint64_t> g_next_uid{1};
+static thread_local std::string g_last_error;
 
 isoloco_status fail(isoloco_status s, const char* fmt, ...) {
   char buf[512];
@@ -50,6 +39,22 @@ isoloco_status fail(isoloco_status s, const char* fmt, ...) {
 isoloco_status hip_fail(hipError_t e, const char* what) {
   return fail(ISOLOCO_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
+
+}  // namespace isoloco
+
+static_assert(kFlagNonfinite == ISOLOCO_FLAG_NONFINITE && kFlagZero == ISOLOCO_FLAG_ZERO &&
+                  kFlagNotConverged == ISOLOCO_FLAG_NOT_CONVERGED &&
+                  kFlagBelowResolution == ISOLOCO_FLAG_BELOW_RESOLUTION,
+              "the kernels' flag bits are the ABI's");
+
+namespace {
+
+// Static workspace (isoloco_aggregate_static): the plan whose tables each
+// device's array holds (by uid; 0 = none), and the source of plan uids.
+constexpr int kStaticMaxDevices = 64;
+std::mutex g_static_mu;
+uint64_t g_static_owner[kStaticMaxDevices] = {};
+std::atomic<uint64_t> g_next_uid{1};
 
 constexpr size_t kAlign = 256;
 
