@@ -15,7 +15,7 @@ ROOT = os.path.dirname(PKG)
 LIB = os.path.join(PKG, "libisoloco.so")
 SOURCES = [os.path.join(PKG, "csrc", f) for f in (
     "isoloco_host.cpp", "isoloco_kernels.hip", "isoloco_products.hip",
-    "isoloco_clip.hip", "isoloco_embedding.hip", "isoloco_logprob.hip", "isoloco_ffn.hip")]
+    "isoloco_clip.hip", "isoloco_embedding.hip", "isoloco_logprob.hip", "isoloco_ffn.hip", "isoloco_ffn_tiles.hip")]
 
 HIPCC_FLAGS = [
     "-O3", "-std=c++17", "-fPIC", "-shared", "--offload-arch=gfx950",

@@ -14,48 +14,12 @@
 
 #include "isoloco_device.h"
 #include "isoloco_error.h"
+#include "isoloco_ffn.h"
 
 namespace isoloco {
 namespace {
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
-
-// act(g) and its derivative
-template <int ACT>
-__device__ __forceinline__ void activate(float g, float& a, float& da) {
-  if constexpr (ACT == ISOLOCO_ACT_SILU) {
-    const float s = 1.f / (1.f + expf(-g));
-    a = g * s;
-    da = s * (1.f + g * (1.f - s));
-  } else {
-    const float cdf = 0.5f * (1.f + erff(g * 0.70710678118654752f));
-    a = g * cdf;
-    da = cdf + g * expf(-0.5f * g * g) * 0.39894228040143268f;
-  }
-}
-
-// An operand of a product: element (row, k) at p + row * rs + k * ks (elements),
-// one of the strides 1.
-struct Operand {
-  const void* p;
-  int64_t rs, ks;
-};
-
-enum Mode {
-  kForward,  // out[0] = act(a b0^T) (a b1^T)
-  kInner,    // out[0] = dh u act'(g), out[1] = dh act(g)
-  kSum,      // out[0] = a[0] b[0]^T + a[1] b[1]^T
-  kPair      // out[z] = a[z] b[0]^T, z = blockIdx.z
-};
-
-struct FfnArgs {
-  Operand a[2], b[2];
-  int64_t m, n, k;
-  void* out[2];
-  int64_t ld_out;
-  const void* dh;
-  int64_t ld_dh;
-};
 
 constexpr int kTile = 64, kStep = 32, kThreads = 256;
 
@@ -154,11 +118,16 @@ struct FfnShape {
   int32_t dtype, act;
 };
 
-// rows of da and du in the workspace start 128-byte aligned
-int64_t inner_ld(int64_t hidden) { return (hidden + 63) / 64 * 64; }
-
 size_t ffn_workspace(const FfnShape& s, bool backward) {
-  return backward ? 2 * (size_t)s.tokens * (size_t)inner_ld(s.hidden) * dtype_bytes(s.dtype) : 0;
+  return backward ? 2 * (size_t)ffn_pad(s.tokens) * (size_t)ffn_pad(s.hidden) * dtype_bytes(s.dtype) : 0;
+}
+
+// the tile kernels load whole 16-byte pieces of rows, at offsets of 32 bits from a tile's first
+bool tile_rows(const void* p, int64_t ld) { return aligned_to(p, 16) && (ld & 7) == 0 && ld <= (1 << 20); }
+
+template <typename T>
+bool on_tiles(const FfnShape& s, const void* x, int64_t ld_x, const void* wg, const void* wu, int64_t ld_w) {
+  return sizeof(T) == 2 && (s.dim & 7) == 0 && tile_rows(x, ld_x) && tile_rows(wg, ld_w) && tile_rows(wu, ld_w);
 }
 
 template <typename T, int ACT>
@@ -173,6 +142,7 @@ hipError_t run_forward(const FfnShape& s, const void* x, int64_t ld_x, const voi
   g.k = s.dim;
   g.out[0] = out;
   g.ld_out = ld_out;
+  if (on_tiles<T>(s, x, ld_x, wg, wu, ld_w)) return launch_ffn_tiles(kForward, ACT, g, st);
   return launch_any<T, kForward, ACT>(g, st);
 }
 
@@ -180,9 +150,10 @@ template <typename T, int ACT>
 hipError_t run_backward(const FfnShape& s, const void* x, int64_t ld_x, const void* wg, const void* wu, int64_t ld_w,
                         const void* dout, int64_t ld_dout, void* dx, int64_t ld_dx, void* dwg, void* dwu,
                         int64_t ld_dw, void* ws, hipStream_t st) {
-  const int64_t ld = inner_ld(s.hidden);
+  const int64_t ld = ffn_pad(s.hidden);
   T* da = static_cast<T*>(ws);
-  T* du = da + s.tokens * ld;
+  T* du = da + ffn_pad(s.tokens) * ld;
+  const bool tiles = on_tiles<T>(s, x, ld_x, wg, wu, ld_w);
   FfnArgs g = {};
   g.a[0] = {x, ld_x, 1};
   g.b[0] = {wg, ld_w, 1};
@@ -195,7 +166,7 @@ hipError_t run_backward(const FfnShape& s, const void* x, int64_t ld_x, const vo
   g.ld_out = ld;
   g.dh = dout;
   g.ld_dh = ld_dout;
-  hipError_t e = launch_any<T, kInner, ACT>(g, st);
+  hipError_t e = tiles ? launch_ffn_tiles(kInner, ACT, g, st) : launch_any<T, kInner, ACT>(g, st);
   if (e == hipSuccess && dx) {
     g = {};
     g.a[0] = {da, ld, 1};
@@ -207,7 +178,7 @@ hipError_t run_backward(const FfnShape& s, const void* x, int64_t ld_x, const vo
     g.k = s.hidden;
     g.out[0] = dx;
     g.ld_out = ld_dx;
-    e = launch_any<T, kSum, ACT>(g, st);
+    e = tiles ? launch_ffn_tiles(kSum, ACT, g, st) : launch_any<T, kSum, ACT>(g, st);
   }
   if (e == hipSuccess && dwg) {
     g = {};
@@ -220,7 +191,7 @@ hipError_t run_backward(const FfnShape& s, const void* x, int64_t ld_x, const vo
     g.out[0] = dwg;
     g.out[1] = dwu;
     g.ld_out = ld_dw;
-    e = launch_any<T, kPair, ACT>(g, st);
+    e = tiles ? launch_ffn_tiles(kPair, ACT, g, st) : launch_any<T, kPair, ACT>(g, st);
   }
   return e;
 }

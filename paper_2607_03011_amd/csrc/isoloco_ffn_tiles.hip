@@ -1,0 +1,401 @@
+// The bfloat16 products of the gated feed-forward block on MFMA tiles (gfx950).
+//
+// One workgroup per output tile; slabs of 64 k values go from memory straight into
+// LDS, one in flight while the one before is multiplied.  The products differ in
+// how their operands lie (k along the rows or across them) and in what becomes of
+// the accumulators, which never leave the registers before that:
+//
+//   kForward, kInner  x rows against rows of both weights, half a tile's columns
+//                     each, so that g and u of one output are in one lane
+//   kSum              da and du rows against columns of the weights, one after the
+//                     other into the same accumulators
+//   kPair             columns of da or du against columns of x
+#include <hip/hip_runtime.h>
+
+#include <stdint.h>
+
+#include "isoloco_device.h"
+#include "isoloco_ffn.h"
+#include "isoloco_lds.h"
+
+namespace isoloco {
+namespace {
+
+// A tile shape: TM x TN outputs per workgroup, WM x WN waves of 32 x 32 blocks.
+template <int TM_, int TN_, int WM_, int WN_>
+struct Shape {
+  static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_;
+  static constexpr int waves = WM * WN, threads = 64 * waves;
+  static constexpr int NA = TM / WM / 32, NB = TN / WN / 32;
+};
+typedef Shape<256, 256, 4, 2> Large;
+typedef Shape<128, 128, 2, 2> Small;
+constexpr int kSlab = kFfnPad;
+
+// ROWS rows of an operand whose k values lie along its rows: 128 bytes of each.
+// The 16-byte pieces of an LDS row are XORed with bits 1-3 of the row, so that a
+// fragment read touches every bank once.
+template <int ROWS, int THREADS>
+struct RowsSlab {
+  static constexpr int kBytes = ROWS * 128, kLoads = ROWS * 8 / THREADS;
+  uint32_t vo[kLoads];
+  __device__ static __forceinline__ int swizzle(int row) { return (row >> 1) & 7; }
+  __device__ static __forceinline__ int piece(int at) { return (at & 7) ^ swizzle(at >> 3); }
+  // rows past the operand's are its last one again: their outputs are not stored
+  __device__ __forceinline__ void init(uint32_t row_bytes, int64_t rows_left) {
+#pragma unroll
+    for (int q = 0; q < kLoads; ++q) {
+      const int at = q * THREADS + threadIdx.x;
+      vo[q] = (uint32_t)min((int64_t)(at >> 3), rows_left - 1) * row_bytes + 16u * piece(at);
+    }
+  }
+  __device__ __forceinline__ void load(uint32_t lds, const void* tile, int64_t slab) const {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const u32x4 r = tile_rsrc((uint64_t)tile + 128u * slab);
+#pragma unroll
+    for (int q = 0; q < kLoads; ++q) load_to_lds(lds + 16u * (q * THREADS + wave * 64), r, vo[q], 0);
+  }
+  // the last slab of an operand whose k values end inside it: zeros past them
+  __device__ __forceinline__ void load_end(char* lds, const void* tile, int64_t slab, int k_left) const {
+#pragma unroll
+    for (int q = 0; q < kLoads; ++q) {
+      const int at = q * THREADS + threadIdx.x;
+      u32x4 v = {};
+      if (piece(at) * 8 < k_left)
+        v = *reinterpret_cast<const u32x4*>(static_cast<const char*>(tile) + 128 * slab + vo[q]);
+      *reinterpret_cast<u32x4*>(lds + 16 * at) = v;
+    }
+  }
+  // 8 k values from k = kk + 8 (lane / 32) of row `row0 + lane % 32`
+  __device__ static __forceinline__ bf16x8 frag(const char* lds, int row0, int kk) {
+    const int lane = threadIdx.x & 63, p = ((kk >> 3) + (lane >> 5)) ^ swizzle(lane & 31);
+    return *reinterpret_cast<const bf16x8*>(lds + (row0 + (lane & 31)) * 128 + p * 16);
+  }
+};
+
+// COLS columns of an operand whose k values lie across its rows (row k of memory
+// holds k's value of every column).  The fragments need k along a lane's registers:
+// they are read with the transposing LDS load (16 lanes read 4 consecutive k of 16
+// columns and receive a column's 4 values each).  The pieces of an LDS row are
+// XORed with k mod 4 above their 64 bytes, so that such a read touches every bank
+// once.
+template <int COLS, int THREADS>
+struct ColsSlab {
+  static constexpr int kRow = COLS * 2, kPieces = kRow / 16;
+  static constexpr int kBytes = kSlab * kRow, kLoads = kBytes / 16 / THREADS;
+  uint32_t vo[kLoads];
+  uint32_t row_bytes;
+  // columns past the operand's: its last 8 again (their outputs are not stored)
+  __device__ __forceinline__ void init(uint32_t bytes, int64_t cols_left) {
+    row_bytes = bytes;
+#pragma unroll
+    for (int q = 0; q < kLoads; ++q) {
+      const int at = q * THREADS + threadIdx.x, k = at / kPieces;
+      const int p = (at % kPieces) ^ ((k & 3) << 2);
+      vo[q] = (uint32_t)k * row_bytes + 16u * (uint32_t)min((int64_t)p, cols_left / 8 - 1);
+    }
+  }
+  // rows from k_left on are the last one again: the other operand is zero there
+  __device__ __forceinline__ void load(uint32_t lds, const void* tile, int64_t slab, int64_t k_left) const {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const u32x4 r = tile_rsrc((uint64_t)tile + (uint64_t)(kSlab * slab) * row_bytes);
+    if (k_left >= kSlab) {
+#pragma unroll
+      for (int q = 0; q < kLoads; ++q) load_to_lds(lds + 16u * (q * THREADS + wave * 64), r, vo[q], 0);
+    } else {
+#pragma unroll
+      for (int q = 0; q < kLoads; ++q) {
+        const int k = (q * THREADS + (int)threadIdx.x) / kPieces;
+        load_to_lds(lds + 16u * (q * THREADS + wave * 64), r,
+                    vo[q] - (uint32_t)max(k - (int)k_left + 1, 0) * row_bytes, 0);
+      }
+    }
+  }
+  // 8 k values from k = kk + 8 (lane / 32) of column `col0 + lane % 32`
+  __device__ static __forceinline__ bf16x8 frag(const char* lds, int col0, int kk) {
+    const int lane = threadIdx.x & 63, j = lane & 15, kq = j >> 2;
+    const int p = (col0 / 8 + ((lane >> 4) & 1) * 2 + ((j & 3) >> 1)) ^ (kq << 2);
+    const char* at = lds + (kk + 8 * (lane >> 5) + kq) * kRow + p * 16 + (j & 1) * 8;
+    const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
+    const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 4 * kRow));
+    return __builtin_shufflevector(__builtin_bit_cast(bf16x4, v0), __builtin_bit_cast(bf16x4, v1), 0, 1, 2, 3, 4, 5, 6,
+                                   7);
+  }
+};
+
+__device__ __forceinline__ bf16x4 rounded(floatx4 v) { return __builtin_convertvector(v, bf16x4); }
+
+// A wave's LDS accesses before are done before those after.
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// A wave's 32 rows x COLS columns between LDS (rows of COLS * 2 + 16 bytes) and
+// memory; rows and columns past the matrix are left out, those before `rows_pad`
+// and `cols_pad` stored as zeros.
+template <int COLS>
+struct Patch {
+  static constexpr int kPitch = COLS * 2 + 16, kBytes = 32 * kPitch, kLanes = COLS / 8, kRows = 64 / kLanes;
+  __device__ static __forceinline__ char* quad(char* ws, int col) { return ws + (threadIdx.x & 31) * kPitch + col * 2; }
+  __device__ static __forceinline__ void store(const char* ws, uint16_t* out, int64_t ld, int64_t row0, int64_t col0,
+                                               int64_t rows, int64_t cols, int64_t rows_pad, int64_t cols_pad, bool vec) {
+    const int lane = threadIdx.x & 63, c8 = lane % kLanes;
+    const int64_t col = col0 + 8 * c8;
+#pragma unroll
+    for (int q = 0; q < 32 / kRows; ++q) {
+      const int r = q * kRows + lane / kLanes;
+      const int64_t row = row0 + r;
+      if (row >= rows_pad || col >= cols_pad) continue;
+      uint16_t* o = out + row * ld + col;
+      if (row < rows && vec && col + 8 <= cols) {
+        *reinterpret_cast<u32x4*>(o) = *reinterpret_cast<const u32x4*>(ws + r * kPitch + c8 * 16);
+      } else {
+        const uint16_t* v = reinterpret_cast<const uint16_t*>(ws + r * kPitch + c8 * 16);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (col + e < cols_pad) o[e] = row < rows && col + e < cols ? v[e] : (uint16_t)0;
+      }
+    }
+  }
+  __device__ static __forceinline__ void load(char* ws, const uint16_t* in, int64_t ld, int64_t row0, int64_t col0,
+                                              int64_t rows, int64_t cols, bool vec) {
+    const int lane = threadIdx.x & 63, c8 = lane % kLanes;
+    const int64_t col = col0 + 8 * c8;
+#pragma unroll
+    for (int q = 0; q < 32 / kRows; ++q) {
+      const int r = q * kRows + lane / kLanes;
+      const int64_t row = row0 + r;
+      u32x4 v = {};
+      const uint16_t* i = in + row * ld + col;
+      if (row < rows) {
+        if (vec && col + 8 <= cols) {
+          v = *reinterpret_cast<const u32x4*>(i);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (col + e < cols) v[e / 2] |= (uint32_t)i[e] << (16 * (e & 1));
+        }
+      }
+      *reinterpret_cast<u32x4*>(ws + r * kPitch + c8 * 16) = v;
+    }
+  }
+};
+
+struct TileArgs {
+  FfnArgs g;
+  int tiles_m, tiles_n, tiles;
+  int vec_out, vec_dh;  // rows of out (dh) 16-byte aligned
+};
+
+// The tile of a workgroup: workgroups go round the 8 XCDs in turn, so each XCD takes
+// a run of tiles, in bands of 8 rows of tiles, whose operands its L2 then holds.
+__device__ __forceinline__ void tile_of(const TileArgs& t, int& tm, int& tn, int& z) {
+  const int xcd = blockIdx.x & 7, q = t.tiles >> 3, r = t.tiles & 7;
+  int i = xcd * q + min(xcd, r) + (int)(blockIdx.x >> 3);
+  const int plane = t.tiles_m * t.tiles_n;
+  z = i / plane;
+  i -= z * plane;
+  const int band = i / (8 * t.tiles_n), in = i - band * 8 * t.tiles_n;
+  const int rows = min(8, t.tiles_m - band * 8);
+  tm = band * 8 + in % rows;
+  tn = in / rows;
+}
+
+template <int MODE, int ACT, class C>
+__global__ void __launch_bounds__(C::threads, 2) ffn_tile_kernel(TileArgs t) {
+  constexpr bool DUAL = MODE == kForward || MODE == kInner, ACOLS = MODE == kPair;
+  constexpr int kCols = DUAL ? C::TN / 2 : C::TN;  // output columns of a tile
+  typedef RowsSlab<C::TM, C::threads> AR;
+  typedef ColsSlab<C::TM, C::threads> AC;
+  typedef RowsSlab<C::TN / 2, C::threads> BR;
+  typedef ColsSlab<C::TN, C::threads> BC;
+  constexpr int kA = C::TM * 128, kStage = kA + C::TN * 128;
+  typedef Patch<(DUAL ? C::NB / 2 : C::NB) * 32> P;
+  constexpr int kPatches = MODE == kInner ? 2 : 1;
+  constexpr int kWs = kPatches * P::kBytes;
+  constexpr int kLds = 2 * kStage > C::waves * kWs ? 2 * kStage : C::waves * kWs;
+  static_assert(kLds <= 160 * 1024, "LDS");
+  __shared__ __attribute__((aligned(1024))) char lds[kLds];
+
+  const FfnArgs& g = t.g;
+  int tm, tn, z;
+  tile_of(t, tm, tn, z);
+  const int64_t i0 = (int64_t)tm * C::TM, j0 = (int64_t)tn * kCols;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / C::WN, wn = wave % C::WN;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)lds;
+
+  AR ar;
+  AC ac;
+  BR br;
+  BC bc;
+  const uint16_t *a[2], *b[2];
+#pragma unroll
+  for (int p = 0; p < 2; ++p) {
+    const Operand &oa = g.a[MODE == kPair ? z : MODE == kSum ? p : 0], &ob = g.b[MODE == kPair ? 0 : p];
+    a[p] = static_cast<const uint16_t*>(oa.p) + i0 * oa.rs;
+    b[p] = static_cast<const uint16_t*>(ob.p) + j0 * ob.rs;
+  }
+  if constexpr (ACOLS) ac.init(2u * (uint32_t)g.a[0].ks, ffn_pad(g.m) - i0);
+  else ar.init(2u * (uint32_t)g.a[0].rs, g.m - i0);
+  if constexpr (DUAL) br.init(2u * (uint32_t)g.b[0].rs, g.n - j0);
+  else bc.init(2u * (uint32_t)g.b[0].ks, g.n - j0);
+  // kSum: the slabs of both parts one after the other
+  const int64_t slabs = (g.k + kSlab - 1) / kSlab, total = MODE == kSum ? 2 * slabs : slabs;
+
+  const auto issue = [&](int64_t s, int buf) {
+    const uint32_t at = lds0 + (uint32_t)buf * kStage;
+    if constexpr (DUAL) {
+      const int64_t k_left = g.k - s * kSlab;
+      if (k_left < kSlab) {
+        char* to = lds + buf * kStage;
+        ar.load_end(to, a[0], s, (int)k_left);
+        br.load_end(to + kA, b[0], s, (int)k_left);
+        br.load_end(to + kA + BR::kBytes, b[1], s, (int)k_left);
+        return;
+      }
+      ar.load(at, a[0], s);
+      br.load(at + kA, b[0], s);
+      br.load(at + kA + BR::kBytes, b[1], s);
+    } else {
+      const bool second = MODE == kSum && s >= slabs;
+      const int64_t sp = second ? s - slabs : s;
+      if constexpr (ACOLS) ac.load(at, a[0], sp, kSlab);
+      else ar.load(at, second ? a[1] : a[0], sp);
+      bc.load(at + kA, second ? b[1] : b[0], sp, g.k - sp * kSlab);
+    }
+  };
+
+  floatx16 acc[C::NA][C::NB];
+#pragma unroll
+  for (int x = 0; x < C::NA; ++x)
+#pragma unroll
+    for (int y = 0; y < C::NB; ++y)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[x][y][e] = 0.f;
+
+  if (total) issue(0, 0);
+#pragma unroll 1
+  for (int64_t s = 0; s < total; ++s) {
+    wait_slabs<0>();  // slab s is in LDS, and every wave is done with the buffer that slab s + 1 takes
+    const int buf = (int)(s & 1);
+    if (s + 1 < total) issue(s + 1, buf ^ 1);
+    const char* at = lds + buf * kStage;
+    const char* bt = at + kA;
+#pragma unroll
+    for (int kk = 0; kk < kSlab; kk += 16) {
+      bf16x8 av[C::NA], bv[C::NB];
+#pragma unroll
+      for (int y = 0; y < C::NB; ++y) {
+        if constexpr (DUAL)  // the first half of a wave's blocks is the gate's, the second the up projection's
+          bv[y] = BR::frag(bt, (y / (C::NB / 2)) * (C::TN / 2) + (wn * (C::NB / 2) + y % (C::NB / 2)) * 32, kk);
+        else
+          bv[y] = BC::frag(bt, (wn * C::NB + y) * 32, kk);
+      }
+#pragma unroll
+      for (int x = 0; x < C::NA; ++x) {
+        if constexpr (ACOLS) av[x] = AC::frag(at, (wm * C::NA + x) * 32, kk);
+        else av[x] = AR::frag(at, (wm * C::NA + x) * 32, kk);
+      }
+      // b first: a lane then holds 4 consecutive columns of one row
+#pragma unroll
+      for (int x = 0; x < C::NA; ++x)
+#pragma unroll
+        for (int y = 0; y < C::NB; ++y)
+          acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bv[y], av[x], acc[x][y], 0, 0, 0);
+    }
+  }
+  wait_slabs<0>();  // every wave is done with the operands: LDS is free
+
+  // acc[x][y][4 q + e] = C(32 x + lane % 32, 32 y + 8 q + 4 (lane / 32) + e)
+  char* ws = lds + wave * kWs;
+  constexpr int kOut = DUAL ? C::NB / 2 : C::NB;
+  const int64_t col0 = j0 + wn * kOut * 32;
+  const int64_t rows_pad = MODE == kInner ? ffn_pad(g.m) : g.m, cols_pad = MODE == kInner ? ffn_pad(g.n) : g.n;
+  uint16_t* out = static_cast<uint16_t*>(g.out[MODE == kPair ? z : 0]);
+#pragma unroll
+  for (int x = 0; x < C::NA; ++x) {
+    const int64_t row0 = i0 + (wm * C::NA + x) * 32;
+    if constexpr (MODE == kInner) {
+      P::load(ws, static_cast<const uint16_t*>(g.dh), g.ld_dh, row0, col0, g.m, g.n, t.vec_dh);
+      wave_fence();
+    }
+#pragma unroll
+    for (int y = 0; y < kOut; ++y)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        char* at = P::quad(ws, 32 * y + 8 * q + 4 * (lane >> 5));
+        floatx4 v;
+        if constexpr (DUAL) {
+          floatx4 dh, w;
+          if constexpr (MODE == kInner) dh = __builtin_convertvector(*reinterpret_cast<const bf16x4*>(at), floatx4);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            float f, df;
+            activate<ACT>(acc[x][y][4 * q + e], f, df);
+            const float u = acc[x][kOut + y][4 * q + e];
+            if constexpr (MODE == kInner) {
+              v[e] = dh[e] * u * df;
+              w[e] = dh[e] * f;
+            } else {
+              v[e] = f * u;
+            }
+          }
+          if constexpr (MODE == kInner) *reinterpret_cast<bf16x4*>(at + P::kBytes) = rounded(w);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = acc[x][y][4 * q + e];
+        }
+        *reinterpret_cast<bf16x4*>(at) = rounded(v);
+      }
+    wave_fence();
+    P::store(ws, out, g.ld_out, row0, col0, g.m, g.n, rows_pad, cols_pad, t.vec_out);
+    if constexpr (MODE == kInner)
+      P::store(ws + P::kBytes, static_cast<uint16_t*>(g.out[1]), g.ld_out, row0, col0, g.m, g.n, rows_pad, cols_pad,
+               t.vec_out);
+    wave_fence();
+  }
+}
+
+template <int MODE, int ACT, class C>
+void launch_shape(TileArgs& t, hipStream_t st) {
+  constexpr int kCols = MODE == kForward || MODE == kInner ? C::TN / 2 : C::TN;
+  t.tiles_m = (int)((t.g.m + C::TM - 1) / C::TM);
+  t.tiles_n = (int)((t.g.n + kCols - 1) / kCols);
+  t.tiles = t.tiles_m * t.tiles_n * (MODE == kPair ? 2 : 1);
+  hipLaunchKernelGGL((ffn_tile_kernel<MODE, ACT, C>), dim3(t.tiles), dim3(C::threads), 0, st, t);
+}
+
+template <int MODE, int ACT>
+hipError_t launch_mode(const FfnArgs& g, hipStream_t st) {
+  if (g.m == 0 || g.n == 0) return hipSuccess;
+  TileArgs t;
+  t.g = g;
+  const auto vec = [](const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && (ld & 7) == 0; };
+  t.vec_out = vec(g.out[0], g.ld_out) && (!g.out[1] || vec(g.out[1], g.ld_out));
+  t.vec_dh = MODE == kInner && vec(g.dh, g.ld_dh);
+  const int64_t cols = MODE == kForward || MODE == kInner ? 128 : 256;
+  const int64_t large = ((g.m + 255) / 256) * ((g.n + cols - 1) / cols) * (MODE == kPair ? 2 : 1);
+  if (large >= 200) launch_shape<MODE, ACT, Large>(t, st);
+  else launch_shape<MODE, ACT, Small>(t, st);
+  return hipGetLastError();
+}
+
+template <int ACT>
+hipError_t launch_act(FfnMode mode, const FfnArgs& g, hipStream_t st) {
+  switch (mode) {
+    case kForward: return launch_mode<kForward, ACT>(g, st);
+    case kInner: return launch_mode<kInner, ACT>(g, st);
+    // (these two apply no activation)
+    case kSum: return launch_mode<kSum, ISOLOCO_ACT_SILU>(g, st);
+    default: return launch_mode<kPair, ISOLOCO_ACT_SILU>(g, st);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_ffn_tiles(FfnMode mode, int act, const FfnArgs& g, hipStream_t st) {
+  return act == ISOLOCO_ACT_SILU ? launch_act<ISOLOCO_ACT_SILU>(mode, g, st) : launch_act<ISOLOCO_ACT_GELU>(mode, g, st);
+}
+
+}  // namespace isoloco

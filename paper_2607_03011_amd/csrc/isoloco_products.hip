@@ -37,15 +37,10 @@
 
 #include "isoloco_device.h"
 #include "isoloco_kernels.h"
+#include "isoloco_lds.h"
 
 namespace isoloco {
 
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) char lds_char;
-typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
 // A tile shape: TM x TN outputs per workgroup, WM x WN waves, ST slabs of 32 k
 // values in LDS (ST - 1 of them in flight while one is multiplied).
@@ -65,38 +60,6 @@ typedef TileShape<256, 256, 2, 4, 2> TileL;
 typedef TileShape<128, 128, 2, 2, 2> TileM;
 typedef TileShape<64, 64, 2, 2, 3> TileS;
 constexpr int kSlabK = 32;
-
-// 16 bytes per lane from memory to LDS: lane l's bytes land at lds_off + 16 l
-// (lds_off is wave-uniform).  No register receives the data; the loads count
-// in vmcnt like any other, and wait_slabs() below waits for them.  m0 holds
-// the LDS address.  It is listed as clobbered, so that the compiler sets it again
-// for any use of its own (it has none here today); m0 is a reserved register,
-// of which the compiler warns.
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-__device__ __forceinline__ void load_to_lds(uint32_t lds_off, u32x4 rsrc, uint32_t voff, uint32_t soff) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
-               :
-               : "s"(lds_off), "v"(voff), "s"(rsrc), "s"(soff)
-               : "memory", "m0");
-}
-#pragma clang diagnostic pop
-
-// Wait until at most N of this wave's loads are outstanding and its LDS reads
-// have returned, then for every wave of the workgroup.
-template <int N>
-__device__ __forceinline__ void wait_slabs() {
-  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
-}
-
-__device__ __forceinline__ u32x4 tile_rsrc(uint64_t base) {
-  u32x4 r;
-  r[0] = __builtin_amdgcn_readfirstlane((uint32_t)base);
-  r[1] = __builtin_amdgcn_readfirstlane((uint32_t)(base >> 32) & 0xffffu);
-  r[2] = 0xffffffffu;
-  r[3] = kBufferFlags;
-  return r;
-}
 
 // The next bf16 part of 4 values, which keep the remainder (exact: the parts
 // are x0 = bf16(x), x1 = bf16(x - x0), x2 = bf16(x - x0 - x1))
