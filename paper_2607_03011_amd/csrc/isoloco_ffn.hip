@@ -12,6 +12,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "isoloco_device.h"
 #include "isoloco_error.h"
 #include "isoloco_ffn.h"
@@ -118,8 +120,17 @@ struct FfnShape {
   int32_t dtype, act;
 };
 
+// The backward workspace: da, du, and the sums of a split product.
+size_t inner_bytes(const FfnShape& s) {
+  return 2 * (size_t)ffn_pad(s.tokens) * (size_t)ffn_pad(s.hidden) * dtype_bytes(s.dtype);
+}
 size_t ffn_workspace(const FfnShape& s, bool backward) {
-  return backward ? 2 * (size_t)ffn_pad(s.tokens) * (size_t)ffn_pad(s.hidden) * dtype_bytes(s.dtype) : 0;
+  if (!backward) return 0;
+  size_t partial = 0;
+  if (s.dtype == ISOLOCO_BF16)
+    partial = std::max(ffn_partial_bytes(kSum, s.tokens, s.dim, s.hidden),
+                       ffn_partial_bytes(kPair, s.hidden, s.dim, s.tokens));
+  return inner_bytes(s) + partial;
 }
 
 // the tile kernels load whole 16-byte pieces of rows, at offsets of 32 bits from a tile's first
@@ -142,7 +153,7 @@ hipError_t run_forward(const FfnShape& s, const void* x, int64_t ld_x, const voi
   g.k = s.dim;
   g.out[0] = out;
   g.ld_out = ld_out;
-  if (on_tiles<T>(s, x, ld_x, wg, wu, ld_w)) return launch_ffn_tiles(kForward, ACT, g, st);
+  if (on_tiles<T>(s, x, ld_x, wg, wu, ld_w)) return launch_ffn_tiles(kForward, ACT, g, nullptr, st);
   return launch_any<T, kForward, ACT>(g, st);
 }
 
@@ -153,6 +164,7 @@ hipError_t run_backward(const FfnShape& s, const void* x, int64_t ld_x, const vo
   const int64_t ld = ffn_pad(s.hidden);
   T* da = static_cast<T*>(ws);
   T* du = da + ffn_pad(s.tokens) * ld;
+  float* partial = reinterpret_cast<float*>(static_cast<char*>(ws) + inner_bytes(s));
   const bool tiles = on_tiles<T>(s, x, ld_x, wg, wu, ld_w);
   FfnArgs g = {};
   g.a[0] = {x, ld_x, 1};
@@ -166,7 +178,7 @@ hipError_t run_backward(const FfnShape& s, const void* x, int64_t ld_x, const vo
   g.ld_out = ld;
   g.dh = dout;
   g.ld_dh = ld_dout;
-  hipError_t e = tiles ? launch_ffn_tiles(kInner, ACT, g, st) : launch_any<T, kInner, ACT>(g, st);
+  hipError_t e = tiles ? launch_ffn_tiles(kInner, ACT, g, partial, st) : launch_any<T, kInner, ACT>(g, st);
   if (e == hipSuccess && dx) {
     g = {};
     g.a[0] = {da, ld, 1};
@@ -178,7 +190,7 @@ hipError_t run_backward(const FfnShape& s, const void* x, int64_t ld_x, const vo
     g.k = s.hidden;
     g.out[0] = dx;
     g.ld_out = ld_dx;
-    e = tiles ? launch_ffn_tiles(kSum, ACT, g, st) : launch_any<T, kSum, ACT>(g, st);
+    e = tiles ? launch_ffn_tiles(kSum, ACT, g, partial, st) : launch_any<T, kSum, ACT>(g, st);
   }
   if (e == hipSuccess && dwg) {
     g = {};
@@ -191,7 +203,7 @@ hipError_t run_backward(const FfnShape& s, const void* x, int64_t ld_x, const vo
     g.out[0] = dwg;
     g.out[1] = dwu;
     g.ld_out = ld_dw;
-    e = tiles ? launch_ffn_tiles(kPair, ACT, g, st) : launch_any<T, kPair, ACT>(g, st);
+    e = tiles ? launch_ffn_tiles(kPair, ACT, g, partial, st) : launch_any<T, kPair, ACT>(g, st);
   }
   return e;
 }

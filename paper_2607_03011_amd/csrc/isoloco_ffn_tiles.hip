@@ -29,6 +29,7 @@ struct Shape {
   static constexpr int NA = TM / WM / 32, NB = TN / WN / 32;
 };
 typedef Shape<256, 256, 4, 2> Large;
+typedef Shape<192, 256, 2, 4> Middle;
 typedef Shape<128, 128, 2, 2> Small;
 constexpr int kSlab = kFfnPad;
 
@@ -76,22 +77,34 @@ struct RowsSlab {
 // COLS columns of an operand whose k values lie across its rows (row k of memory
 // holds k's value of every column).  The fragments need k along a lane's registers:
 // they are read with the transposing LDS load (16 lanes read 4 consecutive k of 16
-// columns and receive a column's 4 values each).  The pieces of an LDS row are
-// XORed with k mod 4 above their 64 bytes, so that such a read touches every bank
-// once.
+// columns and receive a column's 4 values each).  The pieces of an LDS row are moved
+// by 64 bytes times k mod 4 (round the row: 192 columns are no power of two), so that
+// such a read touches every bank once.
 template <int COLS, int THREADS>
 struct ColsSlab {
   static constexpr int kRow = COLS * 2, kPieces = kRow / 16;
   static constexpr int kBytes = kSlab * kRow, kLoads = kBytes / 16 / THREADS;
+  static constexpr bool kPow2 = (kPieces & (kPieces - 1)) == 0;
   uint32_t vo[kLoads];
   uint32_t row_bytes;
+  // where piece p of row k lies, and which piece lies at p
+  __device__ static __forceinline__ int place(int p, int k) {
+    if constexpr (kPow2) return p ^ ((k & 3) << 2);
+    p += (k & 3) << 2;
+    return p >= kPieces ? p - kPieces : p;
+  }
+  __device__ static __forceinline__ int piece(int p, int k) {
+    if constexpr (kPow2) return p ^ ((k & 3) << 2);
+    p -= (k & 3) << 2;
+    return p < 0 ? p + kPieces : p;
+  }
   // columns past the operand's: its last 8 again (their outputs are not stored)
   __device__ __forceinline__ void init(uint32_t bytes, int64_t cols_left) {
     row_bytes = bytes;
 #pragma unroll
     for (int q = 0; q < kLoads; ++q) {
       const int at = q * THREADS + threadIdx.x, k = at / kPieces;
-      const int p = (at % kPieces) ^ ((k & 3) << 2);
+      const int p = piece(at % kPieces, k);
       vo[q] = (uint32_t)k * row_bytes + 16u * (uint32_t)min((int64_t)p, cols_left / 8 - 1);
     }
   }
@@ -114,7 +127,7 @@ struct ColsSlab {
   // 8 k values from k = kk + 8 (lane / 32) of column `col0 + lane % 32`
   __device__ static __forceinline__ bf16x8 frag(const char* lds, int col0, int kk) {
     const int lane = threadIdx.x & 63, j = lane & 15, kq = j >> 2;
-    const int p = (col0 / 8 + ((lane >> 4) & 1) * 2 + ((j & 3) >> 1)) ^ (kq << 2);
+    const int p = place(col0 / 8 + ((lane >> 4) & 1) * 2 + ((j & 3) >> 1), kq);
     const char* at = lds + (kk + 8 * (lane >> 5) + kq) * kRow + p * 16 + (j & 1) * 8;
     const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
     const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 4 * kRow));
@@ -184,16 +197,19 @@ struct Patch {
 
 struct TileArgs {
   FfnArgs g;
-  int tiles_m, tiles_n, tiles;
+  int tiles_m, tiles_n, planes, splits, tiles;  // tiles: of every plane and split
   int vec_out, vec_dh;  // rows of out (dh) 16-byte aligned
+  float* partial;       // splits > 1: the sums of each split, [split][plane][m][n]
 };
 
 // The tile of a workgroup: workgroups go round the 8 XCDs in turn, so each XCD takes
 // a run of tiles, in bands of 8 rows of tiles, whose operands its L2 then holds.
-__device__ __forceinline__ void tile_of(const TileArgs& t, int& tm, int& tn, int& z) {
+__device__ __forceinline__ void tile_of(const TileArgs& t, int& tm, int& tn, int& z, int& slice) {
   const int xcd = blockIdx.x & 7, q = t.tiles >> 3, r = t.tiles & 7;
   int i = xcd * q + min(xcd, r) + (int)(blockIdx.x >> 3);
   const int plane = t.tiles_m * t.tiles_n;
+  slice = i / (plane * t.planes);
+  i -= slice * plane * t.planes;
   z = i / plane;
   i -= z * plane;
   const int band = i / (8 * t.tiles_n), in = i - band * 8 * t.tiles_n;
@@ -219,8 +235,8 @@ __global__ void __launch_bounds__(C::threads, 2) ffn_tile_kernel(TileArgs t) {
   __shared__ __attribute__((aligned(1024))) char lds[kLds];
 
   const FfnArgs& g = t.g;
-  int tm, tn, z;
-  tile_of(t, tm, tn, z);
+  int tm, tn, z, slice;
+  tile_of(t, tm, tn, z, slice);
   const int64_t i0 = (int64_t)tm * C::TM, j0 = (int64_t)tn * kCols;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / C::WN, wn = wave % C::WN;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)lds;
@@ -240,29 +256,36 @@ __global__ void __launch_bounds__(C::threads, 2) ffn_tile_kernel(TileArgs t) {
   else ar.init(2u * (uint32_t)g.a[0].rs, g.m - i0);
   if constexpr (DUAL) br.init(2u * (uint32_t)g.b[0].rs, g.n - j0);
   else bc.init(2u * (uint32_t)g.b[0].ks, g.n - j0);
-  // kSum: the slabs of both parts one after the other
-  const int64_t slabs = (g.k + kSlab - 1) / kSlab, total = MODE == kSum ? 2 * slabs : slabs;
+  // kSum: the slabs of both parts one after the other; a split product's workgroup
+  // takes one run of them
+  const int64_t slabs = (g.k + kSlab - 1) / kSlab, all = MODE == kSum ? 2 * slabs : slabs;
+  const int64_t first = all * slice / t.splits, total = all * (slice + 1) / t.splits - first;
 
-  const auto issue = [&](int64_t s, int buf) {
+  // part 0: the slab of a, part 1: that of b
+  const auto issue = [&](int64_t s, int buf, int part) {
     const uint32_t at = lds0 + (uint32_t)buf * kStage;
     if constexpr (DUAL) {
       const int64_t k_left = g.k - s * kSlab;
       if (k_left < kSlab) {
         char* to = lds + buf * kStage;
-        ar.load_end(to, a[0], s, (int)k_left);
-        br.load_end(to + kA, b[0], s, (int)k_left);
-        br.load_end(to + kA + BR::kBytes, b[1], s, (int)k_left);
-        return;
+        if (part == 0) {
+          ar.load_end(to, a[0], s, (int)k_left);
+        } else {
+          br.load_end(to + kA, b[0], s, (int)k_left);
+          br.load_end(to + kA + BR::kBytes, b[1], s, (int)k_left);
+        }
+      } else if (part == 0) {
+        ar.load(at, a[0], s);
+      } else {
+        br.load(at + kA, b[0], s);
+        br.load(at + kA + BR::kBytes, b[1], s);
       }
-      ar.load(at, a[0], s);
-      br.load(at + kA, b[0], s);
-      br.load(at + kA + BR::kBytes, b[1], s);
     } else {
       const bool second = MODE == kSum && s >= slabs;
       const int64_t sp = second ? s - slabs : s;
-      if constexpr (ACOLS) ac.load(at, a[0], sp, kSlab);
+      if (part == 1) bc.load(at + kA, second ? b[1] : b[0], sp, g.k - sp * kSlab);
+      else if constexpr (ACOLS) ac.load(at, a[0], sp, kSlab);
       else ar.load(at, second ? a[1] : a[0], sp);
-      bc.load(at + kA, second ? b[1] : b[0], sp, g.k - sp * kSlab);
     }
   };
 
@@ -274,40 +297,95 @@ __global__ void __launch_bounds__(C::threads, 2) ffn_tile_kernel(TileArgs t) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[x][y][e] = 0.f;
 
-  if (total) issue(0, 0);
-#pragma unroll 1
-  for (int64_t s = 0; s < total; ++s) {
-    wait_slabs<0>();  // slab s is in LDS, and every wave is done with the buffer that slab s + 1 takes
-    const int buf = (int)(s & 1);
-    if (s + 1 < total) issue(s + 1, buf ^ 1);
+  struct Frags {
+    bf16x8 a[C::NA], b[C::NB];
+  };
+  // the fragments of k values kk .. kk + 15 of the slab in buffer `buf`
+  const auto read = [&](Frags& f, int buf, int kk) {
     const char* at = lds + buf * kStage;
     const char* bt = at + kA;
 #pragma unroll
-    for (int kk = 0; kk < kSlab; kk += 16) {
-      bf16x8 av[C::NA], bv[C::NB];
+    for (int x = 0; x < C::NA; ++x) {
+      if constexpr (ACOLS) f.a[x] = AC::frag(at, (wm * C::NA + x) * 32, kk);
+      else f.a[x] = AR::frag(at, (wm * C::NA + x) * 32, kk);
+    }
+#pragma unroll
+    for (int y = 0; y < C::NB; ++y) {
+      if constexpr (DUAL)  // the first half of a wave's blocks is the gate's, the second the up projection's
+        f.b[y] = BR::frag(bt, (y / (C::NB / 2)) * (C::TN / 2) + (wn * (C::NB / 2) + y % (C::NB / 2)) * 32, kk);
+      else
+        f.b[y] = BC::frag(bt, (wn * C::NB + y) * 32, kk);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // The products of 16 k values (b first: a lane then holds 4 consecutive columns
+  // of one row); part `part` of slab s is asked for behind the first of them.
+  const auto multiply = [&](const Frags& f, bool more, int64_t s, int buf, int part) {
+#pragma unroll
+    for (int x = 0; x < C::NA; ++x)
 #pragma unroll
       for (int y = 0; y < C::NB; ++y) {
-        if constexpr (DUAL)  // the first half of a wave's blocks is the gate's, the second the up projection's
-          bv[y] = BR::frag(bt, (y / (C::NB / 2)) * (C::TN / 2) + (wn * (C::NB / 2) + y % (C::NB / 2)) * 32, kk);
-        else
-          bv[y] = BC::frag(bt, (wn * C::NB + y) * 32, kk);
+        acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.b[y], f.a[x], acc[x][y], 0, 0, 0);
+        if (x == 0 && y == 1) {
+          __builtin_amdgcn_sched_barrier(0);
+          if (more) issue(s, buf, part);
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+  // The fragments of 16 k values are read while those before are multiplied; once
+  // the last of a slab are in registers its buffer is free, so that the wait for
+  // the next slab and the first reads from it pass behind the last products of this
+  // one.  A slab's loads are issued in two parts behind products: 64 of them at
+  // once keep the CU's address unit busy for about half a slab's time, in which
+  // their waves would multiply nothing (all at the barrier: 639 us for the sum over
+  // 2 x 5632 of 16384 x 2048 outputs, in two parts 611).
+  if (total > 0) {
+    issue(first, 0, 0);
+    issue(first, 0, 1);
+    wait_slabs<0>();
+    Frags f[2];
+    read(f[0], 0, 0);
+    if (total > 1) issue(first + 1, 1, 0);
+#pragma unroll 1
+    for (int64_t s = 0; s < total; ++s) {
+      const int buf = (int)(s & 1);
 #pragma unroll
-      for (int x = 0; x < C::NA; ++x) {
-        if constexpr (ACOLS) av[x] = AC::frag(at, (wm * C::NA + x) * 32, kk);
-        else av[x] = AR::frag(at, (wm * C::NA + x) * 32, kk);
+      for (int kk = 16; kk < kSlab; kk += 16) {
+        read(f[(kk / 16) & 1], buf, kk);
+        multiply(f[(kk / 16 + 1) & 1], kk == 16 && s + 1 < total, first + s + 1, buf ^ 1, 1);
       }
-      // b first: a lane then holds 4 consecutive columns of one row
-#pragma unroll
-      for (int x = 0; x < C::NA; ++x)
-#pragma unroll
-        for (int y = 0; y < C::NB; ++y)
-          acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bv[y], av[x], acc[x][y], 0, 0, 0);
+      wait_slabs<0>();  // slab s + 1 is in LDS, and every wave is done reading slab s
+      if (s + 1 < total) read(f[0], buf ^ 1, 0);
+      multiply(f[1], s + 2 < total, first + s + 2, buf, 0);
     }
   }
-  wait_slabs<0>();  // every wave is done with the operands: LDS is free
+  __syncthreads();  // every wave is done with the operands: LDS is free
 
   // acc[x][y][4 q + e] = C(32 x + lane % 32, 32 y + 8 q + 4 (lane / 32) + e)
+  if constexpr (!DUAL) {
+    if (t.splits > 1) {
+      // (n is a multiple of 8: a quad of columns is inside or outside)
+      float* part = t.partial + ((int64_t)slice * t.planes + z) * g.m * g.n;
+#pragma unroll
+      for (int x = 0; x < C::NA; ++x) {
+        const int64_t row = i0 + (wm * C::NA + x) * 32 + (lane & 31);
+        if (row >= g.m) continue;
+#pragma unroll
+        for (int y = 0; y < C::NB; ++y)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const int64_t col = j0 + (wn * C::NB + y) * 32 + 8 * q + 4 * (lane >> 5);
+            if (col < g.n)
+              *reinterpret_cast<floatx4*>(part + row * g.n + col) =
+                  (floatx4){acc[x][y][4 * q], acc[x][y][4 * q + 1], acc[x][y][4 * q + 2], acc[x][y][4 * q + 3]};
+          }
+      }
+      return;
+    }
+  }
   char* ws = lds + wave * kWs;
   constexpr int kOut = DUAL ? C::NB / 2 : C::NB;
   const int64_t col0 = j0 + wn * kOut * 32;
@@ -332,7 +410,7 @@ __global__ void __launch_bounds__(C::threads, 2) ffn_tile_kernel(TileArgs t) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             float f, df;
-            activate<ACT>(acc[x][y][4 * q + e], f, df);
+            activate_fast<ACT>(acc[x][y][4 * q + e], f, df);
             const float u = acc[x][kOut + y][4 * q + e];
             if constexpr (MODE == kInner) {
               v[e] = dh[e] * u * df;
@@ -357,45 +435,122 @@ __global__ void __launch_bounds__(C::threads, 2) ffn_tile_kernel(TileArgs t) {
   }
 }
 
+// The splits of a product added in their order, rounded once.
+__global__ void __launch_bounds__(256) ffn_join_kernel(TileArgs t) {
+  const FfnArgs& g = t.g;
+  const int64_t plane = g.m * g.n, quads = plane / 4;
+  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (at >= quads * t.planes) return;
+  const int z = (int)(at / quads);
+  const int64_t i = (at - z * quads) * 4, row = i / g.n, col = i - row * g.n;
+  const float* p = t.partial + z * plane + i;
+  floatx4 s = *reinterpret_cast<const floatx4*>(p);
+  for (int k = 1; k < t.splits; ++k) s += *reinterpret_cast<const floatx4*>(p + k * t.planes * plane);
+  uint16_t* out = static_cast<uint16_t*>(g.out[z]) + row * g.ld_out + col;
+  const bf16x4 r = rounded(s);
+  if (t.vec_out) {
+    *reinterpret_cast<bf16x4*>(out) = r;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) reinterpret_cast<__bf16*>(out)[e] = r[e];
+  }
+}
+
+enum ShapeId { kLarge, kMiddle, kSmall, kShapes };
+struct ShapeInfo {
+  int tm, tn, per_cu;
+  float slab_us;  // a slab of the tiles that share a CU
+};
+constexpr ShapeInfo kShape[kShapes] = {{256, 256, 1, 1.72f}, {192, 256, 1, 1.40f}, {128, 128, 2, 1.05f}};
+constexpr int kCus = 256;
+constexpr int kMaxSplits = 16;
+
+struct Plan {
+  int shape, splits;
+};
+
+// The tiles and splits that take the least time by the rounds of the launch, the
+// slabs of a round and the traffic of the splits' sums.  Both sides measured, us on
+// 256-square / 192 x 256 / 128-square tiles: weight gradients of 16384 tokens, 2048 x
+// 5632, 774 / 690 / 843 (352 tiles of the first are two rounds of 256, the second of
+// them 3/8 full); its dx 606 / 739 / 802; forward of 2048 tokens, 768 x 2048, 24 / - /
+// 19.  Splits 1 / 2 / 4 / 8 of the dx of 512 tokens, 2048 x 5632: 138 / 79 / 52 / 47.
+Plan plan_of(int mode, int64_t m, int64_t n, int64_t k) {
+  const bool dual = mode == kForward || mode == kInner;
+  const int64_t planes = mode == kPair ? 2 : 1;
+  const int64_t slabs = (k + kSlab - 1) / kSlab * (mode == kSum ? 2 : 1);
+  Plan best = {kSmall, 1};
+  double least = 1e30;
+  for (int s = 0; s < kShapes; ++s) {
+    const ShapeInfo& h = kShape[s];
+    const int64_t tiles = ((m + h.tm - 1) / h.tm) * ((n * (dual ? 2 : 1) + h.tn - 1) / h.tn) * planes;
+    for (int p = 1; p <= (dual ? 1 : kMaxSplits) && (p == 1 || p * 4 <= slabs); ++p) {
+      const int64_t rounds = (tiles * p + kCus * h.per_cu - 1) / (kCus * h.per_cu);
+      double us = rounds * ((double)((slabs + p - 1) / p) * h.slab_us + 4.0);
+      if (p > 1) us += 6.0 + (double)p * planes * m * n * 8 / 3e6;
+      if (us < least) {
+        least = us;
+        best = {s, p};
+      }
+    }
+  }
+  return best;
+}
+
 template <int MODE, int ACT, class C>
 void launch_shape(TileArgs& t, hipStream_t st) {
   constexpr int kCols = MODE == kForward || MODE == kInner ? C::TN / 2 : C::TN;
   t.tiles_m = (int)((t.g.m + C::TM - 1) / C::TM);
   t.tiles_n = (int)((t.g.n + kCols - 1) / kCols);
-  t.tiles = t.tiles_m * t.tiles_n * (MODE == kPair ? 2 : 1);
+  t.tiles = t.tiles_m * t.tiles_n * t.planes * t.splits;
   hipLaunchKernelGGL((ffn_tile_kernel<MODE, ACT, C>), dim3(t.tiles), dim3(C::threads), 0, st, t);
+  if (t.splits > 1)
+    hipLaunchKernelGGL(ffn_join_kernel, dim3((unsigned)((t.planes * t.g.m * t.g.n / 4 + 255) / 256)), dim3(256), 0, st,
+                       t);
 }
 
 template <int MODE, int ACT>
-hipError_t launch_mode(const FfnArgs& g, hipStream_t st) {
+hipError_t launch_mode(const FfnArgs& g, float* partial, hipStream_t st) {
   if (g.m == 0 || g.n == 0) return hipSuccess;
   TileArgs t;
   t.g = g;
   const auto vec = [](const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && (ld & 7) == 0; };
   t.vec_out = vec(g.out[0], g.ld_out) && (!g.out[1] || vec(g.out[1], g.ld_out));
   t.vec_dh = MODE == kInner && vec(g.dh, g.ld_dh);
-  const int64_t cols = MODE == kForward || MODE == kInner ? 128 : 256;
-  const int64_t large = ((g.m + 255) / 256) * ((g.n + cols - 1) / cols) * (MODE == kPair ? 2 : 1);
-  if (large >= 200) launch_shape<MODE, ACT, Large>(t, st);
+  Plan p = plan_of(MODE, g.m, g.n, g.k);
+#ifdef FORCE
+  FORCE
+#endif
+  t.planes = MODE == kPair ? 2 : 1;
+  t.splits = p.splits;
+  t.partial = partial;
+  if (p.shape == kLarge) launch_shape<MODE, ACT, Large>(t, st);
+  else if (p.shape == kMiddle) launch_shape<MODE, ACT, Middle>(t, st);
   else launch_shape<MODE, ACT, Small>(t, st);
   return hipGetLastError();
 }
 
 template <int ACT>
-hipError_t launch_act(FfnMode mode, const FfnArgs& g, hipStream_t st) {
+hipError_t launch_act(FfnMode mode, const FfnArgs& g, float* partial, hipStream_t st) {
   switch (mode) {
-    case kForward: return launch_mode<kForward, ACT>(g, st);
-    case kInner: return launch_mode<kInner, ACT>(g, st);
+    case kForward: return launch_mode<kForward, ACT>(g, partial, st);
+    case kInner: return launch_mode<kInner, ACT>(g, partial, st);
     // (these two apply no activation)
-    case kSum: return launch_mode<kSum, ISOLOCO_ACT_SILU>(g, st);
-    default: return launch_mode<kPair, ISOLOCO_ACT_SILU>(g, st);
+    case kSum: return launch_mode<kSum, ISOLOCO_ACT_SILU>(g, partial, st);
+    default: return launch_mode<kPair, ISOLOCO_ACT_SILU>(g, partial, st);
   }
 }
 
 }  // namespace
 
-hipError_t launch_ffn_tiles(FfnMode mode, int act, const FfnArgs& g, hipStream_t st) {
-  return act == ISOLOCO_ACT_SILU ? launch_act<ISOLOCO_ACT_SILU>(mode, g, st) : launch_act<ISOLOCO_ACT_GELU>(mode, g, st);
+size_t ffn_partial_bytes(FfnMode mode, int64_t m, int64_t n, int64_t k) {
+  const Plan p = plan_of(mode, m, n, k);
+  return p.splits > 1 ? (size_t)p.splits * (mode == kPair ? 2 : 1) * m * n * sizeof(float) : 0;
+}
+
+hipError_t launch_ffn_tiles(FfnMode mode, int act, const FfnArgs& g, float* partial, hipStream_t st) {
+  return act == ISOLOCO_ACT_SILU ? launch_act<ISOLOCO_ACT_SILU>(mode, g, partial, st)
+                                 : launch_act<ISOLOCO_ACT_GELU>(mode, g, partial, st);
 }
 
 }  // namespace isoloco

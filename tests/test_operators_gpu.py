@@ -594,6 +594,36 @@ def test_gated_ffn_backward(iso, tokens, dim, hidden, dtype, act):
     assert only[0] is None and torch.equal(only[1], first[1]) and torch.equal(only[2], first[2])
 
 
+# Sizes at which every tile shape of the bfloat16 products and their splits are the
+# ones that a rule by the launch's rounds picks (256-square tiles: the first two
+# forwards, the third's dx, the fourth's weights; 192 x 256: the fifth's forward, the
+# sixth's weights, the last's dx; 128-square ones with up to 16 splits: the others).
+FFN_TILES = [(6200, 136, 1000), (3000, 264, 4400), (8192, 2048, 256), (256, 2048, 4096), (4100, 520, 2056),
+             (64, 2048, 5632), (700, 1032, 3000), (6144, 2048, 200)]
+
+
+@pytest.mark.parametrize("tokens,dim,hidden", FFN_TILES)
+def test_gated_ffn_tiles(iso, tokens, dim, hidden):
+    x, wg, wu, dh = (t.cuda() for t in ffn_inputs(tokens, dim, hidden, BF16, 11))
+    out = iso.gated_ffn(x, wg, wu).cpu()
+    grads = [t.cpu() for t in iso.gated_ffn_backward(x, wg, wu, dh)]
+    # the same bounds as above, in float64 on the GPU
+    g, u, a, da, eg, eu, ea = ffn_reference(x, wg, wu, "silu")
+    X, G, W, D = (t.double() for t in (x, wg, wu, dh))
+    within(out, (a * u).cpu(), (ea * u.abs() + a.abs() * eu + ea * eu + ROUND[BF16] * (a * u).abs() + 1e-37).cpu())
+    dg, du = D * u * da, D * a
+    edg = D.abs() * ((da.abs() + 1e-6) * eu + u.abs() * (0.8 * eg + 16 * U32) + 0.8 * eg * eu) + ROUND[BF16] * dg.abs()
+    edu = D.abs() * ea + ROUND[BF16] * du.abs()
+    nk, nt = (2 * hidden + 8) * U32, (tokens + 8) * U32
+    want = [dg @ G + du @ W, dg.T @ X, du.T @ X]
+    bound = [edg @ G.abs() + edu @ W.abs() + nk * (dg.abs() @ G.abs() + du.abs() @ W.abs()),
+             edg.T @ X.abs() + nt * (dg.abs().T @ X.abs()), edu.T @ X.abs() + nt * (du.abs().T @ X.abs())]
+    for r, w, b in zip(grads, want, bound):
+        within(r, w.cpu(), (1.01 * b + ROUND[BF16] * w.abs() + 1e-37).cpu())
+        # the rounding of da and du and of the result, as random errors: far below the bound's worst case
+        assert ((r.cuda().double() - w).norm() / w.norm()).item() <= 2.0 ** -8
+
+
 def test_gated_ffn_no_tokens(iso):
     w = torch.ones(6, 4, device="cuda")
     x = torch.empty(0, 4, device="cuda")
