@@ -436,9 +436,20 @@ typedef enum {
 } isoloco_activation;
 
 /* out = act(x w_gate^T) * (x w_up^T); x: tokens x dim, w_gate and w_up: hidden x
- * dim (both ld_w apart), out: tokens x hidden; one dtype. */
+ * dim (both ld_w apart), out: tokens x hidden; one dtype.  float32 products are
+ * formed from three bfloat16 parts of each operand, all six products of order
+ * 2^-16 and above (about float32 accuracy; an infinite operand gives NaN), or, for
+ * up to 64 tokens forward, in float32.
+ *
+ * The workspace's size goes by the call: ISOLOCO_FFN_BACKWARD for the gradient,
+ * ISOLOCO_FFN_ALIGNED where the rows of x and of both weights will be 16-byte
+ * aligned in bfloat16 (ld a multiple of 8), which saves their copies.  Extents
+ * below 2^22. */
+#define ISOLOCO_FFN_BACKWARD 1
+#define ISOLOCO_FFN_ALIGNED 2
+
 isoloco_status isoloco_gated_ffn_workspace_size(int64_t tokens, int64_t dim, int64_t hidden, int32_t dtype,
-                                                int32_t backward, size_t* bytes);
+                                                int32_t flags, size_t* bytes);
 isoloco_status isoloco_gated_ffn(const void* x, int64_t ld_x, const void* w_gate, const void* w_up, int64_t ld_w,
                                  int32_t dtype, int64_t tokens, int64_t dim, int64_t hidden, int32_t act, void* out,
                                  int64_t ld_out, void* workspace, size_t workspace_bytes, void* hip_stream);

@@ -29,6 +29,7 @@ __all__ = [
     "isoloco_token_logprobs_workspace_size", "isoloco_token_logprobs", "isoloco_token_logprobs_backward",
     "isoloco_gated_ffn_workspace_size", "isoloco_gated_ffn", "isoloco_gated_ffn_backward",
     "ISOLOCO_I32", "ISOLOCO_I64", "ISOLOCO_ACT_SILU", "ISOLOCO_ACT_GELU", "ISOLOCO_MAX_TOP",
+    "ISOLOCO_FFN_BACKWARD", "ISOLOCO_FFN_ALIGNED",
 ]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libisoloco.so")
@@ -63,6 +64,8 @@ ISOLOCO_I64 = 1
 ISOLOCO_ACT_SILU = 0
 ISOLOCO_ACT_GELU = 1
 ISOLOCO_MAX_TOP = 32
+ISOLOCO_FFN_BACKWARD = 1
+ISOLOCO_FFN_ALIGNED = 2
 
 EXPORTED_SYMBOLS = (
     "isoloco_plan", "isoloco_workspace_size", "isoloco_set_workspace", "isoloco_aggregate",

@@ -22,97 +22,163 @@ namespace isoloco {
 namespace {
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
+typedef floatx4 floatx4_any __attribute__((aligned(4)));
 
-constexpr int kTile = 64, kStep = 32, kThreads = 256;
+// ---------------------------------------------------------------------------
+// Few tokens
+// ---------------------------------------------------------------------------
+//
+// A product of few rows is bounded by the weights' bytes: every weight is loaded once,
+// from memory into the registers that the MFMA reads (16 hidden rows against 16
+// tokens), and the workgroup's waves split dim so that enough loads are in flight.
 
-// A tile of 64 rows x 32 k in LDS, zeros past the operand's end.
+// The values of k that a lane holds of one row, 16 bytes: its MFMA operands.
 template <typename T>
-struct Tile {
-  // the padding spreads a column's rows over the banks and keeps bfloat16 rows 16-byte aligned
-  static constexpr int kPitch = sizeof(T) == 2 ? kStep + 8 : kStep + 1;
-  T v[kTile * kPitch];
-  __device__ __forceinline__ void load(const Operand& o, int64_t row0, int64_t rows, int64_t k0, int64_t ks) {
-    const T* p = static_cast<const T*>(o.p);
-    if (o.ks == 1) {
-      const int r = threadIdx.x >> 2, c = (threadIdx.x & 3) * 8;
-      const T* at = p + (row0 + r) * o.rs + k0 + c;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[r * kPitch + c + e] = row0 + r < rows && k0 + c + e < ks ? at[e] : (T)0.f;
+struct Lane {
+  static constexpr int N = 16 / sizeof(T);
+  T v[N];
+  __device__ __forceinline__ void load(const T* p, int64_t left) {
+    if (left >= N) {
+      *reinterpret_cast<u32x4*>(v) = *reinterpret_cast<const u32x4_any*>(p);
     } else {
-      const int c = threadIdx.x >> 3, r = (threadIdx.x & 7) * 8;
-      const T* at = p + (k0 + c) * o.ks + row0 + r;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[(r + e) * kPitch + c] = row0 + r + e < rows && k0 + c < ks ? at[e] : (T)0.f;
+      for (int e = 0; e < N; ++e) v[e] = e < left ? p[e] : (T)0.f;
     }
   }
 };
-
-template <typename T>
-__device__ __forceinline__ void multiply(floatx16& acc, const Tile<T>& a, const Tile<T>& b, int i0, int j0) {
-  const int lane = threadIdx.x & 63, row = lane & 31, half = lane >> 5;
-  const T* pa = a.v + (i0 + row) * Tile<T>::kPitch;
-  const T* pb = b.v + (j0 + row) * Tile<T>::kPitch;
-  if constexpr (sizeof(T) == 2) {
+__device__ __forceinline__ floatx4 multiply(const Lane<__bf16>& a, const Lane<__bf16>& b, floatx4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(*reinterpret_cast<const bf16x8_t*>(a.v),
+                                                 *reinterpret_cast<const bf16x8_t*>(b.v), c, 0, 0, 0);
+}
+// (which k a lane's e-th value stands for is the same in both operands)
+__device__ __forceinline__ floatx4 multiply(const Lane<float>& a, const Lane<float>& b, floatx4 c) {
 #pragma unroll
-    for (int k = 0; k < kStep; k += 16)
-      acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8_t*>(pa + k + 8 * half),
-                                                    *reinterpret_cast<const bf16x8_t*>(pb + k + 8 * half), acc, 0, 0, 0);
-  } else {
-#pragma unroll
-    for (int k = 0; k < kStep; k += 2)
-      acc = __builtin_amdgcn_mfma_f32_32x32x2f32(pa[k + half], pb[k + half], acc, 0, 0, 0);
-  }
+  for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[e], b.v[e], c, 0, 0, 0);
+  return c;
 }
 
-// Any sizes, strides and alignments: 64 x 64 outputs per workgroup, 32 x 32 per wave.
-template <typename T, int MODE, int ACT>
-__global__ void __launch_bounds__(kThreads) ffn_any_kernel(FfnArgs g) {
-  constexpr bool DUAL = MODE == kForward || MODE == kInner;
-  __shared__ Tile<T> sa, sb[DUAL ? 2 : 1];
-  const int64_t row0 = (int64_t)blockIdx.y * kTile, col0 = (int64_t)blockIdx.x * kTile;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i0 = (wave >> 1) * 32, j0 = (wave & 1) * 32;
-  floatx16 acc[DUAL ? 2 : 1] = {};
-  for (int part = 0; part < (MODE == kSum ? 2 : 1); ++part) {
-    const Operand& a = MODE == kPair ? g.a[blockIdx.z] : g.a[part];
-    for (int64_t k0 = 0; k0 < g.k; k0 += kStep) {
-      __syncthreads();
-      sa.load(a, row0, g.m, k0, g.k);
-      sb[0].load(g.b[part], col0, g.n, k0, g.k);
-      if constexpr (DUAL) sb[1].load(g.b[1], col0, g.n, k0, g.k);
-      __syncthreads();
-      multiply(acc[0], sa, sb[0], i0, j0);
-      if constexpr (DUAL) multiply(acc[1], sa, sb[1], i0, j0);
-    }
-  }
-  const int64_t j = col0 + j0 + (lane & 31);
-  if (j >= g.n) return;
+constexpr int kFewWaves = 8;
+constexpr int kFewMost = 64;  // tokens
+
+// 16 hidden rows per workgroup, up to 16 NT tokens.
+template <typename T, int ACT, int NT>
+__global__ void __launch_bounds__(64 * kFewWaves) ffn_few_kernel(const T* x, int64_t ld_x, const T* wg, const T* wu,
+                                                                int64_t ld_w, int tokens, int64_t dim, int64_t hidden,
+                                                                T* out, int64_t ld_out) {
+  constexpr int N = Lane<T>::N, kStep = 4 * N;  // k values of one step
+  __shared__ floatx4 sums[kFewWaves][2 * NT][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, kl = (lane >> 4) * N;
+  const int64_t h0 = (int64_t)blockIdx.x * 16;
+  // rows past the matrices are their last ones again: their outputs are not stored
+  const int64_t h = min(h0 + row, hidden - 1);
+  const T* pg = wg + h * ld_w + kl;
+  const T* pu = wu + h * ld_w + kl;
+  const T* px[NT];
 #pragma unroll
-  for (int e = 0; e < 16; ++e) {
-    const int64_t i = row0 + i0 + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3);
-    if (i >= g.m) continue;
-    T* out = static_cast<T*>(g.out[MODE == kPair ? blockIdx.z : 0]) + i * g.ld_out + j;
-    if constexpr (DUAL) {
-      float a, da;
-      activate<ACT>(acc[0][e], a, da);
-      if constexpr (MODE == kForward) {
-        *out = (T)(a * acc[1][e]);
-      } else {
-        const float dh = (float)static_cast<const T*>(g.dh)[i * g.ld_dh + j];
-        *out = (T)(dh * acc[1][e] * da);
-        static_cast<T*>(g.out[1])[i * g.ld_out + j] = (T)(dh * a);
+  for (int n = 0; n < NT; ++n) px[n] = x + (int64_t)min(16 * n + row, tokens - 1) * ld_x + kl;
+  floatx4 g[NT] = {}, u[NT] = {};
+  // kAhead steps' loads are in flight at a time
+  constexpr int kAhead = 4;
+  constexpr int64_t kStride = kFewWaves * kStep;
+  int64_t k = (int64_t)wave * kStep;
+  for (; k + (kAhead - 1) * kStride + kStep <= dim; k += kAhead * kStride) {
+    Lane<T> a[kAhead], b[kAhead], c[kAhead][NT];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      a[i].load(pg + k + i * kStride, N);
+      b[i].load(pu + k + i * kStride, N);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) c[i][n].load(px[n] + k + i * kStride, N);
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        g[n] = multiply(a[i], c[i][n], g[n]);
+        u[n] = multiply(b[i], c[i][n], u[n]);
       }
-    } else {
-      *out = (T)acc[0][e];
+  }
+  for (; k < dim; k += kStride) {
+    const int64_t left = dim - k - kl;
+    Lane<T> a, b, c;
+    a.load(pg + k, left);
+    b.load(pu + k, left);
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      c.load(px[n] + k, left);
+      g[n] = multiply(a, c, g[n]);
+      u[n] = multiply(b, c, u[n]);
     }
+  }
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    sums[wave][2 * n][lane] = g[n];
+    sums[wave][2 * n + 1][lane] = u[n];
+  }
+  __syncthreads();
+  // lane l holds hidden rows 4 (l / 16) .. + 3 of token l % 16; wave n finishes 16 tokens
+  if (wave >= NT) return;
+  floatx4 gate = {}, up = {};
+  for (int w = 0; w < kFewWaves; ++w) {
+    gate += sums[w][2 * wave][lane];
+    up += sums[w][2 * wave + 1][lane];
+  }
+  const int t = 16 * wave + (lane & 15);
+  if (t >= tokens) return;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int64_t j = h0 + 4 * (lane >> 4) + e;
+    float f, df;
+    activate<ACT, sizeof(T) == 4>(gate[e], f, df);
+    if (j < hidden) out[(int64_t)t * ld_out + j] = (T)(f * up[e]);
   }
 }
 
-template <typename T, int MODE, int ACT>
-hipError_t launch_any(const FfnArgs& g, hipStream_t st) {
-  if (g.m == 0 || g.n == 0) return hipSuccess;
-  const dim3 grid((unsigned)((g.n + kTile - 1) / kTile), (unsigned)((g.m + kTile - 1) / kTile), MODE == kPair ? 2 : 1);
-  hipLaunchKernelGGL((ffn_any_kernel<T, MODE, ACT>), grid, dim3(kThreads), 0, st, g);
-  return hipGetLastError();
+// ---------------------------------------------------------------------------
+// Copies for the tile products
+// ---------------------------------------------------------------------------
+
+struct CopyArgs {
+  const void* src[3];
+  uint16_t* dst[3];
+  int64_t rows[3], ld_src[3];
+  int64_t cols, ld_dst;
+  int n;
+};
+
+// Matrices as bfloat16 with rows of ld_dst = ffn_pad(cols), zeros past cols; float32 as
+// three parts, one after the other.  One thread per 8 elements of a row.
+template <typename T>
+__global__ void __launch_bounds__(256) ffn_copy_kernel(CopyArgs c) {
+  const int m = blockIdx.y;
+  const int64_t per_row = c.ld_dst / 8, rows = c.rows[m];
+  const T* src = static_cast<const T*>(c.src[m]);
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * per_row; i += (int64_t)gridDim.x * 256) {
+    const int64_t row = i / per_row, col = (i - row * per_row) * 8;
+    const T* p = src + row * c.ld_src[m] + col;
+    const int64_t left = c.cols - col;
+    uint16_t* q = c.dst[m] + row * c.ld_dst + col;
+    if constexpr (sizeof(T) == 2) {
+      Lane<__bf16> v;
+      v.load(p, left);
+      *reinterpret_cast<u32x4*>(q) = *reinterpret_cast<const u32x4*>(v.v);
+    } else {
+      Lane<float> v[2];
+      v[0].load(p, left);
+      v[1].load(p + 4, left - 4);
+#pragma unroll
+      for (int part = 0; part < kFfnParts; ++part) {
+        bf16x8_t b;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          b[e] = (__bf16)v[e / 4].v[e % 4];
+          v[e / 4].v[e % 4] -= (float)b[e];
+        }
+        *reinterpret_cast<bf16x8_t*>(q + part * rows * c.ld_dst) = b;
+      }
+    }
+  }
 }
 
 struct FfnShape {
@@ -120,97 +186,183 @@ struct FfnShape {
   int32_t dtype, act;
 };
 
-// The backward workspace: da, du, and the sums of a split product.
-size_t inner_bytes(const FfnShape& s) {
-  return 2 * (size_t)ffn_pad(s.tokens) * (size_t)ffn_pad(s.hidden) * dtype_bytes(s.dtype);
-}
-size_t ffn_workspace(const FfnShape& s, bool backward) {
-  if (!backward) return 0;
-  size_t partial = 0;
-  if (s.dtype == ISOLOCO_BF16)
-    partial = std::max(ffn_partial_bytes(kSum, s.tokens, s.dim, s.hidden),
-                       ffn_partial_bytes(kPair, s.hidden, s.dim, s.tokens));
-  return inner_bytes(s) + partial;
+// What a call hands to the tile products, and where its copies lie in the workspace.
+struct FfnPlan {
+  bool few;                        // ffn_few_kernel
+  bool copy_x, copy_w;             // operands that the tiles do not read where they are
+  size_t x, wg, wu, da, du, partial, bytes;  // offsets in the workspace
+};
+
+// the tile products load whole 16-byte pieces of rows
+bool tile_rows(const void* p, int64_t ld) { return aligned_to(p, 16) && (ld & 7) == 0 && ld <= (1 << 22); }
+
+// `x_ok`, `w_ok`: the operand may be read where it is.
+FfnPlan plan_of(const FfnShape& s, bool backward, bool x_ok, bool w_ok) {
+  FfnPlan p = {};
+  const bool f32 = s.dtype == ISOLOCO_F32;
+  p.few = !backward && s.tokens <= kFewMost;
+  if (p.few) return p;
+  p.copy_x = f32 || !x_ok || (s.dim & 7);
+  p.copy_w = f32 || !w_ok || (s.dim & 7);
+  const size_t parts = f32 ? kFfnParts : 1, row = 2 * (size_t)ffn_pad(s.dim) * parts;
+  const auto take = [&](size_t bytes) {
+    const size_t at = p.bytes;
+    p.bytes += (bytes + 255) / 256 * 256;
+    return at;
+  };
+  if (p.copy_x) p.x = take(row * s.tokens);
+  if (p.copy_w) {
+    p.wg = take(row * s.hidden);
+    p.wu = take(row * s.hidden);
+  }
+  if (backward) {
+    const size_t inner = 2 * (size_t)ffn_pad(s.tokens) * (size_t)ffn_pad(s.hidden) * parts;
+    p.da = take(inner);
+    p.du = take(inner);
+    p.partial = take(std::max(ffn_partial_bytes(kSum, f32, s.tokens, s.dim, s.hidden),
+                              ffn_partial_bytes(kPair, f32, s.hidden, s.dim, s.tokens)));
+  }
+  return p;
 }
 
-// the tile kernels load whole 16-byte pieces of rows, at offsets of 32 bits from a tile's first
-bool tile_rows(const void* p, int64_t ld) { return aligned_to(p, 16) && (ld & 7) == 0 && ld <= (1 << 20); }
+template <typename T, int ACT, int NT>
+void launch_few(const FfnShape& s, const void* x, int64_t ld_x, const void* wg, const void* wu, int64_t ld_w, void* out,
+                int64_t ld_out, hipStream_t st) {
+  hipLaunchKernelGGL((ffn_few_kernel<T, ACT, NT>), dim3((unsigned)((s.hidden + 15) / 16)), dim3(64 * kFewWaves), 0, st,
+                     static_cast<const T*>(x), ld_x, static_cast<const T*>(wg), static_cast<const T*>(wu), ld_w,
+                     (int)s.tokens, s.dim, s.hidden, static_cast<T*>(out), ld_out);
+}
 
+// The operands of the tile products, copied where they have to be.
+struct TileOperands {
+  const uint16_t *x, *wg, *wu;
+  int64_t ld_x, ld_w, part_x, part_w;
+  int64_t k;  // dim, padded if both are copies
+};
 template <typename T>
-bool on_tiles(const FfnShape& s, const void* x, int64_t ld_x, const void* wg, const void* wu, int64_t ld_w) {
-  return sizeof(T) == 2 && (s.dim & 7) == 0 && tile_rows(x, ld_x) && tile_rows(wg, ld_w) && tile_rows(wu, ld_w);
+TileOperands copy_operands(const FfnShape& s, const FfnPlan& p, const void* x, int64_t ld_x, const void* wg,
+                           const void* wu, int64_t ld_w, char* ws, hipStream_t st) {
+  const int64_t ld = ffn_pad(s.dim);
+  TileOperands o = {static_cast<const uint16_t*>(x), static_cast<const uint16_t*>(wg), static_cast<const uint16_t*>(wu),
+                    ld_x, ld_w, s.tokens * ld, s.hidden * ld, p.copy_x && p.copy_w ? ld : s.dim};
+  CopyArgs c = {};
+  c.cols = s.dim;
+  c.ld_dst = ld;
+  const auto add = [&](const uint16_t*& from, int64_t& ld_from, int64_t rows, size_t at) {
+    c.src[c.n] = from;
+    c.ld_src[c.n] = ld_from;
+    c.rows[c.n] = rows;
+    c.dst[c.n++] = reinterpret_cast<uint16_t*>(ws + at);
+    from = reinterpret_cast<const uint16_t*>(ws + at);
+  };
+  if (p.copy_x) add(o.x, o.ld_x, s.tokens, p.x);
+  if (p.copy_w) {
+    add(o.wg, o.ld_w, s.hidden, p.wg);
+    add(o.wu, o.ld_w, s.hidden, p.wu);
+  }
+  if (p.copy_x) o.ld_x = ld;
+  if (p.copy_w) o.ld_w = ld;
+  if (c.n) {
+    const int64_t items = std::max(p.copy_x ? s.tokens : 0, p.copy_w ? s.hidden : 0) * (ld / 8);
+    const unsigned grid = (unsigned)std::min<int64_t>((items + 255) / 256, 1 << 20);
+    if (grid) hipLaunchKernelGGL(ffn_copy_kernel<T>, dim3(grid, c.n), dim3(256), 0, st, c);
+  }
+  return o;
 }
 
 template <typename T, int ACT>
 hipError_t run_forward(const FfnShape& s, const void* x, int64_t ld_x, const void* wg, const void* wu, int64_t ld_w,
-                       void* out, int64_t ld_out, hipStream_t st) {
+                       void* out, int64_t ld_out, void* ws, hipStream_t st) {
+  const FfnPlan p = plan_of(s, false, tile_rows(x, ld_x), tile_rows(wg, ld_w) && tile_rows(wu, ld_w));
+  if (p.few) {
+    if (s.tokens <= 16) launch_few<T, ACT, 1>(s, x, ld_x, wg, wu, ld_w, out, ld_out, st);
+    else if (s.tokens <= 32) launch_few<T, ACT, 2>(s, x, ld_x, wg, wu, ld_w, out, ld_out, st);
+    else launch_few<T, ACT, 4>(s, x, ld_x, wg, wu, ld_w, out, ld_out, st);
+    return hipGetLastError();
+  }
+  const TileOperands o = copy_operands<T>(s, p, x, ld_x, wg, wu, ld_w, static_cast<char*>(ws), st);
   FfnArgs g = {};
-  g.a[0] = {x, ld_x, 1};
-  g.b[0] = {wg, ld_w, 1};
-  g.b[1] = {wu, ld_w, 1};
+  g.a[0] = o.x;
+  g.b[0] = o.wg;
+  g.b[1] = o.wu;
+  g.ld_a = o.ld_x;
+  g.ld_b = o.ld_w;
+  g.part_a = o.part_x;
+  g.part_b = o.part_w;
   g.m = s.tokens;
   g.n = s.hidden;
-  g.k = s.dim;
+  g.k = o.k;
   g.out[0] = out;
   g.ld_out = ld_out;
-  if (on_tiles<T>(s, x, ld_x, wg, wu, ld_w)) return launch_ffn_tiles(kForward, ACT, g, nullptr, st);
-  return launch_any<T, kForward, ACT>(g, st);
+  return launch_ffn_tiles(kForward, ACT, sizeof(T) == 4, g, st);
 }
 
 template <typename T, int ACT>
 hipError_t run_backward(const FfnShape& s, const void* x, int64_t ld_x, const void* wg, const void* wu, int64_t ld_w,
                         const void* dout, int64_t ld_dout, void* dx, int64_t ld_dx, void* dwg, void* dwu,
                         int64_t ld_dw, void* ws, hipStream_t st) {
-  const int64_t ld = ffn_pad(s.hidden);
-  T* da = static_cast<T*>(ws);
-  T* du = da + ffn_pad(s.tokens) * ld;
-  float* partial = reinterpret_cast<float*>(static_cast<char*>(ws) + inner_bytes(s));
-  const bool tiles = on_tiles<T>(s, x, ld_x, wg, wu, ld_w);
+  constexpr bool f32 = sizeof(T) == 4;
+  char* base = static_cast<char*>(ws);
+  const FfnPlan p = plan_of(s, true, tile_rows(x, ld_x), tile_rows(wg, ld_w) && tile_rows(wu, ld_w));
+  const TileOperands o = copy_operands<T>(s, p, x, ld_x, wg, wu, ld_w, base, st);
+  const int64_t ld = ffn_pad(s.hidden), part = ffn_pad(s.tokens) * ld, cols = ffn_pad(s.dim);
+  uint16_t* da = reinterpret_cast<uint16_t*>(base + p.da);
+  uint16_t* du = reinterpret_cast<uint16_t*>(base + p.du);
   FfnArgs g = {};
-  g.a[0] = {x, ld_x, 1};
-  g.b[0] = {wg, ld_w, 1};
-  g.b[1] = {wu, ld_w, 1};
+  g.a[0] = o.x;
+  g.b[0] = o.wg;
+  g.b[1] = o.wu;
+  g.ld_a = o.ld_x;
+  g.ld_b = o.ld_w;
+  g.part_a = o.part_x;
+  g.part_b = o.part_w;
   g.m = s.tokens;
   g.n = s.hidden;
-  g.k = s.dim;
+  g.k = o.k;
   g.out[0] = da;
   g.out[1] = du;
   g.ld_out = ld;
+  g.part_out = part;
   g.dh = dout;
   g.ld_dh = ld_dout;
-  hipError_t e = tiles ? launch_ffn_tiles(kInner, ACT, g, partial, st) : launch_any<T, kInner, ACT>(g, st);
+  hipError_t e = launch_ffn_tiles(kInner, ACT, f32, g, st);
+  g = {};
+  g.a[0] = da;
+  g.a[1] = du;
+  g.ld_a = ld;
+  g.part_a = part;
+  g.n = s.dim;
+  g.partial = reinterpret_cast<float*>(base + p.partial);
   if (e == hipSuccess && dx) {
-    g = {};
-    g.a[0] = {da, ld, 1};
-    g.a[1] = {du, ld, 1};
-    g.b[0] = {wg, 1, ld_w};
-    g.b[1] = {wu, 1, ld_w};
+    g.b[0] = o.wg;
+    g.b[1] = o.wu;
+    g.ld_b = o.ld_w;
+    g.part_b = o.part_w;
+    g.cols_b = p.copy_w ? cols : s.dim;
     g.m = s.tokens;
-    g.n = s.dim;
     g.k = s.hidden;
     g.out[0] = dx;
     g.ld_out = ld_dx;
-    e = tiles ? launch_ffn_tiles(kSum, ACT, g, partial, st) : launch_any<T, kSum, ACT>(g, st);
+    e = launch_ffn_tiles(kSum, ACT, f32, g, st);
   }
   if (e == hipSuccess && dwg) {
-    g = {};
-    g.a[0] = {da, 1, ld};
-    g.a[1] = {du, 1, ld};
-    g.b[0] = {x, 1, ld_x};
+    g.b[0] = g.b[1] = o.x;
+    g.ld_b = o.ld_x;
+    g.part_b = o.part_x;
+    g.cols_b = p.copy_x ? cols : s.dim;
     g.m = s.hidden;
-    g.n = s.dim;
     g.k = s.tokens;
     g.out[0] = dwg;
     g.out[1] = dwu;
     g.ld_out = ld_dw;
-    e = tiles ? launch_ffn_tiles(kPair, ACT, g, partial, st) : launch_any<T, kPair, ACT>(g, st);
+    e = launch_ffn_tiles(kPair, ACT, f32, g, st);
   }
   return e;
 }
 
 isoloco_status check_shape(const FfnShape& s) {
-  // the tiles of a launch are counted in 32 bits, those of its rows in 16
-  constexpr int64_t most = (int64_t)65535 * kTile;
+  // a tile's rows are addressed with offsets of 32 bits: 256 rows of 2 bytes times this
+  constexpr int64_t most = ((int64_t)1 << 22) - kFfnPad;
   if (s.tokens < 0 || s.tokens > most || s.dim < 1 || s.dim > most || s.hidden < 1 || s.hidden > most)
     return fail(ISOLOCO_ERR_INVALID_ARG, "%lld tokens, dim %lld, hidden %lld", (long long)s.tokens, (long long)s.dim,
                 (long long)s.hidden);
@@ -253,11 +405,13 @@ using namespace isoloco;
 extern "C" {
 
 isoloco_status isoloco_gated_ffn_workspace_size(int64_t tokens, int64_t dim, int64_t hidden, int32_t dtype,
-                                                int32_t backward, size_t* bytes) {
+                                                int32_t flags, size_t* bytes) {
   if (!bytes) return fail(ISOLOCO_ERR_INVALID_ARG, "bytes is NULL");
   const FfnShape s = {tokens, dim, hidden, dtype, ISOLOCO_ACT_SILU};
   ISOLOCO_TRY(check_shape(s));
-  *bytes = ffn_workspace(s, backward != 0);
+  if (flags & ~(ISOLOCO_FFN_BACKWARD | ISOLOCO_FFN_ALIGNED)) return fail(ISOLOCO_ERR_INVALID_ARG, "flags = %d", flags);
+  const bool ok = flags & ISOLOCO_FFN_ALIGNED;
+  *bytes = plan_of(s, flags & ISOLOCO_FFN_BACKWARD, ok, ok).bytes;
   return ISOLOCO_OK;
 }
 
@@ -267,7 +421,7 @@ isoloco_status isoloco_gated_ffn(const void* x, int64_t ld_x, const void* w_gate
   const FfnShape s = {tokens, dim, hidden, dtype, act};
   ISOLOCO_TRY(check_shape(s));
   if (tokens == 0) return ISOLOCO_OK;
-  const size_t e = dtype_bytes(dtype), need = ffn_workspace(s, false);
+  const size_t e = dtype_bytes(dtype), need = plan_of(s, false, tile_rows(x, ld_x), tile_rows(w_gate, ld_w) && tile_rows(w_up, ld_w)).bytes;
   ISOLOCO_TRY(check_matrix("x", x, tokens, dim, ld_x, e));
   ISOLOCO_TRY(check_matrix("w_gate", w_gate, hidden, dim, ld_w, e));
   ISOLOCO_TRY(check_matrix("w_up", w_up, hidden, dim, ld_w, e));
@@ -278,7 +432,7 @@ isoloco_status isoloco_gated_ffn(const void* x, int64_t ld_x, const void* w_gate
   const Range ins[] = {{"x", x, matrix_bytes(tokens, dim, ld_x, e)}, {"w_gate", w_gate, wb}, {"w_up", w_up, wb}};
   ISOLOCO_TRY(check_apart(outs, ins));
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  const hipError_t r = BY_TYPES(run_forward, s, x, ld_x, w_gate, w_up, ld_w, out, ld_out, st);
+  const hipError_t r = BY_TYPES(run_forward, s, x, ld_x, w_gate, w_up, ld_w, out, ld_out, workspace, st);
   return r == hipSuccess ? ISOLOCO_OK : hip_fail(r, "gated feed-forward block");
 }
 
@@ -289,7 +443,7 @@ isoloco_status isoloco_gated_ffn_backward(const void* x, int64_t ld_x, const voi
                                           size_t workspace_bytes, void* hip_stream) {
   const FfnShape s = {tokens, dim, hidden, dtype, act};
   ISOLOCO_TRY(check_shape(s));
-  const size_t e = dtype_bytes(dtype), need = ffn_workspace(s, true);
+  const size_t e = dtype_bytes(dtype), need = plan_of(s, true, tile_rows(x, ld_x), tile_rows(w_gate, ld_w) && tile_rows(w_up, ld_w)).bytes;
   if ((dw_gate != nullptr) != (dw_up != nullptr))
     return fail(ISOLOCO_ERR_INVALID_ARG, "dw_gate and dw_up go together");
   ISOLOCO_TRY(check_matrix("x", x, tokens, dim, ld_x, e));

@@ -1,4 +1,4 @@
-// The bfloat16 products of the gated feed-forward block on MFMA tiles (gfx950).
+// The products of the gated feed-forward block on bfloat16 MFMA tiles (gfx950).
 //
 // One workgroup per output tile; slabs of 64 k values go from memory straight into
 // LDS, one in flight while the one before is multiplied.  The products differ in
@@ -10,6 +10,10 @@
 //   kSum              da and du rows against columns of the weights, one after the
 //                     other into the same accumulators
 //   kPair             columns of da or du against columns of x
+//
+// float32 operands are three bfloat16 parts each; their products are the same slabs
+// six times over, one pair of parts after the other into the same accumulators, the
+// smallest first.
 #include <hip/hip_runtime.h>
 
 #include <stdint.h>
@@ -144,6 +148,10 @@ __device__ __forceinline__ void wave_fence() {
   __builtin_amdgcn_wave_barrier();
 }
 
+// 16 bytes at the alignment of an element: the hardware takes such accesses whole.
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
+typedef floatx4 floatx4_any __attribute__((aligned(4)));
+
 // A wave's 32 rows x COLS columns between LDS (rows of COLS * 2 + 16 bytes) and
 // memory; rows and columns past the matrix are left out, those before `rows_pad`
 // and `cols_pad` stored as zeros.
@@ -152,7 +160,7 @@ struct Patch {
   static constexpr int kPitch = COLS * 2 + 16, kBytes = 32 * kPitch, kLanes = COLS / 8, kRows = 64 / kLanes;
   __device__ static __forceinline__ char* quad(char* ws, int col) { return ws + (threadIdx.x & 31) * kPitch + col * 2; }
   __device__ static __forceinline__ void store(const char* ws, uint16_t* out, int64_t ld, int64_t row0, int64_t col0,
-                                               int64_t rows, int64_t cols, int64_t rows_pad, int64_t cols_pad, bool vec) {
+                                               int64_t rows, int64_t cols, int64_t rows_pad, int64_t cols_pad) {
     const int lane = threadIdx.x & 63, c8 = lane % kLanes;
     const int64_t col = col0 + 8 * c8;
 #pragma unroll
@@ -161,8 +169,8 @@ struct Patch {
       const int64_t row = row0 + r;
       if (row >= rows_pad || col >= cols_pad) continue;
       uint16_t* o = out + row * ld + col;
-      if (row < rows && vec && col + 8 <= cols) {
-        *reinterpret_cast<u32x4*>(o) = *reinterpret_cast<const u32x4*>(ws + r * kPitch + c8 * 16);
+      if (row < rows && col + 8 <= cols) {
+        *reinterpret_cast<u32x4_any*>(o) = *reinterpret_cast<const u32x4*>(ws + r * kPitch + c8 * 16);
       } else {
         const uint16_t* v = reinterpret_cast<const uint16_t*>(ws + r * kPitch + c8 * 16);
 #pragma unroll
@@ -172,7 +180,7 @@ struct Patch {
     }
   }
   __device__ static __forceinline__ void load(char* ws, const uint16_t* in, int64_t ld, int64_t row0, int64_t col0,
-                                              int64_t rows, int64_t cols, bool vec) {
+                                              int64_t rows, int64_t cols) {
     const int lane = threadIdx.x & 63, c8 = lane % kLanes;
     const int64_t col = col0 + 8 * c8;
 #pragma unroll
@@ -182,8 +190,8 @@ struct Patch {
       u32x4 v = {};
       const uint16_t* i = in + row * ld + col;
       if (row < rows) {
-        if (vec && col + 8 <= cols) {
-          v = *reinterpret_cast<const u32x4*>(i);
+        if (col + 8 <= cols) {
+          v = *reinterpret_cast<const u32x4_any*>(i);
         } else {
 #pragma unroll
           for (int e = 0; e < 8; ++e)
@@ -195,11 +203,34 @@ struct Patch {
   }
 };
 
+// 4 consecutive float32 values, of which the first `left` exist
+__device__ __forceinline__ floatx4 load4(const float* p, int64_t left) {
+  if (left >= 4) return *reinterpret_cast<const floatx4_any*>(p);
+  floatx4 v;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = e < left ? p[e] : 0.f;
+  return v;
+}
+__device__ __forceinline__ void store4(float* p, floatx4 v, int64_t left) {
+  if (left >= 4) {
+    *reinterpret_cast<floatx4_any*>(p) = v;
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (e < left) p[e] = v[e];
+}
+
+// The next bfloat16 part of 4 values, which keep the remainder (exact)
+__device__ __forceinline__ bf16x4 next_part(floatx4& x) {
+  const bf16x4 p = rounded(x);
+  x -= __builtin_convertvector(p, floatx4);
+  return p;
+}
+
 struct TileArgs {
   FfnArgs g;
   int tiles_m, tiles_n, planes, splits, tiles;  // tiles: of every plane and split
-  int vec_out, vec_dh;  // rows of out (dh) 16-byte aligned
-  float* partial;       // splits > 1: the sums of each split, [split][plane][m][n]
 };
 
 // The tile of a workgroup: workgroups go round the 8 XCDs in turn, so each XCD takes
@@ -218,7 +249,7 @@ __device__ __forceinline__ void tile_of(const TileArgs& t, int& tm, int& tn, int
   tn = in / rows;
 }
 
-template <int MODE, int ACT, class C>
+template <int MODE, int ACT, bool F32, class C>
 __global__ void __launch_bounds__(C::threads, 2) ffn_tile_kernel(TileArgs t) {
   constexpr bool DUAL = MODE == kForward || MODE == kInner, ACOLS = MODE == kPair;
   constexpr int kCols = DUAL ? C::TN / 2 : C::TN;  // output columns of a tile
@@ -248,44 +279,52 @@ __global__ void __launch_bounds__(C::threads, 2) ffn_tile_kernel(TileArgs t) {
   const uint16_t *a[2], *b[2];
 #pragma unroll
   for (int p = 0; p < 2; ++p) {
-    const Operand &oa = g.a[MODE == kPair ? z : MODE == kSum ? p : 0], &ob = g.b[MODE == kPair ? 0 : p];
-    a[p] = static_cast<const uint16_t*>(oa.p) + i0 * oa.rs;
-    b[p] = static_cast<const uint16_t*>(ob.p) + j0 * ob.rs;
+    a[p] = g.a[MODE == kPair ? z : MODE == kSum ? p : 0] + i0 * (ACOLS ? 1 : g.ld_a);
+    b[p] = g.b[MODE == kPair ? 0 : p] + j0 * (DUAL ? g.ld_b : 1);
   }
-  if constexpr (ACOLS) ac.init(2u * (uint32_t)g.a[0].ks, ffn_pad(g.m) - i0);
-  else ar.init(2u * (uint32_t)g.a[0].rs, g.m - i0);
-  if constexpr (DUAL) br.init(2u * (uint32_t)g.b[0].rs, g.n - j0);
-  else bc.init(2u * (uint32_t)g.b[0].ks, g.n - j0);
-  // kSum: the slabs of both parts one after the other; a split product's workgroup
-  // takes one run of them
-  const int64_t slabs = (g.k + kSlab - 1) / kSlab, all = MODE == kSum ? 2 * slabs : slabs;
-  const int64_t first = all * slice / t.splits, total = all * (slice + 1) / t.splits - first;
+  if constexpr (ACOLS) ac.init(2u * (uint32_t)g.ld_a, ffn_pad(g.m) - i0);
+  else ar.init(2u * (uint32_t)g.ld_a, g.m - i0);
+  if constexpr (DUAL) br.init(2u * (uint32_t)g.ld_b, g.n - j0);
+  else bc.init(2u * (uint32_t)g.ld_b, g.cols_b - j0);
 
-  // part 0: the slab of a, part 1: that of b
-  const auto issue = [&](int64_t s, int buf, int part) {
+  // A workgroup's slabs: runs of `slabs`, one per term (kSum) and pair of parts
+  // (float32), one after the other; a split product's workgroup takes some of them.
+  constexpr int kPairs = F32 ? 6 : 1, kRuns = (MODE == kSum ? 2 : 1) * kPairs;
+  const int slabs = (int)((g.k + kSlab - 1) / kSlab);
+  const int64_t all = (int64_t)slabs * kRuns;
+  const int64_t first = all * slice / t.splits, total = all * (slice + 1) / t.splits - first;
+  int run = (int)(first / slabs), at_slab = (int)(first - (int64_t)run * slabs);  // of the next slab to load
+
+  // part 0: the next slab of a, part 1: that of b
+  const auto issue = [&](int buf, int part) {
     const uint32_t at = lds0 + (uint32_t)buf * kStage;
+    const int s = at_slab, term = MODE == kSum ? run / kPairs : 0, pair = F32 ? run - term * kPairs : 0;
+    // the parts of a: 2 1 0 1 0 0, of b: 0 1 2 0 1 0
+    const int64_t oa = F32 ? (0x046 >> (2 * pair) & 3) * g.part_a : 0, ob = F32 ? (0x124 >> (2 * pair) & 3) * g.part_b : 0;
     if constexpr (DUAL) {
-      const int64_t k_left = g.k - s * kSlab;
+      const int64_t k_left = g.k - (int64_t)s * kSlab;
       if (k_left < kSlab) {
         char* to = lds + buf * kStage;
         if (part == 0) {
-          ar.load_end(to, a[0], s, (int)k_left);
+          ar.load_end(to, a[0] + oa, s, (int)k_left);
         } else {
-          br.load_end(to + kA, b[0], s, (int)k_left);
-          br.load_end(to + kA + BR::kBytes, b[1], s, (int)k_left);
+          br.load_end(to + kA, b[0] + ob, s, (int)k_left);
+          br.load_end(to + kA + BR::kBytes, b[1] + ob, s, (int)k_left);
         }
       } else if (part == 0) {
-        ar.load(at, a[0], s);
+        ar.load(at, a[0] + oa, s);
       } else {
-        br.load(at + kA, b[0], s);
-        br.load(at + kA + BR::kBytes, b[1], s);
+        br.load(at + kA, b[0] + ob, s);
+        br.load(at + kA + BR::kBytes, b[1] + ob, s);
       }
     } else {
-      const bool second = MODE == kSum && s >= slabs;
-      const int64_t sp = second ? s - slabs : s;
-      if (part == 1) bc.load(at + kA, second ? b[1] : b[0], sp, g.k - sp * kSlab);
-      else if constexpr (ACOLS) ac.load(at, a[0], sp, kSlab);
-      else ar.load(at, second ? a[1] : a[0], sp);
+      if (part == 1) bc.load(at + kA, (term ? b[1] : b[0]) + ob, s, g.k - (int64_t)s * kSlab);
+      else if constexpr (ACOLS) ac.load(at, a[0] + oa, s, kSlab);
+      else ar.load(at, (term ? a[1] : a[0]) + oa, s);
+    }
+    if (part == 1 && ++at_slab == slabs) {
+      at_slab = 0;
+      ++run;
     }
   };
 
@@ -319,8 +358,8 @@ __global__ void __launch_bounds__(C::threads, 2) ffn_tile_kernel(TileArgs t) {
     __builtin_amdgcn_sched_barrier(0);
   };
   // The products of 16 k values (b first: a lane then holds 4 consecutive columns
-  // of one row); part `part` of slab s is asked for behind the first of them.
-  const auto multiply = [&](const Frags& f, bool more, int64_t s, int buf, int part) {
+  // of one row); a part of the next slab is asked for behind the first of them.
+  const auto multiply = [&](const Frags& f, bool more, int buf, int part) {
 #pragma unroll
     for (int x = 0; x < C::NA; ++x)
 #pragma unroll
@@ -328,7 +367,7 @@ __global__ void __launch_bounds__(C::threads, 2) ffn_tile_kernel(TileArgs t) {
         acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.b[y], f.a[x], acc[x][y], 0, 0, 0);
         if (x == 0 && y == 1) {
           __builtin_amdgcn_sched_barrier(0);
-          if (more) issue(s, buf, part);
+          if (more) issue(buf, part);
           __builtin_amdgcn_sched_barrier(0);
         }
       }
@@ -343,116 +382,155 @@ __global__ void __launch_bounds__(C::threads, 2) ffn_tile_kernel(TileArgs t) {
   // their waves would multiply nothing (all at the barrier: 639 us for the sum over
   // 2 x 5632 of 16384 x 2048 outputs, in two parts 611).
   if (total > 0) {
-    issue(first, 0, 0);
-    issue(first, 0, 1);
+    issue(0, 0);
+    issue(0, 1);
     wait_slabs<0>();
     Frags f[2];
     read(f[0], 0, 0);
-    if (total > 1) issue(first + 1, 1, 0);
+    if (total > 1) issue(1, 0);
 #pragma unroll 1
     for (int64_t s = 0; s < total; ++s) {
       const int buf = (int)(s & 1);
 #pragma unroll
       for (int kk = 16; kk < kSlab; kk += 16) {
         read(f[(kk / 16) & 1], buf, kk);
-        multiply(f[(kk / 16 + 1) & 1], kk == 16 && s + 1 < total, first + s + 1, buf ^ 1, 1);
+        multiply(f[(kk / 16 + 1) & 1], kk == 16 && s + 1 < total, buf ^ 1, 1);
       }
       wait_slabs<0>();  // slab s + 1 is in LDS, and every wave is done reading slab s
       if (s + 1 < total) read(f[0], buf ^ 1, 0);
-      multiply(f[1], s + 2 < total, first + s + 2, buf, 0);
+      multiply(f[1], s + 2 < total, buf, 0);
     }
   }
   __syncthreads();  // every wave is done with the operands: LDS is free
 
   // acc[x][y][4 q + e] = C(32 x + lane % 32, 32 y + 8 q + 4 (lane / 32) + e)
-  if constexpr (!DUAL) {
-    if (t.splits > 1) {
-      // (n is a multiple of 8: a quad of columns is inside or outside)
-      float* part = t.partial + ((int64_t)slice * t.planes + z) * g.m * g.n;
-#pragma unroll
-      for (int x = 0; x < C::NA; ++x) {
-        const int64_t row = i0 + (wm * C::NA + x) * 32 + (lane & 31);
-        if (row >= g.m) continue;
-#pragma unroll
-        for (int y = 0; y < C::NB; ++y)
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const int64_t col = j0 + (wn * C::NB + y) * 32 + 8 * q + 4 * (lane >> 5);
-            if (col < g.n)
-              *reinterpret_cast<floatx4*>(part + row * g.n + col) =
-                  (floatx4){acc[x][y][4 * q], acc[x][y][4 * q + 1], acc[x][y][4 * q + 2], acc[x][y][4 * q + 3]};
-          }
-      }
-      return;
-    }
-  }
-  char* ws = lds + wave * kWs;
   constexpr int kOut = DUAL ? C::NB / 2 : C::NB;
   const int64_t col0 = j0 + wn * kOut * 32;
-  const int64_t rows_pad = MODE == kInner ? ffn_pad(g.m) : g.m, cols_pad = MODE == kInner ? ffn_pad(g.n) : g.n;
-  uint16_t* out = static_cast<uint16_t*>(g.out[MODE == kPair ? z : 0]);
+  const auto quad_of = [&](int x, int y, int q) {
+    return (floatx4){acc[x][y][4 * q], acc[x][y][4 * q + 1], acc[x][y][4 * q + 2], acc[x][y][4 * q + 3]};
+  };
+  // v = act(g) u, or v = dh u act'(g) and w = dh act(g), of one quad of outputs
+  const auto inner = [&](int x, int y, int q, floatx4 dh, floatx4& v, floatx4& w) {
+    const floatx4 gate = quad_of(x, y, q), up = quad_of(x, kOut + y, q);
 #pragma unroll
-  for (int x = 0; x < C::NA; ++x) {
-    const int64_t row0 = i0 + (wm * C::NA + x) * 32;
-    if constexpr (MODE == kInner) {
-      P::load(ws, static_cast<const uint16_t*>(g.dh), g.ld_dh, row0, col0, g.m, g.n, t.vec_dh);
+    for (int e = 0; e < 4; ++e) {
+      float f, df;
+      activate<ACT, F32>(gate[e], f, df);
+      v[e] = MODE == kInner ? dh[e] * up[e] * df : f * up[e];
+      w[e] = dh[e] * f;
+    }
+  };
+
+  if (!DUAL && t.splits > 1) {
+    // a split's sums (cols_b is a multiple of 8: a quad of columns is inside or outside)
+    float* part = g.partial + ((int64_t)slice * t.planes + z) * g.m * g.cols_b;
+#pragma unroll
+    for (int x = 0; x < C::NA; ++x) {
+      const int64_t row = i0 + (wm * C::NA + x) * 32 + (lane & 31);
+      if (row >= g.m) continue;
+#pragma unroll
+      for (int y = 0; y < kOut; ++y)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int64_t col = col0 + 32 * y + 8 * q + 4 * (lane >> 5);
+          if (col < g.cols_b) *reinterpret_cast<floatx4*>(part + row * g.cols_b + col) = quad_of(x, y, q);
+        }
+    }
+    return;
+  }
+
+  if constexpr (F32) {
+    const int64_t rows_pad = ffn_pad(g.m), cols_pad = ffn_pad(g.n);
+#pragma unroll
+    for (int x = 0; x < C::NA; ++x) {
+      const int64_t row = i0 + (wm * C::NA + x) * 32 + (lane & 31);
+      if (row >= (MODE == kInner ? rows_pad : g.m)) continue;
+#pragma unroll
+      for (int y = 0; y < kOut; ++y)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int64_t col = col0 + 32 * y + 8 * q + 4 * (lane >> 5);
+          if constexpr (MODE == kInner) {
+            if (col >= cols_pad) continue;
+            floatx4 dh = {}, v = {}, w = {};
+            if (row < g.m) {
+              dh = load4(static_cast<const float*>(g.dh) + row * g.ld_dh + col, g.n - col);
+              inner(x, y, q, dh, v, w);
+#pragma unroll
+              for (int e = 0; e < 4; ++e)  // (the padding's columns are those of another row)
+                if (col + e >= g.n) v[e] = w[e] = 0.f;
+            }
+#pragma unroll
+            for (int p = 0; p < kFfnParts; ++p) {
+              const int64_t at = p * g.part_out + row * g.ld_out + col;
+              *reinterpret_cast<bf16x4*>(static_cast<uint16_t*>(g.out[0]) + at) = next_part(v);
+              *reinterpret_cast<bf16x4*>(static_cast<uint16_t*>(g.out[1]) + at) = next_part(w);
+            }
+          } else {
+            if (col >= g.n) continue;
+            floatx4 v = quad_of(x, y, q), w;
+            if constexpr (DUAL) inner(x, y, q, (floatx4){}, v, w);
+            store4(static_cast<float*>(g.out[z]) + row * g.ld_out + col, v, g.n - col);
+          }
+        }
+    }
+  } else {
+    char* ws = lds + wave * kWs;
+    const int64_t rows_pad = MODE == kInner ? ffn_pad(g.m) : g.m, cols_pad = MODE == kInner ? ffn_pad(g.n) : g.n;
+    uint16_t* out = static_cast<uint16_t*>(g.out[z]);
+#pragma unroll
+    for (int x = 0; x < C::NA; ++x) {
+      const int64_t row0 = i0 + (wm * C::NA + x) * 32;
+      if constexpr (MODE == kInner) {
+        P::load(ws, static_cast<const uint16_t*>(g.dh), g.ld_dh, row0, col0, g.m, g.n);
+        wave_fence();
+      }
+#pragma unroll
+      for (int y = 0; y < kOut; ++y)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          char* at = P::quad(ws, 32 * y + 8 * q + 4 * (lane >> 5));
+          floatx4 v = quad_of(x, y, q), w, dh = {};
+          if constexpr (MODE == kInner) dh = __builtin_convertvector(*reinterpret_cast<const bf16x4*>(at), floatx4);
+          if constexpr (DUAL) inner(x, y, q, dh, v, w);
+          if constexpr (MODE == kInner) *reinterpret_cast<bf16x4*>(at + P::kBytes) = rounded(w);
+          *reinterpret_cast<bf16x4*>(at) = rounded(v);
+        }
+      wave_fence();
+      P::store(ws, out, g.ld_out, row0, col0, g.m, g.n, rows_pad, cols_pad);
+      if constexpr (MODE == kInner)
+        P::store(ws + P::kBytes, static_cast<uint16_t*>(g.out[1]), g.ld_out, row0, col0, g.m, g.n, rows_pad, cols_pad);
       wave_fence();
     }
-#pragma unroll
-    for (int y = 0; y < kOut; ++y)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        char* at = P::quad(ws, 32 * y + 8 * q + 4 * (lane >> 5));
-        floatx4 v;
-        if constexpr (DUAL) {
-          floatx4 dh, w;
-          if constexpr (MODE == kInner) dh = __builtin_convertvector(*reinterpret_cast<const bf16x4*>(at), floatx4);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float f, df;
-            activate_fast<ACT>(acc[x][y][4 * q + e], f, df);
-            const float u = acc[x][kOut + y][4 * q + e];
-            if constexpr (MODE == kInner) {
-              v[e] = dh[e] * u * df;
-              w[e] = dh[e] * f;
-            } else {
-              v[e] = f * u;
-            }
-          }
-          if constexpr (MODE == kInner) *reinterpret_cast<bf16x4*>(at + P::kBytes) = rounded(w);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = acc[x][y][4 * q + e];
-        }
-        *reinterpret_cast<bf16x4*>(at) = rounded(v);
-      }
-    wave_fence();
-    P::store(ws, out, g.ld_out, row0, col0, g.m, g.n, rows_pad, cols_pad, t.vec_out);
-    if constexpr (MODE == kInner)
-      P::store(ws + P::kBytes, static_cast<uint16_t*>(g.out[1]), g.ld_out, row0, col0, g.m, g.n, rows_pad, cols_pad,
-               t.vec_out);
-    wave_fence();
   }
 }
 
 // The splits of a product added in their order, rounded once.
+template <bool F32>
 __global__ void __launch_bounds__(256) ffn_join_kernel(TileArgs t) {
   const FfnArgs& g = t.g;
-  const int64_t plane = g.m * g.n, quads = plane / 4;
+  const int64_t plane = g.m * g.cols_b, quads = plane / 4;
   const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (at >= quads * t.planes) return;
   const int z = (int)(at / quads);
-  const int64_t i = (at - z * quads) * 4, row = i / g.n, col = i - row * g.n;
-  const float* p = t.partial + z * plane + i;
+  const int64_t i = (at - z * quads) * 4, row = i / g.cols_b, col = i - row * g.cols_b;
+  if (col >= g.n) return;
+  const float* p = g.partial + z * plane + i;
   floatx4 s = *reinterpret_cast<const floatx4*>(p);
   for (int k = 1; k < t.splits; ++k) s += *reinterpret_cast<const floatx4*>(p + k * t.planes * plane);
-  uint16_t* out = static_cast<uint16_t*>(g.out[z]) + row * g.ld_out + col;
-  const bf16x4 r = rounded(s);
-  if (t.vec_out) {
-    *reinterpret_cast<bf16x4*>(out) = r;
+  if constexpr (F32) {
+    store4(static_cast<float*>(g.out[z]) + row * g.ld_out + col, s, g.n - col);
   } else {
+    typedef bf16x4 bf16x4_any __attribute__((aligned(2)));
+    __bf16* out = static_cast<__bf16*>(g.out[z]) + row * g.ld_out + col;
+    const bf16x4 r = rounded(s);
+    if (col + 4 <= g.n) {
+      *reinterpret_cast<bf16x4_any*>(out) = r;
+    } else {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) reinterpret_cast<__bf16*>(out)[e] = r[e];
+      for (int e = 0; e < 4; ++e)
+        if (col + e < g.n) out[e] = r[e];
+    }
   }
 }
 
@@ -475,10 +553,10 @@ struct Plan {
 // 5632, 774 / 690 / 843 (352 tiles of the first are two rounds of 256, the second of
 // them 3/8 full); its dx 606 / 739 / 802; forward of 2048 tokens, 768 x 2048, 24 / - /
 // 19.  Splits 1 / 2 / 4 / 8 of the dx of 512 tokens, 2048 x 5632: 138 / 79 / 52 / 47.
-Plan plan_of(int mode, int64_t m, int64_t n, int64_t k) {
+Plan plan_of(int mode, bool f32, int64_t m, int64_t n, int64_t k) {
   const bool dual = mode == kForward || mode == kInner;
   const int64_t planes = mode == kPair ? 2 : 1;
-  const int64_t slabs = (k + kSlab - 1) / kSlab * (mode == kSum ? 2 : 1);
+  const int64_t slabs = (k + kSlab - 1) / kSlab * (mode == kSum ? 2 : 1) * (f32 ? 6 : 1);
   Plan best = {kSmall, 1};
   double least = 1e30;
   for (int s = 0; s < kShapes; ++s) {
@@ -497,60 +575,55 @@ Plan plan_of(int mode, int64_t m, int64_t n, int64_t k) {
   return best;
 }
 
-template <int MODE, int ACT, class C>
+template <int MODE, int ACT, bool F32, class C>
 void launch_shape(TileArgs& t, hipStream_t st) {
   constexpr int kCols = MODE == kForward || MODE == kInner ? C::TN / 2 : C::TN;
   t.tiles_m = (int)((t.g.m + C::TM - 1) / C::TM);
   t.tiles_n = (int)((t.g.n + kCols - 1) / kCols);
   t.tiles = t.tiles_m * t.tiles_n * t.planes * t.splits;
-  hipLaunchKernelGGL((ffn_tile_kernel<MODE, ACT, C>), dim3(t.tiles), dim3(C::threads), 0, st, t);
+  hipLaunchKernelGGL((ffn_tile_kernel<MODE, ACT, F32, C>), dim3(t.tiles), dim3(C::threads), 0, st, t);
   if (t.splits > 1)
-    hipLaunchKernelGGL(ffn_join_kernel, dim3((unsigned)((t.planes * t.g.m * t.g.n / 4 + 255) / 256)), dim3(256), 0, st,
-                       t);
+    hipLaunchKernelGGL(ffn_join_kernel<F32>, dim3((unsigned)((t.planes * t.g.m * t.g.cols_b / 4 + 255) / 256)), dim3(256),
+                       0, st, t);
 }
 
-template <int MODE, int ACT>
-hipError_t launch_mode(const FfnArgs& g, float* partial, hipStream_t st) {
+template <int MODE, int ACT, bool F32>
+hipError_t launch_mode(const FfnArgs& g, hipStream_t st) {
   if (g.m == 0 || g.n == 0) return hipSuccess;
   TileArgs t;
   t.g = g;
-  const auto vec = [](const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && (ld & 7) == 0; };
-  t.vec_out = vec(g.out[0], g.ld_out) && (!g.out[1] || vec(g.out[1], g.ld_out));
-  t.vec_dh = MODE == kInner && vec(g.dh, g.ld_dh);
-  Plan p = plan_of(MODE, g.m, g.n, g.k);
-#ifdef FORCE
-  FORCE
-#endif
+  const Plan p = plan_of(MODE, F32, g.m, g.n, g.k);
   t.planes = MODE == kPair ? 2 : 1;
   t.splits = p.splits;
-  t.partial = partial;
-  if (p.shape == kLarge) launch_shape<MODE, ACT, Large>(t, st);
-  else if (p.shape == kMiddle) launch_shape<MODE, ACT, Middle>(t, st);
-  else launch_shape<MODE, ACT, Small>(t, st);
+  if (p.shape == kLarge) launch_shape<MODE, ACT, F32, Large>(t, st);
+  else if (p.shape == kMiddle) launch_shape<MODE, ACT, F32, Middle>(t, st);
+  else launch_shape<MODE, ACT, F32, Small>(t, st);
   return hipGetLastError();
 }
 
-template <int ACT>
-hipError_t launch_act(FfnMode mode, const FfnArgs& g, float* partial, hipStream_t st) {
+template <bool F32>
+hipError_t launch_type(FfnMode mode, int act, const FfnArgs& g, hipStream_t st) {
+  const bool silu = act == ISOLOCO_ACT_SILU;
   switch (mode) {
-    case kForward: return launch_mode<kForward, ACT>(g, partial, st);
-    case kInner: return launch_mode<kInner, ACT>(g, partial, st);
+    case kForward:
+      return silu ? launch_mode<kForward, ISOLOCO_ACT_SILU, F32>(g, st) : launch_mode<kForward, ISOLOCO_ACT_GELU, F32>(g, st);
+    case kInner:
+      return silu ? launch_mode<kInner, ISOLOCO_ACT_SILU, F32>(g, st) : launch_mode<kInner, ISOLOCO_ACT_GELU, F32>(g, st);
     // (these two apply no activation)
-    case kSum: return launch_mode<kSum, ISOLOCO_ACT_SILU>(g, partial, st);
-    default: return launch_mode<kPair, ISOLOCO_ACT_SILU>(g, partial, st);
+    case kSum: return launch_mode<kSum, ISOLOCO_ACT_SILU, F32>(g, st);
+    default: return launch_mode<kPair, ISOLOCO_ACT_SILU, F32>(g, st);
   }
 }
 
 }  // namespace
 
-size_t ffn_partial_bytes(FfnMode mode, int64_t m, int64_t n, int64_t k) {
-  const Plan p = plan_of(mode, m, n, k);
-  return p.splits > 1 ? (size_t)p.splits * (mode == kPair ? 2 : 1) * m * n * sizeof(float) : 0;
+size_t ffn_partial_bytes(FfnMode mode, bool f32, int64_t m, int64_t n, int64_t k) {
+  const Plan p = plan_of(mode, f32, m, n, k);
+  return p.splits > 1 ? (size_t)p.splits * (mode == kPair ? 2 : 1) * m * ffn_pad(n) * sizeof(float) : 0;
 }
 
-hipError_t launch_ffn_tiles(FfnMode mode, int act, const FfnArgs& g, float* partial, hipStream_t st) {
-  return act == ISOLOCO_ACT_SILU ? launch_act<ISOLOCO_ACT_SILU>(mode, g, partial, st)
-                                 : launch_act<ISOLOCO_ACT_GELU>(mode, g, partial, st);
+hipError_t launch_ffn_tiles(FfnMode mode, int act, bool f32, const FfnArgs& g, hipStream_t st) {
+  return f32 ? launch_type<true>(mode, act, g, st) : launch_type<false>(mode, act, g, st);
 }
 
 }  // namespace isoloco

@@ -15,7 +15,8 @@ from typing import NamedTuple, Optional
 
 import torch
 
-from . import (ISOLOCO_ACT_GELU, ISOLOCO_ACT_SILU, ISOLOCO_BF16, ISOLOCO_F32, ISOLOCO_I32, ISOLOCO_I64, _check, _lib)
+from . import (ISOLOCO_ACT_GELU, ISOLOCO_ACT_SILU, ISOLOCO_BF16, ISOLOCO_F32, ISOLOCO_FFN_ALIGNED,
+               ISOLOCO_FFN_BACKWARD, ISOLOCO_I32, ISOLOCO_I64, _check, _lib)
 
 _DTYPE = {torch.float32: ISOLOCO_F32, torch.bfloat16: ISOLOCO_BF16}
 _INDEX = {torch.int32: ISOLOCO_I32, torch.int64: ISOLOCO_I64}
@@ -82,8 +83,8 @@ def isoloco_token_logprobs_backward(logits, ld_logits, dtype, rows, vocab, targe
            "isoloco_token_logprobs_backward")
 
 
-def isoloco_gated_ffn_workspace_size(tokens, dim, hidden, dtype, backward):
-    return _size_of("isoloco_gated_ffn_workspace_size", tokens, dim, hidden, dtype, backward)
+def isoloco_gated_ffn_workspace_size(tokens, dim, hidden, dtype, flags):
+    return _size_of("isoloco_gated_ffn_workspace_size", tokens, dim, hidden, dtype, flags)
 
 
 def isoloco_gated_ffn(x, ld_x, w_gate, w_up, ld_w, dtype, tokens, dim, hidden, act, out, ld_out, workspace,
@@ -346,18 +347,20 @@ def _ffn_operands(on, x, w_gate, w_up, act):
         raise ValueError("w_gate and w_up must have the same row stride")
     if act not in _ACT:
         raise ValueError("act must be one of %s" % ", ".join(sorted(_ACT)))
-    return dtype, tokens, dim, hidden, ld_x, ld_w, _ACT[act]
+    aligned = (ld_x | ld_w) % 8 == 0 and (x.data_ptr() | w_gate.data_ptr() | w_up.data_ptr()) % 16 == 0
+    return dtype, tokens, dim, hidden, ld_x, ld_w, _ACT[act], ISOLOCO_FFN_ALIGNED if aligned else 0
 
 
 def gated_ffn(x, w_gate, w_up, act="silu", out=None, workspace=None, stream=None):
     """``act(x w_gate^T) * (x w_up^T)`` for x [..., dim] and weights [hidden, dim]; act
     is "silu" or "gelu"."""
     with _On(x, stream) as on:
-        dtype, tokens, dim, hidden, ld_x, ld_w, a = _ffn_operands(on, x, w_gate, w_up, act)
+        dtype, tokens, dim, hidden, ld_x, ld_w, a, flags = _ffn_operands(on, x, w_gate, w_up, act)
         _same_device(on, out=out)
         out = _output(on, "out", out, (*x.shape[:-1], hidden), x.dtype)
         _, ld_out = _rows("out", out)
-        ws, ws_bytes, keep = on.workspace(workspace, isoloco_gated_ffn_workspace_size(tokens, dim, hidden, dtype, 0))
+        ws, ws_bytes, keep = on.workspace(workspace, isoloco_gated_ffn_workspace_size(tokens, dim, hidden, dtype,
+                                                                                               flags))
         isoloco_gated_ffn(x.data_ptr(), ld_x, w_gate.data_ptr(), w_up.data_ptr(), ld_w, dtype, tokens, dim, hidden, a,
                           out.data_ptr(), ld_out, ws, ws_bytes, on.handle)
         return out
@@ -366,7 +369,7 @@ def gated_ffn(x, w_gate, w_up, act="silu", out=None, workspace=None, stream=None
 def gated_ffn_backward(x, w_gate, w_up, dout, act="silu", need_dx=True, need_dw=True, workspace=None, stream=None):
     """(dx, dw_gate, dw_up) from ``dout`` [..., hidden]; None for what is not needed."""
     with _On(x, stream) as on:
-        dtype, tokens, dim, hidden, ld_x, ld_w, a = _ffn_operands(on, x, w_gate, w_up, act)
+        dtype, tokens, dim, hidden, ld_x, ld_w, a, flags = _ffn_operands(on, x, w_gate, w_up, act)
         _same_device(on, dout=dout)
         if dout.dtype != x.dtype or tuple(dout.shape) != (*x.shape[:-1], hidden):
             raise ValueError("dout must be %s of %s" % (x.dtype, (*x.shape[:-1], hidden)))
@@ -374,7 +377,8 @@ def gated_ffn_backward(x, w_gate, w_up, dout, act="silu", need_dx=True, need_dw=
         dx = on.empty(x.shape, x.dtype) if need_dx else None
         dwg = on.empty((hidden, dim), x.dtype) if need_dw else None
         dwu = on.empty((hidden, dim), x.dtype) if need_dw else None
-        ws, ws_bytes, keep = on.workspace(workspace, isoloco_gated_ffn_workspace_size(tokens, dim, hidden, dtype, 1))
+        ws, ws_bytes, keep = on.workspace(workspace, isoloco_gated_ffn_workspace_size(
+            tokens, dim, hidden, dtype, flags | ISOLOCO_FFN_BACKWARD))
         isoloco_gated_ffn_backward(x.data_ptr(), ld_x, w_gate.data_ptr(), w_up.data_ptr(), ld_w, dtype, tokens, dim,
                                    hidden, a, dout.data_ptr(), ld_dout, dx.data_ptr() if need_dx else None, dim,
                                    dwg.data_ptr() if need_dw else None, dwu.data_ptr() if need_dw else None, dim, ws,
