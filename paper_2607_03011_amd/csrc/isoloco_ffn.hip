@@ -32,6 +32,7 @@ typedef floatx4 floatx4_any __attribute__((aligned(4)));
 // A product of few rows is bounded by the weights' bytes: every weight is loaded once,
 // from memory into the registers that the MFMA reads (16 hidden rows against 16
 // tokens), and the workgroup's waves split dim so that enough loads are in flight.
+//
 
 // The values of k that a lane holds of one row, 16 bytes: its MFMA operands.
 template <typename T>
@@ -58,8 +59,10 @@ __device__ __forceinline__ floatx4 multiply(const Lane<float>& a, const Lane<flo
   return c;
 }
 
+// Against the tiles (us, 2048 x 5632): bfloat16, 16 / 32 / 48 / 64 tokens 15 / 18 / 23 /
+// 26 here, 20 there at each; float32 16 / 64 tokens 26 / 58 here, 82 / 86 there.
 constexpr int kFewWaves = 8;
-constexpr int kFewMost = 64;  // tokens
+constexpr int64_t few_most(int32_t dtype) { return dtype == ISOLOCO_BF16 ? 32 : 64; }
 
 // 16 hidden rows per workgroup, up to 16 NT tokens.
 template <typename T, int ACT, int NT>
@@ -200,7 +203,7 @@ bool tile_rows(const void* p, int64_t ld) { return aligned_to(p, 16) && (ld & 7)
 FfnPlan plan_of(const FfnShape& s, bool backward, bool x_ok, bool w_ok) {
   FfnPlan p = {};
   const bool f32 = s.dtype == ISOLOCO_F32;
-  p.few = !backward && s.tokens <= kFewMost;
+  p.few = !backward && s.tokens <= few_most(s.dtype);
   if (p.few) return p;
   p.copy_x = f32 || !x_ok || (s.dim & 7);
   p.copy_w = f32 || !w_ok || (s.dim & 7);
@@ -215,13 +218,15 @@ FfnPlan plan_of(const FfnShape& s, bool backward, bool x_ok, bool w_ok) {
     p.wg = take(row * s.hidden);
     p.wu = take(row * s.hidden);
   }
+  size_t partial = ffn_partial_bytes(backward ? kInner : kForward, f32, s.tokens, s.hidden, s.dim);
   if (backward) {
     const size_t inner = 2 * (size_t)ffn_pad(s.tokens) * (size_t)ffn_pad(s.hidden) * parts;
     p.da = take(inner);
     p.du = take(inner);
-    p.partial = take(std::max(ffn_partial_bytes(kSum, f32, s.tokens, s.dim, s.hidden),
-                              ffn_partial_bytes(kPair, f32, s.hidden, s.dim, s.tokens)));
+    partial = std::max({partial, ffn_partial_bytes(kSum, f32, s.tokens, s.dim, s.hidden),
+                        ffn_partial_bytes(kPair, f32, s.hidden, s.dim, s.tokens)});
   }
+  p.partial = take(partial);
   return p;
 }
 
@@ -277,7 +282,7 @@ hipError_t run_forward(const FfnShape& s, const void* x, int64_t ld_x, const voi
   if (p.few) {
     if (s.tokens <= 16) launch_few<T, ACT, 1>(s, x, ld_x, wg, wu, ld_w, out, ld_out, st);
     else if (s.tokens <= 32) launch_few<T, ACT, 2>(s, x, ld_x, wg, wu, ld_w, out, ld_out, st);
-    else launch_few<T, ACT, 4>(s, x, ld_x, wg, wu, ld_w, out, ld_out, st);
+    else if constexpr (sizeof(T) == 4) launch_few<T, ACT, 4>(s, x, ld_x, wg, wu, ld_w, out, ld_out, st);
     return hipGetLastError();
   }
   const TileOperands o = copy_operands<T>(s, p, x, ld_x, wg, wu, ld_w, static_cast<char*>(ws), st);
@@ -294,6 +299,7 @@ hipError_t run_forward(const FfnShape& s, const void* x, int64_t ld_x, const voi
   g.k = o.k;
   g.out[0] = out;
   g.ld_out = ld_out;
+  g.partial = reinterpret_cast<float*>(static_cast<char*>(ws) + p.partial);
   return launch_ffn_tiles(kForward, ACT, sizeof(T) == 4, g, st);
 }
 
@@ -325,6 +331,7 @@ hipError_t run_backward(const FfnShape& s, const void* x, int64_t ld_x, const vo
   g.part_out = part;
   g.dh = dout;
   g.ld_dh = ld_dout;
+  g.partial = reinterpret_cast<float*>(base + p.partial);
   hipError_t e = launch_ffn_tiles(kInner, ACT, f32, g, st);
   g = {};
   g.a[0] = da;

@@ -228,6 +228,38 @@ __device__ __forceinline__ bf16x4 next_part(floatx4& x) {
   return p;
 }
 
+// v = act(gate) up, or (kInner) v = dh up act'(gate) and w = dh act(gate)
+template <int MODE, int ACT, bool F32>
+__device__ __forceinline__ void gated(floatx4 gate, floatx4 up, floatx4 dh, floatx4& v, floatx4& w) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    float f, df;
+    activate<ACT, F32>(gate[e], f, df);
+    v[e] = MODE == kInner ? dh[e] * up[e] * df : f * up[e];
+    w[e] = dh[e] * f;
+  }
+}
+
+// A quad of da and du, in parts if float32; zeros in the padding (whose columns are
+// the last one's again in the accumulators, whose rows may hold anything).
+template <bool F32>
+__device__ __forceinline__ void store_inner(const FfnArgs& g, int64_t row, int64_t col, floatx4 v, floatx4 w) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (row >= g.m || col + e >= g.n) v[e] = w[e] = 0.f;
+#pragma unroll
+  for (int p = 0; p < (F32 ? kFfnParts : 1); ++p) {
+    const int64_t at = p * g.part_out + row * g.ld_out + col;
+    *reinterpret_cast<bf16x4*>(static_cast<uint16_t*>(g.out[0]) + at) = next_part(v);
+    *reinterpret_cast<bf16x4*>(static_cast<uint16_t*>(g.out[1]) + at) = next_part(w);
+  }
+}
+
+// Columns of a split's sums
+__host__ __device__ inline int64_t partial_cols(int mode, const FfnArgs& g) {
+  return mode == kForward || mode == kInner ? ffn_pad(g.n) : g.cols_b;
+}
+
 struct TileArgs {
   FfnArgs g;
   int tiles_m, tiles_n, planes, splits, tiles;  // tiles: of every plane and split
@@ -409,21 +441,14 @@ __global__ void __launch_bounds__(C::threads, 2) ffn_tile_kernel(TileArgs t) {
   const auto quad_of = [&](int x, int y, int q) {
     return (floatx4){acc[x][y][4 * q], acc[x][y][4 * q + 1], acc[x][y][4 * q + 2], acc[x][y][4 * q + 3]};
   };
-  // v = act(g) u, or v = dh u act'(g) and w = dh act(g), of one quad of outputs
   const auto inner = [&](int x, int y, int q, floatx4 dh, floatx4& v, floatx4& w) {
-    const floatx4 gate = quad_of(x, y, q), up = quad_of(x, kOut + y, q);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      float f, df;
-      activate<ACT, F32>(gate[e], f, df);
-      v[e] = MODE == kInner ? dh[e] * up[e] * df : f * up[e];
-      w[e] = dh[e] * f;
-    }
+    gated<MODE, ACT, F32>(quad_of(x, y, q), quad_of(x, kOut + y, q), dh, v, w);
   };
 
-  if (!DUAL && t.splits > 1) {
-    // a split's sums (cols_b is a multiple of 8: a quad of columns is inside or outside)
-    float* part = g.partial + ((int64_t)slice * t.planes + z) * g.m * g.cols_b;
+  if (t.splits > 1) {
+    // a split's sums (cols is a multiple of 8: a quad of columns is inside or outside)
+    const int64_t cols = partial_cols(MODE, g), plane = g.m * cols;
+    float* part = g.partial + (DUAL ? 2 * slice : slice * t.planes + z) * plane;
 #pragma unroll
     for (int x = 0; x < C::NA; ++x) {
       const int64_t row = i0 + (wm * C::NA + x) * 32 + (lane & 31);
@@ -433,7 +458,10 @@ __global__ void __launch_bounds__(C::threads, 2) ffn_tile_kernel(TileArgs t) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           const int64_t col = col0 + 32 * y + 8 * q + 4 * (lane >> 5);
-          if (col < g.cols_b) *reinterpret_cast<floatx4*>(part + row * g.cols_b + col) = quad_of(x, y, q);
+          if (col >= cols) continue;
+          float* o = part + row * cols + col;
+          *reinterpret_cast<floatx4*>(o) = quad_of(x, y, q);
+          if constexpr (DUAL) *reinterpret_cast<floatx4*>(o + plane) = quad_of(x, kOut + y, q);
         }
     }
     return;
@@ -452,20 +480,9 @@ __global__ void __launch_bounds__(C::threads, 2) ffn_tile_kernel(TileArgs t) {
           const int64_t col = col0 + 32 * y + 8 * q + 4 * (lane >> 5);
           if constexpr (MODE == kInner) {
             if (col >= cols_pad) continue;
-            floatx4 dh = {}, v = {}, w = {};
-            if (row < g.m) {
-              dh = load4(static_cast<const float*>(g.dh) + row * g.ld_dh + col, g.n - col);
-              inner(x, y, q, dh, v, w);
-#pragma unroll
-              for (int e = 0; e < 4; ++e)  // (the padding's columns are those of another row)
-                if (col + e >= g.n) v[e] = w[e] = 0.f;
-            }
-#pragma unroll
-            for (int p = 0; p < kFfnParts; ++p) {
-              const int64_t at = p * g.part_out + row * g.ld_out + col;
-              *reinterpret_cast<bf16x4*>(static_cast<uint16_t*>(g.out[0]) + at) = next_part(v);
-              *reinterpret_cast<bf16x4*>(static_cast<uint16_t*>(g.out[1]) + at) = next_part(w);
-            }
+            floatx4 v = {}, w = {};
+            if (row < g.m) inner(x, y, q, load4(static_cast<const float*>(g.dh) + row * g.ld_dh + col, g.n - col), v, w);
+            store_inner<true>(g, row, col, v, w);
           } else {
             if (col >= g.n) continue;
             floatx4 v = quad_of(x, y, q), w;
@@ -505,32 +522,62 @@ __global__ void __launch_bounds__(C::threads, 2) ffn_tile_kernel(TileArgs t) {
   }
 }
 
-// The splits of a product added in their order, rounded once.
+typedef bf16x4 bf16x4_any __attribute__((aligned(2)));
+
 template <bool F32>
-__global__ void __launch_bounds__(256) ffn_join_kernel(TileArgs t) {
-  const FfnArgs& g = t.g;
-  const int64_t plane = g.m * g.cols_b, quads = plane / 4;
-  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (at >= quads * t.planes) return;
-  const int z = (int)(at / quads);
-  const int64_t i = (at - z * quads) * 4, row = i / g.cols_b, col = i - row * g.cols_b;
-  if (col >= g.n) return;
-  const float* p = g.partial + z * plane + i;
-  floatx4 s = *reinterpret_cast<const floatx4*>(p);
-  for (int k = 1; k < t.splits; ++k) s += *reinterpret_cast<const floatx4*>(p + k * t.planes * plane);
+__device__ __forceinline__ void store_out(void* out, floatx4 v, int64_t left) {
   if constexpr (F32) {
-    store4(static_cast<float*>(g.out[z]) + row * g.ld_out + col, s, g.n - col);
+    store4(static_cast<float*>(out), v, left);
   } else {
-    typedef bf16x4 bf16x4_any __attribute__((aligned(2)));
-    __bf16* out = static_cast<__bf16*>(g.out[z]) + row * g.ld_out + col;
-    const bf16x4 r = rounded(s);
-    if (col + 4 <= g.n) {
-      *reinterpret_cast<bf16x4_any*>(out) = r;
+    const bf16x4 r = rounded(v);
+    if (left >= 4) {
+      *static_cast<bf16x4_any*>(out) = r;
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        if (col + e < g.n) out[e] = r[e];
+        if (e < left) static_cast<__bf16*>(out)[e] = r[e];
     }
+  }
+}
+
+// The splits of a product added in their order, and what the tiles would have made of
+// the whole sums.  One thread per quad of columns.
+template <int MODE, int ACT, bool F32>
+__global__ void __launch_bounds__(256) ffn_join_kernel(TileArgs t) {
+  constexpr bool DUAL = MODE == kForward || MODE == kInner;
+  const FfnArgs& g = t.g;
+  const int64_t cols = partial_cols(MODE, g), plane = g.m * cols;
+  const int64_t quads = (MODE == kInner ? ffn_pad(g.m) : g.m) * cols / 4;
+  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int z = MODE == kPair ? (int)(at / quads) : 0;
+  const int64_t i = (at - z * quads) * 4, row = i / cols, col = i - row * cols;
+  if (at >= quads * t.planes) return;
+  const auto sum = [&](const float* p, int64_t step) {
+    floatx4 s = *reinterpret_cast<const floatx4*>(p);
+    for (int k = 1; k < t.splits; ++k) s += *reinterpret_cast<const floatx4*>(p + k * step);
+    return s;
+  };
+  const int64_t size = F32 ? 4 : 2;
+  if constexpr (DUAL) {
+    floatx4 v = {}, w = {}, dh = {};
+    if (row < g.m) {
+      if constexpr (MODE == kInner) {
+        if constexpr (F32) {
+          dh = load4(static_cast<const float*>(g.dh) + row * g.ld_dh + col, g.n - col);
+        } else {
+          const __bf16* p = static_cast<const __bf16*>(g.dh) + row * g.ld_dh + col;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) dh[e] = col + e < g.n ? (float)p[e] : 0.f;
+        }
+      }
+      gated<MODE, ACT, F32>(sum(g.partial + i, 2 * plane), sum(g.partial + plane + i, 2 * plane), dh, v, w);
+    }
+    if constexpr (MODE == kInner) store_inner<F32>(g, row, col, v, w);
+    else if (col < g.n) store_out<F32>(static_cast<char*>(g.out[0]) + (row * g.ld_out + col) * size, v, g.n - col);
+  } else {
+    if (col < g.n)
+      store_out<F32>(static_cast<char*>(g.out[z]) + (row * g.ld_out + col) * size,
+                     sum(g.partial + z * plane + i, t.planes * plane), g.n - col);
   }
 }
 
@@ -562,10 +609,10 @@ Plan plan_of(int mode, bool f32, int64_t m, int64_t n, int64_t k) {
   for (int s = 0; s < kShapes; ++s) {
     const ShapeInfo& h = kShape[s];
     const int64_t tiles = ((m + h.tm - 1) / h.tm) * ((n * (dual ? 2 : 1) + h.tn - 1) / h.tn) * planes;
-    for (int p = 1; p <= (dual ? 1 : kMaxSplits) && (p == 1 || p * 4 <= slabs); ++p) {
+    for (int p = 1; p <= kMaxSplits && (p == 1 || p * 4 <= slabs); ++p) {
       const int64_t rounds = (tiles * p + kCus * h.per_cu - 1) / (kCus * h.per_cu);
       double us = rounds * ((double)((slabs + p - 1) / p) * h.slab_us + 4.0);
-      if (p > 1) us += 6.0 + (double)p * planes * m * n * 8 / 3e6;
+      if (p > 1) us += 6.0 + (double)p * (dual ? 2 : planes) * m * n * 8 / 3e6;
       if (us < least) {
         least = us;
         best = {s, p};
@@ -582,9 +629,10 @@ void launch_shape(TileArgs& t, hipStream_t st) {
   t.tiles_n = (int)((t.g.n + kCols - 1) / kCols);
   t.tiles = t.tiles_m * t.tiles_n * t.planes * t.splits;
   hipLaunchKernelGGL((ffn_tile_kernel<MODE, ACT, F32, C>), dim3(t.tiles), dim3(C::threads), 0, st, t);
-  if (t.splits > 1)
-    hipLaunchKernelGGL(ffn_join_kernel<F32>, dim3((unsigned)((t.planes * t.g.m * t.g.cols_b / 4 + 255) / 256)), dim3(256),
-                       0, st, t);
+  if (t.splits > 1) {
+    const int64_t quads = t.planes * (MODE == kInner ? ffn_pad(t.g.m) : t.g.m) * partial_cols(MODE, t.g) / 4;
+    hipLaunchKernelGGL((ffn_join_kernel<MODE, ACT, F32>), dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, st, t);
+  }
 }
 
 template <int MODE, int ACT, bool F32>
@@ -619,7 +667,7 @@ hipError_t launch_type(FfnMode mode, int act, const FfnArgs& g, hipStream_t st) 
 
 size_t ffn_partial_bytes(FfnMode mode, bool f32, int64_t m, int64_t n, int64_t k) {
   const Plan p = plan_of(mode, f32, m, n, k);
-  return p.splits > 1 ? (size_t)p.splits * (mode == kPair ? 2 : 1) * m * ffn_pad(n) * sizeof(float) : 0;
+  return p.splits > 1 ? (size_t)p.splits * (mode == kSum ? 1 : 2) * m * ffn_pad(n) * sizeof(float) : 0;
 }
 
 hipError_t launch_ffn_tiles(FfnMode mode, int act, bool f32, const FfnArgs& g, hipStream_t st) {
