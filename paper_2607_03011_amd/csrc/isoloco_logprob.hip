@@ -28,27 +28,21 @@ constexpr float kLog2e = 1.44269504088896340736f;
 
 // e^x, x <= 0 where it counts: the product's rounding moves the result by |x| ulps
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+// e^d is 0 from here on down: a product with it takes this for d (which may be -infinity)
+constexpr float kNothing = -200.f;
 
-// The running softmax of one thread: m is the largest z so far, s and w as above
-// ({-infinity, 0, 0} before the first).
+// The softmax of some of a row's z: their maximum m, and s and w as above against it
+// ({-infinity, 0, 0} of nothing; a NaN or +infinity among them leaves a NaN in s).
 struct Soft {
   float m, s, w;
-  // both sums on the new maximum (both -infinity: nothing was summed; a NaN or
-  // +infinity gets through the exponential and stays)
   __device__ __forceinline__ void raise(float to) {
     if (to == m) return;
     if (m != -INFINITY) {
       const float d = m - to, e = exp_of(d);
-      w = e > 0.f ? e * (w + s * d) : 0.f;  // (s d may leave the range where e is 0)
+      w = e > 0.f ? e * (w + s * d) : 0.f;
       s = e * s;
     }
     m = to;
-  }
-  __device__ __forceinline__ void add(float z) {
-    if (z == -INFINITY) return;
-    const float d = z - m, e = exp_of(d);
-    s += e;
-    if (e > 0.f) w += e * d;
   }
   __device__ __forceinline__ void join(const Soft& o) {
     const float to = fmaxf(m, o.m);
@@ -62,30 +56,26 @@ struct Soft {
 
 // The order of the values: of equal ones (-0 and 0 among them) the lower index is
 // the larger key; NaN is above all.
+__device__ __forceinline__ uint32_t order_of(float x) {
+  const uint32_t u = __float_as_uint(x + 0.f);
+  return x != x ? 0xffffffffu : ((u >> 31) ? ~u : (u | 0x80000000u));
+}
 __device__ __forceinline__ uint64_t key_of(float x, uint32_t index) {
-  uint32_t u = __float_as_uint(x + 0.f);
-  u = x != x ? 0xffffffffu : ((u >> 31) ? ~u : (u | 0x80000000u));
-  return ((uint64_t)u << 32) | (uint32_t)~index;
+  return ((uint64_t)order_of(x) << 32) | (uint32_t)~index;
 }
 __device__ __forceinline__ float value_of(uint64_t key) {
   const uint32_t u = (uint32_t)(key >> 32);
   return __uint_as_float((u >> 31) ? (u & 0x7fffffffu) : ~u);
 }
+__device__ __forceinline__ int64_t index_of(uint64_t key) { return (int64_t)(uint32_t)~(uint32_t)key; }
 __device__ __forceinline__ uint64_t max64(uint64_t a, uint64_t b) { return a > b ? a : b; }
-__device__ __forceinline__ uint64_t shfl_xor64(uint64_t v, int off) {
-  return (uint64_t)__shfl_xor((unsigned long long)v, off, 64);
-}
-
-constexpr int kRowThreads = 1024;
-constexpr int kRowWaves = kRowThreads / 64;
-constexpr int kCandidates = 1024;
 
 template <typename T>
 struct Vec {
   static constexpr int N = 16 / sizeof(T);
 };
 template <typename T>
-__device__ __forceinline__ void unpack(u32x4 v, float (&x)[Vec<T>::N]) {
+__device__ __forceinline__ void unpack(u32x4 v, float* x) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     if constexpr (sizeof(T) == 2) {
@@ -97,21 +87,7 @@ __device__ __forceinline__ void unpack(u32x4 v, float (&x)[Vec<T>::N]) {
   }
 }
 
-// Calls f(logit, index) for the row's elements that a thread reads: 16-byte vectors
-// in turn, then single elements at the end.
-template <typename T, typename F>
-__device__ __forceinline__ void each_logit(const T* row, int64_t vocab, F f) {
-  constexpr int N = Vec<T>::N;
-  const int64_t whole = vocab / N;
-  for (int64_t i = threadIdx.x; i < whole; i += kRowThreads) {
-    float x[N];
-    unpack<T>(*reinterpret_cast<const u32x4_any*>(row + i * N), x);
-#pragma unroll
-    for (int e = 0; e < N; ++e) f(x[e], (uint32_t)(i * N + e));
-  }
-  const int64_t at = whole * N + threadIdx.x;
-  if (at < vocab) f((float)row[at], (uint32_t)at);
-}
+constexpr int kMaxSplits = 64;
 
 struct RowOut {
   float* logprob;
@@ -121,127 +97,236 @@ struct RowOut {
   int64_t* top_index;
 };
 
-// One workgroup per row.
+struct RowArgs {
+  int64_t ld, vocab;
+  float scale;
+  int top_k;
+  int splits;      // workgroups per row
+  int64_t span;    // a split's columns (a multiple of a vector's)
+  Soft* part;      // splits > 1: each one's softmax, and its top_k keys
+  uint64_t* keys;
+  RowOut o;
+};
+
+constexpr int kHeld = 64;         // logits that a thread holds in registers
+constexpr int kCandidates = 1024;
+
+// A row's results, from its softmax and (top_k) its largest keys in falling order:
+// thread i of the workgroup writes alternative i.
 template <typename T, typename ID>
-__global__ void __launch_bounds__(kRowThreads) logprob_kernel(const T* logits, int64_t ld, int64_t vocab,
-                                                              const ID* targets, float scale, int top_k, RowOut o) {
-  __shared__ Soft part[kRowWaves];
-  __shared__ uint64_t best[kRowWaves][64];
+__device__ __forceinline__ void put_row(const RowArgs& g, const T* row, const ID* targets, int64_t r, const Soft& a) {
+  const bool empty = a.m == -INFINITY && a.s == 0.f;
+  const float log_s = logf(a.s);
+  if (g.o.lse) g.o.lse[r] = empty ? -INFINITY : a.m + log_s;
+  if (g.o.entropy) g.o.entropy[r] = empty ? 0.f : log_s - a.w / a.s;
+  if (g.o.logprob) {
+    const int64_t t = targets[r];
+    float lp = 0.f;
+    if (t >= 0 && t < g.vocab) lp = empty ? -INFINITY : fmaf((float)row[t], g.scale, -a.m) - log_s;
+    g.o.logprob[r] = lp;
+  }
+}
+__device__ __forceinline__ void put_top(const RowArgs& g, int64_t r, int place, uint64_t key, const Soft& a) {
+  const bool empty = a.m == -INFINITY && a.s == 0.f;
+  g.o.top_logprob[r * g.top_k + place] = empty ? -INFINITY : fmaf(value_of(key), g.scale, -a.m) - logf(a.s);
+  g.o.top_index[r * g.top_k + place] = index_of(key);
+}
+
+// One workgroup of WAVES waves per row, or per split of a row.
+//
+// Its columns are taken kHeld per thread at a time: the maximum of those, then their
+// sums against it, 10 instructions' time per logit (4 of it the exponential) against
+// the 14 that their bytes' time allows in bfloat16 (a running maximum per vector: 18).
+//
+// Alternatives: the threads of one lane number are a group; the top_k-th largest of
+// the 64 groups' maxima bounds the top_k-th largest logit from below, and few logits
+// reach it.  Those are ranked by value and index.  Where more than kCandidates do
+// (equal values, or all of the largest in few groups), the row is gone through once
+// more per alternative.
+template <typename T, typename ID, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES, 4) logprob_kernel(const T* logits, const ID* targets, RowArgs g) {
+  constexpr int N = Vec<T>::N, kThreads = 64 * WAVES, kVecs = kHeld / N;
+  __shared__ Soft part[WAVES];
+  __shared__ float group[WAVES][64];
   __shared__ uint64_t cand[kCandidates];
-  __shared__ uint64_t wave_best[kRowWaves];
+  __shared__ uint64_t wave_best[WAVES];
   __shared__ int n_cand;
-  const int64_t r = blockIdx.x;
-  const T* row = logits + r * ld;
+  __shared__ float bound_of;
+  const int64_t r = blockIdx.x / g.splits;
+  const int split = (int)(blockIdx.x - r * g.splits);
+  const int64_t begin = split * g.span;
+  const int count = (int)min(g.span, g.vocab - begin), whole = count / N;  // (a row has at most 2^30)
+  const T* row = logits + r * g.ld;
+  const T* p = row + begin;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 
+  // the threads' logits of one turn: vectors, then single ones at the end
+  float x[kHeld], last;
+  const auto load = [&](int base) {
+    u32x4 v[kVecs];
+#pragma unroll
+    for (int c = 0; c < kVecs; ++c) {
+      const int i = base + c * kThreads + (int)threadIdx.x;
+      v[c] = sizeof(T) == 2 ? (u32x4)(0xff80ff80u) : (u32x4)(0xff800000u);  // -infinity
+      if (i < whole) v[c] = *reinterpret_cast<const u32x4_any*>(p + i * N);
+    }
+#pragma unroll
+    for (int c = 0; c < kVecs; ++c) unpack<T>(v[c], x + c * N);
+    const int at = whole * N + (int)threadIdx.x;
+    last = base == 0 && at < count ? (float)p[at] : -INFINITY;
+  };
+  constexpr int turn = kThreads * kVecs;
+  const bool once = whole <= turn;  // the registers hold all of it
+
   Soft a = {-INFINITY, 0.f, 0.f};
-  uint64_t own = 0;
-  {
-    constexpr int N = Vec<T>::N;
-    const int64_t whole = vocab / N;
-    for (int64_t i = threadIdx.x; i < whole; i += kRowThreads) {
-      float x[N];
-      unpack<T>(*reinterpret_cast<const u32x4_any*>(row + i * N), x);
-      float to = a.m;
+  float top = -INFINITY;  // the largest logit
+  for (int base = 0; base == 0 || base < whole; base += turn) {
+    load(base);
+    float most = last;
 #pragma unroll
-      for (int e = 0; e < N; ++e) to = fmaxf(to, x[e] * scale);
-      a.raise(to);
+    for (int c = 0; c < kVecs; ++c)
+      if (base + c * kThreads < whole) {
 #pragma unroll
-      for (int e = 0; e < N; ++e) {
-        a.add(x[e] * scale);
-        if (top_k) own = max64(own, key_of(x[e], (uint32_t)(i * N + e)));
+        for (int e = 0; e < N; ++e) most = fmaxf(most, x[c * N + e]);
       }
-    }
-    const int64_t at = whole * N + threadIdx.x;
-    if (at < vocab) {
-      const float x = (float)row[at];
-      a.raise(fmaxf(a.m, x * scale));
-      a.add(x * scale);
-      if (top_k) own = max64(own, key_of(x, (uint32_t)at));
-    }
+    top = fmaxf(top, most);
+    a.raise(fmaxf(a.m, most * g.scale));
+    const float m = a.m == -INFINITY ? 0.f : a.m;
+    const auto add = [&](float v) {
+      const float d = fmaf(v, g.scale, -m), e = exp_of(d);
+      a.s += e;
+      a.w = fmaf(e, fmaxf(d, kNothing), a.w);
+    };
+#pragma unroll
+    for (int c = 0; c < kVecs; ++c)
+      if (base + c * kThreads < whole) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) add(x[c * N + e]);
+      }
+    if (base == 0) add(last);
   }
+  Soft b = a;
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) {
-    Soft b;
-    b.m = __shfl_xor(a.m, off, 64);
-    b.s = __shfl_xor(a.s, off, 64);
-    b.w = __shfl_xor(a.w, off, 64);
-    a.join(b);
+    Soft o;
+    o.m = __shfl_xor(b.m, off, 64);
+    o.s = __shfl_xor(b.s, off, 64);
+    o.w = __shfl_xor(b.w, off, 64);
+    b.join(o);
   }
-  if (lane == 0) part[wave] = a;
-  if (top_k) {
-    best[wave][lane] = own;
+  if constexpr (WAVES > 1) {
+    if (lane == 0) part[wave] = b;
+  }
+  if (g.top_k) {
+    group[wave][lane] = top;
     if (threadIdx.x == 0) n_cand = 0;
   }
   __syncthreads();
-  a = part[0];
-  for (int w = 1; w < kRowWaves; ++w) a.join(part[w]);
-  const bool empty = a.m == -INFINITY && a.s == 0.f;  // (a NaN is in s)
-  const float log_s = logf(a.s), lse = empty ? -INFINITY : a.m + log_s;
+  if constexpr (WAVES > 1) {
+    b = part[0];
+    for (int w = 1; w < WAVES; ++w) b.join(part[w]);
+  }
+  const bool whole_row = g.splits == 1;
   if (threadIdx.x == 0) {
-    if (o.lse) o.lse[r] = lse;
-    if (o.entropy) o.entropy[r] = empty ? 0.f : log_s - a.w / a.s;
-    if (o.logprob) {
-      const int64_t t = targets[r];
-      float lp = 0.f;
-      if (t >= 0 && t < vocab) lp = empty ? -INFINITY : (float)row[t] * scale - a.m - log_s;
-      o.logprob[r] = lp;
-    }
+    if (whole_row) put_row(g, row, targets, r, b);
+    else g.part[blockIdx.x] = b;
   }
-  if (!top_k) return;
+  if (!g.top_k) return;
+  uint64_t* keys = g.keys + (int64_t)blockIdx.x * g.top_k;
+  const auto put = [&](int place, uint64_t key) {
+    if (whole_row) put_top(g, r, place, key, b);
+    else keys[place] = key;
+  };
 
-  // The threads of one lane number are a group; the top_k-th largest of the 64
-  // groups' largest keys bounds the top_k-th largest of all from below, and few
-  // keys are at or above it.
-  for (int w = 0; w < kRowWaves; ++w) own = max64(own, best[w][lane]);
-  int rank = 0;
+  // (a NaN is above every maximum here: such rows go the long way)
+  const bool odd = b.s != b.s;
+  if (!odd) {
+    // (one wave ranks the groups: all of them doing it took a third of the time)
+    if (wave == 0) {
+      float own = group[0][lane];
+      for (int w = 1; w < WAVES; ++w) own = fmaxf(own, group[w][lane]);
+      int rank = 0;
 #pragma unroll 8
-  for (int i = 0; i < 64; ++i) {
-    const uint64_t other = (uint64_t)__shfl((unsigned long long)own, i, 64);
-    rank += other > own || (other == own && i < lane);
-  }
-  const uint64_t at = __ballot(rank == top_k - 1);
-  const uint64_t bound = (uint64_t)__shfl((unsigned long long)own, __ffsll((unsigned long long)at) - 1, 64);
-  each_logit(row, vocab, [&](float x, uint32_t i) {
-    const uint64_t k = key_of(x, i);
-    if (k >= bound) {
-      const int c = atomicAdd(&n_cand, 1);
-      if (c < kCandidates) cand[c] = k;
+      for (int i = 0; i < 64; ++i) {
+        const float other = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(own), i));
+        rank += other > own || (other == own && i < lane);
+      }
+      if (rank == g.top_k - 1) bound_of = own;
     }
-  });
+    __syncthreads();
+    const float bound = bound_of;
+    const auto take = [&](float v, int i) {
+      if (v >= bound) {
+        const int c = atomicAdd(&n_cand, 1);
+        if (c < kCandidates) cand[c] = key_of(v, (uint32_t)(begin + i));
+      }
+    };
+    for (int base = 0; base == 0 || base < whole; base += turn) {
+      if (!once) load(base);
+#pragma unroll
+      for (int c = 0; c < kVecs; ++c) {
+        const int i = base + c * kThreads + (int)threadIdx.x;
+        float most = x[c * N];
+#pragma unroll
+        for (int e = 1; e < N; ++e) most = fmaxf(most, x[c * N + e]);
+        if (most >= bound && i < whole) {
+#pragma unroll
+          for (int e = 0; e < N; ++e) take(x[c * N + e], i * N + e);
+        }
+      }
+      const int at = whole * N + (int)threadIdx.x;
+      if (base == 0 && at < count) take(last, at);
+    }
+  }
   __syncthreads();
   const int n = n_cand;
-  if (n <= kCandidates) {
-    for (int c = threadIdx.x; c < n; c += kRowThreads) {
+  // (a split may hold fewer columns than alternatives are wanted: the keys after them are 0)
+  const int have = min(g.top_k, count);
+  if (threadIdx.x >= have && threadIdx.x < g.top_k) keys[threadIdx.x] = 0;
+  if (!odd && n <= kCandidates) {
+    for (int c = threadIdx.x; c < n; c += kThreads) {
       const uint64_t k = cand[c];
       int above = 0;
       for (int i = 0; i < n; ++i) above += cand[i] > k;
-      if (above < top_k) {
-        o.top_logprob[r * top_k + above] = empty ? -INFINITY : value_of(k) * scale - a.m - log_s;
-        o.top_index[r * top_k + above] = (int64_t)(uint32_t)~(uint32_t)k;
-      }
+      if (above < have) put(above, k);
     }
     return;
   }
-  // The largest values stand in few of the groups: one pass over the row per alternative.
-  uint64_t below = ~0ull;
-  for (int j = 0; j < top_k; ++j) {
+  uint64_t below = 0;
+  for (int j = 0; j < have; ++j) {
     uint64_t most = 0;
-    each_logit(row, vocab, [&](float x, uint32_t i) {
-      const uint64_t k = key_of(x, i);
-      if (k < below) most = max64(most, k);
-    });
+    for (int i = threadIdx.x; i < count; i += kThreads) {
+      const uint64_t k = key_of((float)p[i], (uint32_t)(begin + i));
+      if (j == 0 || k < below) most = max64(most, k);
+    }
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) most = max64(most, shfl_xor64(most, off));
+    for (int off = 32; off > 0; off >>= 1) most = max64(most, (uint64_t)__shfl_xor((unsigned long long)most, off, 64));
     __syncthreads();
     if (lane == 0) wave_best[wave] = most;
     __syncthreads();
-    for (int w = 0; w < kRowWaves; ++w) most = max64(most, wave_best[w]);
-    if (threadIdx.x == 0) {
-      o.top_logprob[r * top_k + j] = empty ? -INFINITY : value_of(most) * scale - a.m - log_s;
-      o.top_index[r * top_k + j] = (int64_t)(uint32_t)~(uint32_t)most;
-    }
+    for (int w = 0; w < WAVES; ++w) most = max64(most, wave_best[w]);
+    if (threadIdx.x == 0) put(j, most);
     below = most;
+  }
+}
+
+// A row's splits joined, in their order.
+template <typename T, typename ID>
+__global__ void __launch_bounds__(256) logprob_join_kernel(const T* logits, const ID* targets, RowArgs g) {
+  __shared__ uint64_t keys[kMaxSplits * ISOLOCO_MAX_TOP];
+  const int64_t r = blockIdx.x;
+  const Soft* part = g.part + r * g.splits;
+  Soft a = part[0];
+  for (int i = 1; i < g.splits; ++i) a.join(part[i]);
+  if (threadIdx.x == 0) put_row(g, logits + r * g.ld, targets, r, a);
+  const int n = g.splits * g.top_k;
+  for (int i = threadIdx.x; i < n; i += 256) keys[i] = g.keys[r * n + i];
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += 256) {
+    const uint64_t k = keys[i];
+    int above = 0;
+    for (int j = 0; j < n; ++j) above += keys[j] > k;
+    if (k && above < g.top_k) put_top(g, r, above, k, a);
   }
 }
 
@@ -257,11 +342,12 @@ constexpr int kGradVecs = 4;  // 16-byte vectors of a thread
 
 // One workgroup per row and span of kGradThreads * kGradVecs vectors.
 template <typename T, typename ID>
-__global__ void __launch_bounds__(kGradThreads) logprob_grad_kernel(const T* logits, int64_t ld, int64_t vocab,
+__global__ void __launch_bounds__(kGradThreads) logprob_grad_kernel(const T* logits, int64_t ld, int64_t rows, int64_t vocab,
                                                                     const ID* targets, float scale, GradIn in,
                                                                     T* dlogits, int64_t ld_d, int spans) {
   constexpr int N = Vec<T>::N;
-  const int64_t r = blockIdx.x / spans, first = (int64_t)(blockIdx.x % spans) * (kGradThreads * kGradVecs);
+  // (the last rows first: the forward pass read them last, some are still in a cache)
+  const int64_t r = rows - 1 - blockIdx.x / spans, first = (int64_t)(blockIdx.x % spans) * (kGradThreads * kGradVecs);
   const T* row = logits + r * ld;
   T* out = dlogits + r * ld_d;
   const float lse = in.lse[r];
@@ -272,7 +358,7 @@ __global__ void __launch_bounds__(kGradThreads) logprob_grad_kernel(const T* log
   // nothing to hand back: the row's logits are not read
   const bool none = lse == -INFINITY || (dl == 0.f && de == 0.f);
   const auto grad = [&](float x, int64_t i) {
-    const float lp = x * scale - lse, p = exp_of(lp);
+    const float lp = fmaf(x, scale, -lse), p = exp_of(lp);
     float d = (i == t ? 1.f : 0.f) - p;
     d *= dl;
     if (p > 0.f) d -= de * (p * (lp + h));
@@ -314,18 +400,36 @@ isoloco_status check_rows(int64_t rows, int64_t vocab, int32_t dtype, int32_t ta
   return ISOLOCO_OK;
 }
 
+// Workgroups per row: one, unless the rows are few and long.  A row of 32000 takes a
+// workgroup about as long as joining its splits would.
+int splits_of(int64_t rows, int64_t vocab) {
+  if (rows >= 128 || vocab <= 40000) return 1;
+  const int64_t most = vocab / 8192, wanted = 512 / (rows ? rows : 1);
+  const int64_t s = most < wanted ? most : wanted;
+  return (int)(s < 1 ? 1 : s > kMaxSplits ? kMaxSplits : s);
+}
+
+size_t logprob_workspace(int64_t rows, int64_t vocab, int top_k) {
+  const size_t s = (size_t)splits_of(rows, vocab);
+  return s > 1 ? (size_t)rows * s * (16 + 8 * (size_t)top_k) : 0;
+}
+
 template <typename T, typename ID>
-void run_forward(const void* logits, int64_t ld, int64_t rows, int64_t vocab, const void* targets, float scale,
-                 int top_k, const RowOut& o, hipStream_t st) {
-  hipLaunchKernelGGL((logprob_kernel<T, ID>), dim3((unsigned)rows), dim3(kRowThreads), 0, st,
-                     static_cast<const T*>(logits), ld, vocab, static_cast<const ID*>(targets), scale, top_k, o);
+void run_forward(const void* logits, const void* targets, int64_t rows, const RowArgs& g, hipStream_t st) {
+  const T* l = static_cast<const T*>(logits);
+  const ID* t = static_cast<const ID*>(targets);
+  const dim3 grid((unsigned)(rows * g.splits));
+  if (g.span <= 64 * kHeld) hipLaunchKernelGGL((logprob_kernel<T, ID, 1>), grid, dim3(64), 0, st, l, t, g);
+  else if (g.span <= 256 * kHeld) hipLaunchKernelGGL((logprob_kernel<T, ID, 4>), grid, dim3(256), 0, st, l, t, g);
+  else hipLaunchKernelGGL((logprob_kernel<T, ID, 8>), grid, dim3(512), 0, st, l, t, g);
+  if (g.splits > 1) hipLaunchKernelGGL((logprob_join_kernel<T, ID>), dim3((unsigned)rows), dim3(256), 0, st, l, t, g);
 }
 
 template <typename T, typename ID>
 void run_grad(const void* logits, int64_t ld, int64_t rows, int64_t vocab, const void* targets, float scale,
               const GradIn& in, void* dlogits, int64_t ld_d, int spans, hipStream_t st) {
   hipLaunchKernelGGL((logprob_grad_kernel<T, ID>), dim3((unsigned)(rows * spans)), dim3(kGradThreads), 0, st,
-                     static_cast<const T*>(logits), ld, vocab, static_cast<const ID*>(targets), scale, in,
+                     static_cast<const T*>(logits), ld, rows, vocab, static_cast<const ID*>(targets), scale, in,
                      static_cast<T*>(dlogits), ld_d, spans);
 }
 
@@ -351,7 +455,7 @@ isoloco_status isoloco_token_logprobs_workspace_size(int64_t rows, int64_t vocab
   if (!bytes) return fail(ISOLOCO_ERR_INVALID_ARG, "bytes is NULL");
   ISOLOCO_TRY(check_rows(rows, vocab, ISOLOCO_F32, ISOLOCO_I32, 1.f));
   if (top_k < 0 || top_k > ISOLOCO_MAX_TOP || top_k > vocab) return fail(ISOLOCO_ERR_INVALID_ARG, "top_k = %d", top_k);
-  *bytes = 0;
+  *bytes = logprob_workspace(rows, vocab, top_k);
   return ISOLOCO_OK;
 }
 
@@ -383,11 +487,23 @@ isoloco_status isoloco_token_logprobs(const void* logits, int64_t ld_logits, int
     for (const auto* y = outs; y != &x; ++y)
       if (ranges_overlap(x.p, x.bytes, y->p, y->bytes)) return fail(ISOLOCO_ERR_ALIAS, "%s overlaps %s", x.name, y->name);
   }
-  (void)workspace;
-  (void)workspace_bytes;
-  const RowOut o = {logprob, entropy, lse, top_logprob, top_index};
+  const size_t need = logprob_workspace(rows, vocab, top_k);
+  ISOLOCO_TRY(check_workspace(workspace, workspace_bytes, need));
+  if (ranges_overlap(workspace, need, logits, nb)) return fail(ISOLOCO_ERR_ALIAS, "the workspace overlaps the logits");
+  RowArgs g;
+  g.ld = ld_logits;
+  g.vocab = vocab;
+  g.scale = scale;
+  g.top_k = top_k;
+  g.splits = splits_of(rows, vocab);
+  g.span = ((vocab + g.splits - 1) / g.splits + 7) / 8 * 8;
+  g.splits = (int)((vocab + g.span - 1) / g.span);
+  g.keys = static_cast<uint64_t*>(workspace);
+  g.part = reinterpret_cast<Soft*>(g.keys + rows * g.splits * top_k);
+  g.o = {logprob, entropy, lse, top_logprob, top_index};
+  if (rows * g.splits > INT32_MAX) return fail(ISOLOCO_ERR_UNSUPPORTED, "too many rows for one launch");
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  BY_TYPES(run_forward, logits, ld_logits, rows, vocab, targets, scale, top_k, o, st);
+  BY_TYPES(run_forward, logits, targets, rows, g, st);
   const hipError_t err = hipGetLastError();
   return err == hipSuccess ? ISOLOCO_OK : hip_fail(err, "token log probabilities");
 }

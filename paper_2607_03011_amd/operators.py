@@ -4,19 +4,21 @@ The functions named ``isoloco_*`` have the name and the argument order of the C
 functions they marshal (``include/isoloco.h``) and take addresses.  The others
 take tensors: they check shapes, types and strides (``ValueError``), allocate
 what is not given with torch's allocator, and enqueue on the current torch
-stream of the tensors' device (or ``stream``, a raw stream handle).  Matrices
+stream (or ``stream``, a raw stream handle) of the current device, where the tensors
+have to be.  Matrices
 need unit stride along a row; a further leading dimension is allowed where the
 rows stay evenly spaced.  Arguments that the library itself refuses raise
 ``IsoLoCoError``.
 """
 import array
 import ctypes
+import functools
 from typing import NamedTuple, Optional
 
 import torch
 
 from . import (ISOLOCO_ACT_GELU, ISOLOCO_ACT_SILU, ISOLOCO_BF16, ISOLOCO_F32, ISOLOCO_FFN_ALIGNED,
-               ISOLOCO_FFN_BACKWARD, ISOLOCO_I32, ISOLOCO_I64, _check, _lib)
+               ISOLOCO_FFN_BACKWARD, ISOLOCO_I32, ISOLOCO_I64, IsoLoCoError, _check, _lib)
 
 _DTYPE = {torch.float32: ISOLOCO_F32, torch.bfloat16: ISOLOCO_BF16}
 _INDEX = {torch.int32: ISOLOCO_I32, torch.int64: ISOLOCO_I64}
@@ -29,7 +31,9 @@ _ACT = {"silu": ISOLOCO_ACT_SILU, "gelu": ISOLOCO_ACT_GELU}
 
 def _size_of(name, *args):
     n = ctypes.c_size_t()
-    _check(getattr(_lib, name)(*args, ctypes.byref(n)), name)
+    status = getattr(_lib, name)(*args, ctypes.byref(n))
+    if status:
+        raise IsoLoCoError(status, name)
     return n.value
 
 
@@ -104,44 +108,52 @@ def isoloco_gated_ffn_backward(x, ld_x, w_gate, w_up, ld_w, dtype, tokens, dim, 
 # Tensors
 # --------------------------------------------------------------------------
 
-class _On:
-    """The device and stream of a call: memory allocated inside belongs to that stream."""
+# (the public functions make a Stream object per call, 2 us of a small operator's 10)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
+_empty = torch.empty
+_F32 = torch.float32
 
-    def __init__(self, t, stream):
-        if not t.is_cuda:
-            raise ValueError("tensors must be on the GPU")
-        self.device = t.device
-        self.handle = stream
-        self.contexts = []
 
-    def __enter__(self):
-        if self.device.index != torch.cuda.current_device():
-            self.contexts.append(torch.cuda.device(self.device))
-            self.contexts[-1].__enter__()
-        if self.handle is None:
-            self.handle = torch.cuda.current_stream(self.device).cuda_stream
-        else:
-            self.contexts.append(torch.cuda.stream(torch.cuda.ExternalStream(self.handle, self.device)))
-            self.contexts[-1].__enter__()
-        return self
+def _with_stream(f):
+    """Adds ``stream`` (a raw handle): the call runs, and allocates, with it as the
+    current stream."""
+    @functools.wraps(f)
+    def call(*args, stream=None, **kwargs):
+        if stream is None:
+            return f(*args, **kwargs)
+        with torch.cuda.stream(torch.cuda.ExternalStream(stream)):
+            return f(*args, **kwargs)
+    return call
 
-    def __exit__(self, *exc):
-        while self.contexts:
-            self.contexts.pop().__exit__(*exc)
 
-    def empty(self, shape, dtype):
-        return torch.empty(shape, dtype=dtype, device=self.device)
+def _place(t):
+    """The index of the device that t and the call are on."""
+    index = t.get_device()
+    if index < 0:
+        raise ValueError("tensors must be on the GPU")
+    if index != torch.cuda.current_device():
+        raise ValueError("the tensors are on device %d, the current device is %d" % (index, torch.cuda.current_device()))
+    return index
 
-    def workspace(self, given, need):
-        """(address, bytes) of `given` (a uint8 tensor) or of a new one, aligned to 256 bytes."""
-        if need == 0:
-            return None, 0, None
-        t = torch.empty(need + 255, dtype=torch.uint8, device=self.device) if given is None else given
-        if t.dtype != torch.uint8 or not t.is_contiguous() or t.device != self.device:
-            raise ValueError("workspace must be a contiguous uint8 tensor on the operands' device")
-        base = t.data_ptr()
-        at = (base + 255) // 256 * 256
-        return at, max(0, base + t.numel() - at), t
+
+def _same_device(index, *tensors):
+    for t in tensors:
+        if t is not None and t.get_device() != index:
+            raise ValueError("the tensors are on different devices")
+
+
+def _workspace(given, need, device):
+    """(tensor, address, bytes) of ``given`` (uint8) or of a new one, 256-byte aligned."""
+    if need == 0:
+        return None, None, 0
+    if given is None:
+        given = _empty(need + 255, dtype=torch.uint8, device=device)
+    elif given.dtype != torch.uint8 or not given.is_contiguous() or given.device != device:
+        raise ValueError("workspace must be a contiguous uint8 tensor on the operands' device")
+    base = given.data_ptr()
+    at = (base + 255) // 256 * 256
+    return given, at, max(0, base + given.numel() - at)
 
 
 def _type(name, t):
@@ -151,14 +163,15 @@ def _type(name, t):
     return d
 
 
-def _rows(name, t, cols=None):
+def _rows(name, t):
     """(rows, ld) of a tensor seen as a matrix of its last dimension's rows."""
-    if t.dim() == 0 or (cols is not None and t.shape[-1] != cols):
-        raise ValueError("%s must end in a dimension of %s, not %s" % (name, cols, tuple(t.shape)))
+    if t.is_contiguous():
+        if not t.dim():
+            raise ValueError("%s must have a dimension" % name)
+        c = t.shape[-1]
+        return (t.numel() // c if c else 0), c
     c = t.shape[-1]
     n = t.numel() // c if c else 0
-    if t.is_contiguous():
-        return n, c
     if c > 1 and t.stride(-1) != 1:
         raise ValueError("%s must have unit stride along its last dimension" % name)
     if t.dim() == 2:
@@ -174,39 +187,31 @@ def _rows(name, t, cols=None):
     return n, ld
 
 
-def _same_device(on, **tensors):
-    for name, t in tensors.items():
-        if t is not None and t.device != on.device:
-            raise ValueError("%s is on %s, not on %s" % (name, t.device, on.device))
-
-
-def _ids(name, t, n=None):
+def _ids(name, t, n):
     i = _INDEX.get(t.dtype)
     if i is None:
         raise ValueError("%s must be int32 or int64, not %s" % (name, t.dtype))
     if not t.is_contiguous():
         raise ValueError("%s must be contiguous" % name)
-    if n is not None and t.numel() != n:
+    if t.numel() != n:
         raise ValueError("%s must have %d elements, not %d" % (name, n, t.numel()))
     return i
 
 
 def _vector(name, t, n):
-    if t.dtype != torch.float32 or not t.is_contiguous() or t.numel() != n:
+    if t.dtype != _F32 or not t.is_contiguous() or t.numel() != n:
         raise ValueError("%s must be contiguous float32 of %d elements" % (name, n))
     return t.data_ptr()
 
 
-def _output(on, name, t, shape, dtype):
-    """A new tensor, or the given one if it has the shape and type."""
-    if t is None:
-        return on.empty(shape, dtype)
+def _output(name, t, shape, dtype):
     if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
         raise ValueError("%s must be %s of %s" % (name, dtype, tuple(shape)))
     return t
 
 
-def clip_grads(grads, max_norm, out=None, workspace=None, stream=None):
+@_with_stream
+def clip_grads(grads, max_norm, out=None, workspace=None):
     """Scale the tensors of ``grads`` (contiguous, float32 or bfloat16 each) so that
     the norm over all of them is at most ``max_norm``: in place, or into the
     tensors of ``out``.  Returns a float32 tensor [norm before, coefficient] on the
@@ -214,65 +219,76 @@ def clip_grads(grads, max_norm, out=None, workspace=None, stream=None):
     grads = list(grads)
     if not grads:
         raise ValueError("no gradients")
+    index = _place(grads[0])
+    types = [_DTYPE.get(g.dtype, -1) for g in grads]
+    if -1 in types:
+        raise ValueError("gradients must be float32 or bfloat16")
+    if not all([g.is_contiguous() and g.get_device() == index for g in grads]):
+        raise ValueError("gradients must be contiguous and on one device")
+    src = [g.data_ptr() for g in grads]
+    dst = src
     if out is not None:
         out = list(out)
         if len(out) != len(grads):
             raise ValueError("out must have one tensor per gradient")
-    with _On(grads[0], stream) as on:
-        device = on.device
-        for g in grads:
-            if not g.is_contiguous() or g.device != device:
-                raise ValueError("gradients must be contiguous and on one device")
-        if out is not None:
-            for g, o in zip(grads, out):
-                if o.shape != g.shape or o.dtype != g.dtype or not o.is_contiguous() or o.device != device:
-                    raise ValueError("out must match the gradients and be contiguous")
-        types = [_type("a gradient", g) for g in grads]
-        src = [g.data_ptr() for g in grads]
-        ws, ws_bytes, keep = on.workspace(workspace, isoloco_clip_workspace_size(len(grads)))
-        norm = on.empty(2, torch.float32)
-        isoloco_clip_grads(src, src if out is None else [o.data_ptr() for o in out], [g.numel() for g in grads], types,
-                           max_norm, norm.data_ptr(), ws, ws_bytes, on.handle)
-        return norm
+        if not all([o.shape == g.shape and o.dtype == g.dtype and o.is_contiguous() and o.get_device() == index
+                    for g, o in zip(grads, out)]):
+            raise ValueError("out must match the gradients and be contiguous")
+        dst = [o.data_ptr() for o in out]
+    device = grads[0].device
+    keep, ws, ws_bytes = _workspace(workspace, isoloco_clip_workspace_size(len(grads)), device)
+    norm = _empty(2, dtype=_F32, device=device)
+    isoloco_clip_grads(src, dst, [g.numel() for g in grads], types, max_norm, norm.data_ptr(), ws, ws_bytes,
+                       _raw_stream(index))
+    return norm
 
 
-def embedding(table, ids, scale=1.0, out=None, out_dtype=None, stream=None):
+@_with_stream
+def embedding(table, ids, scale=1.0, out=None, out_dtype=None):
     """``scale * table[ids]`` in ``out_dtype`` (default: the table's); ids outside the
     table give rows of zeros."""
     if table.dim() != 2:
         raise ValueError("table must be a matrix")
-    with _On(table, stream) as on:
-        _same_device(on, ids=ids, out=out)
-        vocab, dim = table.shape
-        dtype, id_type = _type("table", table), _ids("ids", ids)
-        _, ld = _rows("table", table)
-        out = _output(on, "out", out, (*ids.shape, dim), out_dtype or (table.dtype if out is None else out.dtype))
-        n, ld_out = _rows("out", out)
-        isoloco_embedding(table.data_ptr(), ld, dtype, vocab, dim, ids.data_ptr(), id_type, ids.numel(), scale,
-                          out.data_ptr(), ld_out, _type("out", out), on.handle)
-        return out
+    index = _place(table)
+    _same_device(index, ids, out)
+    vocab, dim = table.shape
+    n = ids.numel()
+    dtype, id_type, ld = _type("table", table), _ids("ids", ids, n), _rows("table", table)[1]
+    if out is None:
+        out = _empty((*ids.shape, dim), dtype=out_dtype or table.dtype, device=table.device)
+        ld_out = dim
+    else:
+        _output("out", out, (*ids.shape, dim), out_dtype or out.dtype)
+        ld_out = _rows("out", out)[1]
+    isoloco_embedding(table.data_ptr(), ld, dtype, vocab, dim, ids.data_ptr(), id_type, n, scale, out.data_ptr(), ld_out,
+                      _type("out", out), _raw_stream(index))
+    return out
 
 
-def embedding_backward(ids, dout, vocab, scale=1.0, out=None, accumulate=False, out_dtype=None, workspace=None,
-                       stream=None):
+@_with_stream
+def embedding_backward(ids, dout, vocab, scale=1.0, out=None, accumulate=False, out_dtype=None, workspace=None):
     """The table's gradient [vocab, dim] from ``dout`` (ids' shape + [dim]), in
     ``out_dtype`` (default float32).  ``accumulate`` adds it to ``out``."""
     if accumulate and out is None:
         raise ValueError("accumulate needs out")
-    if tuple(dout.shape[:-1]) != tuple(ids.shape):
+    if dout.shape[:-1] != ids.shape:
         raise ValueError("dout must have the shape of ids and one more dimension")
-    with _On(dout, stream) as on:
-        _same_device(on, ids=ids, out=out)
-        dtype, id_type = _type("dout", dout), _ids("ids", ids)
-        dim = dout.shape[-1]
-        n, ld = _rows("dout", dout)
-        out = _output(on, "out", out, (vocab, dim), out_dtype or (torch.float32 if out is None else out.dtype))
-        _, ld_out = _rows("out", out)
-        ws, ws_bytes, keep = on.workspace(workspace, isoloco_embedding_backward_workspace_size(n, vocab, dim))
-        isoloco_embedding_backward(ids.data_ptr(), id_type, n, dout.data_ptr(), ld, dtype, vocab, dim, scale,
-                                   1 if accumulate else 0, out.data_ptr(), ld_out, _type("out", out), ws, ws_bytes,
-                                   on.handle)
-        return out
+    index = _place(dout)
+    _same_device(index, ids, out)
+    dim = dout.shape[-1]
+    n, ld = _rows("dout", dout)
+    dtype, id_type = _type("dout", dout), _ids("ids", ids, n)
+    if out is None:
+        out = _empty((vocab, dim), dtype=out_dtype or _F32, device=dout.device)
+        ld_out = dim
+    else:
+        _output("out", out, (vocab, dim), out_dtype or out.dtype)
+        ld_out = _rows("out", out)[1]
+    keep, ws, ws_bytes = _workspace(workspace, isoloco_embedding_backward_workspace_size(n, vocab, dim), dout.device)
+    isoloco_embedding_backward(ids.data_ptr(), id_type, n, dout.data_ptr(), ld, dtype, vocab, dim, scale,
+                               1 if accumulate else 0, out.data_ptr(), ld_out, _type("out", out), ws, ws_bytes,
+                               _raw_stream(index))
+    return out
 
 
 class TokenLogProbs(NamedTuple):
@@ -285,33 +301,36 @@ class TokenLogProbs(NamedTuple):
     top_index: Optional[torch.Tensor]
 
 
-def token_logprobs(logits, targets=None, scale=1.0, top_k=0, workspace=None, stream=None):
+@_with_stream
+def token_logprobs(logits, targets=None, scale=1.0, top_k=0, workspace=None):
     """Log probabilities of ``targets`` under softmax(scale * logits) over the last
     dimension, with the rows' entropy and log-sum-exp and the ``top_k`` most likely
     tokens (int64, of equal ones the lower index first).  Targets outside the
     vocabulary are ignored (0)."""
-    with _On(logits, stream) as on:
-        _same_device(on, targets=targets)
-        dtype = _type("logits", logits)
-        vocab = logits.shape[-1] if logits.dim() else 0
-        rows, ld = _rows("logits", logits)
-        shape = tuple(logits.shape[:-1])
-        t_type = _ids("targets", targets, rows) if targets is not None else 0
-        logprob = on.empty(shape, torch.float32) if targets is not None else None
-        entropy, lse = on.empty(shape, torch.float32), on.empty(shape, torch.float32)
-        top = on.empty((*shape, top_k), torch.float32) if top_k else None
-        index = on.empty((*shape, top_k), torch.int64) if top_k else None
-        ws, ws_bytes, keep = on.workspace(workspace, isoloco_token_logprobs_workspace_size(rows, vocab, top_k))
-        isoloco_token_logprobs(logits.data_ptr(), ld, dtype, rows, vocab,
-                               targets.data_ptr() if targets is not None else None, t_type, scale, top_k,
-                               logprob.data_ptr() if targets is not None else None, entropy.data_ptr(),
-                               lse.data_ptr(), top.data_ptr() if top_k else None, index.data_ptr() if top_k else None,
-                               ws, ws_bytes, on.handle)
-        return TokenLogProbs(logprob, entropy, lse, top, index)
+    index = _place(logits)
+    dtype = _type("logits", logits)
+    rows, ld = _rows("logits", logits)
+    shape, vocab, device = logits.shape[:-1], logits.shape[-1], logits.device
+    entropy, lse = _empty(shape, dtype=_F32, device=device), _empty(shape, dtype=_F32, device=device)
+    logprob = target_at = logprob_at = top = top_index = top_at = index_at = None
+    t_type = 0
+    if targets is not None:
+        _same_device(index, targets)
+        t_type = _ids("targets", targets, rows)
+        logprob = _empty(shape, dtype=_F32, device=device)
+        target_at, logprob_at = targets.data_ptr(), logprob.data_ptr()
+    if top_k:
+        top = _empty((*shape, top_k), dtype=_F32, device=device)
+        top_index = _empty((*shape, top_k), dtype=torch.int64, device=device)
+        top_at, index_at = top.data_ptr(), top_index.data_ptr()
+    keep, ws, ws_bytes = _workspace(workspace, isoloco_token_logprobs_workspace_size(rows, vocab, top_k), device)
+    isoloco_token_logprobs(logits.data_ptr(), ld, dtype, rows, vocab, target_at, t_type, scale, top_k, logprob_at,
+                           entropy.data_ptr(), lse.data_ptr(), top_at, index_at, ws, ws_bytes, _raw_stream(index))
+    return TokenLogProbs(logprob, entropy, lse, top, top_index)
 
 
-def token_logprobs_backward(logits, targets, lse, dlogprob, entropy=None, dentropy=None, scale=1.0, out=None,
-                            stream=None):
+@_with_stream
+def token_logprobs_backward(logits, targets, lse, dlogprob, entropy=None, dentropy=None, scale=1.0, out=None):
     """The gradient in the logits from that of ``token_logprobs``' logprob (and
     entropy), given its lse (and entropy).  ``targets`` and ``dlogprob`` may both be
     None; ``out`` may be ``logits`` itself."""
@@ -319,68 +338,88 @@ def token_logprobs_backward(logits, targets, lse, dlogprob, entropy=None, dentro
         raise ValueError("targets and dlogprob go together")
     if dentropy is not None and entropy is None:
         raise ValueError("dentropy needs entropy")
-    with _On(logits, stream) as on:
-        _same_device(on, targets=targets, lse=lse, dlogprob=dlogprob, entropy=entropy, dentropy=dentropy, out=out)
-        dtype = _type("logits", logits)
-        vocab = logits.shape[-1] if logits.dim() else 0
-        rows, ld = _rows("logits", logits)
-        t_type = _ids("targets", targets, rows) if targets is not None else 0
-        out = _output(on, "out", out, tuple(logits.shape), logits.dtype)
-        _, ld_out = _rows("out", out)
-        isoloco_token_logprobs_backward(
-            logits.data_ptr(), ld, dtype, rows, vocab, targets.data_ptr() if targets is not None else None, t_type,
-            scale, _vector("lse", lse, rows), _vector("entropy", entropy, rows) if dentropy is not None else None,
-            _vector("dlogprob", dlogprob, rows) if dlogprob is not None else None,
-            _vector("dentropy", dentropy, rows) if dentropy is not None else None, out.data_ptr(), ld_out, on.handle)
-        return out
+    index = _place(logits)
+    _same_device(index, targets, lse, dlogprob, entropy, dentropy, out)
+    dtype = _type("logits", logits)
+    rows, ld = _rows("logits", logits)
+    vocab = logits.shape[-1]
+    target_at = dlogprob_at = entropy_at = dentropy_at = None
+    t_type = 0
+    if targets is not None:
+        t_type = _ids("targets", targets, rows)
+        target_at, dlogprob_at = targets.data_ptr(), _vector("dlogprob", dlogprob, rows)
+    if dentropy is not None:
+        entropy_at, dentropy_at = _vector("entropy", entropy, rows), _vector("dentropy", dentropy, rows)
+    if out is None:
+        out = _empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        ld_out = vocab
+    else:
+        _output("out", out, logits.shape, logits.dtype)
+        ld_out = _rows("out", out)[1]
+    isoloco_token_logprobs_backward(logits.data_ptr(), ld, dtype, rows, vocab, target_at, t_type, scale,
+                                    _vector("lse", lse, rows), entropy_at, dlogprob_at, dentropy_at, out.data_ptr(),
+                                    ld_out, _raw_stream(index))
+    return out
 
 
-def _ffn_operands(on, x, w_gate, w_up, act):
+def _ffn_operands(x, w_gate, w_up, act):
+    index = _place(x)
+    _same_device(index, w_gate, w_up)
     dtype = _type("x", x)
     if w_gate.dim() != 2 or w_gate.shape != w_up.shape or w_gate.dtype != x.dtype or w_up.dtype != x.dtype:
         raise ValueError("w_gate and w_up must be [hidden, dim] matrices of x's type")
-    _same_device(on, w_gate=w_gate, w_up=w_up)
     hidden, dim = w_gate.shape
-    tokens, ld_x = _rows("x", x, dim)
-    ld_w, ld_u = _rows("w_gate", w_gate)[1], _rows("w_up", w_up)[1]
-    if ld_w != ld_u:
+    if not x.dim() or x.shape[-1] != dim:
+        raise ValueError("x must end in a dimension of %d, not %s" % (dim, tuple(x.shape)))
+    tokens, ld_x = _rows("x", x)
+    ld_w = _rows("w_gate", w_gate)[1]
+    if ld_w != _rows("w_up", w_up)[1]:
         raise ValueError("w_gate and w_up must have the same row stride")
-    if act not in _ACT:
+    a = _ACT.get(act)
+    if a is None:
         raise ValueError("act must be one of %s" % ", ".join(sorted(_ACT)))
-    aligned = (ld_x | ld_w) % 8 == 0 and (x.data_ptr() | w_gate.data_ptr() | w_up.data_ptr()) % 16 == 0
-    return dtype, tokens, dim, hidden, ld_x, ld_w, _ACT[act], ISOLOCO_FFN_ALIGNED if aligned else 0
+    at = x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr()
+    aligned = not ((ld_x | ld_w) & 7 or (at[0] | at[1] | at[2]) & 15)
+    return index, dtype, tokens, dim, hidden, ld_x, ld_w, a, at, ISOLOCO_FFN_ALIGNED if aligned else 0
 
 
-def gated_ffn(x, w_gate, w_up, act="silu", out=None, workspace=None, stream=None):
+@_with_stream
+def gated_ffn(x, w_gate, w_up, act="silu", out=None, workspace=None):
     """``act(x w_gate^T) * (x w_up^T)`` for x [..., dim] and weights [hidden, dim]; act
     is "silu" or "gelu"."""
-    with _On(x, stream) as on:
-        dtype, tokens, dim, hidden, ld_x, ld_w, a, flags = _ffn_operands(on, x, w_gate, w_up, act)
-        _same_device(on, out=out)
-        out = _output(on, "out", out, (*x.shape[:-1], hidden), x.dtype)
-        _, ld_out = _rows("out", out)
-        ws, ws_bytes, keep = on.workspace(workspace, isoloco_gated_ffn_workspace_size(tokens, dim, hidden, dtype,
-                                                                                               flags))
-        isoloco_gated_ffn(x.data_ptr(), ld_x, w_gate.data_ptr(), w_up.data_ptr(), ld_w, dtype, tokens, dim, hidden, a,
-                          out.data_ptr(), ld_out, ws, ws_bytes, on.handle)
-        return out
+    index, dtype, tokens, dim, hidden, ld_x, ld_w, a, at, flags = _ffn_operands(x, w_gate, w_up, act)
+    if out is None:
+        out = _empty((*x.shape[:-1], hidden), dtype=x.dtype, device=x.device)
+        ld_out = hidden
+    else:
+        _same_device(index, out)
+        _output("out", out, (*x.shape[:-1], hidden), x.dtype)
+        ld_out = _rows("out", out)[1]
+    keep, ws, ws_bytes = _workspace(workspace, isoloco_gated_ffn_workspace_size(tokens, dim, hidden, dtype, flags),
+                                    x.device)
+    isoloco_gated_ffn(at[0], ld_x, at[1], at[2], ld_w, dtype, tokens, dim, hidden, a, out.data_ptr(), ld_out, ws,
+                      ws_bytes, _raw_stream(index))
+    return out
 
 
-def gated_ffn_backward(x, w_gate, w_up, dout, act="silu", need_dx=True, need_dw=True, workspace=None, stream=None):
+@_with_stream
+def gated_ffn_backward(x, w_gate, w_up, dout, act="silu", need_dx=True, need_dw=True, workspace=None):
     """(dx, dw_gate, dw_up) from ``dout`` [..., hidden]; None for what is not needed."""
-    with _On(x, stream) as on:
-        dtype, tokens, dim, hidden, ld_x, ld_w, a, flags = _ffn_operands(on, x, w_gate, w_up, act)
-        _same_device(on, dout=dout)
-        if dout.dtype != x.dtype or tuple(dout.shape) != (*x.shape[:-1], hidden):
-            raise ValueError("dout must be %s of %s" % (x.dtype, (*x.shape[:-1], hidden)))
-        _, ld_dout = _rows("dout", dout, hidden)
-        dx = on.empty(x.shape, x.dtype) if need_dx else None
-        dwg = on.empty((hidden, dim), x.dtype) if need_dw else None
-        dwu = on.empty((hidden, dim), x.dtype) if need_dw else None
-        ws, ws_bytes, keep = on.workspace(workspace, isoloco_gated_ffn_workspace_size(
-            tokens, dim, hidden, dtype, flags | ISOLOCO_FFN_BACKWARD))
-        isoloco_gated_ffn_backward(x.data_ptr(), ld_x, w_gate.data_ptr(), w_up.data_ptr(), ld_w, dtype, tokens, dim,
-                                   hidden, a, dout.data_ptr(), ld_dout, dx.data_ptr() if need_dx else None, dim,
-                                   dwg.data_ptr() if need_dw else None, dwu.data_ptr() if need_dw else None, dim, ws,
-                                   ws_bytes, on.handle)
-        return dx, dwg, dwu
+    index, dtype, tokens, dim, hidden, ld_x, ld_w, a, at, flags = _ffn_operands(x, w_gate, w_up, act)
+    _same_device(index, dout)
+    if dout.dtype != x.dtype or tuple(dout.shape) != (*x.shape[:-1], hidden):
+        raise ValueError("dout must be %s of %s" % (x.dtype, (*x.shape[:-1], hidden)))
+    ld_dout, device = _rows("dout", dout)[1], x.device
+    dx = dwg = dwu = dx_at = dwg_at = dwu_at = None
+    if need_dx:
+        dx = _empty(x.shape, dtype=x.dtype, device=device)
+        dx_at = dx.data_ptr()
+    if need_dw:
+        dwg = _empty((hidden, dim), dtype=x.dtype, device=device)
+        dwu = _empty((hidden, dim), dtype=x.dtype, device=device)
+        dwg_at, dwu_at = dwg.data_ptr(), dwu.data_ptr()
+    keep, ws, ws_bytes = _workspace(workspace, isoloco_gated_ffn_workspace_size(
+        tokens, dim, hidden, dtype, flags | ISOLOCO_FFN_BACKWARD), device)
+    isoloco_gated_ffn_backward(at[0], ld_x, at[1], at[2], ld_w, dtype, tokens, dim, hidden, a, dout.data_ptr(), ld_dout,
+                               dx_at, dim, dwg_at, dwu_at, dim, ws, ws_bytes, _raw_stream(index))
+    return dx, dwg, dwu
