@@ -12,12 +12,14 @@
 // atomics on the values: the same bits every time).  The grouping is one launch:
 // workgroup b of NB owns the ids that are b modulo NB (frequent ids are
 // neighbours in most vocabularies: this spreads them) and reads all ids, which
-// come from the caches; it counts the tokens of workgroups before it, so no
+// come from the caches; it counts the tokens of the groups before its own, so no
 // workgroup waits for another.  Ids with more than kPiece tokens are summed in
 // pieces of the sorted order, which a last launch adds.
 #include <hip/hip_runtime.h>
 
 #include <stdint.h>
+
+#include <algorithm>
 
 #include "isoloco_device.h"
 #include "isoloco_error.h"
@@ -102,18 +104,15 @@ __global__ void __launch_bounds__(256) embed_kernel(const TT* table, int64_t ld_
 constexpr int kGroupThreads = 1024;
 constexpr int kGroupWaves = kGroupThreads / 64;
 constexpr int kMinGroups = 256;       // one workgroup per CU
-constexpr int kGroupIds = 4096;       // most ids of a workgroup (16 KiB of LDS each for counts and cursors)
+constexpr int kGroupIds = 1024;       // most ids of a workgroup (a count per wave: 64 KiB of LDS)
 constexpr int kPiece = 64;            // tokens that one wave sums
 
-// Workspace: the tokens grouped by id, the tokens as each workgroup found them,
-// per id its first place and its count, the number of grouped tokens, and the
+// Workspace: the tokens grouped by id, per id its first place and its count, the number of grouped tokens, and the
 // sums of the pieces of frequent ids (two places per piece of the order: an id
 // that ends in it and one that begins in it).
 struct GroupTables {
   int32_t* order;   // n
-  int32_t* found;   // n
-  int32_t* first;   // vocab
-  int32_t* count;   // vocab
+  int2* row;        // vocab: an id's first place and its count
   int32_t* total;   // 1
   float* piece;     // 2 * ceil(n / kPiece) * dim
 };
@@ -124,113 +123,160 @@ int groups_of(int64_t vocab) {
   return nb;
 }
 
+// Each wave takes a run of the tokens, kChunk at a time, kHeld per lane; a run of one
+// chunk stays in registers between the counting and the placing.
+constexpr int kHeld = 32;
+constexpr int kChunk = 64 * kHeld;
+
 template <typename ID>
 __global__ void __launch_bounds__(kGroupThreads) group_kernel(const ID* ids, int32_t n, int64_t vocab, int nb_log2,
                                                              GroupTables g) {
-  __shared__ int32_t cursor[kGroupIds];
-  __shared__ int32_t wave_cnt[kGroupWaves], wave_before[kGroupWaves], wave_scan[kGroupWaves];
+  // each wave's tokens by id; then where the next of them goes
+  __shared__ int32_t cursor[kGroupWaves][kGroupIds];
+  __shared__ int32_t wave_before[kGroupWaves], wave_scan[kGroupWaves];
   const int nb = 1 << nb_log2, b = blockIdx.x;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int mine = (int)((vocab - b + nb - 1) >> nb_log2);  // ids b, b + nb, ... below vocab
-  for (int i = threadIdx.x; i < mine; i += kGroupThreads) cursor[i] = 0;
-  __syncthreads();
+  for (int i = lane; i < mine; i += 64) cursor[wave][i] = 0;
 
-  // each wave reads a run of tokens, twice: counts, then places
   const int run = ((n + kGroupWaves - 1) / kGroupWaves + 63) / 64 * 64;
-  const int from = min((int64_t)n, (int64_t)wave * run), to = min((int64_t)n, (int64_t)from + run);
-  int before = 0, cnt = 0;
-  for (int t = from + lane; t < to; t += 64) {
-    const int64_t id = ids[t];
-    if (id >= 0 && id < vocab) {
-      const int grp = (int)(id & (nb - 1));
-      before += grp < b;
-      if (grp == b) {
-        ++cnt;
-        atomicAdd(&cursor[id >> nb_log2], 1);
+  const int from = (int)min((int64_t)n, (int64_t)wave * run), to = (int)min((int64_t)n, (int64_t)from + run);
+  // this lane's ids of the chunk from `at` on, -1 where there is no token, and per 64 of
+  // them which are of this group
+  int32_t held[kHeld];
+  uint64_t mask[kHeld];
+  const auto load = [&](int at) {
+    constexpr int kAtOnce = sizeof(ID) == 8 ? 16 : 32;
+#pragma unroll
+    for (int h = 0; h < kHeld; h += kAtOnce) {
+      ID id[kAtOnce];
+#pragma unroll
+      for (int q = 0; q < kAtOnce; ++q) {
+        const int t0 = at + (h + q) * 64, t = t0 + lane;
+        id[q] = (ID)-1;
+        if (t0 < to && t < to) id[q] = ids[t];
       }
+#pragma unroll
+      for (int q = 0; q < kAtOnce; ++q) {
+        bool valid = (uint32_t)id[q] < (uint32_t)vocab;  // (vocab is below 2^31)
+        if constexpr (sizeof(ID) == 8) valid = valid && (uint32_t)((uint64_t)id[q] >> 32) == 0;
+        held[h + q] = valid ? (int32_t)id[q] : -1;
+        mask[h + q] = __ballot((held[h + q] & (int32_t)(0x80000000u | (nb - 1))) == b);
+      }
+    }
+  };
+  int before = 0;  // tokens of the groups before this one
+  for (int at = from; at < to; at += kChunk) {
+    load(at);
+#pragma unroll
+    for (int q = 0; q < kHeld; ++q) {
+      before += (held[q] & (nb - 1)) < b;  // (-1 is in the last group here: before none)
+      if (mask[q] && ((mask[q] >> lane) & 1)) atomicAdd(&cursor[wave][held[q] >> nb_log2], 1);
     }
   }
 #pragma unroll
-  for (int off = 32; off > 0; off >>= 1) {
-    before += __shfl_xor(before, off, 64);
-    cnt += __shfl_xor(cnt, off, 64);
-  }
-  if (lane == 0) {
-    wave_cnt[wave] = cnt;
-    wave_before[wave] = before;
-  }
+  for (int off = 32; off > 0; off >>= 1) before += __shfl_xor(before, off, 64);
+  if (lane == 0) wave_before[wave] = before;
   __syncthreads();
-  int base = 0, at = 0, m = 0;
-  for (int w = 0; w < kGroupWaves; ++w) {
-    base += wave_before[w];
-    if (w < wave) at += wave_cnt[w];
-    m += wave_cnt[w];
-  }
-  if (b == nb - 1 && threadIdx.x == 0) *g.total = base + m;
-  // the tokens of this workgroup in their order
-  at += base;
-  for (int t0 = from; t0 < to; t0 += 64) {
-    const int t = t0 + lane;
-    const int64_t id = t < to ? (int64_t)ids[t] : -1;
-    const bool hit = id >= 0 && id < vocab && (int)(id & (nb - 1)) == b;
-    const uint64_t mask = __ballot(hit);
-    if (hit) g.found[at + __popcll(mask & ((1ull << lane) - 1))] = t;
-    at += __popcll(mask);
-  }
-  // where each id's tokens go: its counts' running sum, 1024 ids a turn
-  int carry = base;
-  for (int i0 = 0; i0 < mine; i0 += kGroupThreads) {
-    const int i = i0 + threadIdx.x;
-    const int c = i < mine ? cursor[i] : 0;
-    int s = c;
+  // where each id's tokens go: the running sum of the ids' counts, one id per thread, and
+  // of the waves' in it
+  const int i = threadIdx.x;
+  int cnt[kGroupWaves], c = 0, base = 0;
 #pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-      const int o = __shfl_up(s, off, 64);
-      if (lane >= off) s += o;
-    }
-    __syncthreads();
-    if (lane == 63) wave_scan[wave] = s;
-    __syncthreads();
-    int begin = carry + s - c;
+  for (int w = 0; w < kGroupWaves; ++w) {
+    cnt[w] = i < mine ? cursor[w][i] : 0;
+    c += cnt[w];
+    base += wave_before[w];
+  }
+  int s = c;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const int o = __shfl_up(s, off, 64);
+    if (lane >= off) s += o;
+  }
+  if (lane == 63) wave_scan[wave] = s;
+  __syncthreads();
+  int begin = base + s - c, m = 0;
+  for (int w = 0; w < kGroupWaves; ++w) {
+    if (w < wave) begin += wave_scan[w];
+    m += wave_scan[w];
+  }
+  if (i < mine) {
+    g.row[((int64_t)i << nb_log2) + b] = make_int2(begin, c);
+#pragma unroll
     for (int w = 0; w < kGroupWaves; ++w) {
-      if (w < wave) begin += wave_scan[w];
-      carry += wave_scan[w];
-    }
-    if (i < mine) {
-      cursor[i] = begin;
-      const int64_t id = ((int64_t)i << nb_log2) + b;
-      g.first[id] = begin;
-      g.count[id] = c;
+      cursor[w][i] = begin;
+      begin += cnt[w];
     }
   }
-  __syncthreads();  // also: this workgroup's found[] is visible to all of it
-  // each wave places the tokens of the ids that are its own modulo the waves
-  for (int j0 = 0; j0 < m; j0 += 64) {
-    const int j = j0 + lane;
-    const int t = j < m ? g.found[base + j] : -1;
-    const int local = t >= 0 ? (int)((int64_t)ids[t] >> nb_log2) : -1;
-    uint64_t todo = __ballot(t >= 0 && (local & (kGroupWaves - 1)) == wave);
-    while (todo) {
-      const int lead = __ffsll((unsigned long long)todo) - 1;
-      const int which = __shfl(local, lead, 64);
-      const uint64_t same = __ballot(t >= 0 && local == which);
-      int start = 0;
-      if (lane == 0) {
-        start = cursor[which];
-        cursor[which] = start + __popcll(same);
+  if (b == nb - 1 && i == 0) *g.total = base + m;
+  __syncthreads();
+  for (int at = from; at < to; at += kChunk) {
+    if (run > kChunk) load(at);
+#pragma unroll
+    for (int q = 0; q < kHeld; ++q) {
+      uint64_t todo = mask[q];
+      while (todo) {
+        const int id = __builtin_amdgcn_readlane(held[q], __ffsll((unsigned long long)todo) - 1);
+        const uint64_t same = __ballot(held[q] == id);
+        int start = 0;
+        if (lane == 0) {
+          start = cursor[wave][id >> nb_log2];
+          cursor[wave][id >> nb_log2] = start + __popcll(same);
+        }
+        start = __builtin_amdgcn_readfirstlane(start);
+        if ((same >> lane) & 1) g.order[start + __popcll(same & ((1ull << lane) - 1))] = at + q * 64 + lane;
+        todo &= ~same;
       }
-      start = __shfl(start, 0, 64);
-      if ((same >> lane) & 1) g.order[start + __popcll(same & ((1ull << lane) - 1))] = t;
-      todo &= ~same;
     }
   }
 }
 
+// 8 columns of a row as they are stored
 template <typename TD>
-__device__ __forceinline__ floatx8 sum_tokens(const int32_t* order, int from, int to, const TD* dout, int64_t ld,
-                                              int col, int left) {
+struct Raw {
+  u32x4 v[sizeof(TD) / 2];
+  __device__ __forceinline__ void load(const TD* p, int left) {
+    if (left >= kCols) {
+#pragma unroll
+      for (int i = 0; i < (int)sizeof(TD) / 2; ++i)
+        v[i] = *reinterpret_cast<const u32x4_any*>(reinterpret_cast<const char*>(p) + 16 * i);
+    } else {
+      TD x[kCols];
+#pragma unroll
+      for (int i = 0; i < kCols; ++i) x[i] = i < left ? p[i] : (TD)0.f;
+      __builtin_memcpy(v, x, sizeof v);
+    }
+  }
+  __device__ __forceinline__ void add_to(floatx8& s) const { s += load8(reinterpret_cast<const TD*>(v)); }
+};
+
+// The sum of the c <= 64 tokens that the lanes hold (`t` of lane j is the j-th), 16 rows
+// of bfloat16 or 8 of float32 in flight.
+template <typename TD>
+__device__ __forceinline__ floatx8 sum_tokens(int t, int c, const TD* dout, int64_t ld, int col, int left) {
+  constexpr int kAhead = 32 / sizeof(TD);
   floatx8 s = {};
-  for (int j = from; j < to; ++j) s += load8(dout + (int64_t)order[j] * ld + col, left);
+  int j = 0;
+  for (; j + kAhead <= c; j += kAhead) {
+    Raw<TD> v[kAhead];
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) v[a].load(dout + (int64_t)__builtin_amdgcn_readlane(t, j + a) * ld + col, left);
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) v[a].add_to(s);
+  }
+  for (; j + 4 <= c; j += 4) {
+    Raw<TD> v[4];
+#pragma unroll
+    for (int a = 0; a < 4; ++a) v[a].load(dout + (int64_t)__builtin_amdgcn_readlane(t, j + a) * ld + col, left);
+#pragma unroll
+    for (int a = 0; a < 4; ++a) v[a].add_to(s);
+  }
+  for (; j < c; ++j) {
+    Raw<TD> v;
+    v.load(dout + (int64_t)__builtin_amdgcn_readlane(t, j) * ld + col, left);
+    v.add_to(s);
+  }
   return s;
 }
 
@@ -241,41 +287,84 @@ __device__ __forceinline__ void put_row(TG* dtable, int64_t at, floatx8 s, float
   store8(dtable + at, s, left);
 }
 
-// Rows of at most kPiece tokens: one wave per id and span of columns.
-template <typename TD, typename TG>
-__global__ void __launch_bounds__(256) embed_rows_kernel(GroupTables g, const TD* dout, int64_t ld_dout, int64_t vocab,
-                                                         int dim, float scale, int accumulate, TG* dtable,
-                                                         int64_t ld_dtable, int spans) {
-  const int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t v = item / spans;
-  if (v >= vocab) return;
-  const int c = g.count[v];
-  if (c > kPiece || (c == 0 && accumulate)) return;
-  const int col = (int)(item % spans) * kSpan + (threadIdx.x & 63) * kCols;
-  if (col >= dim) return;
-  const int f = g.first[v];
-  const floatx8 s = sum_tokens(g.order, f, f + c, dout, ld_dout, col, dim - col);
-  put_row(dtable, v * ld_dtable + col, s, scale, accumulate, dim - col);
-}
-
 // The frequent ids that the piece [k kPiece, (k + 1) kPiece) of the order touches:
 // such an id has more tokens than a piece, so it holds the piece's first or last place.
 template <typename TD, typename ID>
-__global__ void __launch_bounds__(256) embed_pieces_kernel(GroupTables g, const ID* ids, const TD* dout,
-                                                           int64_t ld_dout, int dim, int spans, int pieces) {
-  const int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int k = (int)(item / spans);
-  if (k >= pieces) return;
-  const int col = (int)(item % spans) * kSpan + (threadIdx.x & 63) * kCols;
-  const int total = *g.total, from = k * kPiece, to = min(total, from + kPiece);
-  if (from >= to || col >= dim) return;
-  const int64_t va = ids[g.order[from]], vb = ids[g.order[to - 1]];
-  if (g.count[va] > kPiece)
-    store8(g.piece + (int64_t)(2 * k) * dim + col,
-           sum_tokens(g.order, from, min(to, g.first[va] + g.count[va]), dout, ld_dout, col, dim - col), dim - col);
-  if (vb != va && g.count[vb] > kPiece)
-    store8(g.piece + (int64_t)(2 * k + 1) * dim + col,
-           sum_tokens(g.order, g.first[vb], to, dout, ld_dout, col, dim - col), dim - col);
+__device__ __forceinline__ void sum_piece(const GroupTables& g, const ID* ids, const TD* dout, int64_t ld_dout, int dim,
+                                          int k, int col) {
+  const int lane = threadIdx.x & 63;
+  const int total = *g.total, from = k * kPiece, c = min(total - from, kPiece);
+  if (c <= 0) return;
+  const int t = g.order[from + min(lane, c - 1)];
+  const int64_t va = ids[__builtin_amdgcn_readlane(t, 0)], vb = ids[__builtin_amdgcn_readlane(t, c - 1)];
+  const int2 ra = g.row[va], rb = g.row[vb];
+  if (ra.y > kPiece) {
+    const floatx8 s = sum_tokens(t, min(c, ra.x + ra.y - from), dout, ld_dout, col, dim - col);
+    if (col < dim) store8(g.piece + (int64_t)(2 * k) * dim + col, s, dim - col);
+  }
+  if (vb != va && rb.y > kPiece) {
+    const int skip = rb.x - from;  // lane j then holds the j-th token of vb
+    const floatx8 s =
+        sum_tokens(__shfl(t, min(lane + skip, c - 1), 64), c - skip, dout, ld_dout, col, dim - col);
+    if (col < dim) store8(g.piece + (int64_t)(2 * k + 1) * dim + col, s, dim - col);
+  }
+}
+
+// One wave per item, many items per wave: first the pieces of frequent ids (the longest
+// items), then the rows of at most kPiece tokens, each times the spans of columns.  A
+// row's place, count and tokens are loaded while the rows before it are summed: most
+// rows have few tokens or none and cost little but the wait for those.
+template <typename TD, typename TG, typename ID>
+__global__ void __launch_bounds__(256) embed_sums_kernel(GroupTables g, const ID* ids, const TD* dout, int64_t ld_dout,
+                                                         int64_t vocab, int dim, float scale, int accumulate,
+                                                         TG* dtable, int64_t ld_dtable, int spans, int pieces) {
+  const int lane = threadIdx.x & 63;
+  const int64_t waves = (int64_t)gridDim.x * 4, first = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t piece_items = (int64_t)pieces * spans;
+  int64_t item = first;
+  for (; item < piece_items; item += waves) {
+    const int k = (int)(item / spans);
+    sum_piece(g, ids, dout, ld_dout, dim, k, ((int)(item - (int64_t)k * spans) * 64 + lane) * kCols);
+  }
+  // the row and span of an item, and of the wave's next one
+  struct Place {
+    int64_t v;
+    int span;
+  };
+  const int64_t step_v = waves / spans;
+  const int step_span = (int)(waves - step_v * spans);
+  const auto after = [&](Place p) {
+    p.v += step_v;
+    p.span += step_span;
+    if (p.span >= spans) {
+      p.span -= spans;
+      ++p.v;
+    }
+    return p;
+  };
+  const auto row_of = [&](Place p) { return p.v < vocab ? g.row[p.v] : make_int2(0, 0); };
+  const auto tokens_of = [&](int2 r) { return r.y > 0 && r.y <= kPiece ? g.order[r.x + min(lane, r.y - 1)] : 0; };
+  Place at;
+  at.v = (item - piece_items) / spans;
+  at.span = (int)(item - piece_items - at.v * spans);
+  Place to = after(at);
+  int2 r = row_of(at), r_next = row_of(to);
+  int t = tokens_of(r);
+  while (at.v < vocab) {
+    const Place then = after(to);
+    const int2 r_then = row_of(then);
+    const int t_next = tokens_of(r_next);
+    const int col = (at.span * 64 + lane) * kCols, c = __builtin_amdgcn_readfirstlane(r.y);
+    if (c <= kPiece && !(c == 0 && accumulate) && col < dim) {
+      const floatx8 s = sum_tokens(t, c, dout, ld_dout, col, dim - col);
+      put_row(dtable, at.v * ld_dtable + col, s, scale, accumulate, dim - col);
+    }
+    at = to;
+    to = then;
+    r = r_next;
+    r_next = r_then;
+    t = t_next;
+  }
 }
 
 // The frequent id that begins in a piece (at most one does), from its pieces' sums.
@@ -286,11 +375,12 @@ __global__ void __launch_bounds__(64) embed_join_kernel(GroupTables g, const ID*
   const int total = *g.total, from = k * kPiece, to = min(total, from + kPiece);
   if (from >= to || col >= dim) return;
   const int64_t v = ids[g.order[to - 1]];
-  const int f = g.first[v], c = g.count[v];
+  const int f = g.row[v].x, c = g.row[v].y;
   if (c <= kPiece || f < from) return;
   const int left = dim - col;
   floatx8 s = load8(g.piece + (int64_t)(2 * k + (f > from)) * dim + col, left);
-  for (int j = k + 1; j * kPiece < f + c; ++j) s += load8(g.piece + (int64_t)(2 * j) * dim + col, left);
+#pragma unroll 8
+  for (int j = k + 1; j <= (f + c - 1) / kPiece; ++j) s += load8(g.piece + (int64_t)(2 * j) * dim + col, left);
   put_row(dtable, v * ld_dtable + col, s, scale, accumulate, left);
 }
 
@@ -306,9 +396,7 @@ size_t group_layout(int64_t n, int64_t vocab, int64_t dim, char* base, GroupTabl
   };
   GroupTables t;
   t.order = reinterpret_cast<int32_t*>(take(4 * (size_t)n));
-  t.found = reinterpret_cast<int32_t*>(take(4 * (size_t)n));
-  t.first = reinterpret_cast<int32_t*>(take(4 * (size_t)vocab));
-  t.count = reinterpret_cast<int32_t*>(take(4 * (size_t)vocab));
+  t.row = reinterpret_cast<int2*>(take(8 * (size_t)vocab));
   t.total = reinterpret_cast<int32_t*>(take(4));
   t.piece = reinterpret_cast<float*>(take(8 * (size_t)((n + kPiece - 1) / kPiece) * (size_t)dim));
   if (g) *g = t;
@@ -337,17 +425,14 @@ hipError_t run_backward(const GroupTables& g, const ID* ids, int64_t n, const TD
   const int nb = groups_of(vocab);
   hipLaunchKernelGGL(group_kernel<ID>, dim3(nb), dim3(kGroupThreads), 0, st, ids, (int32_t)n, vocab,
                      __builtin_ctz(nb), g);
-  unsigned grid;
-  wave_grid(vocab * spans, &grid);
-  hipLaunchKernelGGL((embed_rows_kernel<TD, TG>), dim3(grid), dim3(256), 0, st, g, dout, ld_dout, vocab, dim, scale,
-                     accumulate, dtable, ld_dtable, spans);
-  if (n > kPiece) {
-    wave_grid((int64_t)pieces * spans, &grid);
-    hipLaunchKernelGGL((embed_pieces_kernel<TD, ID>), dim3(grid), dim3(256), 0, st, g, ids, dout, ld_dout, dim, spans,
-                       pieces);
+  const int pieced = n > kPiece ? pieces : 0;
+  // 5 workgroups of 4 waves are on a CU at a time
+  const int64_t items = (vocab + pieced) * spans, blocks = std::min<int64_t>((items + 3) / 4, 5 * 256);
+  hipLaunchKernelGGL((embed_sums_kernel<TD, TG, ID>), dim3((unsigned)blocks), dim3(256), 0, st, g, ids, dout, ld_dout,
+                     vocab, dim, scale, accumulate, dtable, ld_dtable, spans, pieced);
+  if (pieced)
     hipLaunchKernelGGL((embed_join_kernel<ID, TG>), dim3(pieces, spans), dim3(64), 0, st, g, ids, dim, scale,
                        accumulate, dtable, ld_dtable);
-  }
   return hipGetLastError();
 }
 
@@ -448,8 +533,7 @@ isoloco_status isoloco_embedding_backward(const void* ids, int32_t id_type, int6
       ranges_overlap(workspace, need, ids, (size_t)n * ei))
     return fail(ISOLOCO_ERR_ALIAS, "dtable or the workspace overlaps another buffer");
   const int64_t spans = (dim + kSpan - 1) / kSpan;
-  unsigned grid;
-  if (!wave_grid(vocab * spans, &grid) || spans > 65535 || !wave_grid((n / kPiece + 1) * spans, &grid))
+  if (spans > 65535)
     return fail(ISOLOCO_ERR_UNSUPPORTED, "too many elements for one launch");
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
   const hipError_t e =
