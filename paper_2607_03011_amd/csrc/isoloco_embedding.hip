@@ -20,6 +20,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "isoloco_device.h"
 #include "isoloco_error.h"
@@ -28,57 +29,78 @@ namespace isoloco {
 namespace {
 
 typedef float floatx8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef u32x4 u32x4_any __attribute__((aligned(2)));
-typedef floatx4 floatx4_any __attribute__((aligned(4)));
+typedef u32x2 u32x2_any __attribute__((aligned(2)));
 
-constexpr int kCols = 8;            // columns of a row that a lane holds
-constexpr int kSpan = 64 * kCols;   // columns of a row that a wave holds
-
-template <typename T>
-__device__ __forceinline__ floatx8 load8(const T* p) {
-  floatx8 r;
-  if constexpr (sizeof(T) == 2) {
-    const u32x4 v = *reinterpret_cast<const u32x4_any*>(p);
+// N (4 or 8) columns of a row: as stored, and as float32.  A lane holds N, a wave 64 N.
+template <int N>
+struct Cols {
+  typedef float F __attribute__((ext_vector_type(N)));
+  template <typename T>
+  struct Raw {
+    static constexpr int kBytes = N * sizeof(T);
+    uint32_t v[kBytes / 4];
+    // the first n of them, zeros after those
+    __device__ __forceinline__ void load(const T* p, int n) {
+      if (n >= N) {
+        if constexpr (kBytes == 8) {
+          __builtin_memcpy(v, reinterpret_cast<const u32x2_any*>(p), 8);
+        } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      r[2 * i] = bf16_to_f32(v[i] & 0xffffu);
-      r[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
-    }
-  } else {
-    const floatx4 a = *reinterpret_cast<const floatx4_any*>(p), b = *reinterpret_cast<const floatx4_any*>(p + 4);
+          for (int i = 0; i < kBytes / 16; ++i) {
+            const u32x4 x = *reinterpret_cast<const u32x4_any*>(reinterpret_cast<const char*>(p) + 16 * i);
+            __builtin_memcpy(v + 4 * i, &x, 16);
+          }
+        }
+      } else {
+        T x[N];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      r[i] = a[i];
-      r[4 + i] = b[i];
+        for (int i = 0; i < N; ++i) x[i] = i < n ? p[i] : (T)0.f;
+        __builtin_memcpy(v, x, kBytes);
+      }
     }
+    __device__ __forceinline__ F get() const {
+      F r;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        if constexpr (sizeof(T) == 2) r[i] = __uint_as_float(i & 1 ? v[i / 2] & 0xffff0000u : v[i / 2] << 16);
+        else r[i] = __uint_as_float(v[i]);
+      }
+      return r;
+    }
+  };
+  template <typename T>
+  __device__ static __forceinline__ F load(const T* p, int n) {
+    Raw<T> r;
+    r.load(p, n);
+    return r.get();
   }
-  return r;
-}
-// the first n of 8 values, zeros after them
-template <typename T>
-__device__ __forceinline__ floatx8 load8(const T* p, int n) {
-  if (n >= kCols) return load8(p);
-  floatx8 r;
+  template <typename T>
+  __device__ static __forceinline__ void store(T* p, F x, int n) {
+    typedef T TN __attribute__((ext_vector_type(N)));
+    const TN r = __builtin_convertvector(x, TN);
+    if (n >= N) {
+      if constexpr (N * sizeof(T) == 8) {
+        *reinterpret_cast<u32x2_any*>(p) = __builtin_bit_cast(u32x2, r);
+      } else {
+        u32x4 w[N * sizeof(T) / 16];
+        __builtin_memcpy(w, &r, sizeof w);
 #pragma unroll
-  for (int i = 0; i < kCols; ++i) r[i] = i < n ? (float)p[i] : 0.f;
-  return r;
-}
-template <typename T>
-__device__ __forceinline__ void store8(T* p, floatx8 v, int n) {
-  if (n >= kCols) {
-    if constexpr (sizeof(T) == 2) {
-      *reinterpret_cast<u32x4_any*>(p) = __builtin_bit_cast(u32x4, __builtin_convertvector(v, bf16x8_t));
+        for (int i = 0; i < (int)(N * sizeof(T) / 16); ++i)
+          *reinterpret_cast<u32x4_any*>(reinterpret_cast<char*>(p) + 16 * i) = w[i];
+      }
     } else {
-      *reinterpret_cast<floatx4_any*>(p) = (floatx4){v[0], v[1], v[2], v[3]};
-      *reinterpret_cast<floatx4_any*>(p + 4) = (floatx4){v[4], v[5], v[6], v[7]};
-    }
-    return;
-  }
 #pragma unroll
-  for (int i = 0; i < kCols; ++i)
-    if (i < n) p[i] = (T)v[i];
-}
+      for (int i = 0; i < N; ++i)
+        if (i < n) p[i] = r[i];
+    }
+  }
+};
+
+// Columns per lane: 16 bytes of the rows that are written (lookup) or read (gradient), so
+// that a wave's access is one run of memory.
+template <typename T>
+constexpr int kColsOf = 16 / sizeof(T);
 
 // One wave per token and span of columns.
 template <typename TT, typename TO, typename ID>
@@ -88,13 +110,14 @@ __global__ void __launch_bounds__(256) embed_kernel(const TT* table, int64_t ld_
   const int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t t = item / spans;
   if (t >= n) return;
-  const int col = (int)(item % spans) * kSpan + (threadIdx.x & 63) * kCols;
+  typedef Cols<kColsOf<TO>> C;
+  const int col = ((int)(item % spans) * 64 + (threadIdx.x & 63)) * kColsOf<TO>;
   if (col >= dim) return;
   const int64_t id = ids[t];
   const int left = dim - col;
-  floatx8 v = {};
-  if (id >= 0 && id < vocab) v = load8(table + id * ld_table + col, left) * scale;
-  store8(out + t * ld_out + col, v, left);
+  typename C::F v = {};
+  if (id >= 0 && id < vocab) v = C::load(table + id * ld_table + col, left) * scale;
+  C::store(out + t * ld_out + col, v, left);
 }
 
 // ---------------------------------------------------------------------------
@@ -232,64 +255,40 @@ __global__ void __launch_bounds__(kGroupThreads) group_kernel(const ID* ids, int
   }
 }
 
-// 8 columns of a row as they are stored
-template <typename TD>
-struct Raw {
-  u32x4 v[sizeof(TD) / 2];
-  __device__ __forceinline__ void load(const TD* p, int left) {
-    if (left >= kCols) {
-#pragma unroll
-      for (int i = 0; i < (int)sizeof(TD) / 2; ++i)
-        v[i] = *reinterpret_cast<const u32x4_any*>(reinterpret_cast<const char*>(p) + 16 * i);
-    } else {
-      TD x[kCols];
-#pragma unroll
-      for (int i = 0; i < kCols; ++i) x[i] = i < left ? p[i] : (TD)0.f;
-      __builtin_memcpy(v, x, sizeof v);
-    }
-  }
-  __device__ __forceinline__ void add_to(floatx8& s) const { s += load8(reinterpret_cast<const TD*>(v)); }
-};
-
-// The sum of the c <= 64 tokens that the lanes hold (`t` of lane j is the j-th), 16 rows
-// of bfloat16 or 8 of float32 in flight.
-template <typename TD>
-__device__ __forceinline__ floatx8 sum_tokens(int t, int c, const TD* dout, int64_t ld, int col, int left) {
-  constexpr int kAhead = 32 / sizeof(TD);
-  floatx8 s = {};
+// The sum of the c <= 64 tokens that the lanes hold (`t` of lane j is the j-th), with
+// 64 registers' worth of rows in flight.
+template <int N, typename TD>
+__device__ __forceinline__ typename Cols<N>::F sum_tokens(int t, int c, const TD* dout, int64_t ld, int col, int left) {
+  typedef typename Cols<N>::template Raw<TD> Raw;
+  typename Cols<N>::F s = {};
   int j = 0;
-  for (; j + kAhead <= c; j += kAhead) {
-    Raw<TD> v[kAhead];
+  const auto take = [&](auto ahead) {
+    constexpr int kAhead = decltype(ahead)::value;
+    Raw v[kAhead];
 #pragma unroll
     for (int a = 0; a < kAhead; ++a) v[a].load(dout + (int64_t)__builtin_amdgcn_readlane(t, j + a) * ld + col, left);
 #pragma unroll
-    for (int a = 0; a < kAhead; ++a) v[a].add_to(s);
-  }
-  for (; j + 4 <= c; j += 4) {
-    Raw<TD> v[4];
-#pragma unroll
-    for (int a = 0; a < 4; ++a) v[a].load(dout + (int64_t)__builtin_amdgcn_readlane(t, j + a) * ld + col, left);
-#pragma unroll
-    for (int a = 0; a < 4; ++a) v[a].add_to(s);
-  }
-  for (; j < c; ++j) {
-    Raw<TD> v;
-    v.load(dout + (int64_t)__builtin_amdgcn_readlane(t, j) * ld + col, left);
-    v.add_to(s);
-  }
+    for (int a = 0; a < kAhead; ++a) s += v[a].get();
+    j += kAhead;
+  };
+  constexpr int kMost = 256 / Raw::kBytes;
+  while (j + kMost <= c) take(std::integral_constant<int, kMost>());
+  while (j + 4 <= c) take(std::integral_constant<int, 4>());
+  while (j < c) take(std::integral_constant<int, 1>());
   return s;
 }
 
-template <typename TG>
-__device__ __forceinline__ void put_row(TG* dtable, int64_t at, floatx8 s, float scale, int accumulate, int left) {
+template <int N, typename TG>
+__device__ __forceinline__ void put_row(TG* dtable, int64_t at, typename Cols<N>::F s, float scale, int accumulate,
+                                        int left) {
   s *= scale;
-  if (accumulate) s += load8(dtable + at, left);
-  store8(dtable + at, s, left);
+  if (accumulate) s += Cols<N>::load(dtable + at, left);
+  Cols<N>::store(dtable + at, s, left);
 }
 
 // The frequent ids that the piece [k kPiece, (k + 1) kPiece) of the order touches:
 // such an id has more tokens than a piece, so it holds the piece's first or last place.
-template <typename TD, typename ID>
+template <int N, typename TD, typename ID>
 __device__ __forceinline__ void sum_piece(const GroupTables& g, const ID* ids, const TD* dout, int64_t ld_dout, int dim,
                                           int k, int col) {
   const int lane = threadIdx.x & 63;
@@ -299,14 +298,14 @@ __device__ __forceinline__ void sum_piece(const GroupTables& g, const ID* ids, c
   const int64_t va = ids[__builtin_amdgcn_readlane(t, 0)], vb = ids[__builtin_amdgcn_readlane(t, c - 1)];
   const int2 ra = g.row[va], rb = g.row[vb];
   if (ra.y > kPiece) {
-    const floatx8 s = sum_tokens(t, min(c, ra.x + ra.y - from), dout, ld_dout, col, dim - col);
-    if (col < dim) store8(g.piece + (int64_t)(2 * k) * dim + col, s, dim - col);
+    const auto s = sum_tokens<N>(t, min(c, ra.x + ra.y - from), dout, ld_dout, col, dim - col);
+    if (col < dim) Cols<N>::store(g.piece + (int64_t)(2 * k) * dim + col, s, dim - col);
   }
   if (vb != va && rb.y > kPiece) {
     const int skip = rb.x - from;  // lane j then holds the j-th token of vb
-    const floatx8 s =
-        sum_tokens(__shfl(t, min(lane + skip, c - 1), 64), c - skip, dout, ld_dout, col, dim - col);
-    if (col < dim) store8(g.piece + (int64_t)(2 * k + 1) * dim + col, s, dim - col);
+    const auto s =
+        sum_tokens<N>(__shfl(t, min(lane + skip, c - 1), 64), c - skip, dout, ld_dout, col, dim - col);
+    if (col < dim) Cols<N>::store(g.piece + (int64_t)(2 * k + 1) * dim + col, s, dim - col);
   }
 }
 
@@ -318,13 +317,14 @@ template <typename TD, typename TG, typename ID>
 __global__ void __launch_bounds__(256) embed_sums_kernel(GroupTables g, const ID* ids, const TD* dout, int64_t ld_dout,
                                                          int64_t vocab, int dim, float scale, int accumulate,
                                                          TG* dtable, int64_t ld_dtable, int spans, int pieces) {
+  constexpr int N = kColsOf<TD>;
   const int lane = threadIdx.x & 63;
   const int64_t waves = (int64_t)gridDim.x * 4, first = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t piece_items = (int64_t)pieces * spans;
   int64_t item = first;
   for (; item < piece_items; item += waves) {
     const int k = (int)(item / spans);
-    sum_piece(g, ids, dout, ld_dout, dim, k, ((int)(item - (int64_t)k * spans) * 64 + lane) * kCols);
+    sum_piece<N>(g, ids, dout, ld_dout, dim, k, ((int)(item - (int64_t)k * spans) * 64 + lane) * N);
   }
   // the row and span of an item, and of the wave's next one
   struct Place {
@@ -354,10 +354,10 @@ __global__ void __launch_bounds__(256) embed_sums_kernel(GroupTables g, const ID
     const Place then = after(to);
     const int2 r_then = row_of(then);
     const int t_next = tokens_of(r_next);
-    const int col = (at.span * 64 + lane) * kCols, c = __builtin_amdgcn_readfirstlane(r.y);
+    const int col = (at.span * 64 + lane) * N, c = __builtin_amdgcn_readfirstlane(r.y);
     if (c <= kPiece && !(c == 0 && accumulate) && col < dim) {
-      const floatx8 s = sum_tokens(t, c, dout, ld_dout, col, dim - col);
-      put_row(dtable, at.v * ld_dtable + col, s, scale, accumulate, dim - col);
+      const auto s = sum_tokens<N>(t, c, dout, ld_dout, col, dim - col);
+      put_row<N>(dtable, at.v * ld_dtable + col, s, scale, accumulate, dim - col);
     }
     at = to;
     to = then;
@@ -371,17 +371,19 @@ __global__ void __launch_bounds__(256) embed_sums_kernel(GroupTables g, const ID
 template <typename ID, typename TG>
 __global__ void __launch_bounds__(64) embed_join_kernel(GroupTables g, const ID* ids, int dim, float scale,
                                                         int accumulate, TG* dtable, int64_t ld_dtable) {
-  const int k = blockIdx.x, col = blockIdx.y * kSpan + threadIdx.x * kCols;
+  constexpr int N = kColsOf<TG>;
+  typedef Cols<N> C;
+  const int k = blockIdx.x, col = (blockIdx.y * 64 + threadIdx.x) * N;
   const int total = *g.total, from = k * kPiece, to = min(total, from + kPiece);
   if (from >= to || col >= dim) return;
   const int64_t v = ids[g.order[to - 1]];
   const int f = g.row[v].x, c = g.row[v].y;
   if (c <= kPiece || f < from) return;
   const int left = dim - col;
-  floatx8 s = load8(g.piece + (int64_t)(2 * k + (f > from)) * dim + col, left);
+  typename C::F s = C::load(g.piece + (int64_t)(2 * k + (f > from)) * dim + col, left);
 #pragma unroll 8
-  for (int j = k + 1; j <= (f + c - 1) / kPiece; ++j) s += load8(g.piece + (int64_t)(2 * j) * dim + col, left);
-  put_row(dtable, v * ld_dtable + col, s, scale, accumulate, left);
+  for (int j = k + 1; j <= (f + c - 1) / kPiece; ++j) s += C::load(g.piece + (int64_t)(2 * j) * dim + col, left);
+  put_row<N>(dtable, v * ld_dtable + col, s, scale, accumulate, left);
 }
 
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
@@ -421,6 +423,7 @@ bool wave_grid(int64_t items, unsigned* grid) {
 template <typename TD, typename TG, typename ID>
 hipError_t run_backward(const GroupTables& g, const ID* ids, int64_t n, const TD* dout, int64_t ld_dout, int64_t vocab,
                         int dim, float scale, int accumulate, TG* dtable, int64_t ld_dtable, hipStream_t st) {
+  constexpr int kSpan = 64 * kColsOf<TD>;
   const int spans = (dim + kSpan - 1) / kSpan, pieces = (int)((n + kPiece - 1) / kPiece);
   const int nb = groups_of(vocab);
   hipLaunchKernelGGL(group_kernel<ID>, dim3(nb), dim3(kGroupThreads), 0, st, ids, (int32_t)n, vocab,
@@ -431,7 +434,7 @@ hipError_t run_backward(const GroupTables& g, const ID* ids, int64_t n, const TD
   hipLaunchKernelGGL((embed_sums_kernel<TD, TG, ID>), dim3((unsigned)blocks), dim3(256), 0, st, g, ids, dout, ld_dout,
                      vocab, dim, scale, accumulate, dtable, ld_dtable, spans, pieced);
   if (pieced)
-    hipLaunchKernelGGL((embed_join_kernel<ID, TG>), dim3(pieces, spans), dim3(64), 0, st, g, ids, dim, scale,
+    hipLaunchKernelGGL((embed_join_kernel<ID, TG>), dim3(pieces, (dim + 64 * kColsOf<TG> - 1) / (64 * kColsOf<TG>)), dim3(64), 0, st, g, ids, dim, scale,
                        accumulate, dtable, ld_dtable);
   return hipGetLastError();
 }
@@ -483,7 +486,8 @@ isoloco_status isoloco_embedding(const void* table, int64_t ld_table, int32_t dt
   if (ranges_overlap(out, ob, table, matrix_bytes(vocab, dim, ld_table, et)) ||
       ranges_overlap(out, ob, ids, (size_t)n * ei))
     return fail(ISOLOCO_ERR_ALIAS, "out overlaps the table or the ids");
-  const int spans = (int)((dim + kSpan - 1) / kSpan);
+  const int64_t span = 64 * (16 / (int64_t)eo);
+  const int spans = (int)((dim + span - 1) / span);
   unsigned grid;
   if (!wave_grid(n * spans, &grid)) return fail(ISOLOCO_ERR_UNSUPPORTED, "too many elements for one launch");
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
@@ -532,8 +536,7 @@ isoloco_status isoloco_embedding_backward(const void* ids, int32_t id_type, int6
       ranges_overlap(workspace, need, dtable, tb) || ranges_overlap(workspace, need, dout, db) ||
       ranges_overlap(workspace, need, ids, (size_t)n * ei))
     return fail(ISOLOCO_ERR_ALIAS, "dtable or the workspace overlaps another buffer");
-  const int64_t spans = (dim + kSpan - 1) / kSpan;
-  if (spans > 65535)
+  if (dim > 65535 * 256)
     return fail(ISOLOCO_ERR_UNSUPPORTED, "too many elements for one launch");
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
   const hipError_t e =
