@@ -18,8 +18,8 @@ namespace isoloco {
 namespace {
 
 // Tensors per launch: their pointers and sizes travel in the launch's arguments
-// (3.6 of the 4 KiB that these may take), so that no table is copied to the device.
-constexpr int kClipTensors = 128;
+// (3.9 of the 4 KiB that these may take), so that no table is copied to the device.
+constexpr int kClipTensors = 160;
 constexpr int kClipThreads = 512;
 // Four workgroups of 8 waves fill a CU.  The number of partial sums of a launch.
 constexpr int kClipBlocks = 1024;
@@ -30,8 +30,8 @@ constexpr int kChunkBytes = kClipThreads * kVecBytes * kUnroll;
 struct ClipArgs {
   const void* src[kClipTensors];
   void* dst[kClipTensors];
-  int64_t count[kClipTensors];
   int32_t first[kClipTensors + 1];  // first chunk of each tensor; then the number of chunks
+  int32_t last[kClipTensors];       // bytes of its last chunk (the others are whole)
   uint8_t bf16[kClipTensors];
   int32_t n;
 };
@@ -49,6 +49,10 @@ __device__ __forceinline__ int tensor_of(const ClipArgs& a, int chunk) {
     else hi = mid - 1;
   }
   return lo;
+}
+
+__device__ __forceinline__ int chunk_bytes(const ClipArgs& a, int t, int chunk) {
+  return chunk + 1 == a.first[t + 1] ? a.last[t] : kChunkBytes;
 }
 
 // Squares are summed in 64 bits: those of values past 1.8e19 or below 1e-23 leave
@@ -69,7 +73,7 @@ __device__ __forceinline__ void add_squares(double& s, u32x4 v) {
 }
 
 template <bool BF16>
-__device__ __forceinline__ double chunk_squares(const char* p, int64_t bytes) {
+__device__ __forceinline__ double chunk_squares(const char* p, int bytes) {
   constexpr int kElem = BF16 ? 2 : 4;
   double s = 0.0;
   if (bytes >= kChunkBytes) {
@@ -81,11 +85,11 @@ __device__ __forceinline__ double chunk_squares(const char* p, int64_t bytes) {
     for (int u = 0; u < kUnroll; ++u) add_squares<BF16>(s, v[u]);
     return s;
   }
-  const int left = (int)bytes, whole = left / kVecBytes;
+  const int whole = bytes / kVecBytes;
   for (int i = threadIdx.x; i < whole; i += kClipThreads)
     add_squares<BF16>(s, *reinterpret_cast<const u32x4_any*>(p + i * kVecBytes));
   const int at = whole * kVecBytes + (int)threadIdx.x * kElem;
-  if (at < left) {
+  if (at < bytes) {
     const double x = BF16 ? (double)bf16_to_f32(*reinterpret_cast<const uint16_t*>(p + at))
                           : (double)*reinterpret_cast<const float*>(p + at);
     s = fma(x, x, s);
@@ -101,11 +105,9 @@ __global__ void __launch_bounds__(kClipThreads) clip_norm_kernel(ClipArgs a, dou
   const int chunks = a.first[a.n];
   for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
     const int t = tensor_of(a, c);
-    const int elem = a.bf16[t] ? 2 : 4;
-    const int64_t off = (int64_t)(c - a.first[t]) * kChunkBytes;
-    const char* p = static_cast<const char*>(a.src[t]) + off;
-    const int64_t left = a.count[t] * elem - off;
-    s += a.bf16[t] ? chunk_squares<true>(p, left) : chunk_squares<false>(p, left);
+    const char* p = static_cast<const char*>(a.src[t]) + (int64_t)(c - a.first[t]) * kChunkBytes;
+    const int bytes = chunk_bytes(a, t, c);
+    s += a.bf16[t] ? chunk_squares<true>(p, bytes) : chunk_squares<false>(p, bytes);
   }
   s = block_sum<kClipThreads / 64>(s, lds);
   if (threadIdx.x == 0) part[blockIdx.x] = s;
@@ -149,7 +151,7 @@ __device__ __forceinline__ u32x4 scaled(u32x4 v, float c) {
 }
 
 template <bool BF16>
-__device__ __forceinline__ void scale_chunk(const char* p, char* q, int64_t bytes, float c) {
+__device__ __forceinline__ void scale_chunk(const char* p, char* q, int bytes, float c) {
   constexpr int kElem = BF16 ? 2 : 4;
   if (bytes >= kChunkBytes) {
     u32x4 v[kUnroll];
@@ -161,12 +163,12 @@ __device__ __forceinline__ void scale_chunk(const char* p, char* q, int64_t byte
       *reinterpret_cast<u32x4_any*>(q + (u * kClipThreads + (int)threadIdx.x) * kVecBytes) = scaled<BF16>(v[u], c);
     return;
   }
-  const int left = (int)bytes, whole = left / kVecBytes;
+  const int whole = bytes / kVecBytes;
   for (int i = threadIdx.x; i < whole; i += kClipThreads)
     *reinterpret_cast<u32x4_any*>(q + i * kVecBytes) =
         scaled<BF16>(*reinterpret_cast<const u32x4_any*>(p + i * kVecBytes), c);
   const int at = whole * kVecBytes + (int)threadIdx.x * kElem;
-  if (at < left) {
+  if (at < bytes) {
     if constexpr (BF16)
       *reinterpret_cast<uint16_t*>(q + at) = (uint16_t)scale_pair(*reinterpret_cast<const uint16_t*>(p + at), c);
     else
@@ -184,18 +186,17 @@ __global__ void __launch_bounds__(kClipThreads) clip_scale_kernel(ClipArgs a, co
     out[0] = r[0];
     out[1] = r[1];
   }
-  const int chunks = a.first[a.n];
-  for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
+  // the last chunks first: the norm's pass read them last, some are still in a cache
+  for (int c = a.first[a.n] - 1 - (int)blockIdx.x; c >= 0; c -= gridDim.x) {
     const int t = tensor_of(a, c);
     // nothing to write: the tensor stays where it is and as it is
     if (a.dst[t] == a.src[t] && r[1] == 1.f) continue;
-    const int elem = a.bf16[t] ? 2 : 4;
     const int64_t off = (int64_t)(c - a.first[t]) * kChunkBytes;
     const char* p = static_cast<const char*>(a.src[t]) + off;
     char* q = static_cast<char*>(a.dst[t]) + off;
-    const int64_t left = a.count[t] * elem - off;
-    if (a.bf16[t]) scale_chunk<true>(p, q, left, r[1]);
-    else scale_chunk<false>(p, q, left, r[1]);
+    const int bytes = chunk_bytes(a, t, c);
+    if (a.bf16[t]) scale_chunk<true>(p, q, bytes, r[1]);
+    else scale_chunk<false>(p, q, bytes, r[1]);
   }
 }
 
@@ -261,8 +262,8 @@ isoloco_status isoloco_clip_grads(const void* const* src, void* const* dst, cons
         if (chunks + c > INT32_MAX) break;
         a.src[a.n] = src[at];
         a.dst[a.n] = dst ? dst[at] : nullptr;
-        a.count[a.n] = counts[at];
         a.first[a.n] = (int32_t)chunks;
+        a.last[a.n] = (int32_t)(bytes - (c - 1) * kChunkBytes);
         a.bf16[a.n] = dtypes[at] == ISOLOCO_BF16;
         chunks += c;
         ++a.n;
