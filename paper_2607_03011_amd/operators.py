@@ -29,7 +29,9 @@ _ACT = {"silu": ISOLOCO_ACT_SILU, "gelu": ISOLOCO_ACT_GELU}
 # The C functions
 # --------------------------------------------------------------------------
 
+@functools.lru_cache(maxsize=1024)
 def _size_of(name, *args):
+    # (a size is a function of its arguments alone)
     n = ctypes.c_size_t()
     status = getattr(_lib, name)(*args, ctypes.byref(n))
     if status:
@@ -133,7 +135,8 @@ def _place(t):
     if index < 0:
         raise ValueError("tensors must be on the GPU")
     if index != torch.cuda.current_device():
-        raise ValueError("the tensors are on device %d, the current device is %d" % (index, torch.cuda.current_device()))
+        raise ValueError("the tensors are on device %d, the current device is %d" %
+                         (index, torch.cuda.current_device()))
     return index
 
 
@@ -260,8 +263,9 @@ def embedding(table, ids, scale=1.0, out=None, out_dtype=None):
     else:
         _output("out", out, (*ids.shape, dim), out_dtype or out.dtype)
         ld_out = _rows("out", out)[1]
-    isoloco_embedding(table.data_ptr(), ld, dtype, vocab, dim, ids.data_ptr(), id_type, n, scale, out.data_ptr(), ld_out,
-                      _type("out", out), _raw_stream(index))
+    _check(_lib.isoloco_embedding(table.data_ptr(), ld, dtype, vocab, dim, ids.data_ptr(), id_type, n, scale,
+                                  out.data_ptr(), ld_out, _type("out", out), _raw_stream(index)),
+           "isoloco_embedding")
     return out
 
 
@@ -285,9 +289,10 @@ def embedding_backward(ids, dout, vocab, scale=1.0, out=None, accumulate=False, 
         _output("out", out, (vocab, dim), out_dtype or out.dtype)
         ld_out = _rows("out", out)[1]
     keep, ws, ws_bytes = _workspace(workspace, isoloco_embedding_backward_workspace_size(n, vocab, dim), dout.device)
-    isoloco_embedding_backward(ids.data_ptr(), id_type, n, dout.data_ptr(), ld, dtype, vocab, dim, scale,
-                               1 if accumulate else 0, out.data_ptr(), ld_out, _type("out", out), ws, ws_bytes,
-                               _raw_stream(index))
+    _check(_lib.isoloco_embedding_backward(ids.data_ptr(), id_type, n, dout.data_ptr(), ld, dtype, vocab, dim, scale, 1
+                                           if accumulate else 0, out.data_ptr(), ld_out, _type("out", out), ws,
+                                           ws_bytes, _raw_stream(index)),
+           "isoloco_embedding_backward")
     return out
 
 
@@ -311,21 +316,24 @@ def token_logprobs(logits, targets=None, scale=1.0, top_k=0, workspace=None):
     dtype = _type("logits", logits)
     rows, ld = _rows("logits", logits)
     shape, vocab, device = logits.shape[:-1], logits.shape[-1], logits.device
-    entropy, lse = _empty(shape, dtype=_F32, device=device), _empty(shape, dtype=_F32, device=device)
     logprob = target_at = logprob_at = top = top_index = top_at = index_at = None
     t_type = 0
     if targets is not None:
         _same_device(index, targets)
         t_type = _ids("targets", targets, rows)
-        logprob = _empty(shape, dtype=_F32, device=device)
+        entropy, lse, logprob = _empty((3, *shape), dtype=_F32, device=device).unbind()
         target_at, logprob_at = targets.data_ptr(), logprob.data_ptr()
+    else:
+        entropy, lse = _empty((2, *shape), dtype=_F32, device=device).unbind()
     if top_k:
         top = _empty((*shape, top_k), dtype=_F32, device=device)
         top_index = _empty((*shape, top_k), dtype=torch.int64, device=device)
         top_at, index_at = top.data_ptr(), top_index.data_ptr()
     keep, ws, ws_bytes = _workspace(workspace, isoloco_token_logprobs_workspace_size(rows, vocab, top_k), device)
-    isoloco_token_logprobs(logits.data_ptr(), ld, dtype, rows, vocab, target_at, t_type, scale, top_k, logprob_at,
-                           entropy.data_ptr(), lse.data_ptr(), top_at, index_at, ws, ws_bytes, _raw_stream(index))
+    _check(_lib.isoloco_token_logprobs(logits.data_ptr(), ld, dtype, rows, vocab, target_at, t_type, scale, top_k,
+                                       logprob_at, entropy.data_ptr(), lse.data_ptr(), top_at, index_at, ws, ws_bytes,
+                                       _raw_stream(index)),
+           "isoloco_token_logprobs")
     return TokenLogProbs(logprob, entropy, lse, top, top_index)
 
 
@@ -356,9 +364,10 @@ def token_logprobs_backward(logits, targets, lse, dlogprob, entropy=None, dentro
     else:
         _output("out", out, logits.shape, logits.dtype)
         ld_out = _rows("out", out)[1]
-    isoloco_token_logprobs_backward(logits.data_ptr(), ld, dtype, rows, vocab, target_at, t_type, scale,
-                                    _vector("lse", lse, rows), entropy_at, dlogprob_at, dentropy_at, out.data_ptr(),
-                                    ld_out, _raw_stream(index))
+    _check(_lib.isoloco_token_logprobs_backward(logits.data_ptr(), ld, dtype, rows, vocab, target_at, t_type, scale,
+                                                _vector("lse", lse, rows), entropy_at, dlogprob_at, dentropy_at,
+                                                out.data_ptr(), ld_out, _raw_stream(index)),
+           "isoloco_token_logprobs_backward")
     return out
 
 
@@ -397,8 +406,9 @@ def gated_ffn(x, w_gate, w_up, act="silu", out=None, workspace=None):
         ld_out = _rows("out", out)[1]
     keep, ws, ws_bytes = _workspace(workspace, isoloco_gated_ffn_workspace_size(tokens, dim, hidden, dtype, flags),
                                     x.device)
-    isoloco_gated_ffn(at[0], ld_x, at[1], at[2], ld_w, dtype, tokens, dim, hidden, a, out.data_ptr(), ld_out, ws,
-                      ws_bytes, _raw_stream(index))
+    _check(_lib.isoloco_gated_ffn(at[0], ld_x, at[1], at[2], ld_w, dtype, tokens, dim, hidden, a, out.data_ptr(),
+                                  ld_out, ws, ws_bytes, _raw_stream(index)),
+           "isoloco_gated_ffn")
     return out
 
 
@@ -420,6 +430,8 @@ def gated_ffn_backward(x, w_gate, w_up, dout, act="silu", need_dx=True, need_dw=
         dwg_at, dwu_at = dwg.data_ptr(), dwu.data_ptr()
     keep, ws, ws_bytes = _workspace(workspace, isoloco_gated_ffn_workspace_size(
         tokens, dim, hidden, dtype, flags | ISOLOCO_FFN_BACKWARD), device)
-    isoloco_gated_ffn_backward(at[0], ld_x, at[1], at[2], ld_w, dtype, tokens, dim, hidden, a, dout.data_ptr(), ld_dout,
-                               dx_at, dim, dwg_at, dwu_at, dim, ws, ws_bytes, _raw_stream(index))
+    _check(_lib.isoloco_gated_ffn_backward(at[0], ld_x, at[1], at[2], ld_w, dtype, tokens, dim, hidden, a,
+                                           dout.data_ptr(), ld_dout, dx_at, dim, dwg_at, dwu_at, dim, ws, ws_bytes,
+                                           _raw_stream(index)),
+           "isoloco_gated_ffn_backward")
     return dx, dwg, dwu
