@@ -179,14 +179,14 @@ struct Patch {
       }
     }
   }
-  __device__ static __forceinline__ void load(char* ws, const uint16_t* in, int64_t ld, int64_t row0, int64_t col0,
-                                              int64_t rows, int64_t cols) {
+  u32x4 held[32 / kRows];
+  __device__ __forceinline__ void fetch(const uint16_t* in, int64_t ld, int64_t row0, int64_t col0, int64_t rows,
+                                        int64_t cols) {
     const int lane = threadIdx.x & 63, c8 = lane % kLanes;
     const int64_t col = col0 + 8 * c8;
 #pragma unroll
     for (int q = 0; q < 32 / kRows; ++q) {
-      const int r = q * kRows + lane / kLanes;
-      const int64_t row = row0 + r;
+      const int64_t row = row0 + q * kRows + lane / kLanes;
       u32x4 v = {};
       const uint16_t* i = in + row * ld + col;
       if (row < rows) {
@@ -198,8 +198,14 @@ struct Patch {
             if (col + e < cols) v[e / 2] |= (uint32_t)i[e] << (16 * (e & 1));
         }
       }
-      *reinterpret_cast<u32x4*>(ws + r * kPitch + c8 * 16) = v;
+      held[q] = v;
     }
+  }
+  __device__ __forceinline__ void put(char* ws) const {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int q = 0; q < 32 / kRows; ++q)
+      *reinterpret_cast<u32x4*>(ws + (q * kRows + lane / kLanes) * kPitch + (lane % kLanes) * 16) = held[q];
   }
 };
 
@@ -495,11 +501,17 @@ __global__ void __launch_bounds__(C::threads, 2) ffn_tile_kernel(TileArgs t) {
     char* ws = lds + wave * kWs;
     const int64_t rows_pad = MODE == kInner ? ffn_pad(g.m) : g.m, cols_pad = MODE == kInner ? ffn_pad(g.n) : g.n;
     uint16_t* out = static_cast<uint16_t*>(g.out[z]);
+    P dh_of[MODE == kInner ? C::NA : 1];  // all of the wave's dh at once: one wait
+    if constexpr (MODE == kInner) {
+#pragma unroll
+      for (int x = 0; x < C::NA; ++x)
+        dh_of[x].fetch(static_cast<const uint16_t*>(g.dh), g.ld_dh, i0 + (wm * C::NA + x) * 32, col0, g.m, g.n);
+    }
 #pragma unroll
     for (int x = 0; x < C::NA; ++x) {
       const int64_t row0 = i0 + (wm * C::NA + x) * 32;
       if constexpr (MODE == kInner) {
-        P::load(ws, static_cast<const uint16_t*>(g.dh), g.ld_dh, row0, col0, g.m, g.n);
+        dh_of[x].put(ws);
         wave_fence();
       }
 #pragma unroll
