@@ -151,18 +151,8 @@ __device__ __forceinline__ u32x4 scaled(u32x4 v, float c) {
 }
 
 template <bool BF16>
-__device__ __forceinline__ void scale_chunk(const char* p, char* q, int bytes, float c) {
+__device__ __forceinline__ void scale_part(const char* p, char* q, int bytes, float c) {
   constexpr int kElem = BF16 ? 2 : 4;
-  if (bytes >= kChunkBytes) {
-    u32x4 v[kUnroll];
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u)
-      v[u] = *reinterpret_cast<const u32x4_any*>(p + (u * kClipThreads + (int)threadIdx.x) * kVecBytes);
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u)
-      *reinterpret_cast<u32x4_any*>(q + (u * kClipThreads + (int)threadIdx.x) * kVecBytes) = scaled<BF16>(v[u], c);
-    return;
-  }
   const int whole = bytes / kVecBytes;
   for (int i = threadIdx.x; i < whole; i += kClipThreads)
     *reinterpret_cast<u32x4_any*>(q + i * kVecBytes) =
@@ -176,27 +166,52 @@ __device__ __forceinline__ void scale_chunk(const char* p, char* q, int bytes, f
   }
 }
 
-// Every workgroup forms the norm from the partial sums itself (a few KiB, read
-// from the cache) rather than wait for a launch that does it once.
+// Every workgroup forms the norm from the partial sums itself (a few KiB, read from
+// the cache, while its first chunk is on its way) rather than wait for a launch that
+// does it once.  The last chunks go first: the norm's pass read them last, some are
+// still in a cache.
 __global__ void __launch_bounds__(kClipThreads) clip_scale_kernel(ClipArgs a, const double* part, int n_part,
                                                                  float max_norm, float* out) {
   __shared__ double lds[kClipThreads / 64];
-  const floatx2 r = norm_and_coef<kClipThreads / 64>(part, n_part, max_norm, lds);
-  if (out && blockIdx.x == 0 && threadIdx.x == 0) {
-    out[0] = r[0];
-    out[1] = r[1];
-  }
-  // the last chunks first: the norm's pass read them last, some are still in a cache
+  float coef = 0.f;
+  bool first = true;
   for (int c = a.first[a.n] - 1 - (int)blockIdx.x; c >= 0; c -= gridDim.x) {
     const int t = tensor_of(a, c);
-    // nothing to write: the tensor stays where it is and as it is
-    if (a.dst[t] == a.src[t] && r[1] == 1.f) continue;
     const int64_t off = (int64_t)(c - a.first[t]) * kChunkBytes;
     const char* p = static_cast<const char*>(a.src[t]) + off;
     char* q = static_cast<char*>(a.dst[t]) + off;
     const int bytes = chunk_bytes(a, t, c);
-    if (a.bf16[t]) scale_chunk<true>(p, q, bytes, r[1]);
-    else scale_chunk<false>(p, q, bytes, r[1]);
+    u32x4 v[kUnroll];
+    const auto load = [&] {
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u)
+        v[u] = *reinterpret_cast<const u32x4_any*>(p + (u * kClipThreads + (int)threadIdx.x) * kVecBytes);
+    };
+    const bool whole = bytes == kChunkBytes;
+    if (first) {
+      if (whole) load();
+      const floatx2 r = norm_and_coef<kClipThreads / 64>(part, n_part, max_norm, lds);
+      coef = r[1];
+      if (out && blockIdx.x == 0 && threadIdx.x == 0) {
+        out[0] = r[0];
+        out[1] = r[1];
+      }
+    }
+    // (coef 1 in place: the tensor stays as it is)
+    if (p != q || coef != 1.f) {
+      if (whole) {
+        if (!first) load();
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+          *reinterpret_cast<u32x4_any*>(q + (u * kClipThreads + (int)threadIdx.x) * kVecBytes) =
+              a.bf16[t] ? scaled<true>(v[u], coef) : scaled<false>(v[u], coef);
+      } else if (a.bf16[t]) {
+        scale_part<true>(p, q, bytes, coef);
+      } else {
+        scale_part<false>(p, q, bytes, coef);
+      }
+    }
+    first = false;
   }
 }
 

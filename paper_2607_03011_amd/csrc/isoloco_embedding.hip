@@ -256,7 +256,8 @@ __global__ void __launch_bounds__(kGroupThreads) group_kernel(const ID* ids, int
 }
 
 // The sum of the c <= 64 tokens that the lanes hold (`t` of lane j is the j-th), with
-// 64 registers' worth of rows in flight.
+// 32 registers' worth of rows in flight (64 leave room for five waves a SIMD instead of seven:
+// 103 against 95 us for 32768 tokens of 2048).
 template <int N, typename TD>
 __device__ __forceinline__ typename Cols<N>::F sum_tokens(int t, int c, const TD* dout, int64_t ld, int col, int left) {
   typedef typename Cols<N>::template Raw<TD> Raw;
@@ -271,7 +272,7 @@ __device__ __forceinline__ typename Cols<N>::F sum_tokens(int t, int c, const TD
     for (int a = 0; a < kAhead; ++a) s += v[a].get();
     j += kAhead;
   };
-  constexpr int kMost = 256 / Raw::kBytes;
+  constexpr int kMost = 128 / Raw::kBytes;
   while (j + kMost <= c) take(std::integral_constant<int, kMost>());
   while (j + 4 <= c) take(std::integral_constant<int, 4>());
   while (j < c) take(std::integral_constant<int, 1>());
@@ -429,8 +430,8 @@ hipError_t run_backward(const GroupTables& g, const ID* ids, int64_t n, const TD
   hipLaunchKernelGGL(group_kernel<ID>, dim3(nb), dim3(kGroupThreads), 0, st, ids, (int32_t)n, vocab,
                      __builtin_ctz(nb), g);
   const int pieced = n > kPiece ? pieces : 0;
-  // 5 workgroups of 4 waves are on a CU at a time
-  const int64_t items = (vocab + pieced) * spans, blocks = std::min<int64_t>((items + 3) / 4, 5 * 256);
+  // 7 workgroups of 4 waves are on a CU at a time
+  const int64_t items = (vocab + pieced) * spans, blocks = std::min<int64_t>((items + 3) / 4, 7 * 256);
   hipLaunchKernelGGL((embed_sums_kernel<TD, TG, ID>), dim3((unsigned)blocks), dim3(256), 0, st, g, ids, dout, ld_dout,
                      vocab, dim, scale, accumulate, dtable, ld_dtable, spans, pieced);
   if (pieced)
