@@ -30,7 +30,7 @@ typedef floatx4 floatx4_any __attribute__((aligned(4)));
 // ---------------------------------------------------------------------------
 //
 // A product of few rows is bounded by the weights' bytes: every weight is loaded once,
-// from memory into the registers that the MFMA reads (16 hidden rows against 16
+// from memory into the registers that the MFMA reads (16 weight rows against 16
 // tokens), and the workgroup's waves split dim so that enough loads are in flight.
 //
 
@@ -59,73 +59,66 @@ __device__ __forceinline__ floatx4 multiply(const Lane<float>& a, const Lane<flo
   return c;
 }
 
-// Against the tiles (us, 2048 x 5632): bfloat16, 16 / 32 / 48 / 64 tokens 15 / 18 / 23 /
-// 26 here, 20 there at each; float32 16 / 64 tokens 26 / 58 here, 82 / 86 there.
+// Against the tiles (us, 2048 x 5632 / 768 x 2048): bfloat16, 32 tokens 18.9 / 4.6 here,
+// 33 there 16.7 / 8.8; float32, 64 tokens 58 / 10 here, 86 / 29 there.
 constexpr int kFewWaves = 8;
 constexpr int64_t few_most(int32_t dtype) { return dtype == ISOLOCO_BF16 ? 32 : 64; }
 
-// 16 hidden rows per workgroup, up to 16 NT tokens.
+// 8 hidden rows per workgroup, up to 16 NT tokens.  The gate's rows are the first 8 of an
+// MFMA operand, the up projection's the others.  (16 rows of each per workgroup: 352
+// workgroups for 5632, two on some CUs and one on others, 14.3 us for one token of 2048
+// against 11.6.)
 template <typename T, int ACT, int NT>
 __global__ void __launch_bounds__(64 * kFewWaves) ffn_few_kernel(const T* x, int64_t ld_x, const T* wg, const T* wu,
                                                                 int64_t ld_w, int tokens, int64_t dim, int64_t hidden,
                                                                 T* out, int64_t ld_out) {
   constexpr int N = Lane<T>::N, kStep = 4 * N;  // k values of one step
-  __shared__ floatx4 sums[kFewWaves][2 * NT][64];
+  __shared__ floatx4 sums[kFewWaves][NT][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, kl = (lane >> 4) * N;
-  const int64_t h0 = (int64_t)blockIdx.x * 16;
+  const int64_t h0 = (int64_t)blockIdx.x * 8;
   // rows past the matrices are their last ones again: their outputs are not stored
-  const int64_t h = min(h0 + row, hidden - 1);
-  const T* pg = wg + h * ld_w + kl;
-  const T* pu = wu + h * ld_w + kl;
+  const T* pw = (row < 8 ? wg : wu) + min(h0 + (row & 7), hidden - 1) * ld_w + kl;
   const T* px[NT];
 #pragma unroll
   for (int n = 0; n < NT; ++n) px[n] = x + (int64_t)min(16 * n + row, tokens - 1) * ld_x + kl;
-  floatx4 g[NT] = {}, u[NT] = {};
+  floatx4 s[NT] = {};
   // kAhead steps' loads are in flight at a time
   constexpr int kAhead = 4;
   constexpr int64_t kStride = kFewWaves * kStep;
   int64_t k = (int64_t)wave * kStep;
   for (; k + (kAhead - 1) * kStride + kStep <= dim; k += kAhead * kStride) {
-    Lane<T> a[kAhead], b[kAhead], c[kAhead][NT];
+    Lane<T> a[kAhead], c[kAhead][NT];
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
-      a[i].load(pg + k + i * kStride, N);
-      b[i].load(pu + k + i * kStride, N);
+      a[i].load(pw + k + i * kStride, N);
 #pragma unroll
       for (int n = 0; n < NT; ++n) c[i][n].load(px[n] + k + i * kStride, N);
     }
 #pragma unroll
     for (int i = 0; i < kAhead; ++i)
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        g[n] = multiply(a[i], c[i][n], g[n]);
-        u[n] = multiply(b[i], c[i][n], u[n]);
-      }
+      for (int n = 0; n < NT; ++n) s[n] = multiply(a[i], c[i][n], s[n]);
   }
   for (; k < dim; k += kStride) {
     const int64_t left = dim - k - kl;
-    Lane<T> a, b, c;
-    a.load(pg + k, left);
-    b.load(pu + k, left);
+    Lane<T> a, c;
+    a.load(pw + k, left);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       c.load(px[n] + k, left);
-      g[n] = multiply(a, c, g[n]);
-      u[n] = multiply(b, c, u[n]);
+      s[n] = multiply(a, c, s[n]);
     }
   }
 #pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    sums[wave][2 * n][lane] = g[n];
-    sums[wave][2 * n + 1][lane] = u[n];
-  }
+  for (int n = 0; n < NT; ++n) sums[wave][n][lane] = s[n];
   __syncthreads();
-  // lane l holds hidden rows 4 (l / 16) .. + 3 of token l % 16; wave n finishes 16 tokens
-  if (wave >= NT) return;
+  // lanes l < 32 hold rows 4 (l / 16) .. + 3 of the gate for token l % 16, lanes l + 32 the
+  // same of the up projection; wave n finishes 16 tokens
+  if (wave >= NT || lane >= 32) return;
   floatx4 gate = {}, up = {};
   for (int w = 0; w < kFewWaves; ++w) {
-    gate += sums[w][2 * wave][lane];
-    up += sums[w][2 * wave + 1][lane];
+    gate += sums[w][wave][lane];
+    up += sums[w][wave][lane + 32];
   }
   const int t = 16 * wave + (lane & 15);
   if (t >= tokens) return;
@@ -233,7 +226,7 @@ FfnPlan plan_of(const FfnShape& s, bool backward, bool x_ok, bool w_ok) {
 template <typename T, int ACT, int NT>
 void launch_few(const FfnShape& s, const void* x, int64_t ld_x, const void* wg, const void* wu, int64_t ld_w, void* out,
                 int64_t ld_out, hipStream_t st) {
-  hipLaunchKernelGGL((ffn_few_kernel<T, ACT, NT>), dim3((unsigned)((s.hidden + 15) / 16)), dim3(64 * kFewWaves), 0, st,
+  hipLaunchKernelGGL((ffn_few_kernel<T, ACT, NT>), dim3((unsigned)((s.hidden + 7) / 8)), dim3(64 * kFewWaves), 0, st,
                      static_cast<const T*>(x), ld_x, static_cast<const T*>(wg), static_cast<const T*>(wu), ld_w,
                      (int)s.tokens, s.dim, s.hidden, static_cast<T*>(out), ld_out);
 }
