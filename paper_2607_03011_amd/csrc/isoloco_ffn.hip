@@ -38,7 +38,7 @@ typedef floatx4 floatx4_any __attribute__((aligned(4)));
 template <typename T>
 struct Lane {
   static constexpr int N = 16 / sizeof(T);
-  T v[N];
+  alignas(16) T v[N];
   __device__ __forceinline__ void load(const T* p, int64_t left) {
     if (left >= N) {
       *reinterpret_cast<u32x4*>(v) = *reinterpret_cast<const u32x4_any*>(p);
