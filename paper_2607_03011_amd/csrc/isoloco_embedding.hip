@@ -146,14 +146,12 @@ int groups_of(int64_t vocab) {
   return nb;
 }
 
-// Each wave takes a run of the tokens, kChunk at a time, kHeld per lane; a run of one
-// chunk stays in registers between the counting and the placing.
-constexpr int kHeld = 32;
-constexpr int kChunk = 64 * kHeld;
-
-template <typename ID>
+// Each wave takes a run of the tokens, a chunk at a time, kHeld per lane; a run of one chunk
+// stays in registers between the counting and the placing.
+template <typename ID, int kHeld>
 __global__ void __launch_bounds__(kGroupThreads) group_kernel(const ID* ids, int32_t n, int64_t vocab, int nb_log2,
                                                              GroupTables g) {
+  constexpr int kChunk = 64 * kHeld;
   // each wave's tokens by id; then where the next of them goes
   __shared__ int32_t cursor[kGroupWaves][kGroupIds];
   __shared__ int32_t wave_before[kGroupWaves], wave_scan[kGroupWaves];
@@ -169,7 +167,7 @@ __global__ void __launch_bounds__(kGroupThreads) group_kernel(const ID* ids, int
   int32_t held[kHeld];
   uint64_t mask[kHeld];
   const auto load = [&](int at) {
-    constexpr int kAtOnce = sizeof(ID) == 8 ? 16 : 32;
+    constexpr int kAtOnce = kHeld < 16 ? kHeld : 16;
 #pragma unroll
     for (int h = 0; h < kHeld; h += kAtOnce) {
       ID id[kAtOnce];
@@ -427,11 +425,18 @@ hipError_t run_backward(const GroupTables& g, const ID* ids, int64_t n, const TD
   constexpr int kSpan = 64 * kColsOf<TD>;
   const int spans = (dim + kSpan - 1) / kSpan, pieces = (int)((n + kPiece - 1) / kPiece);
   const int nb = groups_of(vocab);
-  hipLaunchKernelGGL(group_kernel<ID>, dim3(nb), dim3(kGroupThreads), 0, st, ids, (int32_t)n, vocab,
-                     __builtin_ctz(nb), g);
+  // (few tokens: without the turns that would find none, 7 us instead of 11 for 5001)
+  if (n <= kGroupWaves * 64 * 8)
+    hipLaunchKernelGGL((group_kernel<ID, 8>), dim3(nb), dim3(kGroupThreads), 0, st, ids, (int32_t)n, vocab,
+                       __builtin_ctz(nb), g);
+  else
+    hipLaunchKernelGGL((group_kernel<ID, 32>), dim3(nb), dim3(kGroupThreads), 0, st, ids, (int32_t)n, vocab,
+                       __builtin_ctz(nb), g);
   const int pieced = n > kPiece ? pieces : 0;
-  // 7 workgroups of 4 waves are on a CU at a time
-  const int64_t items = (vocab + pieced) * spans, blocks = std::min<int64_t>((items + 3) / 4, 7 * 256);
+  // 7 workgroups of 4 waves are on a CU at a time; four times as many even out what the rows
+  // cost (1 / 2 / 4 / 8 times: 96 / 90 / 87 / 82 us for 32768 tokens of 2048, 20.0 / 17.6 /
+  // 17.0 / 19.6 for 5001 of 612)
+  const int64_t items = (vocab + pieced) * spans, blocks = std::min<int64_t>((items + 3) / 4, 4 * 7 * 256);
   hipLaunchKernelGGL((embed_sums_kernel<TD, TG, ID>), dim3((unsigned)blocks), dim3(256), 0, st, g, ids, dout, ld_dout,
                      vocab, dim, scale, accumulate, dtable, ld_dtable, spans, pieced);
   if (pieced)
