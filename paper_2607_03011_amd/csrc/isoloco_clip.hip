@@ -34,6 +34,7 @@ struct ClipArgs {
   int32_t last[kClipTensors];       // bytes of its last chunk (the others are whole)
   uint8_t bf16[kClipTensors];
   int32_t n;
+  int32_t in_place;  // all of them
 };
 
 // 16 bytes at the alignment of an element: a tensor may start anywhere in a flat
@@ -166,9 +167,9 @@ __device__ __forceinline__ void scale_part(const char* p, char* q, int bytes, fl
   }
 }
 
-// Every workgroup forms the norm from the partial sums itself (a few KiB, read from
-// the cache, while its first chunk is on its way) rather than wait for a launch that
-// does it once.  The last chunks go first: the norm's pass read them last, some are
+// Every workgroup forms the norm from the partial sums itself (a few KiB, read from the
+// cache, while its first chunk is on its way) rather than wait for a launch that does it
+// once.  (Not so in place, where a norm below the bound leaves nothing to do.)  The last chunks go first: the norm's pass read them last, some are
 // still in a cache.
 __global__ void __launch_bounds__(kClipThreads) clip_scale_kernel(ClipArgs a, const double* part, int n_part,
                                                                  float max_norm, float* out) {
@@ -189,18 +190,19 @@ __global__ void __launch_bounds__(kClipThreads) clip_scale_kernel(ClipArgs a, co
     };
     const bool whole = bytes == kChunkBytes;
     if (first) {
-      if (whole) load();
+      if (whole && !a.in_place) load();
       const floatx2 r = norm_and_coef<kClipThreads / 64>(part, n_part, max_norm, lds);
       coef = r[1];
       if (out && blockIdx.x == 0 && threadIdx.x == 0) {
         out[0] = r[0];
         out[1] = r[1];
       }
+      if (coef == 1.f && a.in_place) return;
     }
     // (coef 1 in place: the tensor stays as it is)
     if (p != q || coef != 1.f) {
       if (whole) {
-        if (!first) load();
+        if (!first || a.in_place) load();
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u)
           *reinterpret_cast<u32x4_any*>(q + (u * kClipThreads + (int)threadIdx.x) * kVecBytes) =
@@ -269,6 +271,7 @@ isoloco_status isoloco_clip_grads(const void* const* src, void* const* dst, cons
       // the next tensors that hold something, as many as a launch takes (and whose chunks it can count)
       ClipArgs a;
       a.n = 0;
+      a.in_place = 1;
       int64_t chunks = 0;
       for (; at < n_tensors && a.n < kClipTensors; ++at) {
         if (counts[at] == 0) continue;
@@ -277,6 +280,7 @@ isoloco_status isoloco_clip_grads(const void* const* src, void* const* dst, cons
         if (chunks + c > INT32_MAX) break;
         a.src[a.n] = src[at];
         a.dst[a.n] = dst ? dst[at] : nullptr;
+        a.in_place &= a.dst[a.n] == a.src[a.n];
         a.first[a.n] = (int32_t)chunks;
         a.last[a.n] = (int32_t)(bytes - (c - 1) * kChunkBytes);
         a.bf16[a.n] = dtypes[at] == ISOLOCO_BF16;
