@@ -438,8 +438,8 @@ typedef enum {
 /* out = act(x w_gate^T) * (x w_up^T); x: tokens x dim, w_gate and w_up: hidden x
  * dim (both ld_w apart), out: tokens x hidden; one dtype.  float32 products are
  * formed from three bfloat16 parts of each operand, all six products of order
- * 2^-16 and above (about float32 accuracy; an infinite operand gives NaN), or, for
- * up to 64 tokens forward, in float32.
+ * 2^-16 and above (about float32 accuracy; an operand that is infinite or past bfloat16's
+ * range, 3.39e38, gives NaN), or, for up to 64 tokens forward, in float32.
  *
  * The workspace's size goes by the call: ISOLOCO_FFN_BACKWARD for the gradient,
  * ISOLOCO_FFN_ALIGNED where the rows of x and of both weights will be 16-byte

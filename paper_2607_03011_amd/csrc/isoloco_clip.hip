@@ -11,6 +11,10 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <algorithm>
+#include <memory>
+#include <new>
+
 #include "isoloco_device.h"
 #include "isoloco_error.h"
 
@@ -169,7 +173,8 @@ __device__ __forceinline__ void scale_part(const char* p, char* q, int bytes, fl
 
 // Every workgroup forms the norm from the partial sums itself (a few KiB, read from the
 // cache, while its first chunk is on its way) rather than wait for a launch that does it
-// once.  (Not so in place, where a norm below the bound leaves nothing to do.)  The last chunks go first: the norm's pass read them last, some are
+// once.  (The chunk waits for the norm in place, where one below the bound leaves
+// nothing to do.)  The last chunks go first: the norm's pass read them last, some are
 // still in a cache.
 __global__ void __launch_bounds__(kClipThreads) clip_scale_kernel(ClipArgs a, const double* part, int n_part,
                                                                  float max_norm, float* out) {
@@ -222,6 +227,38 @@ size_t clip_workspace(int32_t n_tensors) {
   return (launches ? launches : 1) * kClipBlocks * sizeof(double);
 }
 
+// No result overlaps another tensor or its result: workgroups take the tensors in no
+// order.
+isoloco_status check_results_apart(const void* const* src, void* const* dst, const int64_t* counts,
+                                   const int32_t* dtypes, int32_t n_tensors) {
+  struct Range {
+    uintptr_t from, to;
+    int32_t tensor;
+    bool result;
+  };
+  const std::unique_ptr<Range[]> r(new (std::nothrow) Range[2 * (size_t)n_tensors]);
+  if (!r) return fail(ISOLOCO_ERR_UNSUPPORTED, "no memory to check %d tensors", n_tensors);
+  size_t n = 0;
+  for (int32_t i = 0; i < n_tensors; ++i) {
+    const uintptr_t bytes = (uintptr_t)counts[i] * dtype_bytes(dtypes[i]);
+    const uintptr_t s = reinterpret_cast<uintptr_t>(src[i]), d = reinterpret_cast<uintptr_t>(dst[i]);
+    if (bytes == 0) continue;
+    r[n++] = {d, d + bytes, i, true};
+    if (s != d) r[n++] = {s, s + bytes, i, false};
+  }
+  std::sort(r.get(), r.get() + n, [](const Range& a, const Range& b) { return a.from < b.from; });
+  // the range before that ends last, of all and of the results
+  const Range *any = nullptr, *result = nullptr;
+  for (const Range* x = r.get(); x != r.get() + n; ++x) {
+    const Range* y = x->result ? any : result;
+    if (y && x->from < y->to)
+      return fail(ISOLOCO_ERR_ALIAS, "tensors %d and %d: one's result overlaps the other", y->tensor, x->tensor);
+    if (!any || x->to > any->to) any = x;
+    if (x->result && (!result || x->to > result->to)) result = x;
+  }
+  return ISOLOCO_OK;
+}
+
 }  // namespace
 }  // namespace isoloco
 
@@ -262,6 +299,8 @@ isoloco_status isoloco_clip_grads(const void* const* src, void* const* dst, cons
     if (ranges_overlap(src[i], bytes, norm, 8) || (dst && ranges_overlap(dst[i], bytes, norm, 8)))
       return fail(ISOLOCO_ERR_ALIAS, "tensor %d overlaps norm", i);
   }
+  if (ranges_overlap(norm, 8, workspace, need)) return fail(ISOLOCO_ERR_ALIAS, "norm overlaps the workspace");
+  if (dst && n_tensors > 1) ISOLOCO_TRY(check_results_apart(src, dst, counts, dtypes, n_tensors));
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
   double* part = static_cast<double*>(workspace);
   int n_part = 0;

@@ -416,7 +416,7 @@ isoloco_status check_table(int64_t vocab, int64_t dim, int64_t n, int32_t id_typ
 bool wave_grid(int64_t items, unsigned* grid) {
   const int64_t blocks = (items + 3) / 4;
   *grid = (unsigned)blocks;
-  return blocks <= INT32_MAX;
+  return launchable(blocks, 256);
 }
 
 template <typename TD, typename TG, typename ID>
@@ -440,8 +440,9 @@ hipError_t run_backward(const GroupTables& g, const ID* ids, int64_t n, const TD
   hipLaunchKernelGGL((embed_sums_kernel<TD, TG, ID>), dim3((unsigned)blocks), dim3(256), 0, st, g, ids, dout, ld_dout,
                      vocab, dim, scale, accumulate, dtable, ld_dtable, spans, pieced);
   if (pieced)
-    hipLaunchKernelGGL((embed_join_kernel<ID, TG>), dim3(pieces, (dim + 64 * kColsOf<TG> - 1) / (64 * kColsOf<TG>)), dim3(64), 0, st, g, ids, dim, scale,
-                       accumulate, dtable, ld_dtable);
+    hipLaunchKernelGGL((embed_join_kernel<ID, TG>),
+                       dim3(pieces, (dim + 64 * kColsOf<TG> - 1) / (64 * kColsOf<TG>)), dim3(64), 0, st, g, ids, dim,
+                       scale, accumulate, dtable, ld_dtable);
   return hipGetLastError();
 }
 

@@ -32,6 +32,9 @@ inline bool ranges_overlap(const void* a, size_t na, const void* b, size_t nb) {
 // Sizes the operators accept: any product of two of them stays below 2^62.
 constexpr int64_t kMaxExtent = (int64_t)1 << 31;
 
+// A launch's threads are counted in 32 bits.
+inline bool launchable(int64_t blocks, int threads) { return blocks <= (int64_t)UINT32_MAX / threads; }
+
 #define ISOLOCO_TRY(expr)                          \
   do {                                             \
     const isoloco_status try_status_ = (expr);     \

@@ -32,7 +32,6 @@ typedef floatx4 floatx4_any __attribute__((aligned(4)));
 // A product of few rows is bounded by the weights' bytes: every weight is loaded once,
 // from memory into the registers that the MFMA reads (16 weight rows against 16
 // tokens), and the workgroup's waves split dim so that enough loads are in flight.
-//
 
 // The values of k that a lane holds of one row, 16 bytes: its MFMA operands.
 template <typename T>

@@ -331,7 +331,7 @@ __global__ void __launch_bounds__(C::threads, 2) ffn_tile_kernel(TileArgs t) {
   const int slabs = (int)((g.k + kSlab - 1) / kSlab);
   const int64_t all = (int64_t)slabs * kRuns;
   const int64_t first = all * slice / t.splits, total = all * (slice + 1) / t.splits - first;
-  int run = (int)(first / slabs), at_slab = (int)(first - (int64_t)run * slabs);  // of the next slab to load
+  int run = slabs ? (int)(first / slabs) : 0, at_slab = (int)(first - (int64_t)run * slabs);  // of the next slab to load
 
   // part 0: the next slab of a, part 1: that of b
   const auto issue = [&](int buf, int part) {

@@ -414,13 +414,17 @@ size_t logprob_workspace(int64_t rows, int64_t vocab, int top_k) {
   return s > 1 ? (size_t)rows * s * (16 + 8 * (size_t)top_k) : 0;
 }
 
+// the fewest that hold a row (or split) at once, if any do
+int threads_of(int64_t span) { return span <= 64 * kHeld ? 64 : span <= 256 * kHeld ? 256 : 512; }
+
 template <typename T, typename ID>
 void run_forward(const void* logits, const void* targets, int64_t rows, const RowArgs& g, hipStream_t st) {
   const T* l = static_cast<const T*>(logits);
   const ID* t = static_cast<const ID*>(targets);
   const dim3 grid((unsigned)(rows * g.splits));
-  if (g.span <= 64 * kHeld) hipLaunchKernelGGL((logprob_kernel<T, ID, 1>), grid, dim3(64), 0, st, l, t, g);
-  else if (g.span <= 256 * kHeld) hipLaunchKernelGGL((logprob_kernel<T, ID, 4>), grid, dim3(256), 0, st, l, t, g);
+  const int threads = threads_of(g.span);
+  if (threads == 64) hipLaunchKernelGGL((logprob_kernel<T, ID, 1>), grid, dim3(64), 0, st, l, t, g);
+  else if (threads == 256) hipLaunchKernelGGL((logprob_kernel<T, ID, 4>), grid, dim3(256), 0, st, l, t, g);
   else hipLaunchKernelGGL((logprob_kernel<T, ID, 8>), grid, dim3(512), 0, st, l, t, g);
   if (g.splits > 1) hipLaunchKernelGGL((logprob_join_kernel<T, ID>), dim3((unsigned)rows), dim3(256), 0, st, l, t, g);
 }
@@ -489,7 +493,11 @@ isoloco_status isoloco_token_logprobs(const void* logits, int64_t ld_logits, int
   }
   const size_t need = logprob_workspace(rows, vocab, top_k);
   ISOLOCO_TRY(check_workspace(workspace, workspace_bytes, need));
-  if (ranges_overlap(workspace, need, logits, nb)) return fail(ISOLOCO_ERR_ALIAS, "the workspace overlaps the logits");
+  if (ranges_overlap(workspace, need, logits, nb) ||
+      ranges_overlap(workspace, need, targets, targets ? (size_t)rows * index_bytes(target_type) : 0))
+    return fail(ISOLOCO_ERR_ALIAS, "the workspace overlaps an input");
+  for (const auto& x : outs)
+    if (ranges_overlap(workspace, need, x.p, x.bytes)) return fail(ISOLOCO_ERR_ALIAS, "the workspace overlaps %s", x.name);
   RowArgs g;
   g.ld = ld_logits;
   g.vocab = vocab;
@@ -501,7 +509,7 @@ isoloco_status isoloco_token_logprobs(const void* logits, int64_t ld_logits, int
   g.keys = static_cast<uint64_t*>(workspace);
   g.part = reinterpret_cast<Soft*>(g.keys + rows * g.splits * top_k);
   g.o = {logprob, entropy, lse, top_logprob, top_index};
-  if (rows * g.splits > INT32_MAX) return fail(ISOLOCO_ERR_UNSUPPORTED, "too many rows for one launch");
+  if (!launchable(rows * g.splits, threads_of(g.span))) return fail(ISOLOCO_ERR_UNSUPPORTED, "too many rows for one launch");
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
   BY_TYPES(run_forward, logits, targets, rows, g, st);
   const hipError_t err = hipGetLastError();
@@ -536,7 +544,7 @@ isoloco_status isoloco_token_logprobs_backward(const void* logits, int64_t ld_lo
   }
   const int64_t vecs = vocab / (16 / (int64_t)e);
   const int64_t spans = vecs == 0 ? 1 : (vecs + kGradThreads * kGradVecs - 1) / (kGradThreads * kGradVecs);
-  if (rows * spans > INT32_MAX) return fail(ISOLOCO_ERR_UNSUPPORTED, "too many elements for one launch");
+  if (!launchable(rows * spans, kGradThreads)) return fail(ISOLOCO_ERR_UNSUPPORTED, "too many elements for one launch");
   const GradIn in = {lse, entropy, dlogprob, dentropy};
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
   BY_TYPES(run_grad, logits, ld_logits, rows, vocab, targets, scale, in, dlogits, ld_dlogits, (int)spans, st);

@@ -325,11 +325,12 @@ def token_logprobs(logits, targets=None, scale=1.0, top_k=0, workspace=None):
         target_at, logprob_at = targets.data_ptr(), logprob.data_ptr()
     else:
         entropy, lse = _empty((2, *shape), dtype=_F32, device=device).unbind()
+    ws_need = isoloco_token_logprobs_workspace_size(rows, vocab, top_k)
     if top_k:
         top = _empty((*shape, top_k), dtype=_F32, device=device)
         top_index = _empty((*shape, top_k), dtype=torch.int64, device=device)
         top_at, index_at = top.data_ptr(), top_index.data_ptr()
-    keep, ws, ws_bytes = _workspace(workspace, isoloco_token_logprobs_workspace_size(rows, vocab, top_k), device)
+    keep, ws, ws_bytes = _workspace(workspace, ws_need, device)
     _check(_lib.isoloco_token_logprobs(logits.data_ptr(), ld, dtype, rows, vocab, target_at, t_type, scale, top_k,
                                        logprob_at, entropy.data_ptr(), lse.data_ptr(), top_at, index_at, ws, ws_bytes,
                                        _raw_stream(index)),

@@ -145,3 +145,35 @@ def test_tensors_on_the_host_are_refused():
             f()
     with pytest.raises(ValueError):
         iso.clip_grads([], 1.0)
+
+
+# the results and the other tensors lie 400 bytes (100 float32) and 14 bytes (7 bfloat16) long
+@pytest.mark.parametrize("src,dst", [
+    ([A, A], [A, A]), ([A, B], [C, C]), ([A, B], [C, C + 396]), ([A, B], [C + 12, C]), ([A, B], [B, C]),
+    ([A, A + 200], [A, D]), ([A, B], [C, A + 396]),
+])
+def test_clip_refuses_a_result_over_another_tensor(src, dst):
+    refused(ALIAS, iso.isoloco_clip_grads, *changed(CLIP, src=src, dst=dst, norm=E))
+
+
+def test_clip_finds_the_long_range_before_short_ones():
+    # tensor 0 reaches over 1 and 2, which lie apart from each other
+    refused(ALIAS, iso.isoloco_clip_grads, [A, B, C], [D, D + 1000, D + 2000], [1000, 4, 4], [0, 0, 0], 1.0, E, WS, BIG)
+    refused(ALIAS, iso.isoloco_clip_grads, [A, B, C], [D, E, A + 2000], [1000, 4, 4], [0, 0, 0], 1.0, F, WS, BIG)
+
+
+def test_workspace_overlaps_are_refused():
+    refused(ALIAS, iso.isoloco_clip_grads, *changed(CLIP, norm=WS + 64))
+    # (two rows of 50000: split, so that a workspace is needed)
+    long = dict(LOGPROB, ld=50000, rows=2, vocab=50000)
+    for change in (dict(targets=WS), dict(lse=WS + 8), dict(index=WS + 64), dict(logits=WS)):
+        refused(ALIAS, iso.isoloco_token_logprobs, *changed(long, **change))
+
+
+def test_launches_past_32_bits_of_threads_are_refused():
+    refused(-7, iso.isoloco_embedding, *changed(EMBED, n=1 << 26, dim=64, table=A, ids=1 << 40, out=1 << 41))
+    refused(-7, iso.isoloco_token_logprobs, *changed(
+        LOGPROB, rows=1 << 26, ld=1, vocab=1, top_k=0, targets=1 << 40, logprob=1 << 41, entropy=1 << 42, lse=1 << 43))
+    refused(-7, iso.isoloco_token_logprobs_backward, *changed(
+        LOGPROB_GRAD, rows=1 << 24, ld=1, ld_d=1, vocab=1, targets=1 << 40, lse=1 << 41, entropy=1 << 42,
+        dlogprob=1 << 43, dentropy=1 << 44, dlogits=1 << 45))
