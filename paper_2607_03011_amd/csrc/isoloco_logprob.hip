@@ -109,7 +109,8 @@ struct RowArgs {
 };
 
 constexpr int kHeld = 64;         // logits that a thread holds in registers
-constexpr int kCandidates = 1024;
+// (8 waves a SIMD in bfloat16 leave a workgroup of one 5 KiB of LDS)
+constexpr int candidates_of(int waves) { return waves == 1 ? 512 : 1024; }
 
 // A row's results, from its softmax and (top_k) its largest keys in falling order:
 // thread i of the workgroup writes alternative i.
@@ -134,9 +135,11 @@ __device__ __forceinline__ void put_top(const RowArgs& g, int64_t r, int place, 
 
 // One workgroup of WAVES waves per row, or per split of a row.
 //
-// Its columns are taken kHeld per thread at a time: the maximum of those, then their
-// sums against it, 10 instructions' time per logit (4 of it the exponential) against
-// the 14 that their bytes' time allows in bfloat16 (a running maximum per vector: 18).
+// Its columns are taken kHeld per thread at a time, as they are stored: the maximum of
+// those, then their sums against it, 12 instructions' time per logit (4 of it the
+// exponential) against the 14 that their bytes' time allows in bfloat16 (a running
+// maximum per vector: 18).  Unpacked once, in twice the registers, it is 10, but 4 waves
+// are on a SIMD instead of 8: 122 against 108 us for 8192 rows of 32000, 4.8 TB/s.
 //
 // Alternatives: the threads of one lane number are a group; the top_k-th largest of
 // the 64 groups' maxima bounds the top_k-th largest logit from below, and few logits
@@ -144,14 +147,15 @@ __device__ __forceinline__ void put_top(const RowArgs& g, int64_t r, int place, 
 // (equal values, or all of the largest in few groups), the row is gone through once
 // more per alternative.
 template <typename T, typename ID, int WAVES>
-__global__ void __launch_bounds__(64 * WAVES, 4) logprob_kernel(const T* logits, const ID* targets, RowArgs g) {
-  constexpr int N = Vec<T>::N, kThreads = 64 * WAVES, kVecs = kHeld / N;
+__global__ void __launch_bounds__(64 * WAVES, sizeof(T) == 2 ? 8 : 4)
+    logprob_kernel(const T* logits, const ID* targets, RowArgs g) {
+  constexpr int N = Vec<T>::N, kThreads = 64 * WAVES, kVecs = kHeld / N, kCandidates = candidates_of(WAVES);
   __shared__ Soft part[WAVES];
   __shared__ float group[WAVES][64];
   __shared__ uint64_t cand[kCandidates];
   __shared__ uint64_t wave_best[WAVES];
   __shared__ int n_cand;
-  __shared__ float bound_of;
+  __shared__ int rank[64];
   const int64_t r = blockIdx.x / g.splits;
   const int split = (int)(blockIdx.x - r * g.splits);
   const int64_t begin = split * g.span;
@@ -161,17 +165,15 @@ __global__ void __launch_bounds__(64 * WAVES, 4) logprob_kernel(const T* logits,
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 
   // the threads' logits of one turn: vectors, then single ones at the end
-  float x[kHeld], last;
+  u32x4 v[kVecs];
+  float last;
   const auto load = [&](int base) {
-    u32x4 v[kVecs];
 #pragma unroll
     for (int c = 0; c < kVecs; ++c) {
       const int i = base + c * kThreads + (int)threadIdx.x;
       v[c] = sizeof(T) == 2 ? (u32x4)(0xff80ff80u) : (u32x4)(0xff800000u);  // -infinity
       if (i < whole) v[c] = *reinterpret_cast<const u32x4_any*>(p + i * N);
     }
-#pragma unroll
-    for (int c = 0; c < kVecs; ++c) unpack<T>(v[c], x + c * N);
     const int at = whole * N + (int)threadIdx.x;
     last = base == 0 && at < count ? (float)p[at] : -INFINITY;
   };
@@ -186,9 +188,16 @@ __global__ void __launch_bounds__(64 * WAVES, 4) logprob_kernel(const T* logits,
 #pragma unroll
     for (int c = 0; c < kVecs; ++c)
       if (base + c * kThreads < whole) {
+        float x[N];
+        unpack<T>(v[c], x);
 #pragma unroll
-        for (int e = 0; e < N; ++e) most = fmaxf(most, x[c * N + e]);
+        for (int e = 0; e < N; ++e) most = fmaxf(most, x[e]);
       }
+    // (unpacked again after this: as float32 they would take the registers of half the waves)
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int c = 0; c < kVecs; ++c) asm("" : "+v"(v[c]));
+    }
     top = fmaxf(top, most);
     a.raise(fmaxf(a.m, most * g.scale));
     const float m = a.m == -INFINITY ? 0.f : a.m;
@@ -200,8 +209,10 @@ __global__ void __launch_bounds__(64 * WAVES, 4) logprob_kernel(const T* logits,
 #pragma unroll
     for (int c = 0; c < kVecs; ++c)
       if (base + c * kThreads < whole) {
+        float x[N];
+        unpack<T>(v[c], x);
 #pragma unroll
-        for (int e = 0; e < N; ++e) add(x[c * N + e]);
+        for (int e = 0; e < N; ++e) add(x[e]);
       }
     if (base == 0) add(last);
   }
@@ -219,6 +230,7 @@ __global__ void __launch_bounds__(64 * WAVES, 4) logprob_kernel(const T* logits,
   }
   if (g.top_k) {
     group[wave][lane] = top;
+    if (wave == 0) rank[lane] = 0;
     if (threadIdx.x == 0) n_cand = 0;
   }
   __syncthreads();
@@ -241,20 +253,25 @@ __global__ void __launch_bounds__(64 * WAVES, 4) logprob_kernel(const T* logits,
   // (a NaN is above every maximum here: such rows go the long way)
   const bool odd = b.s != b.s;
   if (!odd) {
-    // (one wave ranks the groups: all of them doing it took a third of the time)
-    if (wave == 0) {
-      float own = group[0][lane];
-      for (int w = 1; w < WAVES; ++w) own = fmaxf(own, group[w][lane]);
-      int rank = 0;
-#pragma unroll 8
-      for (int i = 0; i < 64; ++i) {
-        const float other = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(own), i));
-        rank += other > own || (other == own && i < lane);
-      }
-      if (rank == g.top_k - 1) bound_of = own;
+    // each wave ranks the groups among some of them (one wave alone: 114 against 108 us
+    // for 4096 rows of 32000 in float32)
+    float own = group[0][lane];
+    for (int w = 1; w < WAVES; ++w) own = fmaxf(own, group[w][lane]);
+    int above = 0;
+#pragma unroll
+    for (int q = 0; q < 64 / WAVES; ++q) {
+      const int i = wave * (64 / WAVES) + q;
+      const float other = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(own), i));
+      above += other > own || (other == own && i < lane);
     }
-    __syncthreads();
-    const float bound = bound_of;
+    if constexpr (WAVES > 1) {
+      atomicAdd(&rank[lane], above);
+      __syncthreads();
+      above = rank[lane];
+    }
+    const uint64_t at_bound = __ballot(above == g.top_k - 1);
+    const float bound = __uint_as_float(
+        __builtin_amdgcn_readlane(__float_as_uint(own), __ffsll((unsigned long long)at_bound) - 1));
     const auto take = [&](float v, int i) {
       if (v >= bound) {
         const int c = atomicAdd(&n_cand, 1);
@@ -266,12 +283,14 @@ __global__ void __launch_bounds__(64 * WAVES, 4) logprob_kernel(const T* logits,
 #pragma unroll
       for (int c = 0; c < kVecs; ++c) {
         const int i = base + c * kThreads + (int)threadIdx.x;
-        float most = x[c * N];
+        float x[N];
+        unpack<T>(v[c], x);
+        float most = x[0];
 #pragma unroll
-        for (int e = 1; e < N; ++e) most = fmaxf(most, x[c * N + e]);
+        for (int e = 1; e < N; ++e) most = fmaxf(most, x[e]);
         if (most >= bound && i < whole) {
 #pragma unroll
-          for (int e = 0; e < N; ++e) take(x[c * N + e], i * N + e);
+          for (int e = 0; e < N; ++e) take(x[e], i * N + e);
         }
       }
       const int at = whole * N + (int)threadIdx.x;
