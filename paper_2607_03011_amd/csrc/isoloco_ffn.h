@@ -71,10 +71,16 @@ struct FfnArgs {
   int64_t ld_out, part_out;
   const void* dh;
   int64_t ld_dh;
-  float* partial;  // ffn_partial_bytes() for the sums of a product whose k values are split over workgroups
+  float* partial;  // ..._partial_bytes() for the sums of a product whose k values are split over workgroups
 };
 
-size_t ffn_partial_bytes(FfnMode mode, bool f32, int64_t m, int64_t n, int64_t k);
-hipError_t launch_ffn_tiles(FfnMode mode, int act, bool f32, const FfnArgs& g, hipStream_t st);
+// kForward and kInner of m x n over k
+size_t ffn_projections_partial_bytes(FfnMode mode, bool f32, int64_t m, int64_t n, int64_t k);
+hipError_t launch_ffn_projections(FfnMode mode, int act, bool f32, const FfnArgs& g, hipStream_t st);
+
+// kSum of m x n over k and kPair of k x n over m, either of which may be NULL; their
+// `partial` is the same.
+size_t ffn_gradients_partial_bytes(bool f32, int64_t m, int64_t n, int64_t k);
+hipError_t launch_ffn_gradients(bool f32, const FfnArgs* sum, const FfnArgs* pair, hipStream_t st);
 
 }  // namespace isoloco

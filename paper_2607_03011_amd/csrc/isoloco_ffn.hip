@@ -210,13 +210,12 @@ FfnPlan plan_of(const FfnShape& s, bool backward, bool x_ok, bool w_ok) {
     p.wg = take(row * s.hidden);
     p.wu = take(row * s.hidden);
   }
-  size_t partial = ffn_partial_bytes(backward ? kInner : kForward, f32, s.tokens, s.hidden, s.dim);
+  size_t partial = ffn_projections_partial_bytes(backward ? kInner : kForward, f32, s.tokens, s.hidden, s.dim);
   if (backward) {
     const size_t inner = 2 * (size_t)ffn_pad(s.tokens) * (size_t)ffn_pad(s.hidden) * parts;
     p.da = take(inner);
     p.du = take(inner);
-    partial = std::max({partial, ffn_partial_bytes(kSum, f32, s.tokens, s.dim, s.hidden),
-                        ffn_partial_bytes(kPair, f32, s.hidden, s.dim, s.tokens)});
+    partial = std::max(partial, ffn_gradients_partial_bytes(f32, s.tokens, s.dim, s.hidden));
   }
   p.partial = take(partial);
   return p;
@@ -292,7 +291,7 @@ hipError_t run_forward(const FfnShape& s, const void* x, int64_t ld_x, const voi
   g.out[0] = out;
   g.ld_out = ld_out;
   g.partial = reinterpret_cast<float*>(static_cast<char*>(ws) + p.partial);
-  return launch_ffn_tiles(kForward, ACT, sizeof(T) == 4, g, st);
+  return launch_ffn_projections(kForward, ACT, sizeof(T) == 4, g, st);
 }
 
 template <typename T, int ACT>
@@ -324,7 +323,8 @@ hipError_t run_backward(const FfnShape& s, const void* x, int64_t ld_x, const vo
   g.dh = dout;
   g.ld_dh = ld_dout;
   g.partial = reinterpret_cast<float*>(base + p.partial);
-  hipError_t e = launch_ffn_tiles(kInner, ACT, f32, g, st);
+  const hipError_t e = launch_ffn_projections(kInner, ACT, f32, g, st);
+  if (e != hipSuccess) return e;
   g = {};
   g.a[0] = da;
   g.a[1] = du;
@@ -332,31 +332,26 @@ hipError_t run_backward(const FfnShape& s, const void* x, int64_t ld_x, const vo
   g.part_a = part;
   g.n = s.dim;
   g.partial = reinterpret_cast<float*>(base + p.partial);
-  if (e == hipSuccess && dx) {
-    g.b[0] = o.wg;
-    g.b[1] = o.wu;
-    g.ld_b = o.ld_w;
-    g.part_b = o.part_w;
-    g.cols_b = p.copy_w ? cols : s.dim;
-    g.m = s.tokens;
-    g.k = s.hidden;
-    g.out[0] = dx;
-    g.ld_out = ld_dx;
-    e = launch_ffn_tiles(kSum, ACT, f32, g, st);
-  }
-  if (e == hipSuccess && dwg) {
-    g.b[0] = g.b[1] = o.x;
-    g.ld_b = o.ld_x;
-    g.part_b = o.part_x;
-    g.cols_b = p.copy_x ? cols : s.dim;
-    g.m = s.hidden;
-    g.k = s.tokens;
-    g.out[0] = dwg;
-    g.out[1] = dwu;
-    g.ld_out = ld_dw;
-    e = launch_ffn_tiles(kPair, ACT, f32, g, st);
-  }
-  return e;
+  FfnArgs sum = g, pair = g;
+  sum.b[0] = o.wg;
+  sum.b[1] = o.wu;
+  sum.ld_b = o.ld_w;
+  sum.part_b = o.part_w;
+  sum.cols_b = p.copy_w ? cols : s.dim;
+  sum.m = s.tokens;
+  sum.k = s.hidden;
+  sum.out[0] = dx;
+  sum.ld_out = ld_dx;
+  pair.b[0] = pair.b[1] = o.x;
+  pair.ld_b = o.ld_x;
+  pair.part_b = o.part_x;
+  pair.cols_b = p.copy_x ? cols : s.dim;
+  pair.m = s.hidden;
+  pair.k = s.tokens;
+  pair.out[0] = dwg;
+  pair.out[1] = dwu;
+  pair.ld_out = ld_dw;
+  return launch_ffn_gradients(f32, dx ? &sum : nullptr, dwg ? &pair : nullptr, st);
 }
 
 isoloco_status check_shape(const FfnShape& s) {

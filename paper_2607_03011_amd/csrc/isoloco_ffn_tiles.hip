@@ -18,6 +18,8 @@
 
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "isoloco_device.h"
 #include "isoloco_ffn.h"
 #include "isoloco_lds.h"
@@ -273,9 +275,9 @@ struct TileArgs {
 
 // The tile of a workgroup: workgroups go round the 8 XCDs in turn, so each XCD takes
 // a run of tiles, in bands of 8 rows of tiles, whose operands its L2 then holds.
-__device__ __forceinline__ void tile_of(const TileArgs& t, int& tm, int& tn, int& z, int& slice) {
-  const int xcd = blockIdx.x & 7, q = t.tiles >> 3, r = t.tiles & 7;
-  int i = xcd * q + min(xcd, r) + (int)(blockIdx.x >> 3);
+__device__ __forceinline__ void tile_of(const TileArgs& t, int block, int& tm, int& tn, int& z, int& slice) {
+  const int xcd = block & 7, q = t.tiles >> 3, r = t.tiles & 7;
+  int i = xcd * q + min(xcd, r) + (block >> 3);
   const int plane = t.tiles_m * t.tiles_n;
   slice = i / (plane * t.planes);
   i -= slice * plane * t.planes;
@@ -287,25 +289,31 @@ __device__ __forceinline__ void tile_of(const TileArgs& t, int& tm, int& tn, int
   tn = in / rows;
 }
 
+// Bytes of LDS: two stages of slabs; afterwards the waves' results on their way out.
+template <int MODE, class C>
+struct TileLds {
+  static constexpr bool DUAL = MODE == kForward || MODE == kInner;
+  typedef Patch<(DUAL ? C::NB / 2 : C::NB) * 32> P;
+  static constexpr int kStage = (C::TM + C::TN) * 128, kWs = (MODE == kInner ? 2 : 1) * P::kBytes;
+  static constexpr int kBytes = 2 * kStage > C::waves * kWs ? 2 * kStage : C::waves * kWs;
+  static_assert(kBytes <= 160 * 1024, "LDS");
+};
+
+// One workgroup's tile, workgroup `block` of a product's.
 template <int MODE, int ACT, bool F32, class C>
-__global__ void __launch_bounds__(C::threads, 2) ffn_tile_kernel(TileArgs t) {
+__device__ __forceinline__ void multiply_tile(const TileArgs& t, int block, char* lds) {
   constexpr bool DUAL = MODE == kForward || MODE == kInner, ACOLS = MODE == kPair;
   constexpr int kCols = DUAL ? C::TN / 2 : C::TN;  // output columns of a tile
   typedef RowsSlab<C::TM, C::threads> AR;
   typedef ColsSlab<C::TM, C::threads> AC;
   typedef RowsSlab<C::TN / 2, C::threads> BR;
   typedef ColsSlab<C::TN, C::threads> BC;
-  constexpr int kA = C::TM * 128, kStage = kA + C::TN * 128;
-  typedef Patch<(DUAL ? C::NB / 2 : C::NB) * 32> P;
-  constexpr int kPatches = MODE == kInner ? 2 : 1;
-  constexpr int kWs = kPatches * P::kBytes;
-  constexpr int kLds = 2 * kStage > C::waves * kWs ? 2 * kStage : C::waves * kWs;
-  static_assert(kLds <= 160 * 1024, "LDS");
-  __shared__ __attribute__((aligned(1024))) char lds[kLds];
+  constexpr int kA = C::TM * 128, kStage = TileLds<MODE, C>::kStage, kWs = TileLds<MODE, C>::kWs;
+  typedef typename TileLds<MODE, C>::P P;
 
   const FfnArgs& g = t.g;
   int tm, tn, z, slice;
-  tile_of(t, tm, tn, z, slice);
+  tile_of(t, block, tm, tn, z, slice);
   const int64_t i0 = (int64_t)tm * C::TM, j0 = (int64_t)tn * kCols;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / C::WN, wn = wave % C::WN;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)lds;
@@ -534,6 +542,23 @@ __global__ void __launch_bounds__(C::threads, 2) ffn_tile_kernel(TileArgs t) {
   }
 }
 
+template <int MODE, int ACT, bool F32, class C>
+__global__ void __launch_bounds__(C::threads, 2) ffn_tile_kernel(TileArgs t) {
+  __shared__ __attribute__((aligned(1024))) char lds[TileLds<MODE, C>::kBytes];
+  multiply_tile<MODE, ACT, F32, C>(t, blockIdx.x, lds);
+}
+
+// Both products of the gradients in one launch: neither waits for the other, and where
+// each alone has few tiles they fill the card together.
+template <bool F32, class C>
+__global__ void __launch_bounds__(C::threads, 2) ffn_gradients_kernel(TileArgs sum, TileArgs pair) {
+  constexpr int kS = TileLds<kSum, C>::kBytes, kP = TileLds<kPair, C>::kBytes;
+  __shared__ __attribute__((aligned(1024))) char lds[kS > kP ? kS : kP];
+  const int block = blockIdx.x;
+  if (block < sum.tiles) multiply_tile<kSum, ISOLOCO_ACT_SILU, F32, C>(sum, block, lds);
+  else multiply_tile<kPair, ISOLOCO_ACT_SILU, F32, C>(pair, block - sum.tiles, lds);
+}
+
 typedef bf16x4 bf16x4_any __attribute__((aligned(2)));
 
 template <bool F32>
@@ -555,12 +580,12 @@ __device__ __forceinline__ void store_out(void* out, floatx4 v, int64_t left) {
 // The splits of a product added in their order, and what the tiles would have made of
 // the whole sums.  One thread per quad of columns.
 template <int MODE, int ACT, bool F32>
-__global__ void __launch_bounds__(256) ffn_join_kernel(TileArgs t) {
+__device__ __forceinline__ void join(const TileArgs& t, int64_t block) {
   constexpr bool DUAL = MODE == kForward || MODE == kInner;
   const FfnArgs& g = t.g;
   const int64_t cols = partial_cols(MODE, g), plane = g.m * cols;
   const int64_t quads = (MODE == kInner ? ffn_pad(g.m) : g.m) * cols / 4;
-  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t at = block * 256 + threadIdx.x;
   const int z = MODE == kPair ? (int)(at / quads) : 0;
   const int64_t i = (at - z * quads) * 4, row = i / cols, col = i - row * cols;
   if (at >= quads * t.planes) return;
@@ -593,6 +618,18 @@ __global__ void __launch_bounds__(256) ffn_join_kernel(TileArgs t) {
   }
 }
 
+template <int MODE, int ACT, bool F32>
+__global__ void __launch_bounds__(256) ffn_join_kernel(TileArgs t) {
+  join<MODE, ACT, F32>(t, blockIdx.x);
+}
+
+template <bool F32>
+__global__ void __launch_bounds__(256) ffn_join_gradients_kernel(TileArgs sum, TileArgs pair, int sum_blocks) {
+  const int block = blockIdx.x;
+  if (block < sum_blocks) join<kSum, ISOLOCO_ACT_SILU, F32>(sum, block);
+  else join<kPair, ISOLOCO_ACT_SILU, F32>(pair, block - sum_blocks);
+}
+
 enum ShapeId { kLarge, kMiddle, kSmall, kShapes };
 struct ShapeInfo {
   int tm, tn, per_cu;
@@ -604,7 +641,22 @@ constexpr int kMaxSplits = 16;
 
 struct Plan {
   int shape, splits;
+  double us;
 };
+
+int64_t slabs_of(int mode, bool f32, int64_t k) {
+  return (k + kSlab - 1) / kSlab * (mode == kSum ? 2 : 1) * (f32 ? 6 : 1);
+}
+int64_t tiles_of(const ShapeInfo& h, int mode, int64_t m, int64_t n) {
+  const bool dual = mode == kForward || mode == kInner;
+  return ((m + h.tm - 1) / h.tm) * ((n * (dual ? 2 : 1) + h.tn - 1) / h.tn) * (mode == kPair ? 2 : 1);
+}
+// a round of `slabs`; the splits' sums to memory and back
+double round_us(const ShapeInfo& h, int64_t slabs) { return (double)slabs * h.slab_us + 4.0; }
+double sums_us(int mode, int splits, int64_t m, int64_t n) {
+  return splits > 1 ? (double)splits * (mode == kSum ? 1 : 2) * m * n * 8 / 3e6 : 0.0;
+}
+constexpr double kJoinUs = 6.0;
 
 // The tiles and splits that take the least time by the rounds of the launch, the
 // slabs of a round and the traffic of the splits' sums.  Both sides measured, us on
@@ -613,77 +665,145 @@ struct Plan {
 // them 3/8 full); its dx 606 / 739 / 802; forward of 2048 tokens, 768 x 2048, 24 / - /
 // 19.  Splits 1 / 2 / 4 / 8 of the dx of 512 tokens, 2048 x 5632: 138 / 79 / 52 / 47.
 Plan plan_of(int mode, bool f32, int64_t m, int64_t n, int64_t k) {
-  const bool dual = mode == kForward || mode == kInner;
-  const int64_t planes = mode == kPair ? 2 : 1;
-  const int64_t slabs = (k + kSlab - 1) / kSlab * (mode == kSum ? 2 : 1) * (f32 ? 6 : 1);
-  Plan best = {kSmall, 1};
-  double least = 1e30;
+  const int64_t slabs = slabs_of(mode, f32, k);
+  Plan best = {kSmall, 1, 1e30};
   for (int s = 0; s < kShapes; ++s) {
     const ShapeInfo& h = kShape[s];
-    const int64_t tiles = ((m + h.tm - 1) / h.tm) * ((n * (dual ? 2 : 1) + h.tn - 1) / h.tn) * planes;
+    const int64_t tiles = tiles_of(h, mode, m, n);
     for (int p = 1; p <= kMaxSplits && (p == 1 || p * 4 <= slabs); ++p) {
       const int64_t rounds = (tiles * p + kCus * h.per_cu - 1) / (kCus * h.per_cu);
-      double us = rounds * ((double)((slabs + p - 1) / p) * h.slab_us + 4.0);
-      if (p > 1) us += 6.0 + (double)p * (dual ? 2 : planes) * m * n * 8 / 3e6;
+      const double us =
+          rounds * round_us(h, (slabs + p - 1) / p) + sums_us(mode, p, m, n) + (p > 1 ? kJoinUs : 0.0);
+      if (us < best.us) best = {s, p, us};
+    }
+  }
+  return best;
+}
+
+// kSum of m x n over k with kPair of k x n over m: one launch of 128-square tiles where
+// that takes clearly less than the two apart.  Both sides measured, us of the whole
+// gradient, apart / together: 512 tokens of 768 x 2048 in bfloat16 47 / 38, in float32
+// 129 / 108; 4096 tokens 125 / 100; 1000 tokens of 612 x 1637 in float32 142 / 122.  Where
+// the sums of this rule are within a tenth of each other (2048 tokens of 768 x 2048 in
+// float32) 289 / 306.
+struct GradientsPlan {
+  bool together;
+  Plan sum, pair;
+};
+GradientsPlan plan_gradients(bool f32, int64_t m, int64_t n, int64_t k) {
+  GradientsPlan best = {false, plan_of(kSum, f32, m, n, k), plan_of(kPair, f32, k, n, m)};
+  if (m == 0) return best;
+  double least = 0.85 * (best.sum.us + best.pair.us);
+  const ShapeInfo& h = kShape[kSmall];
+  const int64_t slabs_s = slabs_of(kSum, f32, k), slabs_p = slabs_of(kPair, f32, m);
+  const int64_t tiles_s = tiles_of(h, kSum, m, n), tiles_p = tiles_of(h, kPair, k, n), slots = kCus * h.per_cu;
+  for (int p = 1; p <= kMaxSplits && (p == 1 || p * 4 <= slabs_s); ++p) {
+    // as many splits of the other as its slabs take no longer with
+    const int64_t length = (slabs_s + p - 1) / p;
+    for (int64_t more = 0; more < 2; ++more) {
+      const int64_t q = std::min<int64_t>(kMaxSplits, (slabs_p + length - 1) / length + more);
+      if (q > 1 && q * 4 > slabs_p) continue;
+      const int64_t rounds = (tiles_s * p + tiles_p * q + slots - 1) / slots;
+      const double us = rounds * round_us(h, std::max(length, (slabs_p + q - 1) / q)) + sums_us(kSum, p, m, n) +
+                        sums_us(kPair, (int)q, k, n) + (p > 1 || q > 1 ? kJoinUs : 0.0);
       if (us < least) {
         least = us;
-        best = {s, p};
+        best = {true, {kSmall, p, us}, {kSmall, (int)q, us}};
       }
     }
   }
   return best;
 }
 
-template <int MODE, int ACT, bool F32, class C>
-void launch_shape(TileArgs& t, hipStream_t st) {
+template <int MODE, class C>
+TileArgs tile_args(const FfnArgs& g, int splits) {
   constexpr int kCols = MODE == kForward || MODE == kInner ? C::TN / 2 : C::TN;
-  t.tiles_m = (int)((t.g.m + C::TM - 1) / C::TM);
-  t.tiles_n = (int)((t.g.n + kCols - 1) / kCols);
+  TileArgs t;
+  t.g = g;
+  t.planes = MODE == kPair ? 2 : 1;
+  t.splits = splits;
+  t.tiles_m = (int)((g.m + C::TM - 1) / C::TM);
+  t.tiles_n = (int)((g.n + kCols - 1) / kCols);
   t.tiles = t.tiles_m * t.tiles_n * t.planes * t.splits;
+  return t;
+}
+
+template <int MODE>
+unsigned join_blocks(const TileArgs& t) {
+  const int64_t quads = t.planes * (MODE == kInner ? ffn_pad(t.g.m) : t.g.m) * partial_cols(MODE, t.g) / 4;
+  return t.splits > 1 ? (unsigned)((quads + 255) / 256) : 0;
+}
+
+template <int MODE, int ACT, bool F32, class C>
+void launch_shape(const FfnArgs& g, int splits, hipStream_t st) {
+  const TileArgs t = tile_args<MODE, C>(g, splits);
   hipLaunchKernelGGL((ffn_tile_kernel<MODE, ACT, F32, C>), dim3(t.tiles), dim3(C::threads), 0, st, t);
-  if (t.splits > 1) {
-    const int64_t quads = t.planes * (MODE == kInner ? ffn_pad(t.g.m) : t.g.m) * partial_cols(MODE, t.g) / 4;
-    hipLaunchKernelGGL((ffn_join_kernel<MODE, ACT, F32>), dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, st, t);
-  }
+  if (splits > 1)
+    hipLaunchKernelGGL((ffn_join_kernel<MODE, ACT, F32>), dim3(join_blocks<MODE>(t)), dim3(256), 0, st, t);
 }
 
 template <int MODE, int ACT, bool F32>
-hipError_t launch_mode(const FfnArgs& g, hipStream_t st) {
+hipError_t launch_mode(const FfnArgs& g, const Plan& p, hipStream_t st) {
   if (g.m == 0 || g.n == 0) return hipSuccess;
-  TileArgs t;
-  t.g = g;
-  const Plan p = plan_of(MODE, F32, g.m, g.n, g.k);
-  t.planes = MODE == kPair ? 2 : 1;
-  t.splits = p.splits;
-  if (p.shape == kLarge) launch_shape<MODE, ACT, F32, Large>(t, st);
-  else if (p.shape == kMiddle) launch_shape<MODE, ACT, F32, Middle>(t, st);
-  else launch_shape<MODE, ACT, F32, Small>(t, st);
+  if (p.shape == kLarge) launch_shape<MODE, ACT, F32, Large>(g, p.splits, st);
+  else if (p.shape == kMiddle) launch_shape<MODE, ACT, F32, Middle>(g, p.splits, st);
+  else launch_shape<MODE, ACT, F32, Small>(g, p.splits, st);
   return hipGetLastError();
 }
 
 template <bool F32>
-hipError_t launch_type(FfnMode mode, int act, const FfnArgs& g, hipStream_t st) {
-  const bool silu = act == ISOLOCO_ACT_SILU;
-  switch (mode) {
-    case kForward:
-      return silu ? launch_mode<kForward, ISOLOCO_ACT_SILU, F32>(g, st) : launch_mode<kForward, ISOLOCO_ACT_GELU, F32>(g, st);
-    case kInner:
-      return silu ? launch_mode<kInner, ISOLOCO_ACT_SILU, F32>(g, st) : launch_mode<kInner, ISOLOCO_ACT_GELU, F32>(g, st);
-    // (these two apply no activation)
-    case kSum: return launch_mode<kSum, ISOLOCO_ACT_SILU, F32>(g, st);
-    default: return launch_mode<kPair, ISOLOCO_ACT_SILU, F32>(g, st);
+hipError_t launch_projections(FfnMode mode, int act, const FfnArgs& g, hipStream_t st) {
+  const Plan p = plan_of(mode, F32, g.m, g.n, g.k);
+  if (mode == kForward)
+    return act == ISOLOCO_ACT_SILU ? launch_mode<kForward, ISOLOCO_ACT_SILU, F32>(g, p, st)
+                                   : launch_mode<kForward, ISOLOCO_ACT_GELU, F32>(g, p, st);
+  return act == ISOLOCO_ACT_SILU ? launch_mode<kInner, ISOLOCO_ACT_SILU, F32>(g, p, st)
+                                 : launch_mode<kInner, ISOLOCO_ACT_GELU, F32>(g, p, st);
+}
+
+size_t partial_bytes(const Plan& p, int mode, int64_t m, int64_t n) {
+  return p.splits > 1 ? (size_t)p.splits * (mode == kSum ? 1 : 2) * m * ffn_pad(n) * sizeof(float) : 0;
+}
+
+// (these two apply no activation)  One of them alone goes by the same plan: the same bits.
+template <bool F32>
+hipError_t launch_gradients(const FfnArgs* sum, const FfnArgs* pair, hipStream_t st) {
+  if (!sum && !pair) return hipSuccess;
+  const GradientsPlan p =
+      sum ? plan_gradients(F32, sum->m, sum->n, sum->k) : plan_gradients(F32, pair->k, pair->n, pair->m);
+  if (sum && pair && p.together) {
+    FfnArgs after = *pair;
+    after.partial += partial_bytes(p.sum, kSum, sum->m, sum->n) / sizeof(float);
+    const TileArgs s = tile_args<kSum, Small>(*sum, p.sum.splits), q = tile_args<kPair, Small>(after, p.pair.splits);
+    hipLaunchKernelGGL((ffn_gradients_kernel<F32, Small>), dim3(s.tiles + q.tiles), dim3(Small::threads), 0, st, s, q);
+    const unsigned js = join_blocks<kSum>(s), jq = join_blocks<kPair>(q);
+    if (js + jq) hipLaunchKernelGGL(ffn_join_gradients_kernel<F32>, dim3(js + jq), dim3(256), 0, st, s, q, (int)js);
+    return hipGetLastError();
   }
+  hipError_t e = hipSuccess;
+  if (sum) e = launch_mode<kSum, ISOLOCO_ACT_SILU, F32>(*sum, p.sum, st);
+  if (e == hipSuccess && pair) e = launch_mode<kPair, ISOLOCO_ACT_SILU, F32>(*pair, p.pair, st);
+  return e;
 }
 
 }  // namespace
 
-size_t ffn_partial_bytes(FfnMode mode, bool f32, int64_t m, int64_t n, int64_t k) {
-  const Plan p = plan_of(mode, f32, m, n, k);
-  return p.splits > 1 ? (size_t)p.splits * (mode == kSum ? 1 : 2) * m * ffn_pad(n) * sizeof(float) : 0;
+size_t ffn_projections_partial_bytes(FfnMode mode, bool f32, int64_t m, int64_t n, int64_t k) {
+  return partial_bytes(plan_of(mode, f32, m, n, k), mode, m, n);
 }
 
-hipError_t launch_ffn_tiles(FfnMode mode, int act, bool f32, const FfnArgs& g, hipStream_t st) {
-  return f32 ? launch_type<true>(mode, act, g, st) : launch_type<false>(mode, act, g, st);
+size_t ffn_gradients_partial_bytes(bool f32, int64_t m, int64_t n, int64_t k) {
+  const GradientsPlan p = plan_gradients(f32, m, n, k);
+  const size_t sum = partial_bytes(p.sum, kSum, m, n), pair = partial_bytes(p.pair, kPair, k, n);
+  return p.together ? sum + pair : std::max(sum, pair);
+}
+
+hipError_t launch_ffn_projections(FfnMode mode, int act, bool f32, const FfnArgs& g, hipStream_t st) {
+  return f32 ? launch_projections<true>(mode, act, g, st) : launch_projections<false>(mode, act, g, st);
+}
+
+hipError_t launch_ffn_gradients(bool f32, const FfnArgs* sum, const FfnArgs* pair, hipStream_t st) {
+  return f32 ? launch_gradients<true>(sum, pair, st) : launch_gradients<false>(sum, pair, st);
 }
 
 }  // namespace isoloco
