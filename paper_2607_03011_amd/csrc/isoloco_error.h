@@ -35,6 +35,10 @@ constexpr int64_t kMaxExtent = (int64_t)1 << 31;
 // A launch's threads are counted in 32 bits.
 inline bool launchable(int64_t blocks, int threads) { return blocks <= (int64_t)UINT32_MAX / threads; }
 
+// The card's last cache.  A result that is larger is stored past the caches: its reader
+// would not find it there, and what is there stays.
+constexpr int64_t kCacheBytes = (int64_t)256 << 20;
+
 #define ISOLOCO_TRY(expr)                          \
   do {                                             \
     const isoloco_status try_status_ = (expr);     \

@@ -359,8 +359,9 @@ struct GradIn {
 constexpr int kGradThreads = 256;
 constexpr int kGradVecs = 4;  // 16-byte vectors of a thread
 
-// One workgroup per row and span of kGradThreads * kGradVecs vectors.
-template <typename T, typename ID>
+// One workgroup per row and span of kGradThreads * kGradVecs vectors.  PAST: the result
+// goes past the caches.
+template <typename T, typename ID, bool PAST>
 __global__ void __launch_bounds__(kGradThreads) logprob_grad_kernel(const T* logits, int64_t ld, int64_t rows, int64_t vocab,
                                                                     const ID* targets, float scale, GradIn in,
                                                                     T* dlogits, int64_t ld_d, int spans) {
@@ -403,7 +404,9 @@ __global__ void __launch_bounds__(kGradThreads) logprob_grad_kernel(const T* log
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = __float_as_uint(x[e]);
       }
-      *reinterpret_cast<u32x4_any*>(out + i * N) = v;
+      u32x4_any* to = reinterpret_cast<u32x4_any*>(out + i * N);
+      if constexpr (PAST) __builtin_nontemporal_store(v, to);
+      else *to = v;
     }
   }
   const int64_t at = whole * N + threadIdx.x;
@@ -451,7 +454,11 @@ void run_forward(const void* logits, const void* targets, int64_t rows, const Ro
 template <typename T, typename ID>
 void run_grad(const void* logits, int64_t ld, int64_t rows, int64_t vocab, const void* targets, float scale,
               const GradIn& in, void* dlogits, int64_t ld_d, int spans, hipStream_t st) {
-  hipLaunchKernelGGL((logprob_grad_kernel<T, ID>), dim3((unsigned)(rows * spans)), dim3(kGradThreads), 0, st,
+  // Both sides measured, stored past the caches / stored, us of both passes over rows of 32000
+  // in bfloat16: 8192 rows 286 / 314 (and what scales the gradient after them takes as
+  // long); 2048 rows 72 / 72, but what reads the gradient then takes 8 longer.
+  const bool past = dlogits != logits && rows * vocab * (int64_t)sizeof(T) > kCacheBytes;
+  hipLaunchKernelGGL((past ? logprob_grad_kernel<T, ID, true> : logprob_grad_kernel<T, ID, false>), dim3((unsigned)(rows * spans)), dim3(kGradThreads), 0, st,
                      static_cast<const T*>(logits), ld, rows, vocab, static_cast<const ID*>(targets), scale, in,
                      static_cast<T*>(dlogits), ld_d, spans);
 }
