@@ -738,3 +738,34 @@ def test_graph_replays(iso, tokens):
         torch.cuda.synchronize()
         for a, b in zip(got, eager):
             assert torch.equal(a, b)
+
+
+# --------------------------------------------------------------------------
+# Results larger than the caches, which are stored past them
+# --------------------------------------------------------------------------
+
+def test_clip_of_large_results(iso):
+    """The scaled elements one by one, at odd alignments and with a shorter last chunk."""
+    flat = torch.randn(36_000_011, device="cuda")
+    grads = [flat[1:30_000_000], flat[30_000_000:], torch.randn(5_000_001, device="cuda").to(BF16)[1:]]
+    outs = [torch.empty(g.numel() + 3, device="cuda", dtype=g.dtype)[3:] for g in grads]
+    for max_norm in (1.0, 1e9):
+        coef = iso.clip_grads(grads, max_norm, out=outs)[1]
+        for g, o in zip(grads, outs):
+            assert torch.equal(o, (g.float() * coef).to(g.dtype))
+
+
+@pytest.mark.parametrize("rows,vocab,dtype", [(4200, 32003, BF16), (1100, 64001, F32)])
+def test_token_logprobs_backward_of_large_results(iso, rows, vocab, dtype):
+    """The same bits as in calls of few rows, whose results stay in the caches."""
+    t = torch.randn(rows, vocab, device="cuda").to(dtype)
+    targets = torch.arange(rows, device="cuda") * 7 % vocab
+    w = torch.randn(2, rows, device="cuda")
+    r = iso.token_logprobs(t, targets)
+    d = iso.token_logprobs_backward(t, targets, r.lse, w[0], entropy=r.entropy, dentropy=w[1])
+    assert d.numel() * d.element_size() > 256 << 20
+    for a in range(0, rows, 500):
+        b = min(rows, a + 500)
+        part = iso.token_logprobs_backward(t[a:b], targets[a:b], r.lse[a:b], w[0, a:b], entropy=r.entropy[a:b],
+                                           dentropy=w[1, a:b])
+        assert torch.equal(d[a:b], part)
