@@ -113,7 +113,7 @@ def isoloco_gated_ffn_backward(x, ld_x, w_gate, w_up, ld_w, dtype, tokens, dim, 
 # (the public functions make a Stream object per call, 2 us of a small operator's 10)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda index: torch.cuda.current_stream(index).cuda_stream)
-_empty = torch.empty
+_empty = torch.empty  # (its sizes one by one: 0.3 us less than as a tuple)
 _F32 = torch.float32
 
 
@@ -258,7 +258,7 @@ def embedding(table, ids, scale=1.0, out=None, out_dtype=None):
     n = ids.numel()
     dtype, id_type, ld = _type("table", table), _ids("ids", ids, n), _rows("table", table)[1]
     if out is None:
-        out = _empty((*ids.shape, dim), dtype=out_dtype or table.dtype, device=table.device)
+        out = _empty(*ids.shape, dim, dtype=out_dtype or table.dtype, device=table.device)
         ld_out = dim
     else:
         _output("out", out, (*ids.shape, dim), out_dtype or out.dtype)
@@ -283,7 +283,7 @@ def embedding_backward(ids, dout, vocab, scale=1.0, out=None, accumulate=False, 
     n, ld = _rows("dout", dout)
     dtype, id_type = _type("dout", dout), _ids("ids", ids, n)
     if out is None:
-        out = _empty((vocab, dim), dtype=out_dtype or _F32, device=dout.device)
+        out = _empty(vocab, dim, dtype=out_dtype or _F32, device=dout.device)
         ld_out = dim
     else:
         _output("out", out, (vocab, dim), out_dtype or out.dtype)
@@ -321,14 +321,14 @@ def token_logprobs(logits, targets=None, scale=1.0, top_k=0, workspace=None):
     if targets is not None:
         _same_device(index, targets)
         t_type = _ids("targets", targets, rows)
-        entropy, lse, logprob = _empty((3, *shape), dtype=_F32, device=device).unbind()
+        entropy, lse, logprob = _empty(3, *shape, dtype=_F32, device=device).unbind()
         target_at, logprob_at = targets.data_ptr(), logprob.data_ptr()
     else:
-        entropy, lse = _empty((2, *shape), dtype=_F32, device=device).unbind()
+        entropy, lse = _empty(2, *shape, dtype=_F32, device=device).unbind()
     ws_need = isoloco_token_logprobs_workspace_size(rows, vocab, top_k)
     if top_k:
-        top = _empty((*shape, top_k), dtype=_F32, device=device)
-        top_index = _empty((*shape, top_k), dtype=torch.int64, device=device)
+        top = _empty(*shape, top_k, dtype=_F32, device=device)
+        top_index = _empty(*shape, top_k, dtype=torch.int64, device=device)
         top_at, index_at = top.data_ptr(), top_index.data_ptr()
     keep, ws, ws_bytes = _workspace(workspace, ws_need, device)
     _check(_lib.isoloco_token_logprobs(logits.data_ptr(), ld, dtype, rows, vocab, target_at, t_type, scale, top_k,
@@ -360,7 +360,7 @@ def token_logprobs_backward(logits, targets, lse, dlogprob, entropy=None, dentro
     if dentropy is not None:
         entropy_at, dentropy_at = _vector("entropy", entropy, rows), _vector("dentropy", dentropy, rows)
     if out is None:
-        out = _empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        out = _empty(*logits.shape, dtype=logits.dtype, device=logits.device)
         ld_out = vocab
     else:
         _output("out", out, logits.shape, logits.dtype)
@@ -399,7 +399,7 @@ def gated_ffn(x, w_gate, w_up, act="silu", out=None, workspace=None):
     is "silu" or "gelu"."""
     index, dtype, tokens, dim, hidden, ld_x, ld_w, a, at, flags = _ffn_operands(x, w_gate, w_up, act)
     if out is None:
-        out = _empty((*x.shape[:-1], hidden), dtype=x.dtype, device=x.device)
+        out = _empty(*x.shape[:-1], hidden, dtype=x.dtype, device=x.device)
         ld_out = hidden
     else:
         _same_device(index, out)
@@ -423,11 +423,11 @@ def gated_ffn_backward(x, w_gate, w_up, dout, act="silu", need_dx=True, need_dw=
     ld_dout, device = _rows("dout", dout)[1], x.device
     dx = dwg = dwu = dx_at = dwg_at = dwu_at = None
     if need_dx:
-        dx = _empty(x.shape, dtype=x.dtype, device=device)
+        dx = _empty(*x.shape, dtype=x.dtype, device=device)
         dx_at = dx.data_ptr()
     if need_dw:
-        dwg = _empty((hidden, dim), dtype=x.dtype, device=device)
-        dwu = _empty((hidden, dim), dtype=x.dtype, device=device)
+        dwg = _empty(hidden, dim, dtype=x.dtype, device=device)
+        dwu = _empty(hidden, dim, dtype=x.dtype, device=device)
         dwg_at, dwu_at = dwg.data_ptr(), dwu.data_ptr()
     keep, ws, ws_bytes = _workspace(workspace, isoloco_gated_ffn_workspace_size(
         tokens, dim, hidden, dtype, flags | ISOLOCO_FFN_BACKWARD), device)
