@@ -550,13 +550,14 @@ __global__ void __launch_bounds__(C::threads, 2) ffn_tile_kernel(TileArgs t) {
 
 // Both products of the gradients in one launch: neither waits for the other, and where
 // each alone has few tiles they fill the card together.
-template <bool F32, class C>
-__global__ void __launch_bounds__(C::threads, 2) ffn_gradients_kernel(TileArgs sum, TileArgs pair) {
-  constexpr int kS = TileLds<kSum, C>::kBytes, kP = TileLds<kPair, C>::kBytes;
+template <bool F32, class CS, class CP>
+__global__ void __launch_bounds__(CS::threads, 2) ffn_gradients_kernel(TileArgs sum, TileArgs pair) {
+  static_assert(CS::threads == CP::threads, "one launch");
+  constexpr int kS = TileLds<kSum, CS>::kBytes, kP = TileLds<kPair, CP>::kBytes;
   __shared__ __attribute__((aligned(1024))) char lds[kS > kP ? kS : kP];
   const int block = blockIdx.x;
-  if (block < sum.tiles) multiply_tile<kSum, ISOLOCO_ACT_SILU, F32, C>(sum, block, lds);
-  else multiply_tile<kPair, ISOLOCO_ACT_SILU, F32, C>(pair, block - sum.tiles, lds);
+  if (block < sum.tiles) multiply_tile<kSum, ISOLOCO_ACT_SILU, F32, CS>(sum, block, lds);
+  else multiply_tile<kPair, ISOLOCO_ACT_SILU, F32, CP>(pair, block - sum.tiles, lds);
 }
 
 typedef bf16x4 bf16x4_any __attribute__((aligned(2)));
@@ -680,35 +681,42 @@ Plan plan_of(int mode, bool f32, int64_t m, int64_t n, int64_t k) {
   return best;
 }
 
-// kSum of m x n over k with kPair of k x n over m: one launch of 128-square tiles where
-// that takes clearly less than the two apart.  Both sides measured, us of the whole
-// gradient, apart / together: 512 tokens of 768 x 2048 in bfloat16 47 / 38, in float32
-// 129 / 108; 4096 tokens 125 / 100; 1000 tokens of 612 x 1637 in float32 142 / 122.  Where
-// the sums of this rule are within a tenth of each other (2048 tokens of 768 x 2048 in
-// float32) 289 / 306.
+// kSum of m x n over k with kPair of k x n over m: one launch where that takes less than
+// the two apart by the same rule (1.06: of which it leaves out that the first of two
+// drains before the second fills the card).  Both sides measured, us of the whole
+// gradient, apart / together: bfloat16, 512 tokens of 768 x 2048 47 / 38, 4096 tokens 125
+// / 99, 1024 of 2048 x 5632 175 / 157, 4096 of them 536 / 503, 8192 of 1024 x 4096 427 /
+// 370; float32, 1000 tokens of 612 x 1637 142 / 122, 2048 of 768 x 2048 289 / 272.
+// Everything together (1.15): 3000 tokens of 1001 x 2777 in float32 723 / 771.
 struct GradientsPlan {
   bool together;
   Plan sum, pair;
 };
+constexpr int kTogether[][2] = {{kSmall, kSmall}, {kLarge, kLarge}, {kLarge, kMiddle}};
 GradientsPlan plan_gradients(bool f32, int64_t m, int64_t n, int64_t k) {
   GradientsPlan best = {false, plan_of(kSum, f32, m, n, k), plan_of(kPair, f32, k, n, m)};
   if (m == 0) return best;
-  double least = 0.85 * (best.sum.us + best.pair.us);
-  const ShapeInfo& h = kShape[kSmall];
+  double least = 1.06 * (best.sum.us + best.pair.us);
   const int64_t slabs_s = slabs_of(kSum, f32, k), slabs_p = slabs_of(kPair, f32, m);
-  const int64_t tiles_s = tiles_of(h, kSum, m, n), tiles_p = tiles_of(h, kPair, k, n), slots = kCus * h.per_cu;
-  for (int p = 1; p <= kMaxSplits && (p == 1 || p * 4 <= slabs_s); ++p) {
-    // as many splits of the other as its slabs take no longer with
-    const int64_t length = (slabs_s + p - 1) / p;
-    for (int64_t more = 0; more < 2; ++more) {
-      const int64_t q = std::min<int64_t>(kMaxSplits, (slabs_p + length - 1) / length + more);
-      if (q > 1 && q * 4 > slabs_p) continue;
-      const int64_t rounds = (tiles_s * p + tiles_p * q + slots - 1) / slots;
-      const double us = rounds * round_us(h, std::max(length, (slabs_p + q - 1) / q)) + sums_us(kSum, p, m, n) +
-                        sums_us(kPair, (int)q, k, n) + (p > 1 || q > 1 ? kJoinUs : 0.0);
-      if (us < least) {
-        least = us;
-        best = {true, {kSmall, p, us}, {kSmall, (int)q, us}};
+  for (const auto& shapes : kTogether) {
+    const ShapeInfo &hs = kShape[shapes[0]], &hp = kShape[shapes[1]];
+    const int64_t tiles_s = tiles_of(hs, kSum, m, n), tiles_p = tiles_of(hp, kPair, k, n), slots = kCus * hs.per_cu;
+    for (int p = 1; p <= kMaxSplits && (p == 1 || p * 4 <= slabs_s); ++p) {
+      // as many splits of the other as its slabs take no longer with
+      const int64_t length = (slabs_s + p - 1) / p;
+      for (int64_t more = 0; more < 2; ++more) {
+        const int64_t q = std::min<int64_t>(kMaxSplits, (slabs_p + length - 1) / length + more);
+        if (q > 1 && q * 4 > slabs_p) continue;
+        const double us_s = round_us(hs, length), us_p = round_us(hp, (slabs_p + q - 1) / q);
+        const int64_t ns = tiles_s * p, np = tiles_p * q;
+        // the workgroups follow each other; the last of them end at different times
+        double us = std::max(us_s, us_p);
+        if (ns + np > slots) us = std::max(us, (ns * us_s + np * us_p) / slots + 0.5 * us_p);
+        us += sums_us(kSum, p, m, n) + sums_us(kPair, (int)q, k, n) + (p > 1 || q > 1 ? kJoinUs : 0.0);
+        if (us < least) {
+          least = us;
+          best = {true, {shapes[0], p, us}, {shapes[1], (int)q, us}};
+        }
       }
     }
   }
@@ -765,6 +773,17 @@ size_t partial_bytes(const Plan& p, int mode, int64_t m, int64_t n) {
   return p.splits > 1 ? (size_t)p.splits * (mode == kSum ? 1 : 2) * m * ffn_pad(n) * sizeof(float) : 0;
 }
 
+template <bool F32, class CS, class CP>
+hipError_t launch_together(const FfnArgs& sum, const FfnArgs& pair, const GradientsPlan& p, hipStream_t st) {
+  FfnArgs after = pair;
+  after.partial += partial_bytes(p.sum, kSum, sum.m, sum.n) / sizeof(float);
+  const TileArgs s = tile_args<kSum, CS>(sum, p.sum.splits), q = tile_args<kPair, CP>(after, p.pair.splits);
+  hipLaunchKernelGGL((ffn_gradients_kernel<F32, CS, CP>), dim3(s.tiles + q.tiles), dim3(CS::threads), 0, st, s, q);
+  const unsigned js = join_blocks<kSum>(s), jq = join_blocks<kPair>(q);
+  if (js + jq) hipLaunchKernelGGL(ffn_join_gradients_kernel<F32>, dim3(js + jq), dim3(256), 0, st, s, q, (int)js);
+  return hipGetLastError();
+}
+
 // (these two apply no activation)  One of them alone goes by the same plan: the same bits.
 template <bool F32>
 hipError_t launch_gradients(const FfnArgs* sum, const FfnArgs* pair, hipStream_t st) {
@@ -772,13 +791,9 @@ hipError_t launch_gradients(const FfnArgs* sum, const FfnArgs* pair, hipStream_t
   const GradientsPlan p =
       sum ? plan_gradients(F32, sum->m, sum->n, sum->k) : plan_gradients(F32, pair->k, pair->n, pair->m);
   if (sum && pair && p.together) {
-    FfnArgs after = *pair;
-    after.partial += partial_bytes(p.sum, kSum, sum->m, sum->n) / sizeof(float);
-    const TileArgs s = tile_args<kSum, Small>(*sum, p.sum.splits), q = tile_args<kPair, Small>(after, p.pair.splits);
-    hipLaunchKernelGGL((ffn_gradients_kernel<F32, Small>), dim3(s.tiles + q.tiles), dim3(Small::threads), 0, st, s, q);
-    const unsigned js = join_blocks<kSum>(s), jq = join_blocks<kPair>(q);
-    if (js + jq) hipLaunchKernelGGL(ffn_join_gradients_kernel<F32>, dim3(js + jq), dim3(256), 0, st, s, q, (int)js);
-    return hipGetLastError();
+    if (p.sum.shape == kSmall) return launch_together<F32, Small, Small>(*sum, *pair, p, st);
+    if (p.pair.shape == kLarge) return launch_together<F32, Large, Large>(*sum, *pair, p, st);
+    return launch_together<F32, Large, Middle>(*sum, *pair, p, st);
   }
   hipError_t e = hipSuccess;
   if (sum) e = launch_mode<kSum, ISOLOCO_ACT_SILU, F32>(*sum, p.sum, st);
