@@ -769,3 +769,33 @@ def test_token_logprobs_backward_of_large_results(iso, rows, vocab, dtype):
         part = iso.token_logprobs_backward(t[a:b], targets[a:b], r.lse[a:b], w[0, a:b], entropy=r.entropy[a:b],
                                            dentropy=w[1, a:b])
         assert torch.equal(d[a:b], part)
+
+
+# Sizes at which dx and the weights' products share a launch: of 256-square tiles in 16
+# and in 4 splits, of 256-square and 192 x 256 tiles, of 128-square ones; in float32 of
+# 256-square ones in 8 splits and of 128-square ones.
+@pytest.mark.parametrize("tokens,dim,hidden,dtype", [
+    (130, 1500, 8000, BF16), (1024, 2048, 5632, BF16), (1500, 1500, 4000, BF16), (1100, 1300, 2900, BF16),
+    (700, 1032, 3000, F32), (640, 1544, 4104, F32),
+])
+def test_gated_ffn_gradients_together(iso, tokens, dim, hidden, dtype):
+    x, wg, wu, dh = (t.cuda() for t in ffn_inputs(tokens, dim, hidden, dtype, 12))
+    grads = iso.gated_ffn_backward(x, wg, wu, dh)
+    g, u, a, da, eg, eu, ea = ffn_reference(x, wg, wu, "silu")
+    X, G, W, D = (t.double() for t in (x, wg, wu, dh))
+    dg, du = D * u * da, D * a
+    rnd = ROUND[dtype] if dtype == BF16 else 4 * U32
+    edg = D.abs() * ((da.abs() + 1e-6) * eu + u.abs() * (0.8 * eg + 16 * U32) + 0.8 * eg * eu) + rnd * dg.abs()
+    edu = D.abs() * ea + rnd * du.abs()
+    nk, nt = (2 * hidden + 8) * U32, (tokens + 8) * U32
+    want = [dg @ G + du @ W, dg.T @ X, du.T @ X]
+    bound = [edg @ G.abs() + edu @ W.abs() + nk * (dg.abs() @ G.abs() + du.abs() @ W.abs()),
+             edg.T @ X.abs() + nt * (dg.abs().T @ X.abs()), edu.T @ X.abs() + nt * (du.abs().T @ X.abs())]
+    for r, w, b in zip(grads, want, bound):
+        within(r.cpu(), w.cpu(), (1.01 * b + ROUND[dtype] * w.abs() + 1e-37).cpu())
+        # random errors: far below the bound's worst case
+        assert ((r.double() - w).norm() / w.norm()).item() <= (2.0 ** -8 if dtype == BF16 else 2.0 ** -20)
+    # one of them alone: the same bits
+    assert torch.equal(iso.gated_ffn_backward(x, wg, wu, dh, need_dw=False)[0], grads[0])
+    only = iso.gated_ffn_backward(x, wg, wu, dh, need_dx=False)
+    assert torch.equal(only[1], grads[1]) and torch.equal(only[2], grads[2])
