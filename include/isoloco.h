@@ -408,7 +408,9 @@ isoloco_status isoloco_embedding_backward(const void* ids, int32_t id_type, int6
  * and lse may be NULL.  A target outside [0, vocab) is ignored: logprob 0.
  * Logits of -infinity are masked (p = 0); a row of nothing else has lse =
  * logprob = -infinity and entropy 0.  A NaN or +infinity among a row's logits
- * makes its results NaN. */
+ * makes its results NaN.  Finite logits of any size are taken as they are: a
+ * result is infinite only where its value is past float32's range (logits that
+ * lie further apart than that count as infinitely far). */
 isoloco_status isoloco_token_logprobs_workspace_size(int64_t rows, int64_t vocab, int32_t top_k, size_t* bytes);
 isoloco_status isoloco_token_logprobs(const void* logits, int64_t ld_logits, int32_t dtype, int64_t rows,
                                       int64_t vocab, const void* targets, int32_t target_type, float scale,

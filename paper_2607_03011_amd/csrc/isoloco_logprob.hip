@@ -1,11 +1,15 @@
 // Log probabilities of given tokens, with entropy and the best alternatives, and
-// their gradient.  With z = scale * logits of a row, m = max z:
+// their gradient.  With x the logits of a row, m = max x, t_j = scale (x_j - m) log2 e:
 //
-//   lse = m + log sum_j e^(z_j - m)         logprob = z_target - lse
-//   entropy = log s - w / s,  s = sum e^(z_j - m),  w = sum e^(z_j - m) (z_j - m)
+//   s = sum_j 2^t_j,  w = sum_j 2^t_j t_j
+//   lse = scale m + log s                   logprob = scale (x_target - m) - log s
+//   entropy = log s - w log 2 / s
 //   dlogits_j = scale (dlogprob (1[j = target] - p_j) - dentropy p_j (log p_j + entropy))
 //
-// Forward: one pass over a row with the running maximum and sums of its softmax.
+// Forward: one pass over a row with the running maximum and sums of its softmax.  The
+// maximum is kept as a logit and taken from the logits before the scale: the largest
+// one's t is then 0 whatever the products' rounding, which past |scale x| = 1e9 (masks
+// that are written as a large number) is more than an exponential's range.
 // A column of -infinity (a mask) has p = 0 and adds nothing; a row of nothing but
 // those has lse = logprob = -infinity, entropy 0 and no gradient.  A NaN or a
 // logit of +infinity makes the row's results NaN.
@@ -13,6 +17,7 @@
 // them again and writes as much.
 #include <hip/hip_runtime.h>
 
+#include <float.h>
 #include <math.h>
 #include <stdint.h>
 
@@ -24,31 +29,32 @@ namespace {
 
 typedef u32x4 u32x4_any __attribute__((aligned(2)));
 
-constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLog2e = 1.44269504088896340736f, kLog2 = 0.69314718055994530942f;
 
 // e^x, x <= 0 where it counts: the product's rounding moves the result by |x| ulps
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
-// e^d is 0 from here on down: a product with it takes this for d (which may be -infinity)
+// 2^t is 0 from here on down: a product with it takes this for t (which may be -infinity)
 constexpr float kNothing = -200.f;
 
-// The softmax of some of a row's z: their maximum m, and s and w as above against it
+// The softmax of some of a row's logits: their maximum m, and s and w as above against it
 // ({-infinity, 0, 0} of nothing; a NaN or +infinity among them leaves a NaN in s).
+// `rate` is scale log2 e.
 struct Soft {
   float m, s, w;
-  __device__ __forceinline__ void raise(float to) {
+  __device__ __forceinline__ void raise(float to, float rate) {
     if (to == m) return;
     if (m != -INFINITY) {
-      const float d = m - to, e = exp_of(d);
-      w = e > 0.f ? e * (w + s * d) : 0.f;
+      const float t = (m - to) * rate, e = __builtin_amdgcn_exp2f(t);
+      w = e > 0.f ? e * (w + s * t) : 0.f;
       s = e * s;
     }
     m = to;
   }
-  __device__ __forceinline__ void join(const Soft& o) {
+  __device__ __forceinline__ void join(const Soft& o, float rate) {
     const float to = fmaxf(m, o.m);
     Soft b = o;
-    raise(to);
-    b.raise(to);
+    raise(to, rate);
+    b.raise(to, rate);
     s += b.s;
     w += b.w;
   }
@@ -99,7 +105,7 @@ struct RowOut {
 
 struct RowArgs {
   int64_t ld, vocab;
-  float scale;
+  float scale, rate;  // rate: scale log2 e
   int top_k;
   int splits;      // workgroups per row
   int64_t span;    // a split's columns (a multiple of a vector's)
@@ -118,18 +124,18 @@ template <typename T, typename ID>
 __device__ __forceinline__ void put_row(const RowArgs& g, const T* row, const ID* targets, int64_t r, const Soft& a) {
   const bool empty = a.m == -INFINITY && a.s == 0.f;
   const float log_s = logf(a.s);
-  if (g.o.lse) g.o.lse[r] = empty ? -INFINITY : a.m + log_s;
-  if (g.o.entropy) g.o.entropy[r] = empty ? 0.f : log_s - a.w / a.s;
+  if (g.o.lse) g.o.lse[r] = empty ? -INFINITY : fmaf(a.m, g.scale, log_s);
+  if (g.o.entropy) g.o.entropy[r] = empty ? 0.f : log_s - a.w * kLog2 / a.s;
   if (g.o.logprob) {
     const int64_t t = targets[r];
     float lp = 0.f;
-    if (t >= 0 && t < g.vocab) lp = empty ? -INFINITY : fmaf((float)row[t], g.scale, -a.m) - log_s;
+    if (t >= 0 && t < g.vocab) lp = empty ? -INFINITY : ((float)row[t] - a.m) * g.scale - log_s;
     g.o.logprob[r] = lp;
   }
 }
 __device__ __forceinline__ void put_top(const RowArgs& g, int64_t r, int place, uint64_t key, const Soft& a) {
   const bool empty = a.m == -INFINITY && a.s == 0.f;
-  g.o.top_logprob[r * g.top_k + place] = empty ? -INFINITY : fmaf(value_of(key), g.scale, -a.m) - logf(a.s);
+  g.o.top_logprob[r * g.top_k + place] = empty ? -INFINITY : (value_of(key) - a.m) * g.scale - logf(a.s);
   g.o.top_index[r * g.top_k + place] = index_of(key);
 }
 
@@ -181,7 +187,6 @@ __global__ void __launch_bounds__(64 * WAVES, sizeof(T) == 2 ? 8 : 4)
   const bool once = whole <= turn;  // the registers hold all of it
 
   Soft a = {-INFINITY, 0.f, 0.f};
-  float top = -INFINITY;  // the largest logit
   for (int base = 0; base == 0 || base < whole; base += turn) {
     load(base);
     float most = last;
@@ -198,13 +203,12 @@ __global__ void __launch_bounds__(64 * WAVES, sizeof(T) == 2 ? 8 : 4)
 #pragma unroll
       for (int c = 0; c < kVecs; ++c) asm("" : "+v"(v[c]));
     }
-    top = fmaxf(top, most);
-    a.raise(fmaxf(a.m, most * g.scale));
+    a.raise(fmaxf(a.m, most), g.rate);
     const float m = a.m == -INFINITY ? 0.f : a.m;
     const auto add = [&](float v) {
-      const float d = fmaf(v, g.scale, -m), e = exp_of(d);
+      const float t = (v - m) * g.rate, e = __builtin_amdgcn_exp2f(t);
       a.s += e;
-      a.w = fmaf(e, fmaxf(d, kNothing), a.w);
+      a.w = fmaf(e, fmaxf(t, kNothing), a.w);
     };
 #pragma unroll
     for (int c = 0; c < kVecs; ++c)
@@ -223,20 +227,20 @@ __global__ void __launch_bounds__(64 * WAVES, sizeof(T) == 2 ? 8 : 4)
     o.m = __shfl_xor(b.m, off, 64);
     o.s = __shfl_xor(b.s, off, 64);
     o.w = __shfl_xor(b.w, off, 64);
-    b.join(o);
+    b.join(o, g.rate);
   }
   if constexpr (WAVES > 1) {
     if (lane == 0) part[wave] = b;
   }
   if (g.top_k) {
-    group[wave][lane] = top;
+    group[wave][lane] = a.m;
     if (wave == 0) rank[lane] = 0;
     if (threadIdx.x == 0) n_cand = 0;
   }
   __syncthreads();
   if constexpr (WAVES > 1) {
     b = part[0];
-    for (int w = 1; w < WAVES; ++w) b.join(part[w]);
+    for (int w = 1; w < WAVES; ++w) b.join(part[w], g.rate);
   }
   const bool whole_row = g.splits == 1;
   if (threadIdx.x == 0) {
@@ -336,7 +340,7 @@ __global__ void __launch_bounds__(256) logprob_join_kernel(const T* logits, cons
   const int64_t r = blockIdx.x;
   const Soft* part = g.part + r * g.splits;
   Soft a = part[0];
-  for (int i = 1; i < g.splits; ++i) a.join(part[i]);
+  for (int i = 1; i < g.splits; ++i) a.join(part[i], g.rate);
   if (threadIdx.x == 0) put_row(g, logits + r * g.ld, targets, r, a);
   const int n = g.splits * g.top_k;
   for (int i = threadIdx.x; i < n; i += 256) keys[i] = g.keys[r * n + i];
@@ -528,6 +532,7 @@ isoloco_status isoloco_token_logprobs(const void* logits, int64_t ld_logits, int
   g.ld = ld_logits;
   g.vocab = vocab;
   g.scale = scale;
+  g.rate = fminf(scale * kLog2e, FLT_MAX);  // (0 times it stays 0)
   g.top_k = top_k;
   g.splits = splits_of(rows, vocab);
   g.span = ((vocab + g.splits - 1) / g.splits + 7) / 8 * 8;

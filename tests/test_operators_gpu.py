@@ -510,6 +510,67 @@ def test_token_logprobs_past_32_bits(iso):
     assert 0 < d[rows - 1, vocab - 1].item() < 1e-3
 
 
+# Large finite logits under a scale that rounds the products: masks written as a number.
+
+MASK_SCALES = [1.0, 0.7, 0.9, 1.25, 1 / 1.3]
+
+
+def masked_rows(vocab, dtype):
+    """Rows with large finite values on some columns, on all but one and on all, where
+    whole threads, waves and splits hold nothing else."""
+    g = gen(vocab)
+    low = torch.finfo(dtype).min
+    rows = []
+    for fill in (-1e4, -1e9, -1e10, -1e30, low, 1e10):
+        normal = randn(g, vocab, std=3.0, dtype=dtype)
+        some = torch.full((vocab,), fill, dtype=dtype)
+        some[torch.randperm(vocab, generator=g)[:50]] = normal[:50]
+        one = torch.full((vocab,), fill, dtype=dtype)
+        one[vocab // 3] = 2.5
+        half = normal.clone()
+        half[:vocab // 2] = fill
+        rows += [some, one, half, torch.full((vocab,), fill, dtype=dtype)]
+    mixed = torch.full((vocab,), low, dtype=dtype)
+    mixed[::3], mixed[1::3] = -math.inf, -1e10
+    rows += [mixed, torch.where(torch.arange(vocab) == vocab - 1, low, -math.inf).to(dtype)]
+    return torch.stack(rows)
+
+
+def as_float32(t):
+    """float64 values that float32 rounds to infinity are infinite."""
+    return torch.where(t.float().isinf(), t.float().double(), t)
+
+
+def masked_reference(host, targets, scale, top):
+    """float64 results and their bounds.  A term e^d, d = scale (x - max), is off by
+    (4 |d| + 2) u of itself, where |d| e^d < 0.37, so the sum's logarithm is off by 4 u for
+    each of the terms that follow each other; a log probability is d less that logarithm,
+    off by 4 u |d| more, and the log-sum-exp is rounded once."""
+    z, lse, logp, p, h, lp, index = logprob_reference(host, targets, scale, top)
+    vocab = host.shape[1]
+    n = vocab / 1024 + 40
+    logs = (n * 4 + 2 * math.log(vocab + 1)) * U32
+    near = lambda t: logs + 4 * U32 * torch.nan_to_num(t, 0, 0, 0).abs()  # noqa: E731
+    near_h = n * U32 * (2 + math.log(vocab) + h) * 2
+    return (z, lse, logp, p, h, lp, index), (near(lse), near_h, near(lp), near(logp))
+
+
+@pytest.mark.parametrize("vocab,top", [(130, 9), (1111, 32), (32000, 5), (33000, 6), (200000, 8)])
+@pytest.mark.parametrize("scale", MASK_SCALES)
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_token_logprobs_large_finite_masks(iso, vocab, top, scale, dtype):
+    host = masked_rows(vocab, dtype)
+    for column in (vocab // 3, vocab - 1):
+        targets = torch.full((len(host),), column)
+        (z, lse, logp, p, h, lp, index), (near_lse, near_h, near_lp, near_logp) = masked_reference(host, targets, scale, top)
+        r = iso.token_logprobs(host.cuda(), targets.cuda(), scale=scale, top_k=top)
+        within(r.lse, as_float32(lse), near_lse)
+        within(r.entropy, h, near_h)
+        within(r.logprob, as_float32(lp), near_lp)
+        assert torch.equal(r.top_index.cpu(), index)
+        within(r.top_logprob, as_float32(logp.gather(1, index)), near_logp.gather(1, index))
+
+
 # --------------------------------------------------------------------------
 # Gated feed-forward block
 # --------------------------------------------------------------------------
