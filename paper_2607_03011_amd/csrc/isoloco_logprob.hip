@@ -36,9 +36,12 @@ __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f
 // 2^t is 0 from here on down: a product with it takes this for t (which may be -infinity)
 constexpr float kNothing = -200.f;
 
+// scale log2 e, finite: 0 times it stays 0
+__host__ __device__ inline float rate_of(float scale) { return fminf(scale * kLog2e, FLT_MAX); }
+
 // The softmax of some of a row's logits: their maximum m, and s and w as above against it
 // ({-infinity, 0, 0} of nothing; a NaN or +infinity among them leaves a NaN in s).
-// `rate` is scale log2 e.
+// `rate` is rate_of(scale).
 struct Soft {
   float m, s, w;
   __device__ __forceinline__ void raise(float to, float rate) {
@@ -93,6 +96,21 @@ __device__ __forceinline__ void unpack(u32x4 v, float* x) {
   }
 }
 
+template <typename T>
+__device__ __forceinline__ u32x4 pack(const float* x) {
+  u32x4 v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 2) {
+      typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+      v[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((floatx2){x[2 * i], x[2 * i + 1]}, bf16x2_t));
+    } else {
+      v[i] = __float_as_uint(x[i]);
+    }
+  }
+  return v;
+}
+
 constexpr int kMaxSplits = 64;
 
 struct RowOut {
@@ -105,7 +123,7 @@ struct RowOut {
 
 struct RowArgs {
   int64_t ld, vocab;
-  float scale, rate;  // rate: scale log2 e
+  float scale, rate;
   int top_k;
   int splits;      // workgroups per row
   int64_t span;    // a split's columns (a multiple of a vector's)
@@ -363,6 +381,77 @@ struct GradIn {
 constexpr int kGradThreads = 256;
 constexpr int kGradVecs = 4;  // 16-byte vectors of a thread
 
+// p is formed from the lse, a float32: off by 2^-24 |lse| of itself, and for masks written
+// as a large number all of it.  From here on a row's maximum and sum are formed again: in
+// float32 where p would be off by 2^-16, in bfloat16 by 2^-11, a quarter of the result's
+// rounding.  (Rows of 32000, above and below the line: 8192 in bfloat16 628 and 181 us, 4096
+// in float32 610 and 185: three readings instead of one.)
+template <typename T>
+constexpr float kSureLse = sizeof(T) == 2 ? 8192.f : 256.f;
+
+// The row's gradient without its lse: its maximum and sum against that, then the gradient,
+// by one workgroup (in place, nobody else may read the row).  grad(log p, column).
+template <typename T, typename Grad>
+__device__ __forceinline__ void grad_of_row(const T* row, T* out, int64_t vocab, float scale, const Grad& grad) {
+  constexpr int N = Vec<T>::N, kWaves = kGradThreads / 64, kAtOnce = 4;
+  __shared__ float most_of[kWaves], sum_of[kWaves];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t whole = vocab / N, rest = whole * N + threadIdx.x;
+  // take(logits, first column) of the thread's vectors
+  const auto vectors = [&](const auto& take) {
+    for (int64_t base = threadIdx.x; base < whole; base += kAtOnce * kGradThreads) {
+      u32x4 v[kAtOnce];
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u) {
+        const int64_t i = base + u * kGradThreads;
+        if (i < whole) v[u] = *reinterpret_cast<const u32x4_any*>(row + i * N);
+      }
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u) {
+        const int64_t i = base + u * kGradThreads;
+        float x[N];
+        unpack<T>(v[u], x);
+        if (i < whole) take(x, i * N);
+      }
+    }
+  };
+  float m = rest < vocab ? (float)row[rest] : -INFINITY, s = 0.f;
+  vectors([&](const float* x, int64_t) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) m = fmaxf(m, x[e]);
+  });
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
+  if (lane == 0) most_of[wave] = m;
+  __syncthreads();
+  for (int w = 0; w < kWaves; ++w) m = fmaxf(m, most_of[w]);
+  const bool empty = m == -INFINITY;
+  if (!empty) {
+    const float rate = rate_of(scale);
+    const auto term = [&](float x) { return __builtin_amdgcn_exp2f((x - m) * rate); };
+    if (rest < vocab) s = term((float)row[rest]);
+    vectors([&](const float* x, int64_t) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) s += term(x[e]);
+    });
+  }
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) s += __shfl_xor(s, off, 64);
+  if (lane == 0) sum_of[wave] = s;
+  __syncthreads();
+  s = 0.f;
+  for (int w = 0; w < kWaves; ++w) s += sum_of[w];
+  const float log_s = logf(s);
+  const auto grad_of = [&](float x, int64_t i) { return empty ? 0.f : grad((x - m) * scale - log_s, i); };
+  vectors([&](const float* x, int64_t i) {
+    float d[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) d[e] = grad_of(x[e], i + e);
+    *reinterpret_cast<u32x4_any*>(out + i) = pack<T>(d);
+  });
+  if (rest < vocab) out[rest] = (T)grad_of((float)row[rest], rest);
+}
+
 // One workgroup per row and span of kGradThreads * kGradVecs vectors.  PAST: the result
 // goes past the caches.
 template <typename T, typename ID, bool PAST>
@@ -380,14 +469,20 @@ __global__ void __launch_bounds__(kGradThreads) logprob_grad_kernel(const T* log
   const float dl = given ? in.dlogprob[r] : 0.f;
   const float de = in.dentropy ? in.dentropy[r] : 0.f, h = in.dentropy ? in.entropy[r] : 0.f;
   // nothing to hand back: the row's logits are not read
-  const bool none = lse == -INFINITY || (dl == 0.f && de == 0.f);
-  const auto grad = [&](float x, int64_t i) {
-    const float lp = fmaf(x, scale, -lse), p = exp_of(lp);
+  const bool none = dl == 0.f && de == 0.f;
+  const auto grad_at = [&](float lp, int64_t i) {
+    const float p = exp_of(lp);
     float d = (i == t ? 1.f : 0.f) - p;
     d *= dl;
     if (p > 0.f) d -= de * (p * (lp + h));
     return d * scale;
   };
+  if (!none && fabsf(lse) >= kSureLse<T>) {
+    // one of the row's workgroups, another one from row to row: their XCDs take turns
+    if ((int)(blockIdx.x % spans) == (int)(r % spans)) grad_of_row(row, out, vocab, scale, grad_at);
+    return;
+  }
+  const auto grad = [&](float x, int64_t i) { return grad_at(fmaf(x, scale, -lse), i); };
   const int64_t whole = vocab / N;
 #pragma unroll
   for (int u = 0; u < kGradVecs; ++u) {
@@ -399,15 +494,7 @@ __global__ void __launch_bounds__(kGradThreads) logprob_grad_kernel(const T* log
       unpack<T>(v, x);
 #pragma unroll
       for (int e = 0; e < N; ++e) x[e] = none ? 0.f : grad(x[e], i * N + e);
-      if constexpr (sizeof(T) == 2) {
-        typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          v[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector((floatx2){x[2 * e], x[2 * e + 1]}, bf16x2_t));
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = __float_as_uint(x[e]);
-      }
+      v = pack<T>(x);
       u32x4_any* to = reinterpret_cast<u32x4_any*>(out + i * N);
       if constexpr (PAST) __builtin_nontemporal_store(v, to);
       else *to = v;
@@ -532,7 +619,7 @@ isoloco_status isoloco_token_logprobs(const void* logits, int64_t ld_logits, int
   g.ld = ld_logits;
   g.vocab = vocab;
   g.scale = scale;
-  g.rate = fminf(scale * kLog2e, FLT_MAX);  // (0 times it stays 0)
+  g.rate = rate_of(scale);
   g.top_k = top_k;
   g.splits = splits_of(rows, vocab);
   g.span = ((vocab + g.splits - 1) / g.splits + 7) / 8 * 8;

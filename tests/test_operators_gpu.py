@@ -571,6 +571,74 @@ def test_token_logprobs_large_finite_masks(iso, vocab, top, scale, dtype):
         within(r.top_logprob, as_float32(logp.gather(1, index)), near_logp.gather(1, index))
 
 
+# |lse| up to which its rounding to float32 may show in the gradient (2^-24 |lse| of p)
+SURE_LSE = {F32: 256.0, BF16: 8192.0}
+
+
+def large_lse_reference(host, targets, scale, dl, de):
+    """float64 gradient and its bound.  p = e^q with q = log p is off by (6 |q| + 2) u of itself
+    for q's own roundings and the exponential, 4 u for each term that follows another in the
+    sum, and lse's rounding up to SURE_LSE; the entropy that is handed back has its own error."""
+    dtype = host.dtype
+    (z, lse, logp, p, h, lp, index), (_, near_h, _, _) = masked_reference(host, targets, scale, 1)
+    want, _ = logprob_grad_reference(host, targets, scale, dl, de, dtype)
+    n = host.shape[1] / 1024 + 40
+    q = torch.nan_to_num(logp, 0, 0, 0).abs().clamp(max=150)
+    near_q = U32 * (6 * q + 4 * n + 64 + 2 * torch.nan_to_num(lse, 0, SURE_LSE[dtype], 0).abs().clamp(max=SURE_LSE[dtype])[:, None])
+    ok = (targets >= 0) & (targets < host.shape[1])
+    one = torch.zeros_like(p)
+    one[ok.nonzero()[:, 0], targets[ok].long()] = 1.0
+    dl, de = torch.where(ok, dl.double(), 0.0).abs()[:, None], de.double().abs()[:, None]
+    lph = torch.where(p > 0, (logp + h[:, None]).abs(), torch.zeros_like(p))
+    part = p * dl * (near_q + 4 * U32) + one * dl * 4 * U32 + de * p * (lph * (near_q + 4 * U32) + near_q + near_h[:, None])
+    return want, scale * torch.nan_to_num(part, 0, 0, 0) * 1.01 + ROUND[dtype] * torch.nan_to_num(want, 0, 0, 0).abs() + 1e-37
+
+
+@pytest.mark.parametrize("vocab", [3, 130, 1111, 33000])
+@pytest.mark.parametrize("scale", MASK_SCALES)
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_token_logprobs_backward_large_lse(iso, vocab, scale, dtype):
+    """Rows whose log-sum-exp is so large that its rounding hides the sum."""
+    g = gen(vocab + 7)
+    shifts = torch.tensor([-1e6, -5e4, -3000.0, -500.0, -90.0, 90.0, 500.0, 3000.0, 5e4, 1e6, 1e20, 3e38])
+    # (bfloat16 rounds the larger ones together: rows of a few distinct values)
+    shifted = (randn(g, len(shifts), vocab, std=3.0) + shifts[:, None]).to(dtype)
+    host = torch.cat([shifted] + ([masked_rows(vocab, dtype)] if vocab > 50 else []) + [odd_rows(vocab, dtype)])
+    rows = len(host)
+    targets = torch.randint(0, vocab, (rows,), generator=g)
+    targets[::5] = -1
+    dl, de = randn(g, rows), randn(g, rows, std=0.1)
+    de[::3] = 0.0
+    for pad in (None, 3):
+        dev = host.cuda() if pad is None else strided(host, pad)
+        r = iso.token_logprobs(dev, targets.cuda(), scale=scale)
+        got = iso.token_logprobs_backward(dev, targets.cuda(), r.lse, dl.cuda(), entropy=r.entropy, dentropy=de.cuda(),
+                                          scale=scale)
+        within(got, *large_lse_reference(host, targets, scale, dl, de))
+        again = iso.token_logprobs_backward(dev, targets.cuda(), r.lse, dl.cuda(), entropy=r.entropy,
+                                            dentropy=de.cuda(), scale=scale, out=dev)
+        assert again is dev and torch.equal(got.view(torch.uint8), again.contiguous().view(torch.uint8))
+
+
+def test_token_logprobs_backward_large_lse_of_large_results(iso):
+    """The same where the result is stored past the caches: the bits of calls of few rows."""
+    rows, vocab = 4200, 32003
+    t = torch.randn(rows, vocab, device="cuda")
+    t[::7] += 5e4
+    t[3::7] = -1e10
+    t = t.to(BF16)
+    targets = torch.arange(rows, device="cuda") * 7 % vocab
+    w = torch.randn(2, rows, device="cuda")
+    r = iso.token_logprobs(t, targets, scale=0.7)
+    d = iso.token_logprobs_backward(t, targets, r.lse, w[0], entropy=r.entropy, dentropy=w[1], scale=0.7)
+    assert d.numel() * d.element_size() > 256 << 20 and torch.isfinite(d).all()
+    for a in range(0, rows, 500):
+        b = min(rows, a + 500)
+        part = iso.token_logprobs_backward(t[a:b], targets[a:b], r.lse[a:b], w[0, a:b], entropy=r.entropy[a:b],
+                                           dentropy=w[1, a:b], scale=0.7)
+        assert torch.equal(d[a:b], part)
+
+
 # --------------------------------------------------------------------------
 # Gated feed-forward block
 # --------------------------------------------------------------------------
