@@ -21,45 +21,9 @@ sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 import paper_2607_03011_amd as iso  # noqa: E402
 
 
-class Embedding(torch.autograd.Function):
-    @staticmethod
-    def forward(ctx, table, ids, scale):
-        ctx.save_for_backward(ids)
-        ctx.vocab, ctx.scale = table.shape[0], scale
-        return iso.embedding(table, ids, scale=scale, out_dtype=torch.bfloat16)
-
-    @staticmethod
-    def backward(ctx, dout):
-        ids, = ctx.saved_tensors
-        return iso.embedding_backward(ids, dout.contiguous(), ctx.vocab, scale=ctx.scale), None, None
-
-
-class GatedFFN(torch.autograd.Function):
-    @staticmethod
-    def forward(ctx, x, w_gate, w_up):
-        ctx.save_for_backward(x, w_gate, w_up)
-        return iso.gated_ffn(x, w_gate, w_up)
-
-    @staticmethod
-    def backward(ctx, dout):
-        return iso.gated_ffn_backward(*ctx.saved_tensors, dout.contiguous())
-
-
-class TokenLoss(torch.autograd.Function):
+def token_loss(logits, targets):
     """The mean of -log p(target); targets of -1 are ignored."""
-
-    @staticmethod
-    def forward(ctx, logits, targets):
-        r = iso.token_logprobs(logits, targets)
-        count = (targets >= 0).sum().clamp(min=1)
-        ctx.save_for_backward(logits, targets, r.lse, count)
-        return -r.logprob.sum() / count
-
-    @staticmethod
-    def backward(ctx, grad):
-        logits, targets, lse, count = ctx.saved_tensors
-        dlogprob = (-grad / count).expand(targets.shape).contiguous()
-        return iso.token_logprobs_backward(logits, targets, lse, dlogprob), None
+    return -iso.token_logprobs(logits, targets).logprob.sum() / (targets >= 0).sum().clamp(min=1)
 
 
 class Model:
@@ -88,10 +52,10 @@ class Model:
 
     def logits(self, params, ids):
         table = params[0]
-        h = Embedding.apply(table, ids, self.scale)
+        h = iso.embedding(table, ids, scale=self.scale, out_dtype=torch.bfloat16)
         for gain, w_gate, w_up, w_down in zip(*[iter(params[1:])] * 4):
             x = torch.nn.functional.rms_norm(h.float(), gain.shape, gain).bfloat16()
-            h = h + GatedFFN.apply(x, w_gate.bfloat16(), w_up.bfloat16()) @ w_down.bfloat16().T
+            h = h + iso.gated_ffn(x, w_gate.bfloat16(), w_up.bfloat16()) @ w_down.bfloat16().T
         return h @ table.bfloat16().T
 
 
@@ -160,7 +124,7 @@ def main(argv=None):
                 for p in params[k]:
                     p.grad.zero_()
                 ids, targets = source.batch(a.tokens, g)
-                TokenLoss.apply(model.logits(params[k], ids), targets).backward()
+                token_loss(model.logits(params[k], ids), targets).backward()
                 norm = iso.clip_grads([p.grad for p in params[k]], a.max_norm)
                 optimizers[k].step()
             print("round %d, worker %d: gradient norm %.3f, scaled by %.3f" % (r, k, *norm.tolist()), flush=True)

@@ -9,6 +9,10 @@ have to be.  Matrices
 need unit stride along a row; a further leading dimension is allowed where the
 rows stay evenly spaced.  Arguments that the library itself refuses raise
 ``IsoLoCoError``.
+
+``embedding``, ``token_logprobs`` and ``gated_ffn`` are differentiable: where an
+operand requires a gradient, the result carries the function that forms it (once:
+there is no second derivative).  ``out`` is refused then, as torch's functions do.
 """
 import array
 import ctypes
@@ -16,6 +20,7 @@ import functools
 from typing import NamedTuple, Optional
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import (ISOLOCO_ACT_GELU, ISOLOCO_ACT_SILU, ISOLOCO_BF16, ISOLOCO_F32, ISOLOCO_FFN_ALIGNED,
                ISOLOCO_FFN_BACKWARD, ISOLOCO_I32, ISOLOCO_I64, IsoLoCoError, _check, _lib)
@@ -213,6 +218,15 @@ def _output(name, t, shape, dtype):
     return t
 
 
+def _recorded(out):
+    """Whether a call with an operand that requires a gradient is recorded for one."""
+    if not torch.is_grad_enabled():
+        return False
+    if out is not None:
+        raise ValueError("a result written to out carries no gradient, and an operand requires one")
+    return True
+
+
 @_with_stream
 def clip_grads(grads, max_norm, out=None, workspace=None):
     """Scale the tensors of ``grads`` (contiguous, float32 or bfloat16 each) so that
@@ -250,6 +264,8 @@ def clip_grads(grads, max_norm, out=None, workspace=None):
 def embedding(table, ids, scale=1.0, out=None, out_dtype=None):
     """``scale * table[ids]`` in ``out_dtype`` (default: the table's); ids outside the
     table give rows of zeros."""
+    if table.requires_grad and _recorded(out):
+        return _Embedding.apply(table, ids, scale, out_dtype)
     if table.dim() != 2:
         raise ValueError("table must be a matrix")
     index = _place(table)
@@ -296,9 +312,24 @@ def embedding_backward(ids, dout, vocab, scale=1.0, out=None, accumulate=False, 
     return out
 
 
+class _Embedding(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, table, ids, scale, out_dtype):
+        ctx.save_for_backward(ids)
+        ctx.vocab, ctx.scale, ctx.dtype = table.shape[0], scale, table.dtype
+        return embedding(table, ids, scale, out_dtype=out_dtype)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dout):
+        ids, = ctx.saved_tensors
+        return embedding_backward(ids, dout.contiguous(), ctx.vocab, ctx.scale, out_dtype=ctx.dtype), None, None, None
+
+
 class TokenLogProbs(NamedTuple):
     """What ``token_logprobs`` returns, with the logits' leading shape; the last two
-    have one more dimension of ``top_k`` and are None without it."""
+    have one more dimension of ``top_k`` and are None without it.  ``logprob`` and
+    ``entropy`` hand gradients back."""
     logprob: Optional[torch.Tensor]
     entropy: torch.Tensor
     lse: torch.Tensor
@@ -312,6 +343,8 @@ def token_logprobs(logits, targets=None, scale=1.0, top_k=0, workspace=None):
     dimension, with the rows' entropy and log-sum-exp and the ``top_k`` most likely
     tokens (int64, of equal ones the lower index first).  Targets outside the
     vocabulary are ignored (0)."""
+    if logits.requires_grad and _recorded(None):
+        return TokenLogProbs(*_TokenLogProbs.apply(logits, targets, scale, top_k, workspace))
     index = _place(logits)
     dtype = _type("logits", logits)
     rows, ld = _rows("logits", logits)
@@ -372,6 +405,33 @@ def token_logprobs_backward(logits, targets, lse, dlogprob, entropy=None, dentro
     return out
 
 
+class _TokenLogProbs(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, targets, scale, top_k, workspace):
+        r = token_logprobs(logits, targets, scale, top_k, workspace)
+        ctx.save_for_backward(logits, targets, r.lse, r.entropy)
+        ctx.scale = scale
+        ctx.set_materialize_grads(False)
+        if top_k:
+            ctx.mark_non_differentiable(r.top_index)
+        return tuple(r)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dlogprob, dentropy, dlse, dtop, _):
+        if dlse is not None or dtop is not None:
+            raise NotImplementedError("lse and top_logprob have no gradient: detach them")
+        logits, targets, lse, entropy = ctx.saved_tensors
+        if dlogprob is None:
+            targets = None
+        else:
+            dlogprob = dlogprob.contiguous()
+        if dentropy is not None:
+            dentropy = dentropy.contiguous()
+        d = token_logprobs_backward(logits, targets, lse, dlogprob, entropy, dentropy, ctx.scale)
+        return d, None, None, None, None
+
+
 def _ffn_operands(x, w_gate, w_up, act):
     index = _place(x)
     _same_device(index, w_gate, w_up)
@@ -397,6 +457,8 @@ def _ffn_operands(x, w_gate, w_up, act):
 def gated_ffn(x, w_gate, w_up, act="silu", out=None, workspace=None):
     """``act(x w_gate^T) * (x w_up^T)`` for x [..., dim] and weights [hidden, dim]; act
     is "silu" or "gelu"."""
+    if (x.requires_grad or w_gate.requires_grad or w_up.requires_grad) and _recorded(out):
+        return _GatedFfn.apply(x, w_gate, w_up, act, workspace)
     index, dtype, tokens, dim, hidden, ld_x, ld_w, a, at, flags = _ffn_operands(x, w_gate, w_up, act)
     if out is None:
         out = _empty(*x.shape[:-1], hidden, dtype=x.dtype, device=x.device)
@@ -436,3 +498,18 @@ def gated_ffn_backward(x, w_gate, w_up, dout, act="silu", need_dx=True, need_dw=
                                            _raw_stream(index)),
            "isoloco_gated_ffn_backward")
     return dx, dwg, dwu
+
+
+class _GatedFfn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w_gate, w_up, act, workspace):
+        ctx.save_for_backward(x, w_gate, w_up)
+        ctx.act = act
+        return gated_ffn(x, w_gate, w_up, act, workspace=workspace)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dout):
+        need_x, need_gate, need_up = ctx.needs_input_grad[:3]
+        dx, dwg, dwu = gated_ffn_backward(*ctx.saved_tensors, dout.contiguous(), ctx.act, need_x, need_gate or need_up)
+        return dx, dwg if need_gate else None, dwu if need_up else None, None, None

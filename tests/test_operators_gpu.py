@@ -870,6 +870,82 @@ def test_graph_replays(iso, tokens):
 
 
 # --------------------------------------------------------------------------
+# Autograd
+# --------------------------------------------------------------------------
+
+def wanted(t):
+    return t.detach().clone().requires_grad_()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_autograd_reaches_every_operand(iso, dtype):
+    """The gradients are those of the functions that form them, given what a chain of the
+    operators hands back; without a wish for one nothing is attached."""
+    s = _state(dtype)
+    table, wg, wu = (wanted(s[k]) for k in ("table", "wg", "wu"))
+    x = iso.embedding(table, s["ids"], scale=2.0)
+    h = iso.gated_ffn(x, wg, wu, act="gelu")
+    r = iso.token_logprobs(h, s["targets"], scale=0.8, top_k=2)
+    (r.logprob * s["dl"] + 0.25 * r.entropy).sum().backward()
+    x0 = iso.embedding(s["table"], s["ids"], scale=2.0)
+    h0 = iso.gated_ffn(x0, s["wg"], s["wu"], act="gelu")
+    r0 = iso.token_logprobs(h0, s["targets"], scale=0.8, top_k=2)
+    assert not x0.requires_grad and not h0.requires_grad and not r0.logprob.requires_grad
+    assert torch.equal(x, x0) and torch.equal(h, h0) and all(torch.equal(a, b) for a, b in zip(r, r0))
+    dh = iso.token_logprobs_backward(h0, s["targets"], r0.lse, s["dl"], entropy=r0.entropy,
+                                     dentropy=torch.full_like(s["dl"], 0.25), scale=0.8)
+    dx, dwg, dwu = iso.gated_ffn_backward(x0, s["wg"], s["wu"], dh, act="gelu")
+    dt = iso.embedding_backward(s["ids"], dx, 400, scale=2.0, out_dtype=dtype)
+    assert torch.equal(wg.grad, dwg) and torch.equal(wu.grad, dwu) and torch.equal(table.grad, dt)
+
+
+def test_autograd_of_some_operands(iso):
+    """One operand alone; results nobody uses; gradients that arrive expanded or strided;
+    leading shapes; no targets."""
+    s = _state(F32, 24)
+    x0 = iso.embedding(s["table"], s["ids"]).view(2, 3, 4, 136)
+    w = torch.randn(2, 3, 520, 4, device="cuda").transpose(-1, -2)
+    for which in range(3):
+        ts = [x0.clone(), s["wg"].clone(), s["wu"].clone()]
+        ts[which].requires_grad_()
+        iso.gated_ffn(*ts).backward(w)
+        want = iso.gated_ffn_backward(x0, s["wg"], s["wu"], w.contiguous())[which]
+        assert torch.equal(ts[which].grad, want) and all(ts[i].grad is None for i in range(3) if i != which)
+    x = wanted(x0)
+    iso.gated_ffn(x, s["wg"], s["wu"]).sum().backward()
+    assert torch.equal(x.grad, iso.gated_ffn_backward(x0, s["wg"], s["wu"], torch.ones(2, 3, 4, 520, device="cuda"))[0])
+    z = wanted(torch.randn(2, 3, 50, device="cuda"))
+    r = iso.token_logprobs(z)
+    r.entropy.mean().backward()
+    want = iso.token_logprobs_backward(z.detach(), None, r.lse.detach(), None, entropy=r.entropy.detach(),
+                                       dentropy=torch.full((2, 3), 1 / 6, device="cuda"))
+    assert torch.equal(z.grad, want)
+    # a float32 table looked up in bfloat16: the gradient has the table's type
+    table = wanted(s["table"])
+    iso.embedding(table, s["ids"], out_dtype=BF16).float().sum().backward()
+    assert table.grad.dtype == F32 and table.grad.sum().item() == 136 * ((s["ids"] >= 0) & (s["ids"] < 400)).sum().item()
+
+
+def test_autograd_does_not_drop_what_it_lacks(iso):
+    """The log-sum-exp and the alternatives hand back no gradient, and say so; results
+    written into a given tensor carry none."""
+    z = wanted(torch.randn(4, 50, device="cuda"))
+    t = torch.zeros(4, dtype=torch.int64, device="cuda")
+    for pick in (lambda r: r.lse, lambda r: r.top_logprob, lambda r: r.logprob[:, None] + r.top_logprob):
+        with pytest.raises(NotImplementedError):
+            pick(iso.token_logprobs(z, t, top_k=2)).sum().backward()
+    assert z.grad is None
+    w = wanted(torch.randn(6, 50, device="cuda"))
+    with pytest.raises(ValueError):
+        iso.gated_ffn(z, w, w, out=torch.empty(4, 6, device="cuda"))
+    with pytest.raises(ValueError):
+        iso.embedding(w, t, out=torch.empty(4, 50, device="cuda"))
+    with torch.no_grad():
+        out = torch.empty(4, 6, device="cuda")
+        assert iso.gated_ffn(z, w, w, out=out) is out and not out.requires_grad
+
+
+# --------------------------------------------------------------------------
 # Results larger than the caches, which are stored past them
 # --------------------------------------------------------------------------
 
