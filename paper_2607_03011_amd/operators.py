@@ -218,6 +218,10 @@ def _output(name, t, shape, dtype):
     return t
 
 
+# raises tensors' version counters, by which autograd finds that one it kept has changed
+_written = torch.autograd.graph.increment_version
+
+
 def _recorded(out):
     """Whether a call with an operand that requires a gradient is recorded for one."""
     if not torch.is_grad_enabled():
@@ -243,9 +247,9 @@ def clip_grads(grads, max_norm, out=None, workspace=None):
     if not all([g.is_contiguous() and g.get_device() == index for g in grads]):
         raise ValueError("gradients must be contiguous and on one device")
     src = [g.data_ptr() for g in grads]
-    dst = src
+    dst, results = src, grads
     if out is not None:
-        out = list(out)
+        results = out = list(out)
         if len(out) != len(grads):
             raise ValueError("out must have one tensor per gradient")
         if not all([o.shape == g.shape and o.dtype == g.dtype and o.is_contiguous() and o.get_device() == index
@@ -257,6 +261,7 @@ def clip_grads(grads, max_norm, out=None, workspace=None):
     norm = _empty(2, dtype=_F32, device=device)
     isoloco_clip_grads(src, dst, [g.numel() for g in grads], types, max_norm, norm.data_ptr(), ws, ws_bytes,
                        _raw_stream(index))
+    _written(results)
     return norm
 
 
@@ -279,6 +284,7 @@ def embedding(table, ids, scale=1.0, out=None, out_dtype=None):
     else:
         _output("out", out, (*ids.shape, dim), out_dtype or out.dtype)
         ld_out = _rows("out", out)[1]
+        _written(out)
     _check(_lib.isoloco_embedding(table.data_ptr(), ld, dtype, vocab, dim, ids.data_ptr(), id_type, n, scale,
                                   out.data_ptr(), ld_out, _type("out", out), _raw_stream(index)),
            "isoloco_embedding")
@@ -304,6 +310,7 @@ def embedding_backward(ids, dout, vocab, scale=1.0, out=None, accumulate=False, 
     else:
         _output("out", out, (vocab, dim), out_dtype or out.dtype)
         ld_out = _rows("out", out)[1]
+        _written(out)
     keep, ws, ws_bytes = _workspace(workspace, isoloco_embedding_backward_workspace_size(n, vocab, dim), dout.device)
     _check(_lib.isoloco_embedding_backward(ids.data_ptr(), id_type, n, dout.data_ptr(), ld, dtype, vocab, dim, scale, 1
                                            if accumulate else 0, out.data_ptr(), ld_out, _type("out", out), ws,
@@ -398,6 +405,7 @@ def token_logprobs_backward(logits, targets, lse, dlogprob, entropy=None, dentro
     else:
         _output("out", out, logits.shape, logits.dtype)
         ld_out = _rows("out", out)[1]
+        _written(out)
     _check(_lib.isoloco_token_logprobs_backward(logits.data_ptr(), ld, dtype, rows, vocab, target_at, t_type, scale,
                                                 _vector("lse", lse, rows), entropy_at, dlogprob_at, dentropy_at,
                                                 out.data_ptr(), ld_out, _raw_stream(index)),
@@ -467,6 +475,7 @@ def gated_ffn(x, w_gate, w_up, act="silu", out=None, workspace=None):
         _same_device(index, out)
         _output("out", out, (*x.shape[:-1], hidden), x.dtype)
         ld_out = _rows("out", out)[1]
+        _written(out)
     keep, ws, ws_bytes = _workspace(workspace, isoloco_gated_ffn_workspace_size(tokens, dim, hidden, dtype, flags),
                                     x.device)
     _check(_lib.isoloco_gated_ffn(at[0], ld_x, at[1], at[2], ld_w, dtype, tokens, dim, hidden, a, out.data_ptr(),

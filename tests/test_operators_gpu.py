@@ -945,6 +945,34 @@ def test_autograd_does_not_drop_what_it_lacks(iso):
         assert iso.gated_ffn(z, w, w, out=out) is out and not out.requires_grad
 
 
+@pytest.mark.parametrize("call", ["clip", "clip out", "embedding", "embedding gradient", "logits' gradient", "ffn"])
+def test_autograd_sees_what_is_written(iso, call):
+    """A tensor that was saved for a backward pass and is then written by an operator is
+    found out."""
+    a = torch.ones(8, 8, device="cuda")
+    x = wanted(a)
+    kept = torch.ones(8, 8, device="cuda")
+    y = (x * kept).sum()
+    version = kept._version
+    ids = torch.arange(8, device="cuda")
+    v = torch.ones(8, device="cuda")
+    if call == "clip":
+        iso.clip_grads([a, kept], 1.0)
+    elif call == "clip out":
+        iso.clip_grads([a], 1.0, out=[kept])
+    elif call == "embedding":
+        iso.embedding(a, ids, out=kept)
+    elif call == "embedding gradient":
+        iso.embedding_backward(ids, a, 8, out=kept, accumulate=True)
+    elif call == "logits' gradient":
+        iso.token_logprobs_backward(a, ids, v, v, out=kept)
+    else:
+        iso.gated_ffn(a, a, a, out=kept)
+    assert kept._version == version + 1
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
+
+
 # --------------------------------------------------------------------------
 # Results larger than the caches, which are stored past them
 # --------------------------------------------------------------------------
