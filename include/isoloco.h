@@ -448,8 +448,8 @@ typedef enum {
  *
  * The workspace's size goes by the call: ISOLOCO_FFN_BACKWARD for the gradient,
  * ISOLOCO_FFN_ALIGNED where the rows of x and of both weights will be 16-byte
- * aligned in bfloat16 (ld a multiple of 8), which saves their copies.  Extents
- * below 2^22. */
+ * aligned in bfloat16 (ld a multiple of 8) and at most 2^22 elements apart, which
+ * saves their copies.  Extents are at most 2^22 - 64. */
 #define ISOLOCO_FFN_BACKWARD 1
 #define ISOLOCO_FFN_ALIGNED 2
 

@@ -27,6 +27,7 @@ from . import (ISOLOCO_ACT_GELU, ISOLOCO_ACT_SILU, ISOLOCO_BF16, ISOLOCO_F32, IS
 
 _DTYPE = {torch.float32: ISOLOCO_F32, torch.bfloat16: ISOLOCO_BF16}
 _INDEX = {torch.int32: ISOLOCO_I32, torch.int64: ISOLOCO_I64}
+_FFN_LD = 1 << 22  # rows further apart are copied
 _ACT = {"silu": ISOLOCO_ACT_SILU, "gelu": ISOLOCO_ACT_GELU}
 
 
@@ -457,7 +458,7 @@ def _ffn_operands(x, w_gate, w_up, act):
     if a is None:
         raise ValueError("act must be one of %s" % ", ".join(sorted(_ACT)))
     at = x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr()
-    aligned = not ((ld_x | ld_w) & 7 or (at[0] | at[1] | at[2]) & 15)
+    aligned = not ((ld_x | ld_w) & 7 or (at[0] | at[1] | at[2]) & 15) and ld_x <= _FFN_LD and ld_w <= _FFN_LD
     return index, dtype, tokens, dim, hidden, ld_x, ld_w, a, at, ISOLOCO_FFN_ALIGNED if aligned else 0
 
 

@@ -753,6 +753,22 @@ def test_gated_ffn_tiles(iso, tokens, dim, hidden):
         assert ((r.cuda().double() - w).norm() / w.norm()).item() <= 2.0 ** -8
 
 
+@pytest.mark.parametrize("far", ["x", "weights"])
+def test_gated_ffn_rows_far_apart(iso, far):
+    """Operands that are columns of a matrix of more than 2^22: past the tiles' offsets."""
+    tokens, dim, hidden, apart = 40, 24, 16, (1 << 22) + 8
+    x, wg, wu, dh = ffn_inputs(tokens, dim, hidden, BF16, 2)
+    want = iso.gated_ffn(x.cuda(), wg.cuda(), wu.cuda())
+    grads = iso.gated_ffn_backward(x.cuda(), wg.cuda(), wu.cuda(), dh.cuda())
+    if far == "x":
+        ops = [strided(x, apart - dim), wg.cuda(), wu.cuda()]
+    else:
+        ops = [x.cuda(), strided(wg, apart - dim), strided(wu, apart - dim)]
+    assert torch.equal(iso.gated_ffn(*ops), want)
+    for a, b in zip(iso.gated_ffn_backward(*ops, dh.cuda()), grads):
+        assert torch.equal(a, b)
+
+
 def test_gated_ffn_no_tokens(iso):
     w = torch.ones(6, 4, device="cuda")
     x = torch.empty(0, 4, device="cuda")
