@@ -373,7 +373,10 @@ typedef enum { ISOLOCO_I32 = 0, ISOLOCO_I64 = 1 } isoloco_index_type;
  * nothing is then written where coef is 1); a tensor's result must not overlap
  * another tensor.  dst = NULL: the norm only.  norm: two device floats, which
  * receive norm and coef.  A norm that is infinite or NaN leaves the gradients
- * as they are, and tells the caller so.  Squares are summed in 64 bits.
+ * as they are, and tells the caller so.  Squares are summed in 64 bits: a norm
+ * past float32's range is stored as infinity, with the coef that was applied
+ * (less than 1).  coef is applied with all of its bits, also where the float
+ * that is stored has lost some (below 2^-126).
  * max_norm >= 0 (infinity: never clip). */
 isoloco_status isoloco_clip_workspace_size(int32_t n_tensors, size_t* bytes);
 isoloco_status isoloco_clip_grads(const void* const* src, void* const* dst, const int64_t* counts,

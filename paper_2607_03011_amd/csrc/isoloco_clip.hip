@@ -8,6 +8,7 @@
 // scaling reads and writes it.
 #include <hip/hip_runtime.h>
 
+#include <float.h>
 #include <math.h>
 #include <stdint.h>
 
@@ -118,56 +119,68 @@ __global__ void __launch_bounds__(kClipThreads) clip_norm_kernel(ClipArgs a, dou
   if (threadIdx.x == 0) part[blockIdx.x] = s;
 }
 
+// A coefficient as two factors, taken one after the other: below 2^-126 it has fewer
+// bits in float32, or none, while its product with a large gradient has them all.  (The
+// first of them is 2^-126 there and 1 otherwise; what it takes from a value the product
+// has no place for either.)
+struct Coef {
+  float pre, c;
+  __device__ __forceinline__ float of(float x) const { return x * pre * c; }
+};
+
 // The norm and the coefficient from the n partial sums of every launch, on every
 // thread of a workgroup.
 template <int WAVES>
-__device__ __forceinline__ floatx2 norm_and_coef(const double* part, int n, float max_norm, double* lds) {
+__device__ __forceinline__ floatx2 norm_and_coef(const double* part, int n, float max_norm, double* lds, Coef& k) {
   double s = 0.0;
   for (int i = threadIdx.x; i < n; i += WAVES * 64) s += part[i];
   s = block_sum<WAVES>(s, lds);
   if (threadIdx.x == 0) lds[0] = s;
   __syncthreads();
   const double norm = sqrt(lds[0]);
-  const float coef = norm > (double)max_norm && norm < (double)INFINITY ? (float)((double)max_norm / norm) : 1.f;
-  return (floatx2){(float)norm, coef};
+  const double coef = norm > (double)max_norm && norm < (double)INFINITY ? (double)max_norm / norm : 1.0;
+  const bool small = coef < (double)FLT_MIN;
+  k = {small ? FLT_MIN : 1.f, (float)(small ? coef / (double)FLT_MIN : coef)};
+  return (floatx2){(float)norm, (float)coef};
 }
 
 __global__ void __launch_bounds__(256) clip_finish_kernel(const double* part, int n, float max_norm, float* out) {
   __shared__ double lds[4];
-  const floatx2 r = norm_and_coef<4>(part, n, max_norm, lds);
+  Coef k;
+  const floatx2 r = norm_and_coef<4>(part, n, max_norm, lds, k);
   if (threadIdx.x == 0) {
     out[0] = r[0];
     out[1] = r[1];
   }
 }
 
-__device__ __forceinline__ uint32_t scale_pair(uint32_t v, float c) {
+__device__ __forceinline__ uint32_t scale_pair(uint32_t v, Coef k) {
   typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-  const bf16x2_t r = __builtin_convertvector((floatx2){bf16_to_f32(v & 0xffffu) * c, __uint_as_float(v & 0xffff0000u) * c},
+  const bf16x2_t r = __builtin_convertvector((floatx2){k.of(bf16_to_f32(v & 0xffffu)), k.of(__uint_as_float(v & 0xffff0000u))},
                                              bf16x2_t);
   return __builtin_bit_cast(uint32_t, r);
 }
 
 template <bool BF16>
-__device__ __forceinline__ u32x4 scaled(u32x4 v, float c) {
+__device__ __forceinline__ u32x4 scaled(u32x4 v, Coef k) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = BF16 ? scale_pair(v[i], c) : __float_as_uint(__uint_as_float(v[i]) * c);
+  for (int i = 0; i < 4; ++i) v[i] = BF16 ? scale_pair(v[i], k) : __float_as_uint(k.of(__uint_as_float(v[i])));
   return v;
 }
 
 template <bool BF16>
-__device__ __forceinline__ void scale_part(const char* p, char* q, int bytes, float c) {
+__device__ __forceinline__ void scale_part(const char* p, char* q, int bytes, Coef k) {
   constexpr int kElem = BF16 ? 2 : 4;
   const int whole = bytes / kVecBytes;
   for (int i = threadIdx.x; i < whole; i += kClipThreads)
     *reinterpret_cast<u32x4_any*>(q + i * kVecBytes) =
-        scaled<BF16>(*reinterpret_cast<const u32x4_any*>(p + i * kVecBytes), c);
+        scaled<BF16>(*reinterpret_cast<const u32x4_any*>(p + i * kVecBytes), k);
   const int at = whole * kVecBytes + (int)threadIdx.x * kElem;
   if (at < bytes) {
     if constexpr (BF16)
-      *reinterpret_cast<uint16_t*>(q + at) = (uint16_t)scale_pair(*reinterpret_cast<const uint16_t*>(p + at), c);
+      *reinterpret_cast<uint16_t*>(q + at) = (uint16_t)scale_pair(*reinterpret_cast<const uint16_t*>(p + at), k);
     else
-      *reinterpret_cast<float*>(q + at) = *reinterpret_cast<const float*>(p + at) * c;
+      *reinterpret_cast<float*>(q + at) = k.of(*reinterpret_cast<const float*>(p + at));
   }
 }
 
@@ -180,7 +193,7 @@ template <bool PAST>
 __global__ void __launch_bounds__(kClipThreads) clip_scale_kernel(ClipArgs a, const double* part, int n_part,
                                                                  float max_norm, float* out) {
   __shared__ double lds[kClipThreads / 64];
-  float coef = 0.f;
+  Coef k = {0.f, 0.f};
   bool first = true;
   for (int c = a.first[a.n] - 1 - (int)blockIdx.x; c >= 0; c -= gridDim.x) {
     const int t = tensor_of(a, c);
@@ -197,29 +210,28 @@ __global__ void __launch_bounds__(kClipThreads) clip_scale_kernel(ClipArgs a, co
     const bool whole = bytes == kChunkBytes;
     if (first) {
       if (whole && !a.in_place) load();
-      const floatx2 r = norm_and_coef<kClipThreads / 64>(part, n_part, max_norm, lds);
-      coef = r[1];
+      const floatx2 r = norm_and_coef<kClipThreads / 64>(part, n_part, max_norm, lds, k);
       if (out && blockIdx.x == 0 && threadIdx.x == 0) {
         out[0] = r[0];
         out[1] = r[1];
       }
-      if (coef == 1.f && a.in_place) return;
+      if (k.of(1.f) == 1.f && a.in_place) return;
     }
     // (coef 1 in place: the tensor stays as it is)
-    if (p != q || coef != 1.f) {
+    if (p != q || k.of(1.f) != 1.f) {
       if (whole) {
         if (!first || a.in_place) load();
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
           u32x4_any* to = reinterpret_cast<u32x4_any*>(q + (u * kClipThreads + (int)threadIdx.x) * kVecBytes);
-          const u32x4 r = a.bf16[t] ? scaled<true>(v[u], coef) : scaled<false>(v[u], coef);
+          const u32x4 r = a.bf16[t] ? scaled<true>(v[u], k) : scaled<false>(v[u], k);
           if constexpr (PAST) __builtin_nontemporal_store(r, to);
           else *to = r;
         }
       } else if (a.bf16[t]) {
-        scale_part<true>(p, q, bytes, coef);
+        scale_part<true>(p, q, bytes, k);
       } else {
-        scale_part<false>(p, q, bytes, coef);
+        scale_part<false>(p, q, bytes, k);
       }
     }
     first = false;

@@ -137,6 +137,25 @@ def test_clip_range(iso, value):
     within(t, torch.full((1000,), value / math.sqrt(1000.0), dtype=torch.float64), 1e-6 * value)
 
 
+@pytest.mark.parametrize("max_norm", [1.0, 1e-3, 1e-10, 1e-37])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_clip_small_coefficients(iso, max_norm, in_place):
+    """Coefficients below float32's normal range, applied to gradients near its top (and to
+    some that vanish)."""
+    g = gen(4)
+    host = [randn(g, 1000, std=1e38).clamp(-3e38, 3e38), randn(g, 37, std=1e38, dtype=BF16),
+            torch.tensor([1e-10, 1.0, 1e30, -3e38, 0.0])]
+    norm, coef, want = clip_reference(host, float(torch.tensor(max_norm, dtype=F32)))
+    assert coef < 2.0 ** -126
+    dev = [t.cuda() for t in host]
+    outs = None if in_place else [torch.empty_like(t) for t in dev]
+    got = iso.clip_grads(dev, max_norm, out=outs)
+    within(got[1:], torch.tensor([coef], dtype=torch.float64), 2.0 ** -149)
+    for t, h, w in zip(dev if in_place else outs, host, want):
+        # two products, then the result's own rounding; below 2^-126 a value's steps are 2^-149 (2^-133) apart
+        within(t, w, (ROUND[h.dtype] + 2 * U32) * w.abs() + (2.0 ** -148 if h.dtype == F32 else 2.0 ** -133))
+
+
 @pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
 def test_clip_nonfinite(iso, bad):
     host = [randn(gen(1), 100), randn(gen(2), 40, dtype=BF16)]
