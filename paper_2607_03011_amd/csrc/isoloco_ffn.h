@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include "isoloco.h"
+#include "isoloco_ffn_plan.h"
 
 namespace isoloco {
 
@@ -43,19 +44,6 @@ __device__ __forceinline__ void activate(float g, float& a, float& da) {
 // bf16(x - p0), p2 = bf16(x - p0 - p1), of which the six products of order 2^-16 and
 // above are summed: about float32 accuracy.
 constexpr int kFfnParts = 3;
-
-// da and du, and copies of x and the weights, have their columns padded to multiples of
-// this (the k values of a slab), da and du their rows too, zeros in the padding: the
-// products that sum over a padded extent need no bounds there.
-constexpr int kFfnPad = 64;
-__host__ __device__ inline int64_t ffn_pad(int64_t v) { return (v + kFfnPad - 1) / kFfnPad * kFfnPad; }
-
-enum FfnMode {
-  kForward,  // out[0] = act(a b0^T) (a b1^T)
-  kInner,    // out[0] = dh u act'(g), out[1] = dh act(g), padded; in parts if float32
-  kSum,      // out[0] = a[0] b[0]^T + a[1] b[1]^T
-  kPair      // out[z] = a[z] b[0]^T, z = 0, 1
-};
 
 // The tile products.  Operands: rows of ld elements (multiples of 8, at most 2^22),
 // 16-byte aligned, parts part_a (part_b) elements apart.

@@ -742,10 +742,11 @@ def test_gated_ffn_backward(iso, tokens, dim, hidden, dtype, act):
     assert only[0] is None and torch.equal(only[1], first[1]) and torch.equal(only[2], first[2])
 
 
-# Sizes at which every tile shape of the bfloat16 products and their splits are the
-# ones that a rule by the launch's rounds picks (256-square tiles: the first two
-# forwards, the third's dx, the fourth's weights; 192 x 256: the fifth's forward, the
-# sixth's weights, the last's dx; 128-square ones with up to 16 splits: the others).
+# Sizes of bfloat16 products on larger tiles and in splits (the instances one by one, with
+# the tiles that each takes: _ffn_cases.py): forward on 256-square tiles in the first two,
+# on 192 x 256 in the fifth, on 128-square ones, in 4 splits in the sixth, in the others; dx
+# on 256-square tiles in the third, on 192 x 256 in the last; in the others dx shares a
+# launch with the weights' gradients, on 256-square tiles in the seventh.
 FFN_TILES = [(6200, 136, 1000), (3000, 264, 4400), (8192, 2048, 256), (256, 2048, 4096), (4100, 520, 2056),
              (64, 2048, 5632), (700, 1032, 3000), (6144, 2048, 200)]
 
