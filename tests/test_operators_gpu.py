@@ -167,6 +167,30 @@ def test_clip_nonfinite(iso, bad):
         assert torch.equal(t.cpu().view(torch.int16), h.view(torch.int16))
 
 
+@pytest.mark.parametrize("name", sorted(CLIP_SETS))
+def test_clip_norm_only(iso, name):
+    """Without results the norm has a launch of its own, and nothing is scaled."""
+    shapes, dtypes = CLIP_SETS[name]
+    g = gen(12)
+    host = [randn(g, *s, dtype=dtypes[i % len(dtypes)]) for i, s in enumerate(shapes)]
+    dev = [at_offset(t, i % 8) for i, t in enumerate(host)]
+    types = [iso.ISOLOCO_F32 if t.dtype == F32 else iso.ISOLOCO_BF16 for t in dev]
+    ws = torch.empty(iso.isoloco_clip_workspace_size(len(dev)), dtype=torch.uint8, device="cuda")
+    for share in (0.25, 4.0):
+        norm, coef, _ = clip_reference(host, share * clip_reference(host, 1.0)[0])
+        got = torch.empty(2, device="cuda")
+        iso.isoloco_clip_grads([t.data_ptr() for t in dev], None, [t.numel() for t in dev], types, share * norm,
+                               got.data_ptr(), ws.data_ptr(), ws.numel(), torch.cuda.current_stream().cuda_stream)
+        within(got, torch.tensor([norm, coef], dtype=torch.float64), 2 * U32 * torch.tensor([norm, coef]))
+        assert all(torch.equal(t.cpu(), h) for t, h in zip(dev, host))
+
+
+def test_clip_of_nothing(iso):
+    """Tensors that hold no element: norm 0, coefficient 1."""
+    empty = torch.empty(0, 5, device="cuda")
+    assert iso.clip_grads([empty, empty.bfloat16()], 1.0).tolist() == [0.0, 1.0]
+
+
 def test_clip_past_32_bits(iso):
     n = 2 ** 31 + 4099
     t = torch.zeros(n, dtype=BF16, device="cuda")
@@ -809,6 +833,32 @@ def test_gated_ffn_nonfinite_stays_in_its_row(iso, tokens, dtype):
     want = torch.zeros_like(bad)
     want[1], want[:, 7] = True, True
     assert torch.equal(bad, want)
+
+
+@pytest.mark.parametrize("tokens", [1, 64, 65, 200])
+def test_gated_ffn_infinite_operand(iso, tokens):
+    """In float32 an infinity, or a value past bfloat16's range, is taken as it is by up to 64
+    tokens and gives NaN by more; in bfloat16 an infinity is always taken as it is."""
+    few = tokens <= 64
+    for dtype in (F32, BF16):
+        x, wg, wu, _ = ffn_inputs(tokens, 48, 40, dtype, 3)
+        x[0] = 0.0
+        x[0, 5] = math.inf
+        wg[:, 5], wu[:, 5] = 0.5, torch.where(torch.arange(40) % 2 == 0, 1.0, -1.0)
+        out = iso.gated_ffn(x.cuda(), wg.cuda(), wu.cuda()).cpu()
+        assert torch.isfinite(out[1:]).all()
+        if few or dtype == BF16:
+            assert torch.equal(out[0], torch.where(torch.arange(40) % 2 == 0, math.inf, -math.inf).to(dtype))
+        else:
+            assert torch.isnan(out[0]).all()
+    x, wg, wu, _ = ffn_inputs(tokens, 48, 40, F32, 3)
+    x[0], wg[:], wu[:] = 0.0, 0.0, 0.0
+    x[0, 5], wg[:, 5], wu[:, 5] = 3.4e38, 1e-37, 1e-37
+    out = iso.gated_ffn(x.cuda(), wg.cuda(), wu.cuda()).cpu()
+    if few:
+        within(out[0], torch.full((40,), 34.0 * 34.0 / (1 + math.exp(-34.0)), dtype=torch.float64), 1156 * 1e-5)
+    else:
+        assert torch.isnan(out[0]).all()
 
 
 def test_gated_ffn_against_differences(iso):
