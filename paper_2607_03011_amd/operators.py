@@ -417,13 +417,15 @@ def token_logprobs_backward(logits, targets, lse, dlogprob, entropy=None, dentro
 class _TokenLogProbs(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, targets, scale, top_k, workspace):
-        r = token_logprobs(logits, targets, scale, top_k, workspace)
-        ctx.save_for_backward(logits, targets, r.lse, r.entropy)
+        # (the vectors are views of one allocation, which autograd lets nobody write: .data are none)
+        logprob, entropy, lse, top, top_index = (
+            None if t is None else t.data for t in token_logprobs(logits, targets, scale, top_k, workspace))
+        ctx.save_for_backward(logits, targets, lse, entropy)
         ctx.scale = scale
         ctx.set_materialize_grads(False)
         if top_k:
-            ctx.mark_non_differentiable(r.top_index)
-        return tuple(r)
+            ctx.mark_non_differentiable(top_index)
+        return logprob, entropy, lse, top, top_index
 
     @staticmethod
     @once_differentiable

@@ -1031,6 +1031,25 @@ def test_autograd_does_not_drop_what_it_lacks(iso):
         assert iso.gated_ffn(z, w, w, out=out) is out and not out.requires_grad
 
 
+def test_autograd_of_results_written_in_place(iso):
+    """A result may be written, as a mask over the log probabilities does it; one that the
+    backward pass needs is found out."""
+    z0 = torch.randn(6, 40, device="cuda")
+    t = torch.arange(6, device="cuda")
+    z = wanted(z0)
+    lp = iso.token_logprobs(z, t, scale=1.1, top_k=1).logprob
+    lp.masked_fill_(t < 2, 0.0)
+    lp[5] *= 3.0
+    lp.sum().backward()
+    w = torch.tensor([0.0, 0.0, 1.0, 1.0, 1.0, 3.0], device="cuda")
+    lse = iso.token_logprobs(z0, t, scale=1.1).lse
+    assert torch.equal(z.grad, iso.token_logprobs_backward(z0, t, lse, w, scale=1.1))
+    r = iso.token_logprobs(wanted(z0), t)
+    r.entropy.mul_(2.0)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        r.entropy.sum().backward()
+
+
 @pytest.mark.parametrize("call", ["clip", "clip out", "embedding", "embedding gradient", "logits' gradient", "ffn"])
 def test_autograd_sees_what_is_written(iso, call):
     """A tensor that was saved for a backward pass and is then written by an operator is
