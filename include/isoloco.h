@@ -371,9 +371,10 @@ typedef enum { ISOLOCO_I32 = 0, ISOLOCO_I64 = 1 } isoloco_index_type;
  * call returns): each tensor's device pointer, its result's, its contiguous
  * elements (0 is allowed) and its type.  dst[i] may be src[i] (in place;
  * nothing is then written where coef is 1); a tensor's result must not overlap
- * another tensor.  dst = NULL: the norm only.  norm: two device floats, which
- * receive norm and coef.  A norm that is infinite or NaN leaves the gradients
- * as they are, and tells the caller so.  Squares are summed in 64 bits: a norm
+ * another tensor, so a gradient that two names share is given once.  dst =
+ * NULL: the norm only.  norm: two device floats, which receive norm and coef.
+ * A norm that is infinite or NaN leaves the gradients as they are, and tells
+ * the caller so.  Squares are summed in 64 bits: a norm
  * past float32's range is stored as infinity, with the coef that was applied
  * (less than 1).  coef is applied with all of its bits, also where the float
  * that is stored has lost some (below 2^-126).

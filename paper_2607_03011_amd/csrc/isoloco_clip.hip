@@ -320,9 +320,9 @@ isoloco_status isoloco_clip_grads(const void* const* src, void* const* dst, cons
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
   double* part = static_cast<double*>(workspace);
   // Results apart from their sources go past the caches if both do not fit in them.  Both
-  // sides measured, us of a call and of one that scales the result, stored / stored past:
-  // 32M float32 61 + 36 / 60 + 40, 110M bfloat16 116 + 80 / 100 + 88, 888M bfloat16
-  // 985 + 608 / 957 + 626.
+  // sides measured, us of a call, and with a pass that scales the results after it, stored /
+  // stored past: 32M float32 65 / 64 and 107 / 123, 110M bfloat16 116 / 100 and 300 / 285,
+  // 888M bfloat16 1026 / 993 and 2345 / 2328.
   int64_t results = 0;
   for (int i = 0; dst && i < n_tensors; ++i)
     if (dst[i] != src[i]) results += counts[i] * (int64_t)dtype_bytes(dtypes[i]);

@@ -425,7 +425,8 @@ hipError_t run_backward(const GroupTables& g, const ID* ids, int64_t n, const TD
   constexpr int kSpan = 64 * kColsOf<TD>;
   const int spans = (dim + kSpan - 1) / kSpan, pieces = (int)((n + kPiece - 1) / kPiece);
   const int nb = groups_of(vocab);
-  // (few tokens: without the turns that would find none, 7 us instead of 11 for 5001)
+  // (few tokens: without the turns that would find none.  Us a call with 8 / 32 ids a lane: 5001
+  // tokens 26.0 / 29.4, 8192 91 / 94, 32768 126 / 124)
   if (n <= kGroupWaves * 64 * 8)
     hipLaunchKernelGGL((group_kernel<ID, 8>), dim3(nb), dim3(kGroupThreads), 0, st, ids, (int32_t)n, vocab,
                        __builtin_ctz(nb), g);
@@ -434,8 +435,9 @@ hipError_t run_backward(const GroupTables& g, const ID* ids, int64_t n, const TD
                        __builtin_ctz(nb), g);
   const int pieced = n > kPiece ? pieces : 0;
   // 7 workgroups of 4 waves are on a CU at a time; four times as many even out what the rows
-  // cost (1 / 2 / 4 / 8 times: 96 / 90 / 87 / 82 us for 32768 tokens of 2048, 20.0 / 17.6 /
-  // 17.0 / 19.6 for 5001 of 612)
+  // cost (us a call at 1 / 2 / 4 / 8 / 16 times: 134 / 127 / 124 / 121 / 122 for 32768 tokens
+  // of 2048 in bfloat16, 54 / 51 / 50 / 51 / 55 for 768 in float32, 30.1 / 27.5 / 26.0 / 28.4 /
+  // 33.0 for 5001 of 612)
   const int64_t items = (vocab + pieced) * spans, blocks = std::min<int64_t>((items + 3) / 4, 4 * 7 * 256);
   hipLaunchKernelGGL((embed_sums_kernel<TD, TG, ID>), dim3((unsigned)blocks), dim3(256), 0, st, g, ids, dout, ld_dout,
                      vocab, dim, scale, accumulate, dtable, ld_dtable, spans, pieced);

@@ -58,8 +58,16 @@ __device__ __forceinline__ floatx4 multiply(const Lane<float>& a, const Lane<flo
   return c;
 }
 
-// Against the tiles (us, 2048 x 5632 / 768 x 2048): bfloat16, 32 tokens 18.9 / 4.6 here,
-// 33 there 16.7 / 8.8; float32, 64 tokens 58 / 10 here, 86 / 29 there.
+// Up to few_most() tokens come here, the others go to the tiles.  Both sides measured, us a
+// call of a graph, weights in a cache, here / tiles:
+//                           16 tokens    17           32           33           64
+//   bfloat16   768 x 2048   3.9 / 8.3    4.3 / 8.2    4.6 / 8.8    5.4 / 8.7    6.1 / 9.8
+//             1000 x 2777   4.9 / 9.3    6.1 / 9.3    6.4 / 10.1   8.4 / 10.3   9.6 / 12.1
+//             2048 x 5632   13.5 / 15.1  14.7 / 15.1  18.7 / 15.9  21.4 / 16.3  29.7 / 18.0
+//   float32    768 x 2048   5.3 / 28.7   5.9 / 29.0   6.6 / 28.0   8.5 / 28.3   9.9 / 27.9
+//             2048 x 5632   24.5 / 81.7  26.8 / 82.1  34.7 / 83.2  47.4 / 83.6  57.8 / 88.8
+// One line for every width: the wide bfloat16 block is better off with the tiles from 18
+// tokens on, the narrow ones here up to 64.
 constexpr int kFewWaves = 8;
 constexpr int64_t few_most(int32_t dtype) { return dtype == ISOLOCO_BF16 ? 32 : 64; }
 

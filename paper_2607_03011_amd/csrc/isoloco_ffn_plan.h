@@ -52,11 +52,13 @@ inline double sums_us(int mode, int splits, int64_t m, int64_t n) {
 constexpr double kJoinUs = 6.0;
 
 // The tiles and splits that take the least time by the rounds of the launch, the
-// slabs of a round and the traffic of the splits' sums.  Both sides measured, us on
-// 256-square / 192 x 256 / 128-square tiles: weight gradients of 16384 tokens, 2048 x
-// 5632, 774 / 690 / 843 (352 tiles of the first are two rounds of 256, the second of
-// them 3/8 full); its dx 606 / 739 / 802; forward of 2048 tokens, 768 x 2048, 24 / - /
-// 19.  Splits 1 / 2 / 4 / 8 of the dx of 512 tokens, 2048 x 5632: 138 / 79 / 52 / 47.
+// slabs of a round and the traffic of the splits' sums.  Both sides measured, us of calls
+// in turn on 256-square / 192 x 256 / 128-square tiles: 16384 tokens of 2048 x 5632,
+// forward 629 / 665 / 774, dx 635 / 769 / 805, weight gradients 727 / 724 / 887 (352
+// tiles of the first are two rounds of 256, the second of them 3/8 full, and cards differ
+// in which of the first two is ahead); forward of 2048 tokens, 768 x 2048, 22.4 / 18.9 /
+// 17.8.  Splits 1 / 2 / 4 / 8 / 16 of the dx of 512 tokens, 2048 x 5632: 126 / 73 / 45 /
+// 44 / 59.
 inline Plan plan_of(int mode, bool f32, int64_t m, int64_t n, int64_t k) {
   const int64_t slabs = slabs_of(mode, f32, k);
   Plan best = {kSmall, 1, 1e30};
@@ -76,10 +78,10 @@ inline Plan plan_of(int mode, bool f32, int64_t m, int64_t n, int64_t k) {
 // kSum of m x n over k with kPair of k x n over m: one launch where that takes less than
 // the two apart by the same rule (1.06: of which it leaves out that the first of two
 // drains before the second fills the card).  Both sides measured, us of the whole
-// gradient, apart / together: bfloat16, 512 tokens of 768 x 2048 47 / 38, 4096 tokens 125
-// / 99, 1024 of 2048 x 5632 175 / 157, 4096 of them 536 / 503, 8192 of 1024 x 4096 427 /
-// 370; float32, 1000 tokens of 612 x 1637 142 / 122, 2048 of 768 x 2048 289 / 272.
-// Everything together (1.15): 3000 tokens of 1001 x 2777 in float32 723 / 771.
+// gradient, apart / together: bfloat16, 512 tokens of 768 x 2048 42 / 35, 4096 tokens 121
+// / 97, 1024 of 2048 x 5632 172 / 155, 4096 of them 543 / 501, 8192 of 1024 x 4096 423 /
+// 375; float32, 1000 tokens of 612 x 1637 140 / 122, 2048 of 768 x 2048 292 / 268.  Where
+// the rule keeps them apart: 3000 tokens of 1001 x 2777 in float32 729 / 774.
 struct GradientsPlan {
   bool together;
   Plan sum, pair;

@@ -84,8 +84,9 @@ struct RowsSlab {
 // holds k's value of every column).  The fragments need k along a lane's registers:
 // they are read with the transposing LDS load (16 lanes read 4 consecutive k of 16
 // columns and receive a column's 4 values each).  The pieces of an LDS row are moved
-// by 64 bytes times k mod 4 (round the row: 192 columns are no power of two), so that
-// such a read touches every bank once.
+// by 64 bytes times k mod 4, so that such a read touches every bank once.  (192 columns are
+// no power of two: pieces go round the end of their row, and reads of the last 96 columns
+// find two of them in a bank.)
 template <int COLS, int THREADS>
 struct ColsSlab {
   static constexpr int kRow = COLS * 2, kPieces = kRow / 16;

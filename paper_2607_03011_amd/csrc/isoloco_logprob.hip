@@ -384,8 +384,8 @@ constexpr int kGradVecs = 4;  // 16-byte vectors of a thread
 // p is formed from the lse, a float32: off by 2^-24 |lse| of itself, and for masks written
 // as a large number all of it.  From here on a row's maximum and sum are formed again: in
 // float32 where p would be off by 2^-16, in bfloat16 by 2^-11, a quarter of the result's
-// rounding.  (Rows of 32000, above and below the line: 8192 in bfloat16 628 and 181 us, 4096
-// in float32 610 and 185: three readings instead of one.)
+// rounding.  (Us for rows of 32000 above and below the line: 8192 in bfloat16 628 and 181,
+// 4096 in float32 610 and 185, for three readings instead of one.)
 template <typename T>
 constexpr float kSureLse = sizeof(T) == 2 ? 8192.f : 256.f;
 
@@ -513,8 +513,16 @@ isoloco_status check_rows(int64_t rows, int64_t vocab, int32_t dtype, int32_t ta
   return ISOLOCO_OK;
 }
 
-// Workgroups per row: one, unless the rows are few and long.  A row of 32000 takes a
-// workgroup about as long as joining its splits would.
+// Workgroups per row: one, unless the rows are few and long.  Both sides measured, us a
+// call of a graph with 8 alternatives in bfloat16, 1 / 2 / 4 / 8 splits:
+//           1 row                      64 rows                    127 or 256 rows
+//    32000  8.5 / 9.6 / 9.7 / 12.3     9.3 / 10.9 / 10.8 / 13.5   11.0 / 14.4 / 15.4 / 17.5 (256)
+//    50257  11.4 / 10.4 / 10.1 / 10.7  14.2 / 12.4 / 11.9 / 12.9  14.6 / 13.2 / 14.2 / 16.1 (127),
+//                                                                 15.7 / 16.7 / 17.8 / 21.4 (256)
+//   128000  19.3 / 14.6 / 11.4 / 11.4  20.9 / 17.0 / 14.6 / 15.8  22.3 / 18.8 / 18.3 / 19.5 (127),
+//                                                                 27.0 / 27.7 / 25.3 / 26.5 (256)
+// (Without a graph the second launch costs the host 4 us more: one row of 50257 12.5 whole,
+// 17.0 in splits.)
 int splits_of(int64_t rows, int64_t vocab) {
   if (rows >= 128 || vocab <= 40000) return 1;
   const int64_t most = vocab / 8192, wanted = 512 / (rows ? rows : 1);
@@ -546,8 +554,9 @@ template <typename T, typename ID>
 void run_grad(const void* logits, int64_t ld, int64_t rows, int64_t vocab, const void* targets, float scale,
               const GradIn& in, void* dlogits, int64_t ld_d, int spans, hipStream_t st) {
   // Both sides measured, stored past the caches / stored, us of both passes over rows of 32000
-  // in bfloat16: 8192 rows 286 / 314 (and what scales the gradient after them takes as
-  // long); 2048 rows 72 / 72, but what reads the gradient then takes 8 longer.
+  // in bfloat16, and with a pass that scales the gradient after them: 8192 rows 273 / 301 and
+  // 469 / 477; 4096 rows (just below the line) 129 / 153 and 236 / 241; 2048 rows 73 / 74 and
+  // 113 / 109.
   const bool past = dlogits != logits && rows * vocab * (int64_t)sizeof(T) > kCacheBytes;
   hipLaunchKernelGGL((past ? logprob_grad_kernel<T, ID, true> : logprob_grad_kernel<T, ID, false>), dim3((unsigned)(rows * spans)), dim3(kGradThreads), 0, st,
                      static_cast<const T*>(logits), ld, rows, vocab, static_cast<const ID*>(targets), scale, in,

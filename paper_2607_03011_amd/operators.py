@@ -237,7 +237,8 @@ def clip_grads(grads, max_norm, out=None, workspace=None):
     """Scale the tensors of ``grads`` (contiguous, float32 or bfloat16 each) so that
     the norm over all of them is at most ``max_norm``: in place, or into the
     tensors of ``out``.  Returns a float32 tensor [norm before, coefficient] on the
-    device.  An infinite or NaN norm leaves them as they are."""
+    device.  An infinite or NaN norm leaves them as they are.  No tensor may be given
+    twice (a tied gradient counts once) or overlap another one's result."""
     grads = list(grads)
     if not grads:
         raise ValueError("no gradients")
