@@ -432,7 +432,7 @@ isoloco_status isoloco_token_logprobs(const void* logits, int64_t ld_logits, int
  * dentropy are zero, or whose logits are all -infinity, has a zero gradient.
  * p_j is e^(z_j - lse): off by 2^-24 |lse| of itself for lse's rounding.  Where
  * |lse| is 256 or more (8192 in bfloat16) the row's maximum and sum are formed
- * again instead. */
+ * again instead, unless lse is not theirs (of a vocabulary in parts, say). */
 isoloco_status isoloco_token_logprobs_backward(const void* logits, int64_t ld_logits, int32_t dtype, int64_t rows,
                                                int64_t vocab, const void* targets, int32_t target_type, float scale,
                                                const float* lse, const float* entropy, const float* dlogprob,

@@ -390,9 +390,12 @@ template <typename T>
 constexpr float kSureLse = sizeof(T) == 2 ? 8192.f : 256.f;
 
 // The row's gradient without its lse: its maximum and sum against that, then the gradient,
-// by one workgroup (in place, nobody else may read the row).  grad(log p, column).
+// by one workgroup (in place, nobody else may read the row).  grad(log p, column).  An lse
+// that the row's own sum cannot have been rounded to is of more than this row (a vocabulary
+// in parts): it is taken as it is.
 template <typename T, typename Grad>
-__device__ __forceinline__ void grad_of_row(const T* row, T* out, int64_t vocab, float scale, const Grad& grad) {
+__device__ __forceinline__ void grad_of_row(const T* row, T* out, int64_t vocab, float scale, float lse,
+                                            const Grad& grad) {
   constexpr int N = Vec<T>::N, kWaves = kGradThreads / 64, kAtOnce = 4;
   __shared__ float most_of[kWaves], sum_of[kWaves];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -441,7 +444,8 @@ __device__ __forceinline__ void grad_of_row(const T* row, T* out, int64_t vocab,
   __syncthreads();
   s = 0.f;
   for (int w = 0; w < kWaves; ++w) s += sum_of[w];
-  const float log_s = logf(s);
+  const float own = logf(s), given = fmaf(-m, scale, lse);
+  const float log_s = isinf(lse) || fabsf(given - own) <= fmaf(fabsf(lse), 0x1p-23f, 0x1p-16f) ? own : given;
   const auto grad_of = [&](float x, int64_t i) { return empty ? 0.f : grad((x - m) * scale - log_s, i); };
   vectors([&](const float* x, int64_t i) {
     float d[N];
@@ -479,7 +483,7 @@ __global__ void __launch_bounds__(kGradThreads) logprob_grad_kernel(const T* log
   };
   if (!none && fabsf(lse) >= kSureLse<T>) {
     // one of the row's workgroups, another one from row to row: their XCDs take turns
-    if ((int)(blockIdx.x % spans) == (int)(r % spans)) grad_of_row(row, out, vocab, scale, grad_at);
+    if ((int)(blockIdx.x % spans) == (int)(r % spans)) grad_of_row(row, out, vocab, scale, lse, grad_at);
     return;
   }
   const auto grad = [&](float x, int64_t i) { return grad_at(fmaf(x, scale, -lse), i); };

@@ -663,6 +663,31 @@ def test_token_logprobs_backward_large_lse(iso, vocab, scale, dtype):
         assert again is dev and torch.equal(got.view(torch.uint8), again.contiguous().view(torch.uint8))
 
 
+@pytest.mark.parametrize("shift", [0.0, 300.0, -3000.0, 20000.0])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_token_logprobs_backward_of_a_part(iso, dtype, shift):
+    """Rows that are parts of longer ones, with the log-sum-exp of the whole: p is e^(z - lse)
+    with the lse that is given, off by (6 |log p| + 64) u of itself and, where p is formed from
+    z and lse as they stand, by the rounding of lse."""
+    g = gen(31)
+    rows, vocab = 9, 700
+    whole = (randn(g, rows, 3 * vocab, std=3.0) + shift).to(dtype)
+    lse = torch.logsumexp(whole.double() * 0.75, 1).to(F32)
+    dl = randn(g, rows)
+    for at in range(3):
+        host = whole[:, at * vocab:(at + 1) * vocab].contiguous()
+        targets = torch.randint(-vocab, vocab, (rows,), generator=g)
+        got = iso.token_logprobs_backward(host.cuda(), targets.cuda(), lse.cuda(), dl.cuda(), scale=0.75)
+        q = host.double() * 0.75 - lse.double()[:, None]
+        p, ok = q.exp(), targets >= 0
+        one = torch.zeros_like(p)
+        one[ok.nonzero()[:, 0], targets[ok]] = 1.0
+        d = torch.where(ok, dl.double(), 0.0)[:, None]
+        want = 0.75 * d * (one - p)
+        near = U32 * (6 * q.abs().clamp(max=150) + 64 + 2 * lse.double().abs().clamp(max=SURE_LSE[dtype])[:, None])
+        within(got, want, 0.75 * d.abs() * (p * near + one * 4 * U32) * 1.01 + ROUND[dtype] * want.abs() + 1e-37)
+
+
 def test_token_logprobs_backward_large_lse_of_large_results(iso):
     """The same where the result is stored past the caches: the bits of calls of few rows."""
     rows, vocab = 4200, 32003
