@@ -473,6 +473,144 @@ isoloco_status isoloco_gated_ffn_backward(const void* x, int64_t ld_x, const voi
                                           void* dw_gate, void* dw_up, int64_t ld_dw, void* workspace,
                                           size_t workspace_bytes, void* hip_stream);
 
+/* Routing of tokens to experts.  With x the scores of a token (tokens x experts)
+ * and p their softmax, its top_k largest scores (of equal ones the lower expert
+ * first) give
+ *
+ *   expert (tokens x top_k, in falling order), and weight: p at those, or
+ *   (normalize != 0) p over its sum at those, the softmax of the chosen scores
+ *
+ * and the slots (token, j) are grouped by expert, within one in their order:
+ *
+ *   offsets (experts + 1): expert e has the places offsets[e] .. offsets[e + 1] - 1
+ *   row (tokens x top_k): a slot's place;  token (tokens * top_k): a place's token
+ *
+ * so that row is a permutation of 0 .. tokens * top_k - 1.  A score of -infinity
+ * is no expert to choose: a slot that finds none has expert -1 and weight 0, and
+ * its place is behind the last expert's.  NaN ranks above all and makes the
+ * token's weights NaN, as +infinity does.  top_k <= min(ISOLOCO_MAX_TOP,
+ * experts); tokens * top_k < 2^31. */
+#define ISOLOCO_MAX_EXPERTS 1024
+
+isoloco_status isoloco_route_tokens_workspace_size(int64_t tokens, int64_t experts, size_t* bytes);
+isoloco_status isoloco_route_tokens(const void* scores, int64_t ld_scores, int32_t dtype, int64_t tokens,
+                                    int64_t experts, int32_t top_k, int32_t normalize, float* weight, int32_t* expert,
+                                    int32_t* row, int32_t* token, int32_t* offsets, void* workspace,
+                                    size_t workspace_bytes, void* hip_stream);
+
+/* The gradient of weight in the scores, g_j = dweight of slot j, from the experts
+ * that were chosen (slots outside 0 .. experts - 1 take none):
+ *
+ *   normalize:  dx at expert_j = w_j (g_j - sum_i w_i g_i), 0 elsewhere
+ *   otherwise:  dx_e = p_e (the g_j with expert_j = e, less sum_i w_i g_i)       */
+isoloco_status isoloco_route_tokens_backward(const void* scores, int64_t ld_scores, int32_t dtype, int64_t tokens,
+                                             int64_t experts, int32_t top_k, int32_t normalize, const int32_t* expert,
+                                             const float* dweight, void* dscores, int64_t ld_dscores,
+                                             void* hip_stream);
+
+/* Matrix products grouped by expert: out[r] = x_r w[e]^T for the rows r =
+ * offsets[e] .. offsets[e + 1] - 1 of each expert e, where x_r is row token[r] of
+ * x (tokens x dim), or row r if token is NULL (tokens = rows then).  w: experts
+ * matrices of cols x dim, ld_w the distance of two rows and stride_w that of two
+ * matrices; out: rows x cols.  offsets (experts + 1, not falling, from 0 to at
+ * most rows) and token (rows) are of index_type and stay on the device: their
+ * values are not known to the host, and nothing outside the tensors is touched
+ * whatever they are.  Rows from offsets[experts] on are zeros, and a token
+ * outside 0 .. tokens - 1 stands for a row of zeros.  An expert may have no rows.
+ * float32 products are formed as in isoloco_gated_ffn.
+ *
+ * The workspace's size goes by the call: ISOLOCO_EXPERTS_BACKWARD for the
+ * gradient, ISOLOCO_EXPERTS_GATHERED where token is given, and
+ * ISOLOCO_EXPERTS_ALIGNED where the operands that are read (x, w; backward: and
+ * dout) will be 16-byte aligned with dim and cols, all ld and stride_w multiples of 8 and all
+ * ld at most 2^22, which saves their copies in bfloat16.  dim and cols are at most 2^22 - 64. */
+#define ISOLOCO_EXPERTS_BACKWARD 1
+#define ISOLOCO_EXPERTS_ALIGNED 2
+#define ISOLOCO_EXPERTS_GATHERED 4
+
+isoloco_status isoloco_expert_matmul_workspace_size(int64_t tokens, int64_t rows, int64_t experts, int64_t dim,
+                                                    int64_t cols, int32_t dtype, int32_t flags, size_t* bytes);
+isoloco_status isoloco_expert_matmul(const void* x, int64_t ld_x, int64_t tokens, const void* token, const void* w,
+                                     int64_t ld_w, int64_t stride_w, int32_t dtype, const void* offsets,
+                                     int32_t index_type, int64_t experts, int64_t rows, int64_t dim, int64_t cols,
+                                     void* out, int64_t ld_out, void* workspace, size_t workspace_bytes,
+                                     void* hip_stream);
+
+/* Its gradients from dout (rows x cols), either of which may be NULL:
+ *
+ *   dx[r] = dout[r] w[e] (rows x dim: of the grouped rows; rows of no expert: zeros)
+ *   dw[e] = sum over the rows of e of dout[r]^T x_r (zeros without any)
+ *
+ * With token given, the gradient of x is the sum of dx over a token's rows: what
+ * isoloco_combine_tokens without weight forms. */
+isoloco_status isoloco_expert_matmul_backward(const void* x, int64_t ld_x, int64_t tokens, const void* token,
+                                              const void* w, int64_t ld_w, int64_t stride_w, int32_t dtype,
+                                              const void* offsets, int32_t index_type, int64_t experts, int64_t rows,
+                                              int64_t dim, int64_t cols, const void* dout, int64_t ld_dout, void* dx,
+                                              int64_t ld_dx, void* dw, int64_t ld_dw, int64_t stride_dw,
+                                              void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* out[t] = sum_j weight[t, j] y[row[t, j]]; y: rows x dim, row and weight: tokens x
+ * top_k (weight NULL: ones), out: tokens x dim.  Entries of row outside 0 .. rows
+ * - 1 add nothing.  top_k <= ISOLOCO_MAX_TOP. */
+isoloco_status isoloco_combine_tokens(const void* y, int64_t ld_y, int32_t dtype, int64_t rows, int64_t dim,
+                                      const void* row, int32_t index_type, const float* weight, int64_t tokens,
+                                      int32_t top_k, void* out, int64_t ld_out, void* hip_stream);
+
+/* Its gradients, either of which may be NULL:
+ *
+ *   dy[row[t, j]] = weight[t, j] dout[t]          dweight[t, j] = <dout[t], y[row[t, j]]>
+ *
+ * No two entries of row may be the same; rows of dy that none names are left as
+ * they were.  dweight is 0 where the entry is outside.  y is read for dweight only. */
+isoloco_status isoloco_combine_tokens_backward(const void* dout, int64_t ld_dout, const void* y, int64_t ld_y,
+                                               int32_t dtype, int64_t rows, int64_t dim, const void* row,
+                                               int32_t index_type, const float* weight, int64_t tokens, int32_t top_k,
+                                               void* dy, int64_t ld_dy, float* dweight, void* hip_stream);
+
+/* Distillation from a teacher's most likely tokens.  With z = scale * logits of a
+ * row (scale > 0), q their softmax, and the row's top_k entries t_i = top_logprob
+ * (log probabilities) of the columns c_i = top_index:
+ *
+ *   ISOLOCO_REST_DROP     p_i = e^t_i / sum_i e^t_i  (t_i may be logits too)
+ *                         loss = sum_i p_i (log p_i - log q_ci)
+ *   ISOLOCO_REST_BUCKET   p_i = e^t_i, p_r = 1 - sum_i p_i, if positive
+ *                         loss = sum_i p_i (log p_i - log q_ci) + p_r (log p_r - log q_r)
+ *
+ * where q_r is the sum of q over the columns that are not listed: what the teacher
+ * gives to all others is compared as one (left out where the student has no such
+ * column, or only masked ones).  An entry outside the vocabulary is none; a row
+ * without entries has no loss and no gradient.  t_i = -infinity adds nothing; a
+ * column that is listed twice counts as often.  Logits of -infinity are masked: q =
+ * 0, and the loss is infinite where p_i > 0 there.  A NaN or +infinity among a row's
+ * logits, or NaN among its t, makes its results NaN.
+ * loss: rows floats.  stats: rows x ISOLOCO_DISTILL_STATS floats for the gradient,
+ * of which [6] is the row's log-sum-exp of z.  top_k <= ISOLOCO_MAX_TEACHER. */
+#define ISOLOCO_MAX_TEACHER 128
+#define ISOLOCO_DISTILL_STATS 8
+
+typedef enum { ISOLOCO_REST_DROP = 0, ISOLOCO_REST_BUCKET = 1 } isoloco_rest;
+
+isoloco_status isoloco_distill_loss_workspace_size(int64_t rows, int64_t vocab, size_t* bytes);
+isoloco_status isoloco_distill_loss(const void* logits, int64_t ld_logits, int32_t dtype, int64_t rows, int64_t vocab,
+                                    const float* top_logprob, const void* top_index, int32_t index_type, int32_t top_k,
+                                    float scale, int32_t rest, float* loss, float* stats, void* workspace,
+                                    size_t workspace_bytes, void* hip_stream);
+
+/* The gradient of the above in the logits, from the stats it gave and dloss (rows):
+ *
+ *   dlogits_j = dloss * scale * (q_j W - the p_i with c_i = j, less p_r q_j / q_r
+ *               where j is not listed),  W = sum_i p_i (+ p_r)
+ *
+ * dlogits has the logits' type and may be the logits themselves (same pointer and
+ * ld).  A row whose dloss is zero, without entries, or whose logits are all
+ * -infinity, has a zero gradient. */
+isoloco_status isoloco_distill_loss_backward(const void* logits, int64_t ld_logits, int32_t dtype, int64_t rows,
+                                             int64_t vocab, const float* top_logprob, const void* top_index,
+                                             int32_t index_type, int32_t top_k, float scale, int32_t rest,
+                                             const float* stats, const float* dloss, void* dlogits, int64_t ld_dlogits,
+                                             void* hip_stream);
+
 const char* isoloco_status_string(isoloco_status s);
 
 /* Message of the last failed call on this thread ("" if none). */

@@ -7,8 +7,9 @@ torch-allocated workspace.  All arithmetic runs in the HIP kernels of the
 library: if the library is missing, importing the binding raises.
 
 The operators of the workers' inner training step (clipping, embedding, token
-log probabilities, gated feed-forward block) are in ``operators.py`` and are
-reached from here under the same names.
+log probabilities, gated feed-forward block) are in ``operators.py``, those of a
+block of experts and of distillation in ``experts.py``; they are reached from here
+under the same names.
 """
 import ctypes
 import os
@@ -30,6 +31,14 @@ __all__ = [
     "isoloco_gated_ffn_workspace_size", "isoloco_gated_ffn", "isoloco_gated_ffn_backward",
     "ISOLOCO_I32", "ISOLOCO_I64", "ISOLOCO_ACT_SILU", "ISOLOCO_ACT_GELU", "ISOLOCO_MAX_TOP",
     "ISOLOCO_FFN_BACKWARD", "ISOLOCO_FFN_ALIGNED",
+    "route_tokens", "route_tokens_backward", "TokenRoutes", "expert_matmul", "expert_matmul_backward",
+    "combine_tokens", "combine_tokens_backward", "distill_loss", "distill_loss_backward", "DistillLoss",
+    "isoloco_route_tokens_workspace_size", "isoloco_route_tokens", "isoloco_route_tokens_backward",
+    "isoloco_expert_matmul_workspace_size", "isoloco_expert_matmul", "isoloco_expert_matmul_backward",
+    "isoloco_combine_tokens", "isoloco_combine_tokens_backward",
+    "isoloco_distill_loss_workspace_size", "isoloco_distill_loss", "isoloco_distill_loss_backward",
+    "ISOLOCO_MAX_EXPERTS", "ISOLOCO_EXPERTS_BACKWARD", "ISOLOCO_EXPERTS_ALIGNED", "ISOLOCO_EXPERTS_GATHERED",
+    "ISOLOCO_MAX_TEACHER", "ISOLOCO_DISTILL_STATS", "ISOLOCO_REST_DROP", "ISOLOCO_REST_BUCKET",
 ]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libisoloco.so")
@@ -66,6 +75,14 @@ ISOLOCO_ACT_GELU = 1
 ISOLOCO_MAX_TOP = 32
 ISOLOCO_FFN_BACKWARD = 1
 ISOLOCO_FFN_ALIGNED = 2
+ISOLOCO_MAX_EXPERTS = 1024
+ISOLOCO_EXPERTS_BACKWARD = 1
+ISOLOCO_EXPERTS_ALIGNED = 2
+ISOLOCO_EXPERTS_GATHERED = 4
+ISOLOCO_MAX_TEACHER = 128
+ISOLOCO_DISTILL_STATS = 8
+ISOLOCO_REST_DROP = 0
+ISOLOCO_REST_BUCKET = 1
 
 EXPORTED_SYMBOLS = (
     "isoloco_plan", "isoloco_workspace_size", "isoloco_set_workspace", "isoloco_aggregate",
@@ -76,6 +93,10 @@ EXPORTED_SYMBOLS = (
     "isoloco_embedding_backward_workspace_size", "isoloco_embedding_backward",
     "isoloco_token_logprobs_workspace_size", "isoloco_token_logprobs", "isoloco_token_logprobs_backward",
     "isoloco_gated_ffn_workspace_size", "isoloco_gated_ffn", "isoloco_gated_ffn_backward",
+    "isoloco_route_tokens_workspace_size", "isoloco_route_tokens", "isoloco_route_tokens_backward",
+    "isoloco_expert_matmul_workspace_size", "isoloco_expert_matmul", "isoloco_expert_matmul_backward",
+    "isoloco_combine_tokens", "isoloco_combine_tokens_backward",
+    "isoloco_distill_loss_workspace_size", "isoloco_distill_loss", "isoloco_distill_loss_backward",
 )
 
 
@@ -165,6 +186,23 @@ _sig = {
                                          _P]),
     "isoloco_gated_ffn_backward": (ctypes.c_int, [_P, _I64, _P, _P, _I64, _I32, _I64, _I64, _I64, _I32, _P, _I64, _P,
                                                   _I64, _P, _P, _I64, _P, _SIZE, _P]),
+    "isoloco_route_tokens_workspace_size": (ctypes.c_int, [_I64, _I64, ctypes.POINTER(_SIZE)]),
+    "isoloco_route_tokens": (ctypes.c_int, [_P, _I64, _I32, _I64, _I64, _I32, _I32, _P, _P, _P, _P, _P, _P, _SIZE, _P]),
+    "isoloco_route_tokens_backward": (ctypes.c_int, [_P, _I64, _I32, _I64, _I64, _I32, _I32, _P, _P, _P, _I64, _P]),
+    "isoloco_expert_matmul_workspace_size": (ctypes.c_int, [_I64, _I64, _I64, _I64, _I64, _I32, _I32,
+                                                            ctypes.POINTER(_SIZE)]),
+    "isoloco_expert_matmul": (ctypes.c_int, [_P, _I64, _I64, _P, _P, _I64, _I64, _I32, _P, _I32, _I64, _I64, _I64, _I64,
+                                             _P, _I64, _P, _SIZE, _P]),
+    "isoloco_expert_matmul_backward": (ctypes.c_int, [_P, _I64, _I64, _P, _P, _I64, _I64, _I32, _P, _I32, _I64, _I64,
+                                                      _I64, _I64, _P, _I64, _P, _I64, _P, _I64, _I64, _P, _SIZE, _P]),
+    "isoloco_combine_tokens": (ctypes.c_int, [_P, _I64, _I32, _I64, _I64, _P, _I32, _P, _I64, _I32, _P, _I64, _P]),
+    "isoloco_combine_tokens_backward": (ctypes.c_int, [_P, _I64, _P, _I64, _I32, _I64, _I64, _P, _I32, _P, _I64, _I32,
+                                                       _P, _I64, _P, _P]),
+    "isoloco_distill_loss_workspace_size": (ctypes.c_int, [_I64, _I64, ctypes.POINTER(_SIZE)]),
+    "isoloco_distill_loss": (ctypes.c_int, [_P, _I64, _I32, _I64, _I64, _P, _P, _I32, _I32, _F, _I32, _P, _P, _P, _SIZE,
+                                            _P]),
+    "isoloco_distill_loss_backward": (ctypes.c_int, [_P, _I64, _I32, _I64, _I64, _P, _P, _I32, _I32, _F, _I32, _P, _P,
+                                                     _P, _I64, _P]),
     "isoloco_status_string": (ctypes.c_char_p, [ctypes.c_int]),
     "isoloco_last_error": (ctypes.c_char_p, []),
 }
@@ -393,3 +431,9 @@ from .operators import (  # noqa: E402,F401
     isoloco_embedding_backward_workspace_size, isoloco_gated_ffn, isoloco_gated_ffn_backward,
     isoloco_gated_ffn_workspace_size, isoloco_token_logprobs, isoloco_token_logprobs_backward,
     isoloco_token_logprobs_workspace_size, token_logprobs, token_logprobs_backward)
+from .experts import (  # noqa: E402,F401
+    DistillLoss, TokenRoutes, combine_tokens, combine_tokens_backward, distill_loss, distill_loss_backward,
+    expert_matmul, expert_matmul_backward, isoloco_combine_tokens, isoloco_combine_tokens_backward,
+    isoloco_distill_loss, isoloco_distill_loss_backward, isoloco_distill_loss_workspace_size, isoloco_expert_matmul,
+    isoloco_expert_matmul_backward, isoloco_expert_matmul_workspace_size, isoloco_route_tokens,
+    isoloco_route_tokens_backward, isoloco_route_tokens_workspace_size, route_tokens, route_tokens_backward)

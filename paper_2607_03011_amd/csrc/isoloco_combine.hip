@@ -1,0 +1,233 @@
+// The sum of a token's rows, as they come back from the experts:
+//
+//   out[t] = sum_j weight[t, j] y[row[t, j]]
+//   dy[row[t, j]] = weight[t, j] dout[t],   dweight[t, j] = <dout[t], y[row[t, j]]>
+//
+// The terms of a sum are added in the order of j; no two slots name one row, so that
+// nothing is added across tokens.  Bounded by memory: every row is read once (backward:
+// and its gradient written once).
+#include <hip/hip_runtime.h>
+
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "isoloco_device.h"
+#include "isoloco_error.h"
+#include "isoloco_vec.h"
+
+namespace isoloco {
+namespace {
+
+struct CombineArgs {
+  Index row;
+  const float* weight;  // or NULL: ones
+  int64_t tokens, rows, dim, ld_y, ld_out;
+  int top_k;
+};
+
+constexpr int kAtOnce = 8;  // rows whose pieces a thread has in flight
+
+// One thread per piece of 16 bytes of the result.
+template <typename T>
+__global__ void __launch_bounds__(256) combine_kernel(const T* y, T* out, CombineArgs g, int pieces) {
+  constexpr int N = Vec<T>::N;
+  const int64_t item = (int64_t)blockIdx.x * 256 + threadIdx.x, t = item / pieces;
+  if (t >= g.tokens) return;
+  const int64_t col = (item - t * pieces) * N, left = g.dim - col;
+  float sum[N] = {};
+  for (int j0 = 0; j0 < g.top_k; j0 += kAtOnce) {
+    float x[kAtOnce][N], w[kAtOnce];
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+      const int j = j0 + u;
+      const int64_t r = j < g.top_k ? g.row.get(t * g.top_k + j) : -1;
+      const bool in = r >= 0 && r < g.rows;
+      w[u] = in ? (g.weight ? g.weight[t * g.top_k + j] : 1.f) : 0.f;
+#pragma unroll
+      for (int e = 0; e < N; ++e) x[u][e] = 0.f;
+      if (in) load_piece<T>(y + r * g.ld_y + col, left, x[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u)
+#pragma unroll
+      for (int e = 0; e < N; ++e) sum[e] = fmaf(w[u], x[u][e], sum[e]);
+  }
+  store_piece<T>(out + t * g.ld_out + col, left, sum);
+}
+
+struct CombineGradArgs {
+  Index row;
+  const float* weight;
+  int64_t tokens, rows, dim, ld_dout, ld_y, ld_dy;
+  int top_k;
+  float* dweight;
+  int lanes_log2;  // threads of a token: 2^this
+};
+
+// 2^lanes_log2 threads per token (all of a workgroup's 256 at most), which go through its
+// columns kAtOnce slots at a time.
+template <typename T, bool DY, bool DW>
+__global__ void __launch_bounds__(256) combine_grad_kernel(const T* dout, const T* y, T* dy, CombineGradArgs g) {
+  constexpr int N = Vec<T>::N;
+  __shared__ float part[4][kAtOnce];
+  const int lanes = 1 << g.lanes_log2, in = threadIdx.x & (lanes - 1);
+  const int64_t t = ((int64_t)blockIdx.x << (8 - g.lanes_log2)) + (threadIdx.x >> g.lanes_log2);
+  const bool live = t < g.tokens;
+  const T* d = dout + t * g.ld_dout;
+  for (int j0 = 0; j0 < g.top_k; j0 += kAtOnce) {
+    int64_t r[kAtOnce];
+    float w[kAtOnce], dot[kAtOnce];
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+      const int j = j0 + u;
+      r[u] = live && j < g.top_k ? g.row.get(t * g.top_k + j) : -1;
+      if (r[u] >= g.rows) r[u] = -1;
+      w[u] = r[u] >= 0 && g.weight ? g.weight[t * g.top_k + j] : 1.f;
+      dot[u] = 0.f;
+    }
+    if (live) {
+      for (int64_t col = (int64_t)in * N; col < g.dim; col += (int64_t)lanes * N) {
+        const int64_t left = g.dim - col;
+        float a[N];
+        load_piece<T>(d + col, left, a);
+        if constexpr (DW) {
+          float x[kAtOnce][N];
+#pragma unroll
+          for (int u = 0; u < kAtOnce; ++u) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) x[u][e] = 0.f;
+            if (r[u] >= 0) load_piece<T>(y + r[u] * g.ld_y + col, left, x[u]);
+          }
+#pragma unroll
+          for (int u = 0; u < kAtOnce; ++u)
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+              if (r[u] >= 0) dot[u] = fmaf(a[e], x[u][e], dot[u]);
+        }
+        if constexpr (DY) {
+#pragma unroll
+          for (int u = 0; u < kAtOnce; ++u) {
+            float v[N];
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[e] = w[u] * a[e];
+            if (r[u] >= 0) store_piece<T>(dy + r[u] * g.ld_dy + col, left, v);
+          }
+        }
+      }
+    }
+    if constexpr (DW) {
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u)
+        for (int off = std::min(lanes, 64) >> 1; off > 0; off >>= 1) dot[u] += __shfl_xor(dot[u], off, 64);
+      if (lanes > 64) {
+        const int wave = threadIdx.x >> 6, waves = lanes >> 6, first = wave & ~(waves - 1);
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+          for (int u = 0; u < kAtOnce; ++u) part[wave][u] = dot[u];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+          dot[u] = part[first][u];
+          for (int v = 1; v < waves; ++v) dot[u] += part[first + v][u];
+        }
+      }
+      if (live && in == 0) {
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u)
+          if (j0 + u < g.top_k) g.dweight[t * g.top_k + j0 + u] = dot[u];
+      }
+    }
+  }
+}
+
+template <typename T>
+void run_forward(const void* y, void* out, const CombineArgs& g, int pieces, int64_t blocks, hipStream_t st) {
+  hipLaunchKernelGGL(combine_kernel<T>, dim3((unsigned)blocks), dim3(256), 0, st, static_cast<const T*>(y),
+                     static_cast<T*>(out), g, pieces);
+}
+
+template <typename T>
+void run_grad(const void* dout, const void* y, void* dy, const CombineGradArgs& g, int64_t blocks, hipStream_t st) {
+  const dim3 grid((unsigned)blocks);
+  const T *d = static_cast<const T*>(dout), *x = static_cast<const T*>(y);
+  T* o = static_cast<T*>(dy);
+  if (dy && g.dweight) hipLaunchKernelGGL((combine_grad_kernel<T, true, true>), grid, dim3(256), 0, st, d, x, o, g);
+  else if (dy) hipLaunchKernelGGL((combine_grad_kernel<T, true, false>), grid, dim3(256), 0, st, d, x, o, g);
+  else hipLaunchKernelGGL((combine_grad_kernel<T, false, true>), grid, dim3(256), 0, st, d, x, o, g);
+}
+
+isoloco_status check_shape(int32_t dtype, int64_t tokens, int64_t rows, int64_t dim, int32_t index_type, int32_t top_k) {
+  if (tokens < 0 || tokens > kMaxExtent / 2 || rows < 0 || rows > kMaxExtent || dim < 1 || dim > kMaxExtent / 2)
+    return fail(ISOLOCO_ERR_INVALID_ARG, "%lld tokens of %lld rows, dim %lld", (long long)tokens, (long long)rows,
+                (long long)dim);
+  if (top_k < 1 || top_k > ISOLOCO_MAX_TOP)
+    return fail(ISOLOCO_ERR_INVALID_ARG, "top_k = %d, of 1 to %d", top_k, ISOLOCO_MAX_TOP);
+  if (!is_dtype(dtype)) return fail(ISOLOCO_ERR_INVALID_ARG, "dtype %d", dtype);
+  if (!is_index_type(index_type)) return fail(ISOLOCO_ERR_INVALID_ARG, "index type %d", index_type);
+  return ISOLOCO_OK;
+}
+
+}  // namespace
+}  // namespace isoloco
+
+using namespace isoloco;
+
+extern "C" {
+
+isoloco_status isoloco_combine_tokens(const void* y, int64_t ld_y, int32_t dtype, int64_t rows, int64_t dim,
+                                      const void* row, int32_t index_type, const float* weight, int64_t tokens,
+                                      int32_t top_k, void* out, int64_t ld_out, void* hip_stream) {
+  ISOLOCO_TRY(check_shape(dtype, tokens, rows, dim, index_type, top_k));
+  if (tokens == 0) return ISOLOCO_OK;
+  const size_t e = dtype_bytes(dtype), ib = index_bytes(index_type), n = (size_t)tokens * top_k;
+  ISOLOCO_TRY(check_matrix("y", y, rows, dim, ld_y, e));
+  ISOLOCO_TRY(check_matrix("out", out, tokens, dim, ld_out, e));
+  const Operand ins[] = {{"y", y, matrix_bytes(rows, dim, ld_y, e), e},
+                         {"row", row, n * ib, ib},
+                         {"weight", weight, weight ? n * 4 : 0, 4}};
+  const Operand outs[] = {{"out", out, matrix_bytes(tokens, dim, ld_out, e), e}};
+  ISOLOCO_TRY(check_operands(outs, 1, ins, 3));
+  const int64_t per = 16 / (int64_t)e, pieces = (dim + per - 1) / per, blocks = (tokens * pieces + 255) / 256;
+  if (!launchable(blocks, 256)) return fail(ISOLOCO_ERR_UNSUPPORTED, "too many elements for one launch");
+  const CombineArgs g = {{row, index_type == ISOLOCO_I64}, weight, tokens, rows, dim, ld_y, ld_out, top_k};
+  const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  if (dtype == ISOLOCO_F32) run_forward<float>(y, out, g, (int)pieces, blocks, st);
+  else run_forward<__bf16>(y, out, g, (int)pieces, blocks, st);
+  const hipError_t err = hipGetLastError();
+  return err == hipSuccess ? ISOLOCO_OK : hip_fail(err, "combination of tokens");
+}
+
+isoloco_status isoloco_combine_tokens_backward(const void* dout, int64_t ld_dout, const void* y, int64_t ld_y,
+                                               int32_t dtype, int64_t rows, int64_t dim, const void* row,
+                                               int32_t index_type, const float* weight, int64_t tokens, int32_t top_k,
+                                               void* dy, int64_t ld_dy, float* dweight, void* hip_stream) {
+  ISOLOCO_TRY(check_shape(dtype, tokens, rows, dim, index_type, top_k));
+  if (dweight && !weight) return fail(ISOLOCO_ERR_INVALID_ARG, "dweight needs weight");
+  if (tokens == 0 || (!dy && !dweight)) return ISOLOCO_OK;
+  const size_t e = dtype_bytes(dtype), ib = index_bytes(index_type), n = (size_t)tokens * top_k;
+  ISOLOCO_TRY(check_matrix("dout", dout, tokens, dim, ld_dout, e));
+  if (dweight) ISOLOCO_TRY(check_matrix("y", y, rows, dim, ld_y, e));
+  if (dy) ISOLOCO_TRY(check_matrix("dy", dy, rows, dim, ld_dy, e));
+  const Operand ins[] = {{"dout", dout, matrix_bytes(tokens, dim, ld_dout, e), e},
+                         {"y", y, dweight ? matrix_bytes(rows, dim, ld_y, e) : 0, e},
+                         {"row", row, n * ib, ib},
+                         {"weight", weight, weight ? n * 4 : 0, 4}};
+  const Operand outs[] = {{"dy", dy, dy ? matrix_bytes(rows, dim, ld_dy, e) : 0, e},
+                          {"dweight", dweight, dweight ? n * 4 : 0, 4}};
+  ISOLOCO_TRY(check_operands(outs, 2, ins, 4));
+  CombineGradArgs g = {{row, index_type == ISOLOCO_I64}, weight, tokens, rows, dim, ld_dout, ld_y, ld_dy, top_k, dweight, 3};
+  const int64_t per = 16 / (int64_t)e;
+  while (g.lanes_log2 < 8 && (per << g.lanes_log2) < dim) ++g.lanes_log2;
+  const int64_t blocks = (tokens + (256 >> g.lanes_log2) - 1) >> (8 - g.lanes_log2);
+  if (!launchable(blocks, 256)) return fail(ISOLOCO_ERR_UNSUPPORTED, "too many tokens for one launch");
+  const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  if (dtype == ISOLOCO_F32) run_grad<float>(dout, y, dy, g, blocks, st);
+  else run_grad<__bf16>(dout, y, dy, g, blocks, st);
+  const hipError_t err = hipGetLastError();
+  return err == hipSuccess ? ISOLOCO_OK : hip_fail(err, "gradient of the combination of tokens");
+}
+
+}  // extern "C"

@@ -1,0 +1,569 @@
+// Distillation from a teacher's most likely tokens: the loss of each row and its
+// gradient in the student's logits.  With x the logits of a row, z = scale x, q their
+// softmax, and t_i the teacher's log probabilities of the columns c_i:
+//
+//   drop     p_i = e^t_i / sum_i e^t_i                loss = sum_i p_i (log p_i - log q_ci)
+//   bucket   p_i = e^t_i, p_r = 1 - sum_i p_i         loss = the same + p_r (log p_r - log q_r)
+//            with q_r the sum of q over the columns that are not listed
+//
+//   W = sum_i p_i (+ p_r);  dz_j = q_j W - sum of the p_i with c_i = j, less p_r q_j / q_r
+//   where j is not listed
+//
+// The loss is the difference of nearly equal numbers once the student has learnt, so what
+// is formed once a row is formed in 64 bits; the sums over the vocabulary are of float32
+// exponentials.  q_r is summed from the columns that are not listed, not taken as one less
+// the others (which leaves nothing of a small one): the listed columns are marked in a
+// bitmap in LDS, and the pass over the row takes a marked column for -infinity.
+//
+// Bounded by memory: the loss reads the logits once, the gradient reads them again and
+// writes as much.
+#include <hip/hip_runtime.h>
+
+#include <math.h>
+#include <stdint.h>
+
+#include "isoloco_device.h"
+#include "isoloco_error.h"
+#include "isoloco_vec.h"
+
+namespace isoloco {
+namespace {
+
+constexpr int kMaxSplits = 64;
+constexpr int kHeld = 64;               // logits that a thread holds in registers
+constexpr int64_t kMostSpan = 1 << 17;  // columns of a workgroup with a bitmap: 16 KiB of it
+constexpr int kPerLane = (ISOLOCO_MAX_TEACHER + 63) / 64;
+
+// Sums of e^((x - m) scale) over some of a row's logits ({-infinity, 0} of nothing).
+struct Sum {
+  float m, s;
+  __device__ __forceinline__ void raise(float to, float rate) {
+    if (to == m) return;
+    s = m == -INFINITY ? s : s * __builtin_amdgcn_exp2f((m - to) * rate);
+    m = to;
+  }
+  __device__ __forceinline__ void join(Sum o, float rate) {
+    const float to = fmaxf(m, o.m);
+    raise(to, rate);
+    o.raise(to, rate);
+    s += o.s;
+  }
+};
+
+struct LossArgs {
+  int64_t ld, vocab;
+  const float* top;
+  int top_k;
+  float scale, rate;
+  int splits;    // workgroups per row
+  int64_t span;  // a split's columns (a multiple of a vector's)
+  Sum* part;     // splits > 1: each one's sum
+  float* loss;
+  float* stats;
+};
+
+__device__ __forceinline__ double wave_max(double v) {
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) v = fmax(v, __shfl_xor(v, off, 64));
+  return v;
+}
+
+// Whether no entry before the i-th names its column
+__device__ __forceinline__ bool first_of_its_column(const int32_t* column, int i) {
+  const int32_t c = column[i];
+  bool first = true;
+  for (int j = 0; j < i; ++j) first &= column[j] != c;
+  return first;
+}
+
+// The row's loss, by one wave: `a` is the sum over all of its columns, or (bucket) over
+// those that are not listed.  `column`: the entries' columns, -1 where there is none.
+template <typename T, bool BUCKET>
+__device__ void put_loss(const LossArgs& g, const T* row, const int32_t* column, int64_t r, const Sum& a) {
+  const int lane = threadIdx.x & 63;
+  const double scale = g.scale;
+  double t[kPerLane], x[kPerLane];
+  bool given[kPerLane];
+  double tm = -INFINITY, xm = a.m;
+#pragma unroll
+  for (int u = 0; u < kPerLane; ++u) {
+    const int i = 64 * u + lane;
+    given[u] = i < g.top_k && column[i] >= 0;
+    t[u] = given[u] ? (double)g.top[r * g.top_k + i] : -INFINITY;
+    x[u] = given[u] ? (double)(float)row[column[i]] : -INFINITY;
+    tm = fmax(tm, t[u]);
+    xm = fmax(xm, x[u]);
+  }
+  tm = BUCKET ? 0.0 : wave_max(tm);
+  xm = BUCKET ? wave_max(xm) : (double)a.m;
+  // (a maximum passes over NaN: with 0 in its place the sum does not)
+  bool odd = false;
+#pragma unroll
+  for (int u = 0; u < kPerLane; ++u) odd |= given[u] && t[u] != t[u];
+  if (__any(odd)) tm = 0.0;
+  // sums against xm: the listed columns' (bucket: each column once), and those of the rest
+  double s = 0.0, p_sum = 0.0, p[kPerLane];
+  const bool none = tm == -INFINITY;
+#pragma unroll
+  for (int u = 0; u < kPerLane; ++u) {
+    const int i = 64 * u + lane;
+    p[u] = given[u] && !none ? exp(t[u] - tm) : 0.0;
+    p_sum += p[u];
+    if (BUCKET && given[u] && (x[u] > -INFINITY || x[u] != x[u]) && first_of_its_column(column, i))
+      s += exp((x[u] - xm) * scale);
+  }
+  p_sum = wave_sum(p_sum);
+  const double others = a.m == -INFINITY ? (double)a.s : (double)a.s * exp(((double)a.m - xm) * scale);
+  s = BUCKET ? wave_sum(s) + others : (double)a.s;
+  const double log_s = log(s), inv_p = BUCKET ? 1.0 : 1.0 / p_sum, log_p = BUCKET ? 0.0 : tm + log(p_sum);
+  double loss = 0.0, weight = 0.0;
+#pragma unroll
+  for (int u = 0; u < kPerLane; ++u) {
+    const double mass = none ? 0.0 : p[u] * inv_p;
+    weight += mass;
+    if (given[u] && mass != 0.0) {
+      const double log_q = s == 0.0 ? -INFINITY : (x[u] - xm) * scale - log_s;
+      loss += mass * (t[u] - log_p - log_q);
+    }
+  }
+  loss = wave_sum(loss);
+  weight = wave_sum(weight);
+  double rest_factor = weight;
+  if (BUCKET) {
+    // (columns that are all masked, or none, are no bucket: what the rounding of the
+    // teacher's values leaves of one less their sum would make the loss infinite)
+    const double p_r = 1.0 - weight;
+    if (p_r > 0.0 && others > 0.0) {
+      const double log_r = log(others) - log_s;
+      loss += p_r * (log(p_r) - log_r);
+      rest_factor = 1.0 - p_r * exp(-log_r);
+      weight = 1.0;
+    } else if (others != others) {
+      loss = others;
+    }
+  }
+  if (lane == 0) {
+    g.loss[r] = (float)loss;
+    // what the gradient takes: q_j = stats[1] e^((x_j - stats[0]) scale), the factors of q
+    // at listed and other columns, and p_i = stats[5] e^(t_i - stats[4])
+    float* o = g.stats + r * ISOLOCO_DISTILL_STATS;
+    o[0] = s != s ? NAN : (float)xm;
+    o[1] = (float)(1.0 / s);
+    o[2] = (float)weight;
+    o[3] = (float)rest_factor;
+    o[4] = none ? 0.f : (float)tm;
+    o[5] = none ? 0.f : (float)inv_p;
+    o[6] = s == 0.0 ? -INFINITY : (float)(xm * scale + log_s);
+    o[7] = 0.f;
+  }
+}
+
+// a row without a teacher: no loss, and the gradient of nothing
+__device__ __forceinline__ void put_none(const LossArgs& g, int64_t r) {
+  g.loss[r] = 0.f;
+  for (int i = 0; i < ISOLOCO_DISTILL_STATS; ++i) g.stats[r * ISOLOCO_DISTILL_STATS + i] = 0.f;
+}
+
+// The row's columns into `column`; whether there is any.
+template <typename ID>
+__device__ __forceinline__ bool load_columns(const ID* index, int64_t r, int top_k, int64_t vocab, int32_t* column) {
+  bool any = false;
+  for (int i = threadIdx.x; i < top_k; i += blockDim.x) {
+    const int64_t c = index[r * top_k + i];
+    const bool in = c >= 0 && c < vocab;
+    column[i] = in ? (int32_t)c : -1;
+    any |= in;
+  }
+  return __syncthreads_or(any);
+}
+
+// One workgroup of WAVES waves per row, or per split of a row: kHeld columns per thread at
+// a time, as they are stored, their maximum and then their sum against it.
+template <typename T, typename ID, int WAVES, bool BUCKET>
+__global__ void __launch_bounds__(64 * WAVES, sizeof(T) == 2 ? 8 : 4)
+    distill_kernel(const T* logits, const ID* index, LossArgs g) {
+  constexpr int N = Vec<T>::N, kThreads = 64 * WAVES, kVecs = kHeld / N;
+  constexpr int turn = kThreads * kVecs;  // vectors that the workgroup holds
+  constexpr int kWords = !BUCKET ? 1 : (WAVES == 8 ? (int)kMostSpan : turn * N) / 32;
+  __shared__ Sum part[WAVES];
+  __shared__ int32_t column[ISOLOCO_MAX_TEACHER];
+  __shared__ uint32_t marks[kWords];
+  const int64_t r = blockIdx.x / g.splits;
+  const int split = (int)(blockIdx.x - r * g.splits);
+  const int64_t begin = split * g.span;
+  const int count = (int)min(g.span, g.vocab - begin), whole = count / N;
+  const T* row = logits + r * g.ld;
+  const T* p = row + begin;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+
+  u32x4 v[kVecs];
+  float last;
+  const auto load = [&](int base) {
+#pragma unroll
+    for (int c = 0; c < kVecs; ++c) {
+      const int i = base + c * kThreads + (int)threadIdx.x;
+      v[c] = sizeof(T) == 2 ? (u32x4)(0xff80ff80u) : (u32x4)(0xff800000u);  // -infinity
+      if (i < whole) v[c] = *reinterpret_cast<const u32x4_any*>(p + (int64_t)i * N);
+    }
+    const int at = whole * N + (int)threadIdx.x;
+    last = base == 0 && at < count ? (float)p[at] : -INFINITY;
+  };
+  if constexpr (BUCKET) {
+    for (int i = threadIdx.x; i < (count + 31) / 32; i += kThreads) marks[i] = 0;
+  }
+  const bool any = load_columns(index, r, g.top_k, g.vocab, column);
+  if (!any) {
+    if (split == 0 && threadIdx.x == 0) put_none(g, r);
+    return;
+  }
+  if constexpr (BUCKET) {
+    for (int i = threadIdx.x; i < g.top_k; i += kThreads) {
+      const int64_t c = column[i] - begin;
+      if (column[i] >= 0 && c >= 0 && c < count) atomicOr(&marks[c >> 5], 1u << (c & 31));
+    }
+    __syncthreads();
+  }
+
+  Sum a = {-INFINITY, 0.f};
+  for (int base = 0; base == 0 || base < whole; base += turn) {
+    load(base);
+    if constexpr (BUCKET) {
+#pragma unroll
+      for (int c = 0; c < kVecs; ++c) {
+        const int i = base + c * kThreads + (int)threadIdx.x;
+        if (i < whole) {
+          uint32_t bits = reinterpret_cast<const uint8_t*>(marks)[i * N / 8];
+          if (N == 4) bits = (bits >> (4 * (i & 1))) & 15u;
+          if (bits) {
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+              if constexpr (N == 4) {
+                if (bits >> w & 1u) v[c][w] = 0xff800000u;
+              } else {
+                if (bits >> (2 * w) & 1u) v[c][w] = (v[c][w] & 0xffff0000u) | 0xff80u;
+                if (bits >> (2 * w + 1) & 1u) v[c][w] = (v[c][w] & 0xffffu) | 0xff800000u;
+              }
+            }
+          }
+        }
+      }
+      const int at = whole * N + (int)threadIdx.x;
+      if (at < count && (marks[at >> 5] >> (at & 31) & 1u)) last = -INFINITY;
+    }
+    float most = last;
+#pragma unroll
+    for (int c = 0; c < kVecs; ++c)
+      if (base + c * kThreads < whole) {
+        float x[N];
+        unpack<T>(v[c], x);
+#pragma unroll
+        for (int e = 0; e < N; ++e) most = fmaxf(most, x[e]);
+      }
+    // (unpacked again after this: as float32 they would take the registers of half the waves)
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int c = 0; c < kVecs; ++c) asm("" : "+v"(v[c]));
+    }
+    a.raise(fmaxf(a.m, most), g.rate);
+    const float m = a.m == -INFINITY ? 0.f : a.m;
+#pragma unroll
+    for (int c = 0; c < kVecs; ++c)
+      if (base + c * kThreads < whole) {
+        float x[N];
+        unpack<T>(v[c], x);
+#pragma unroll
+        for (int e = 0; e < N; ++e) a.s += __builtin_amdgcn_exp2f((x[e] - m) * g.rate);
+      }
+    if (base == 0) a.s += __builtin_amdgcn_exp2f((last - m) * g.rate);
+  }
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) {
+    Sum o;
+    o.m = __shfl_xor(a.m, off, 64);
+    o.s = __shfl_xor(a.s, off, 64);
+    a.join(o, g.rate);
+  }
+  if constexpr (WAVES > 1) {
+    if (lane == 0) part[wave] = a;
+    __syncthreads();
+    a = part[0];
+    for (int w = 1; w < WAVES; ++w) a.join(part[w], g.rate);
+  }
+  if (wave > 0) return;
+  if (g.splits > 1) {
+    if (lane == 0) g.part[blockIdx.x] = a;
+  } else {
+    put_loss<T, BUCKET>(g, row, column, r, a);
+  }
+}
+
+// A row's splits joined, in their order, by one wave.
+template <typename T, typename ID, bool BUCKET>
+__global__ void __launch_bounds__(64) distill_join_kernel(const T* logits, const ID* index, LossArgs g) {
+  __shared__ int32_t column[ISOLOCO_MAX_TEACHER];
+  const int64_t r = blockIdx.x;
+  if (!load_columns(index, r, g.top_k, g.vocab, column)) return;  // (put_none is done)
+  const Sum* part = g.part + r * g.splits;
+  Sum a = part[0];
+  for (int i = 1; i < g.splits; ++i) a.join(part[i], g.rate);
+  put_loss<T, BUCKET>(g, logits + r * g.ld, column, r, a);
+}
+
+struct GradArgs {
+  int64_t ld, rows, vocab, ld_d;
+  const float* top;
+  int top_k;
+  float scale, rate;
+  const float* stats;
+  const float* dloss;
+  int spans;
+};
+
+constexpr int kGradThreads = 256;
+constexpr int kGradVecs = 4;  // 16-byte vectors of a thread
+
+// One workgroup per row and span of kGradThreads * kGradVecs vectors: every column as one
+// that is not listed, then the listed ones over them (their logits are read before: the
+// result may lie over the logits).  PAST: the result goes past the caches.
+template <typename T, typename ID, bool PAST>
+__global__ void __launch_bounds__(kGradThreads) distill_grad_kernel(const T* logits, const ID* index, T* dlogits,
+                                                                    GradArgs g) {
+  constexpr int N = Vec<T>::N;
+  __shared__ int32_t column[ISOLOCO_MAX_TEACHER];
+  __shared__ float mass[ISOLOCO_MAX_TEACHER];
+  static_assert(ISOLOCO_MAX_TEACHER <= kGradThreads, "one entry a thread");
+  // (the last rows first: the forward pass read them last, some are still in a cache)
+  const int64_t r = g.rows - 1 - blockIdx.x / g.spans;
+  const int span = (int)(blockIdx.x % g.spans);
+  const int64_t first = (int64_t)span * (kGradThreads * kGradVecs), whole = g.vocab / N;
+  const T* row = logits + r * g.ld;
+  T* out = dlogits + r * g.ld_d;
+  const float* st = g.stats + r * ISOLOCO_DISTILL_STATS;
+  const float m = st[0], inv_s = st[1], factor = st[2], rest_factor = st[3], tm = st[4], inv_p = st[5];
+  const float dl = g.dloss[r] * g.scale;
+  // nothing to hand back: no loss wanted, no teacher, no student
+  const bool none = dl == 0.f || inv_p == 0.f || m == -INFINITY;
+  const float from = none ? 0.f : m;
+  u32x4 v[kGradVecs];
+#pragma unroll
+  for (int u = 0; u < kGradVecs; ++u) {
+    const int64_t i = first + u * kGradThreads + threadIdx.x;
+    v[u] = (u32x4){};
+    if (!none && i < whole) v[u] = *reinterpret_cast<const u32x4_any*>(row + i * N);
+  }
+  const int64_t at = whole * N + threadIdx.x;
+  const bool single = span == 0 && at < g.vocab;
+  const float end = single && !none ? (float)row[at] : 0.f;
+  // this thread's entry, if its column is of this span
+  const int i = threadIdx.x;
+  bool mine = false;
+  int64_t c = -1;
+  float x_top = 0.f;
+  if (!none && i < g.top_k) {
+    c = index[r * g.top_k + i];
+    const bool in = c >= 0 && c < g.vocab;
+    column[i] = in ? (int32_t)c : -1;
+    mass[i] = in ? inv_p * exp2f((g.top[r * g.top_k + i] - tm) * kLog2e) : 0.f;
+    const int64_t vec = c / N;
+    mine = in && (vec >= whole ? span == 0 : vec >= first && vec < first + kGradThreads * kGradVecs);
+    if (mine) x_top = (float)row[c];
+  }
+  __syncthreads();
+  const float other = none ? 0.f : inv_s * rest_factor * dl;
+  const auto grad = [&](float x) { return none ? 0.f : __builtin_amdgcn_exp2f((x - from) * g.rate) * other; };
+#pragma unroll
+  for (int u = 0; u < kGradVecs; ++u) {
+    const int64_t j = first + u * kGradThreads + threadIdx.x;
+    if (j < whole) {
+      float x[N];
+      unpack<T>(v[u], x);
+#pragma unroll
+      for (int e = 0; e < N; ++e) x[e] = grad(x[e]);
+      const u32x4 d = pack<T>(x);
+      u32x4_any* to = reinterpret_cast<u32x4_any*>(out + j * N);
+      if constexpr (PAST) __builtin_nontemporal_store(d, to);
+      else *to = d;
+    }
+  }
+  if (single) out[at] = (T)grad(end);
+  if (none) return;
+  // every wave's stores are done before the listed columns' go over them
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (!mine || !first_of_its_column(column, i)) return;
+  float p = 0.f;
+  for (int j = i; j < g.top_k; ++j) p += column[j] == (int32_t)c ? mass[j] : 0.f;
+  const float q = __builtin_amdgcn_exp2f((x_top - from) * g.rate) * inv_s;
+  out[c] = (T)((q * factor - p) * dl);
+}
+
+struct DistillShape {
+  int64_t rows, vocab;
+  int32_t dtype, index_type, top_k, rest;
+  float scale;
+};
+
+isoloco_status check_shape(const DistillShape& s) {
+  if (s.rows < 0 || s.rows > kMaxExtent / 2 || s.vocab < 1 || s.vocab > kMaxExtent / 2)
+    return fail(ISOLOCO_ERR_INVALID_ARG, "%lld rows of %lld logits", (long long)s.rows, (long long)s.vocab);
+  if (!is_dtype(s.dtype)) return fail(ISOLOCO_ERR_INVALID_ARG, "dtype %d", s.dtype);
+  if (!is_index_type(s.index_type)) return fail(ISOLOCO_ERR_INVALID_ARG, "index type %d", s.index_type);
+  if (s.top_k < 1 || s.top_k > ISOLOCO_MAX_TEACHER)
+    return fail(ISOLOCO_ERR_INVALID_ARG, "top_k = %d, of 1 to %d", s.top_k, ISOLOCO_MAX_TEACHER);
+  if (s.rest != ISOLOCO_REST_DROP && s.rest != ISOLOCO_REST_BUCKET) return fail(ISOLOCO_ERR_INVALID_ARG, "rest %d", s.rest);
+  if (!(s.scale > 0.f) || isinf(s.scale))
+    return fail(ISOLOCO_ERR_INVALID_ARG, "scale = %g: a positive number is wanted", (double)s.scale);
+  return ISOLOCO_OK;
+}
+
+// Workgroups per row: one, unless the rows are few and long, or longer than a bitmap.
+int splits_of(int64_t rows, int64_t vocab) {
+  int64_t s = 1;
+  if (rows < 128 && vocab > 40000) {
+    const int64_t most = vocab / 8192, wanted = 512 / (rows ? rows : 1);
+    s = most < wanted ? most : wanted;
+    s = s < 1 ? 1 : s > kMaxSplits ? kMaxSplits : s;
+  }
+  const int64_t least = (vocab + kMostSpan - 8) / (kMostSpan - 7);
+  return (int)(s > least ? s : least);
+}
+
+size_t distill_workspace(int64_t rows, int64_t vocab) {
+  const size_t s = (size_t)splits_of(rows, vocab);
+  return s > 1 ? (size_t)rows * s * sizeof(Sum) : 0;
+}
+
+// the fewest that hold a row (or split) at once, if any do
+int threads_of(int64_t span) { return span <= 64 * kHeld ? 64 : span <= 256 * kHeld ? 256 : 512; }
+
+template <typename T, typename ID, bool BUCKET>
+void run_loss(const T* l, const ID* index, int64_t rows, const LossArgs& g, hipStream_t st) {
+  const dim3 grid((unsigned)(rows * g.splits));
+  const int threads = threads_of(g.span);
+  if (threads == 64) hipLaunchKernelGGL((distill_kernel<T, ID, 1, BUCKET>), grid, dim3(64), 0, st, l, index, g);
+  else if (threads == 256) hipLaunchKernelGGL((distill_kernel<T, ID, 4, BUCKET>), grid, dim3(256), 0, st, l, index, g);
+  else hipLaunchKernelGGL((distill_kernel<T, ID, 8, BUCKET>), grid, dim3(512), 0, st, l, index, g);
+  if (g.splits > 1)
+    hipLaunchKernelGGL((distill_join_kernel<T, ID, BUCKET>), dim3((unsigned)rows), dim3(64), 0, st, l, index, g);
+}
+
+template <typename T, typename ID>
+void run_forward(const void* logits, const void* index, int64_t rows, int rest, const LossArgs& g, hipStream_t st) {
+  const T* l = static_cast<const T*>(logits);
+  const ID* i = static_cast<const ID*>(index);
+  if (rest == ISOLOCO_REST_BUCKET) run_loss<T, ID, true>(l, i, rows, g, st);
+  else run_loss<T, ID, false>(l, i, rows, g, st);
+}
+
+template <typename T, typename ID>
+void run_grad(const void* logits, const void* index, void* dlogits, const GradArgs& g, hipStream_t st) {
+  const bool past = dlogits != logits && g.rows * g.vocab * (int64_t)sizeof(T) > kCacheBytes;
+  hipLaunchKernelGGL((past ? distill_grad_kernel<T, ID, true> : distill_grad_kernel<T, ID, false>),
+                     dim3((unsigned)(g.rows * g.spans)), dim3(kGradThreads), 0, st, static_cast<const T*>(logits),
+                     static_cast<const ID*>(index), static_cast<T*>(dlogits), g);
+}
+
+}  // namespace
+}  // namespace isoloco
+
+using namespace isoloco;
+
+#define BY_TYPES(RUN, ...)                                                             \
+  do {                                                                                 \
+    if (dtype == ISOLOCO_F32) {                                                        \
+      if (index_type == ISOLOCO_I32) RUN<float, int32_t>(__VA_ARGS__);                 \
+      else RUN<float, int64_t>(__VA_ARGS__);                                           \
+    } else {                                                                           \
+      if (index_type == ISOLOCO_I32) RUN<__bf16, int32_t>(__VA_ARGS__);                \
+      else RUN<__bf16, int64_t>(__VA_ARGS__);                                          \
+    }                                                                                  \
+  } while (0)
+
+extern "C" {
+
+isoloco_status isoloco_distill_loss_workspace_size(int64_t rows, int64_t vocab, size_t* bytes) {
+  if (!bytes) return fail(ISOLOCO_ERR_INVALID_ARG, "bytes is NULL");
+  ISOLOCO_TRY(check_shape({rows, vocab, ISOLOCO_F32, ISOLOCO_I32, 1, ISOLOCO_REST_DROP, 1.f}));
+  *bytes = distill_workspace(rows, vocab);
+  return ISOLOCO_OK;
+}
+
+isoloco_status isoloco_distill_loss(const void* logits, int64_t ld_logits, int32_t dtype, int64_t rows, int64_t vocab,
+                                    const float* top_logprob, const void* top_index, int32_t index_type, int32_t top_k,
+                                    float scale, int32_t rest, float* loss, float* stats, void* workspace,
+                                    size_t workspace_bytes, void* hip_stream) {
+  ISOLOCO_TRY(check_shape({rows, vocab, dtype, index_type, top_k, rest, scale}));
+  if (rows == 0) return ISOLOCO_OK;
+  const size_t e = dtype_bytes(dtype), ib = index_bytes(index_type), n = (size_t)rows * top_k;
+  ISOLOCO_TRY(check_matrix("logits", logits, rows, vocab, ld_logits, e));
+  const size_t need = distill_workspace(rows, vocab);
+  ISOLOCO_TRY(check_workspace(workspace, workspace_bytes, need));
+  const Operand ins[] = {{"logits", logits, matrix_bytes(rows, vocab, ld_logits, e), e},
+                         {"top_logprob", top_logprob, n * 4, 4},
+                         {"top_index", top_index, n * ib, ib}};
+  const Operand outs[] = {{"loss", loss, (size_t)rows * 4, 4},
+                          {"stats", stats, (size_t)rows * 4 * ISOLOCO_DISTILL_STATS, 4},
+                          {"the workspace", workspace, need, 1}};
+  ISOLOCO_TRY(check_operands(outs, 3, ins, 3));
+  LossArgs g;
+  g.ld = ld_logits;
+  g.vocab = vocab;
+  g.top = top_logprob;
+  g.top_k = top_k;
+  g.scale = scale;
+  g.rate = rate_of(scale);
+  g.splits = splits_of(rows, vocab);
+  g.span = ((vocab + g.splits - 1) / g.splits + 7) / 8 * 8;
+  g.splits = (int)((vocab + g.span - 1) / g.span);
+  g.part = static_cast<Sum*>(workspace);
+  g.loss = loss;
+  g.stats = stats;
+  if (!launchable(rows * g.splits, threads_of(g.span)))
+    return fail(ISOLOCO_ERR_UNSUPPORTED, "too many rows for one launch");
+  const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  BY_TYPES(run_forward, logits, top_index, rows, rest, g, st);
+  const hipError_t err = hipGetLastError();
+  return err == hipSuccess ? ISOLOCO_OK : hip_fail(err, "distillation loss");
+}
+
+isoloco_status isoloco_distill_loss_backward(const void* logits, int64_t ld_logits, int32_t dtype, int64_t rows,
+                                             int64_t vocab, const float* top_logprob, const void* top_index,
+                                             int32_t index_type, int32_t top_k, float scale, int32_t rest,
+                                             const float* stats, const float* dloss, void* dlogits, int64_t ld_dlogits,
+                                             void* hip_stream) {
+  ISOLOCO_TRY(check_shape({rows, vocab, dtype, index_type, top_k, rest, scale}));
+  if (rows == 0) return ISOLOCO_OK;
+  const size_t e = dtype_bytes(dtype), ib = index_bytes(index_type), n = (size_t)rows * top_k;
+  ISOLOCO_TRY(check_matrix("logits", logits, rows, vocab, ld_logits, e));
+  ISOLOCO_TRY(check_matrix("dlogits", dlogits, rows, vocab, ld_dlogits, e));
+  // in place: every element is read before it is written
+  const bool in_place = dlogits == logits && ld_dlogits == ld_logits;
+  const Operand ins[] = {{"top_logprob", top_logprob, n * 4, 4},
+                         {"top_index", top_index, n * ib, ib},
+                         {"stats", stats, (size_t)rows * 4 * ISOLOCO_DISTILL_STATS, 4},
+                         {"dloss", dloss, (size_t)rows * 4, 4},
+                         {"the logits", logits, in_place ? 0 : matrix_bytes(rows, vocab, ld_logits, e), e}};
+  const Operand outs[] = {{"dlogits", dlogits, matrix_bytes(rows, vocab, ld_dlogits, e), e}};
+  ISOLOCO_TRY(check_operands(outs, 1, ins, 5));
+  const int64_t vecs = vocab / (16 / (int64_t)e);
+  const int64_t spans = vecs == 0 ? 1 : (vecs + kGradThreads * kGradVecs - 1) / (kGradThreads * kGradVecs);
+  if (!launchable(rows * spans, kGradThreads)) return fail(ISOLOCO_ERR_UNSUPPORTED, "too many elements for one launch");
+  GradArgs g;
+  g.ld = ld_logits;
+  g.rows = rows;
+  g.vocab = vocab;
+  g.ld_d = ld_dlogits;
+  g.top = top_logprob;
+  g.top_k = top_k;
+  g.scale = scale;
+  g.rate = rate_of(scale);
+  g.stats = stats;
+  g.dloss = dloss;
+  g.spans = (int)spans;
+  const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  BY_TYPES(run_grad, logits, top_index, dlogits, g, st);
+  const hipError_t err = hipGetLastError();
+  return err == hipSuccess ? ISOLOCO_OK : hip_fail(err, "gradient of the distillation loss");
+}
+
+}  // extern "C"

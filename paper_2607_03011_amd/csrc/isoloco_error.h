@@ -65,4 +65,30 @@ inline isoloco_status check_workspace(const void* ws, size_t have, size_t need) 
   return ISOLOCO_OK;
 }
 
+struct Operand {
+  const char* name;
+  const void* p;
+  size_t bytes, align;
+};
+
+// Operands of a call: inputs and outputs not NULL unless empty, aligned to their elements,
+// outputs apart from inputs and from each other.
+inline isoloco_status check_operands(const Operand* outs, int n_out, const Operand* ins, int n_in) {
+  for (int i = 0; i < n_in; ++i) {
+    if (ins[i].bytes && !ins[i].p) return fail(ISOLOCO_ERR_INVALID_ARG, "%s is NULL", ins[i].name);
+    if (!aligned_to(ins[i].p, ins[i].align)) return fail(ISOLOCO_ERR_ALIGN, "%s is not aligned to its elements", ins[i].name);
+  }
+  for (int i = 0; i < n_out; ++i) {
+    if (outs[i].bytes && !outs[i].p) return fail(ISOLOCO_ERR_INVALID_ARG, "%s is NULL", outs[i].name);
+    if (!aligned_to(outs[i].p, outs[i].align)) return fail(ISOLOCO_ERR_ALIGN, "%s is not aligned to its elements", outs[i].name);
+    for (int j = 0; j < n_in; ++j)
+      if (ranges_overlap(outs[i].p, outs[i].bytes, ins[j].p, ins[j].bytes))
+        return fail(ISOLOCO_ERR_ALIAS, "%s overlaps %s", outs[i].name, ins[j].name);
+    for (int j = 0; j < i; ++j)
+      if (ranges_overlap(outs[i].p, outs[i].bytes, outs[j].p, outs[j].bytes))
+        return fail(ISOLOCO_ERR_ALIAS, "%s overlaps %s", outs[i].name, outs[j].name);
+  }
+  return ISOLOCO_OK;
+}
+
 }  // namespace isoloco

@@ -23,21 +23,17 @@
 
 #include "isoloco_device.h"
 #include "isoloco_error.h"
+#include "isoloco_vec.h"
 
 namespace isoloco {
 namespace {
 
-typedef u32x4 u32x4_any __attribute__((aligned(2)));
-
-constexpr float kLog2e = 1.44269504088896340736f, kLog2 = 0.69314718055994530942f;
+constexpr float kLog2 = 0.69314718055994530942f;
 
 // e^x, x <= 0 where it counts: the product's rounding moves the result by |x| ulps
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 // 2^t is 0 from here on down: a product with it takes this for t (which may be -infinity)
 constexpr float kNothing = -200.f;
-
-// scale log2 e, finite: 0 times it stays 0
-__host__ __device__ inline float rate_of(float scale) { return fminf(scale * kLog2e, FLT_MAX); }
 
 // The softmax of some of a row's logits: their maximum m, and s and w as above against it
 // ({-infinity, 0, 0} of nothing; a NaN or +infinity among them leaves a NaN in s).
@@ -62,54 +58,6 @@ struct Soft {
     w += b.w;
   }
 };
-
-// The order of the values: of equal ones (-0 and 0 among them) the lower index is
-// the larger key; NaN is above all.
-__device__ __forceinline__ uint32_t order_of(float x) {
-  const uint32_t u = __float_as_uint(x + 0.f);
-  return x != x ? 0xffffffffu : ((u >> 31) ? ~u : (u | 0x80000000u));
-}
-__device__ __forceinline__ uint64_t key_of(float x, uint32_t index) {
-  return ((uint64_t)order_of(x) << 32) | (uint32_t)~index;
-}
-__device__ __forceinline__ float value_of(uint64_t key) {
-  const uint32_t u = (uint32_t)(key >> 32);
-  return __uint_as_float((u >> 31) ? (u & 0x7fffffffu) : ~u);
-}
-__device__ __forceinline__ int64_t index_of(uint64_t key) { return (int64_t)(uint32_t)~(uint32_t)key; }
-__device__ __forceinline__ uint64_t max64(uint64_t a, uint64_t b) { return a > b ? a : b; }
-
-template <typename T>
-struct Vec {
-  static constexpr int N = 16 / sizeof(T);
-};
-template <typename T>
-__device__ __forceinline__ void unpack(u32x4 v, float* x) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if constexpr (sizeof(T) == 2) {
-      x[2 * i] = bf16_to_f32(v[i] & 0xffffu);
-      x[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
-    } else {
-      x[i] = __uint_as_float(v[i]);
-    }
-  }
-}
-
-template <typename T>
-__device__ __forceinline__ u32x4 pack(const float* x) {
-  u32x4 v;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if constexpr (sizeof(T) == 2) {
-      typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-      v[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((floatx2){x[2 * i], x[2 * i + 1]}, bf16x2_t));
-    } else {
-      v[i] = __float_as_uint(x[i]);
-    }
-  }
-  return v;
-}
 
 constexpr int kMaxSplits = 64;
 
