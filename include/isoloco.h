@@ -529,7 +529,8 @@ isoloco_status isoloco_route_tokens_backward(const void* scores, int64_t ld_scor
 #define ISOLOCO_EXPERTS_GATHERED 4
 
 isoloco_status isoloco_expert_matmul_workspace_size(int64_t tokens, int64_t rows, int64_t experts, int64_t dim,
-                                                    int64_t cols, int32_t dtype, int32_t flags, size_t* bytes);
+                                                    int64_t cols, int64_t ld_x, int32_t dtype, int32_t flags,
+                                                    size_t* bytes);
 isoloco_status isoloco_expert_matmul(const void* x, int64_t ld_x, int64_t tokens, const void* token, const void* w,
                                      int64_t ld_w, int64_t stride_w, int32_t dtype, const void* offsets,
                                      int32_t index_type, int64_t experts, int64_t rows, int64_t dim, int64_t cols,

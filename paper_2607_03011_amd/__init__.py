@@ -189,7 +189,7 @@ _sig = {
     "isoloco_route_tokens_workspace_size": (ctypes.c_int, [_I64, _I64, ctypes.POINTER(_SIZE)]),
     "isoloco_route_tokens": (ctypes.c_int, [_P, _I64, _I32, _I64, _I64, _I32, _I32, _P, _P, _P, _P, _P, _P, _SIZE, _P]),
     "isoloco_route_tokens_backward": (ctypes.c_int, [_P, _I64, _I32, _I64, _I64, _I32, _I32, _P, _P, _P, _I64, _P]),
-    "isoloco_expert_matmul_workspace_size": (ctypes.c_int, [_I64, _I64, _I64, _I64, _I64, _I32, _I32,
+    "isoloco_expert_matmul_workspace_size": (ctypes.c_int, [_I64, _I64, _I64, _I64, _I64, _I64, _I32, _I32,
                                                             ctypes.POINTER(_SIZE)]),
     "isoloco_expert_matmul": (ctypes.c_int, [_P, _I64, _I64, _P, _P, _I64, _I64, _I32, _P, _I32, _I64, _I64, _I64, _I64,
                                              _P, _I64, _P, _SIZE, _P]),

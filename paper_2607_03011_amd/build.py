@@ -16,7 +16,8 @@ LIB = os.path.join(PKG, "libisoloco.so")
 SOURCES = [os.path.join(PKG, "csrc", f) for f in (
     "isoloco_host.cpp", "isoloco_kernels.hip", "isoloco_products.hip",
     "isoloco_clip.hip", "isoloco_embedding.hip", "isoloco_logprob.hip", "isoloco_ffn.hip", "isoloco_ffn_tiles.hip",
-    "isoloco_route.hip", "isoloco_experts.hip", "isoloco_combine.hip", "isoloco_distill.hip")]
+    "isoloco_route.hip", "isoloco_experts.hip", "isoloco_experts_tiles.hip",
+    "isoloco_combine.hip", "isoloco_distill.hip")]
 
 HIPCC_FLAGS = [
     "-O3", "-std=c++17", "-fPIC", "-shared", "--offload-arch=gfx950",

@@ -1,0 +1,489 @@
+// The products grouped by expert on bfloat16 MFMA tiles (gfx950).
+//
+// Workgroups stay, one or two a CU, and go from tile to tile; slabs of 64 k values go from
+// memory straight into LDS, one in flight while the one before is multiplied.  The products
+// differ in how their operands lie:
+//
+//   kOut  rows of a (those that token names) against rows of the expert's matrix
+//   kDx   rows of a against columns of the expert's matrix
+//   kDw   columns of a against columns of b, over an expert's rows
+//
+// An expert's rows end inside tiles and slabs: what a load asks for past them it receives as
+// zeros, by the bounds of its buffer.  Each XCD takes a run of the tiles, so that its L2 holds
+// the operands that they share, cut by tiles (kDw: by their slabs, which differ from expert
+// to expert).
+//
+// float32 operands are three bfloat16 parts each; their products are the same slabs six times
+// over, one pair of parts after the other into the same accumulators, the smallest first.
+#include <hip/hip_runtime.h>
+
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "isoloco_device.h"
+#include "isoloco_experts.h"
+#include "isoloco_ffn.h"
+#include "isoloco_slabs.h"
+
+namespace isoloco {
+namespace {
+
+struct TileArgs {
+  ExpertArgs g;
+  int tiles_m, tiles_n, splits;  // tiles_m: of kDw
+};
+
+// A tile of the output, and its k values (kDw: rows of the operands).
+struct Tile {
+  int group, tm, tn, slice;
+  int64_t begin, end;  // the group's rows
+};
+
+constexpr int64_t kTileCost = 4;  // slabs that a tile's start and end take
+
+// What a group's tiles are and cost (kDw: slabs of its rows).
+template <ExpertProduct P, class C>
+__device__ __forceinline__ void group_of(const TileArgs& t, int e, int64_t& begin, int64_t& end, int64_t& tiles,
+                                         int64_t& cost) {
+  begin = end = tiles = cost = 0;
+  if (e > t.g.groups.experts || (P == kDw && e == t.g.groups.experts)) return;
+  t.g.groups.rows_of(e, begin, end);
+  if (P == kDw) {
+    tiles = (int64_t)t.tiles_m * t.tiles_n * t.splits;
+    cost = (end - begin + kSlab - 1) / kSlab + kTileCost * t.splits;
+  } else {
+    tiles = (end - begin + C::TM - 1) / C::TM * t.tiles_n * t.splits;
+    cost = 1;
+  }
+  cost *= tiles;
+}
+
+__device__ __forceinline__ int64_t scan64(int64_t v) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const int64_t o = __shfl_up((long long)v, off, 64);
+    if (lane >= off) v += o;
+  }
+  return v;
+}
+
+// Lane `at`'s value, in scalar registers
+__device__ __forceinline__ int64_t lane_of(int64_t v, int at) {
+  const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)v, at), hi = __builtin_amdgcn_readlane((uint32_t)(v >> 32), at);
+  return (int64_t)((uint64_t)hi << 32 | lo);
+}
+
+// The tile at which the costs of those before reach `cost` (all tiles, if none does); the
+// costs of all tiles.  Every wave by itself.
+template <ExpertProduct P, class C>
+__device__ __forceinline__ int64_t tile_at_cost(const TileArgs& t, int64_t cost, int64_t& all) {
+  int64_t tiles_before = 0, found = -1;
+  all = 0;
+  for (int base = 0; base <= t.g.groups.experts; base += 64) {
+    int64_t b, f, tiles, c;
+    group_of<P, C>(t, base + (threadIdx.x & 63), b, f, tiles, c);
+    const int64_t cost_sum = scan64(c), tile_sum = scan64(tiles);
+    const uint64_t past = __ballot(all + cost_sum > cost);
+    if (found < 0 && past) {
+      const int at = __ffsll((unsigned long long)past) - 1;
+      const int64_t own = tiles == 0 ? 0 : (cost - all - (cost_sum - c)) / (c / tiles);
+      found = lane_of(tiles_before + tile_sum - tiles + own, at);
+    }
+    all += lane_of(cost_sum, 63);
+    tiles_before += lane_of(tile_sum, 63);
+  }
+  return found < 0 ? tiles_before : found;
+}
+
+// The index-th tile.  Within a group slices come first, then bands of 8 rows of tiles.
+template <ExpertProduct P, class C>
+__device__ __forceinline__ bool find_tile(const TileArgs& t, int64_t index, Tile& o) {
+  int64_t before = 0;
+  for (int base = 0; base <= t.g.groups.experts; base += 64) {
+    int64_t b, f, tiles, c;
+    group_of<P, C>(t, base + (threadIdx.x & 63), b, f, tiles, c);
+    const int64_t sum = scan64(tiles);
+    const uint64_t past = __ballot(before + sum > index);
+    if (past) {
+      const int at = __ffsll((unsigned long long)past) - 1;
+      o.group = base + at;
+      o.begin = lane_of(b, at);
+      o.end = lane_of(f, at);
+      const int64_t i = lane_of(index - before - (sum - tiles), at);
+      const int tiles_m = P == kDw ? t.tiles_m : (int)((o.end - o.begin + C::TM - 1) / C::TM);
+      const int64_t plane = (int64_t)tiles_m * t.tiles_n, band_of = (int64_t)8 * t.tiles_n;
+      o.slice = (int)(i / plane);
+      int64_t in = i - o.slice * plane;
+      const int band = (int)(in / band_of);
+      in -= band * band_of;
+      const int rows = min(8, tiles_m - band * 8);
+      o.tm = band * 8 + (int)(in % rows);
+      o.tn = (int)(in / rows);
+      return true;
+    }
+    before += lane_of(sum, 63);
+  }
+  return false;
+}
+
+// Bytes from a place to the end of its buffer, as a buffer's size
+__device__ __forceinline__ uint32_t bounded(int64_t bytes) { return (uint32_t)min(max(bytes, (int64_t)0), (int64_t)kMostBytes); }
+
+template <class C>
+struct TileLds {
+  typedef Patch<C::NB * 32> P;
+  static constexpr int kStage = (C::TM + C::TN) * 128, kWs = P::kBytes;
+  static constexpr int kBytes = 2 * kStage > C::waves * kWs ? 2 * kStage : C::waves * kWs;
+  static_assert(kBytes <= 160 * 1024, "LDS");
+};
+
+template <ExpertProduct P, bool F32, bool GATHER, class C>
+__device__ __forceinline__ void multiply_tile(const TileArgs& t, const Tile& tile, char* lds) {
+  constexpr bool ACOLS = P == kDw, BCOLS = P != kOut;
+  typedef RowsSlab<C::TM, C::threads> AR;
+  typedef ColsSlab<C::TM, C::threads> AC;
+  typedef RowsSlab<C::TN, C::threads> BR;
+  typedef ColsSlab<C::TN, C::threads> BC;
+  constexpr int kA = C::TM * 128, kStage = TileLds<C>::kStage;
+  typedef typename TileLds<C>::P Patch_;
+
+  const ExpertArgs& g = t.g;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / C::WN, wn = wave % C::WN;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)lds;
+  const bool none = tile.group >= g.groups.experts;  // rows of no expert: zeros
+  const int64_t len = tile.end - tile.begin, i0 = (int64_t)tile.tm * C::TM, j0 = (int64_t)tile.tn * C::TN;
+  const int64_t m_all = P == kDw ? g.m : len;  // rows of this output
+  const int64_t depth = none ? 0 : P == kDw ? len : g.k;
+  const int64_t row_a = 2 * g.ld_a, row_b = 2 * g.ld_b;  // bytes
+  const int64_t gathered = 2 * g.tokens * (P == kDw ? g.ld_b : g.ld_a);  // bytes of what token reads
+
+  AR ar;
+  AC ac;
+  BR br;
+  BC bc;
+  const char* a = reinterpret_cast<const char*>(g.a);
+  const char* b = reinterpret_cast<const char*>(g.b);
+  if constexpr (ACOLS) {
+    a += tile.begin * row_a + 2 * i0;
+    ac.init((uint32_t)row_a, g.cols_a - i0);
+  } else if constexpr (GATHER) {
+#pragma unroll
+    for (int q = 0; q < AR::kLoads; ++q) {
+      const int at = q * C::threads + threadIdx.x;
+      const int64_t r = min((int64_t)(at >> 3), len - i0 - 1);
+      const int64_t s = g.token.get(tile.begin + i0 + r);
+      ar.vo[q] = s >= 0 && s < g.tokens ? (uint32_t)(s * row_a) + 16u * AR::piece(at) : kOutside;
+    }
+  } else {
+    a += (tile.begin + i0) * row_a;
+    ar.init((uint32_t)row_a, len - i0);
+  }
+  if constexpr (P == kOut) {
+    b += 2 * (tile.group * g.stride_b) + j0 * row_b;
+    br.init((uint32_t)row_b, g.n - j0);
+  } else {
+    if constexpr (P == kDx) b += 2 * (tile.group * g.stride_b + j0);
+    else if constexpr (GATHER) b += 0;
+    else b += tile.begin * row_b + 2 * j0;
+    bc.init((uint32_t)row_b, g.cols_b - j0);
+  }
+
+  // the slabs of this workgroup: runs, one per pair of parts, of which a split takes some
+  constexpr int kPairs = F32 ? 6 : 1;
+  const int slabs = (int)((depth + kSlab - 1) / kSlab);
+  const int64_t all = (int64_t)slabs * kPairs;
+  const int64_t first = all * tile.slice / t.splits, total = all * (tile.slice + 1) / t.splits - first;
+  int pair = slabs ? (int)(first / slabs) : 0, at_slab = (int)(first - (int64_t)pair * slabs);  // of the next slab to load
+
+  // kDw, gathered: where the rows of b's next slab lie.  Their tokens are asked for a slab
+  // ahead and taken once that slab has come, so that nothing waits for them.
+  constexpr bool kSeek = P == kDw && GATHER;
+  uint32_t seek[BC::kLoads], token[BC::kLoads], token_high[BC::kLoads];
+  const auto ask = [&]() {
+    if constexpr (kSeek) {
+#pragma unroll
+      for (int q = 0; q < BC::kLoads; ++q) {
+        const int64_t r = (int64_t)at_slab * kSlab + (q * C::threads + (int)threadIdx.x) / BC::kPieces;
+        const int64_t at = tile.begin + min(r, len - 1);
+        const uint32_t* p = static_cast<const uint32_t*>(g.token.p);
+        token[q] = p[g.token.wide ? 2 * at : at];
+        if (g.token.wide) token_high[q] = p[2 * at + 1];
+      }
+    }
+  };
+  const auto take = [&]() {
+    if constexpr (kSeek) {
+#pragma unroll
+      for (int q = 0; q < BC::kLoads; ++q) {
+        const int k = (q * C::threads + (int)threadIdx.x) / BC::kPieces;
+        const int64_t r = (int64_t)at_slab * kSlab + k;
+        const bool in = r < len && (!g.token.wide || token_high[q] == 0) && token[q] < (uint64_t)g.tokens;
+        // (the piece's 16 bytes of the tile's columns)
+        const uint32_t col = bc.vo[q] - (uint32_t)k * bc.row_bytes + 2u * (uint32_t)j0;
+        seek[q] = in ? token[q] * (uint32_t)row_b + col : kOutside;
+        asm volatile("" : "+v"(seek[q]));
+      }
+    }
+  };
+
+  // part 0: the next slab of a, part 1: that of b
+  const auto issue = [&](int buf, int part) {
+    const uint32_t at = lds0 + (uint32_t)buf * kStage;
+    const int64_t s = at_slab, k_left = depth - s * kSlab;
+    // the parts of a: 2 1 0 1 0 0, of b: 0 1 2 0 1 0
+    const int64_t oa = F32 ? (0x046 >> (2 * pair) & 3) * g.part_a : 0, ob = F32 ? (0x124 >> (2 * pair) & 3) * g.part_b : 0;
+    if (part == 0) {
+      const uint64_t pa = (uint64_t)(a + 2 * oa);
+      if constexpr (ACOLS) ac.load_bounded(at, pa + s * kSlab * row_a, bounded((k_left - 1) * row_a + 2 * (g.cols_a - i0)));
+      else ar.load(at, pa + 128 * s, GATHER ? bounded(gathered - 128 * s) : kMostBytes, k_left);
+      return;
+    }
+    const uint64_t pb = (uint64_t)(b + 2 * ob);
+    if constexpr (P == kOut) {
+      br.load(at + kA, pb + 128 * s, kMostBytes, k_left);
+    } else if constexpr (kSeek) {
+      const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+      const u32x4 r = tile_rsrc(pb, bounded(gathered));
+#pragma unroll
+      for (int q = 0; q < BC::kLoads; ++q) load_to_lds(at + kA + 16u * (q * C::threads + w * 64), r, seek[q], 0);
+    } else {
+      bc.load_bounded(at + kA, pb + s * kSlab * row_b, bounded((k_left - 1) * row_b + 2 * (g.cols_b - j0)));
+    }
+    if (++at_slab == slabs) {
+      at_slab = 0;
+      ++pair;
+    }
+  };
+
+  floatx16 acc[C::NA][C::NB];
+#pragma unroll
+  for (int x = 0; x < C::NA; ++x)
+#pragma unroll
+    for (int y = 0; y < C::NB; ++y)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[x][y][e] = 0.f;
+
+  struct Frags {
+    bf16x8 a[C::NA], b[C::NB];
+  };
+  // the fragments of k values kk .. kk + 15 of the slab in buffer `buf`
+  const auto read = [&](Frags& f, int buf, int kk) {
+    const char* at = lds + buf * kStage;
+    const char* bt = at + kA;
+#pragma unroll
+    for (int x = 0; x < C::NA; ++x) {
+      if constexpr (ACOLS) f.a[x] = AC::frag(at, (wm * C::NA + x) * 32, kk);
+      else f.a[x] = AR::frag(at, (wm * C::NA + x) * 32, kk);
+    }
+#pragma unroll
+    for (int y = 0; y < C::NB; ++y) {
+      if constexpr (BCOLS) f.b[y] = BC::frag(bt, (wn * C::NB + y) * 32, kk);
+      else f.b[y] = BR::frag(bt, (wn * C::NB + y) * 32, kk);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // The products of 16 k values (b first: a lane then holds 4 consecutive columns
+  // of one row); a part of the next slab is asked for behind the first of them.
+  const auto multiply = [&](const Frags& f, bool more, int buf, int part) {
+#pragma unroll
+    for (int x = 0; x < C::NA; ++x)
+#pragma unroll
+      for (int y = 0; y < C::NB; ++y) {
+        acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.b[y], f.a[x], acc[x][y], 0, 0, 0);
+        if (x == 0 && y == 1) {
+          __builtin_amdgcn_sched_barrier(0);
+          if (more) issue(buf, part);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+  // The fragments of 16 k values are read while those before are multiplied; once the last of
+  // a slab are in registers its buffer is free, so that the wait for the next slab and the
+  // first reads from it pass behind the last products of this one.
+  if (total > 0) {
+    ask();
+    take();
+    issue(0, 0);
+    issue(0, 1);
+    if (total > 1) ask();
+    wait_slabs<0>();
+    if (total > 1) take();
+    Frags f[2];
+    read(f[0], 0, 0);
+    if (total > 1) issue(1, 0);
+#pragma unroll 1
+    for (int64_t s = 0; s < total; ++s) {
+      const int buf = (int)(s & 1);
+#pragma unroll
+      for (int kk = 16; kk < kSlab; kk += 16) {
+        read(f[(kk / 16) & 1], buf, kk);
+        multiply(f[(kk / 16 + 1) & 1], kk == 16 && s + 1 < total, buf ^ 1, 1);
+        if (kk == 16 && s + 2 < total) ask();
+      }
+      wait_slabs<0>();  // slab s + 1 is in LDS, and every wave is done reading slab s
+      if (s + 2 < total) take();
+      if (s + 1 < total) read(f[0], buf ^ 1, 0);
+      multiply(f[1], s + 2 < total, buf, 0);
+    }
+  }
+  __syncthreads();  // every wave is done with the operands: LDS is free
+
+  // acc[x][y][4 q + e] = C(32 x + lane % 32, 32 y + 8 q + 4 (lane / 32) + e)
+  const int64_t col0 = j0 + wn * C::NB * 32;
+  const auto quad_of = [&](int x, int y, int q) {
+    return (floatx4){acc[x][y][4 * q], acc[x][y][4 * q + 1], acc[x][y][4 * q + 2], acc[x][y][4 * q + 3]};
+  };
+  const int64_t row_base = P == kDw ? 0 : tile.begin;
+
+  if (t.splits > 1) {
+    // a split's sums (its columns are padded: a quad of them is inside or outside)
+    const int64_t cols = ffn_pad(g.n), rows = P == kDw ? g.groups.experts * g.m : g.groups.rows;
+    float* part = g.partial + (tile.slice * rows + (P == kDw ? tile.group * g.m : row_base)) * cols;
+#pragma unroll
+    for (int x = 0; x < C::NA; ++x) {
+      const int64_t row = i0 + (wm * C::NA + x) * 32 + (lane & 31);
+      if (row >= m_all) continue;
+#pragma unroll
+      for (int y = 0; y < C::NB; ++y)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int64_t col = col0 + 32 * y + 8 * q + 4 * (lane >> 5);
+          if (col < cols) *reinterpret_cast<floatx4*>(part + row * cols + col) = quad_of(x, y, q);
+        }
+    }
+    return;
+  }
+
+  const int64_t out_at = (P == kDw ? tile.group * g.stride_out : 0) + row_base * g.ld_out;
+  if constexpr (F32) {
+    float* out = static_cast<float*>(g.out) + out_at;
+#pragma unroll
+    for (int x = 0; x < C::NA; ++x) {
+      const int64_t row = i0 + (wm * C::NA + x) * 32 + (lane & 31);
+      if (row >= m_all) continue;
+#pragma unroll
+      for (int y = 0; y < C::NB; ++y)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int64_t col = col0 + 32 * y + 8 * q + 4 * (lane >> 5);
+          if (col < g.n) store4(out + row * g.ld_out + col, quad_of(x, y, q), g.n - col);
+        }
+    }
+  } else {
+    char* ws = lds + wave * TileLds<C>::kWs;
+    uint16_t* out = static_cast<uint16_t*>(g.out) + out_at;
+#pragma unroll
+    for (int x = 0; x < C::NA; ++x) {
+#pragma unroll
+      for (int y = 0; y < C::NB; ++y)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          *reinterpret_cast<bf16x4*>(Patch_::quad(ws, 32 * y + 8 * q + 4 * (lane >> 5))) = rounded(quad_of(x, y, q));
+      wave_fence();
+      Patch_::store(ws, out, g.ld_out, i0 + (wm * C::NA + x) * 32, col0, m_all, g.n, m_all, g.n);
+      wave_fence();
+    }
+  }
+}
+
+template <ExpertProduct P, bool F32, bool GATHER, class C>
+__global__ void __launch_bounds__(C::threads, 2) expert_tile_kernel(TileArgs t) {
+  __shared__ __attribute__((aligned(1024))) char lds[TileLds<C>::kBytes];
+  // workgroups go round the 8 XCDs in turn
+  const int xcd = blockIdx.x & 7, slot = blockIdx.x >> 3, slots = gridDim.x >> 3;
+  int64_t all;
+  tile_at_cost<P, C>(t, 0, all);
+  const int64_t from = tile_at_cost<P, C>(t, all * xcd / 8, all), to = tile_at_cost<P, C>(t, all * (xcd + 1) / 8, all);
+  for (int64_t i = from + slot; i < to; i += slots) {
+    Tile tile;
+    if (!find_tile<P, C>(t, i, tile)) return;
+    multiply_tile<P, F32, GATHER, C>(t, tile, lds);
+    __syncthreads();  // the results have left LDS
+  }
+}
+
+typedef bf16x4 bf16x4_any __attribute__((aligned(2)));
+
+// The splits of a product added in their order.  One thread per quad of columns.
+template <ExpertProduct P, bool F32>
+__global__ void __launch_bounds__(256) expert_join_kernel(TileArgs t) {
+  const ExpertArgs& g = t.g;
+  const int64_t cols = ffn_pad(g.n), rows = P == kDw ? g.groups.experts * g.m : g.groups.rows;
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4, row = i / cols, col = i - row * cols;
+  if (row >= rows || col >= g.n) return;
+  floatx4 s = *reinterpret_cast<const floatx4*>(g.partial + i);
+  for (int k = 1; k < t.splits; ++k) s += *reinterpret_cast<const floatx4*>(g.partial + k * rows * cols + i);
+  int64_t at = row * g.ld_out + col;
+  if (P == kDw) {
+    const int64_t e = row / g.m;
+    at = e * g.stride_out + (row - e * g.m) * g.ld_out + col;
+  }
+  if constexpr (F32) {
+    store4(static_cast<float*>(g.out) + at, s, g.n - col);
+  } else {
+    uint16_t* out = static_cast<uint16_t*>(g.out) + at;
+    const bf16x4 r = rounded(s);
+    if (col + 4 <= g.n) {
+      *reinterpret_cast<bf16x4_any*>(out) = r;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (col + e < g.n) reinterpret_cast<__bf16*>(out)[e] = r[e];
+    }
+  }
+}
+
+template <ExpertProduct P, bool F32, bool GATHER, class C>
+void launch_shape(const ExpertArgs& g, int splits, int per_cu, hipStream_t st) {
+  TileArgs t;
+  t.g = g;
+  t.splits = splits;
+  t.tiles_n = (int)((g.n + C::TN - 1) / C::TN);
+  t.tiles_m = P == kDw ? (int)((g.m + C::TM - 1) / C::TM) : 0;
+  // (the most that the experts' sizes can make)
+  const int64_t tiles_m = P == kDw ? (int64_t)g.groups.experts * t.tiles_m
+                                   : g.groups.rows / C::TM + std::min<int64_t>(g.groups.rows, g.groups.experts + 1);
+  const int64_t most = tiles_m * t.tiles_n * splits, stay = (int64_t)kCus * per_cu;
+  const unsigned grid = (unsigned)std::min(stay, (most + 7) / 8 * 8);
+  hipLaunchKernelGGL((expert_tile_kernel<P, F32, GATHER, C>), dim3(grid), dim3(C::threads), 0, st, t);
+  if (splits > 1) {
+    const int64_t quads = (P == kDw ? g.groups.experts * g.m : g.groups.rows) * ffn_pad(g.n) / 4;
+    hipLaunchKernelGGL((expert_join_kernel<P, F32>), dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, st, t);
+  }
+}
+
+template <ExpertProduct P, bool F32, bool GATHER>
+hipError_t launch(const ExpertArgs& g, hipStream_t st) {
+  const ExpertPlan p = expert_plan(P, F32, g.groups.rows, g.groups.experts, g.m, g.n, g.k);
+  const int per_cu = kShape[p.shape].per_cu;
+  if (p.shape == kLarge) launch_shape<P, F32, GATHER, Large>(g, p.splits, per_cu, st);
+  else if (p.shape == kMiddle) launch_shape<P, F32, GATHER, Middle>(g, p.splits, per_cu, st);
+  else launch_shape<P, F32, GATHER, Small>(g, p.splits, per_cu, st);
+  return hipGetLastError();
+}
+
+template <ExpertProduct P, bool F32>
+hipError_t launch_product(const ExpertArgs& g, hipStream_t st) {
+  if constexpr (P != kDx) {
+    if (g.token.p) return launch<P, F32, true>(g, st);
+  }
+  return launch<P, F32, false>(g, st);
+}
+
+}  // namespace
+
+size_t expert_partial_bytes(ExpertProduct product, bool f32, int64_t rows, int64_t experts, int64_t m, int64_t n, int64_t k) {
+  return expert_partial_bytes(expert_plan(product, f32, rows, experts, m, n, k), product, rows, experts, m, n);
+}
+
+hipError_t launch_expert_tiles(ExpertProduct product, bool f32, const ExpertArgs& g, hipStream_t st) {
+  if (product == kOut) return f32 ? launch_product<kOut, true>(g, st) : launch_product<kOut, false>(g, st);
+  if (product == kDx) return f32 ? launch_product<kDx, true>(g, st) : launch_product<kDx, false>(g, st);
+  return f32 ? launch_product<kDw, true>(g, st) : launch_product<kDw, false>(g, st);
+}
+
+}  // namespace isoloco

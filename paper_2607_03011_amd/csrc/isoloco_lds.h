@@ -38,13 +38,17 @@ __device__ __forceinline__ void wait_slabs() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
-__device__ __forceinline__ u32x4 tile_rsrc(uint64_t base) {
+// A buffer of `bytes` bytes from base: loads at offsets past them give zeros.
+__device__ __forceinline__ u32x4 tile_rsrc(uint64_t base, uint32_t bytes = 0xffffffffu) {
   u32x4 r;
   r[0] = __builtin_amdgcn_readfirstlane((uint32_t)base);
   r[1] = __builtin_amdgcn_readfirstlane((uint32_t)(base >> 32) & 0xffffu);
-  r[2] = 0xffffffffu;
+  r[2] = __builtin_amdgcn_readfirstlane(bytes);
   r[3] = kBufferFlags;
   return r;
 }
+
+// An offset past any buffer of at most kMostBytes, that leaves room for 16 bytes and a slab's step
+constexpr uint32_t kOutside = 0xfffff000u, kMostBytes = 0xffffe000u;
 
 }  // namespace isoloco

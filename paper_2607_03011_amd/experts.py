@@ -52,8 +52,8 @@ def isoloco_route_tokens_backward(scores, ld_scores, dtype, tokens, experts, top
                                               dweight, dscores, ld_dscores, stream), "isoloco_route_tokens_backward")
 
 
-def isoloco_expert_matmul_workspace_size(tokens, rows, experts, dim, cols, dtype, flags):
-    return _size_of("isoloco_expert_matmul_workspace_size", tokens, rows, experts, dim, cols, dtype, flags)
+def isoloco_expert_matmul_workspace_size(tokens, rows, experts, dim, cols, ld_x, dtype, flags):
+    return _size_of("isoloco_expert_matmul_workspace_size", tokens, rows, experts, dim, cols, ld_x, dtype, flags)
 
 
 def isoloco_expert_matmul(x, ld_x, tokens, token, w, ld_w, stride_w, dtype, offsets, index_type, experts, rows, dim,
@@ -236,7 +236,7 @@ def expert_matmul(x, w, offsets, token=None, row=None, out=None, workspace=None)
         ld_out = _rows("out", out)[1]
         _written(out)
     keep, ws, ws_bytes = _workspace(workspace, isoloco_expert_matmul_workspace_size(
-        tokens, rows, experts, dim, cols, dtype, flags), x.device)
+        tokens, rows, experts, dim, cols, ld_x, dtype, flags), x.device)
     _check(_lib.isoloco_expert_matmul(at[0], ld_x, tokens, token_at, at[1], ld_w, stride_w, dtype, offsets.data_ptr(),
                                       index_type, experts, rows, dim, cols, out.data_ptr(), ld_out, ws, ws_bytes,
                                       _raw_stream(index)), "isoloco_expert_matmul")
@@ -267,7 +267,7 @@ def expert_matmul_backward(x, w, offsets, dout, token=None, row=None, need_dx=Tr
         dw = _empty(experts, cols, dim, dtype=x.dtype, device=device)
         dw_at = dw.data_ptr()
     keep, ws, ws_bytes = _workspace(workspace, isoloco_expert_matmul_workspace_size(
-        tokens, rows, experts, dim, cols, dtype, flags | ISOLOCO_EXPERTS_BACKWARD), device)
+        tokens, rows, experts, dim, cols, ld_x, dtype, flags | ISOLOCO_EXPERTS_BACKWARD), device)
     _check(_lib.isoloco_expert_matmul_backward(at[0], ld_x, tokens, token_at, at[1], ld_w, stride_w, dtype,
                                                offsets.data_ptr(), index_type, experts, rows, dim, cols, d_at, ld_dout,
                                                dx_at, dim, dw_at, dim, cols * dim, ws, ws_bytes, _raw_stream(index)),

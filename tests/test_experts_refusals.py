@@ -68,6 +68,9 @@ EXPERTS = dict(x=A, ld_x=64, tokens=20, token=B, w=C, ld_w=64, stride_w=2048, dt
     (ALIGN, dict(x=A + 1)), (ALIGN, dict(w=C + 1)), (ALIGN, dict(out=E + 1)), (ALIGN, dict(offsets=D + 2)),
     (ALIGN, dict(token=B + 1)), (ALIAS, dict(out=A)), (ALIAS, dict(out=C + 64)), (ALIAS, dict(out=B)),
     (ALIAS, dict(out=D)),
+    # (float32, and rows of 60: copies)
+    (WORKSPACE, dict(dtype=0, workspace=0)), (WORKSPACE, dict(dim=60, ws_bytes=64)),
+    (WORKSPACE, dict(dtype=0, workspace=WS + 8)), (ALIAS, dict(dtype=0, out=WS + 256)),
 ])
 def test_expert_matmul_refuses(status, change):
     refused(status, iso.isoloco_expert_matmul, *changed(EXPERTS, **change))
@@ -83,6 +86,7 @@ EXPERTS_GRAD = dict(x=A, ld_x=64, tokens=20, token=B, w=C, ld_w=64, stride_w=204
     (INVALID, dict(token=0)), (INVALID, dict(ld_dx=10)), (INVALID, dict(ld_dw=10)), (INVALID, dict(ld_dout=31)),
     (INVALID, dict(stride_dw=100)), (INVALID, dict(index_type=-1)), (ALIGN, dict(dx=F + 2)), (ALIGN, dict(dw=F + 65537)),
     (ALIGN, dict(offsets=D + 4)), (ALIAS, dict(dx=A)), (ALIAS, dict(dw=F)), (ALIAS, dict(dw=E)), (ALIAS, dict(dx=C)),
+    (WORKSPACE, dict(workspace=0)), (WORKSPACE, dict(ws_bytes=64)), (WORKSPACE, dict(workspace=WS + 16)),
 ])
 def test_expert_matmul_backward_refuses(status, change):
     refused(status, iso.isoloco_expert_matmul_backward, *changed(EXPERTS_GRAD, **change))
@@ -154,8 +158,8 @@ def test_distill_backward_refuses(status, change):
 def test_workspace_sizes_refuse():
     refused(INVALID, iso.isoloco_route_tokens_workspace_size, -1, 8)
     refused(INVALID, iso.isoloco_route_tokens_workspace_size, 5, 0)
-    refused(INVALID, iso.isoloco_expert_matmul_workspace_size, 5, 5, 0, 8, 8, 0, 0)
-    refused(INVALID, iso.isoloco_expert_matmul_workspace_size, 5, 5, 1, 8, 8, 0, 8)
+    refused(INVALID, iso.isoloco_expert_matmul_workspace_size, 5, 5, 0, 8, 8, 8, 0, 0)
+    refused(INVALID, iso.isoloco_expert_matmul_workspace_size, 5, 5, 1, 8, 8, 8, 0, 8)
     refused(INVALID, iso.isoloco_distill_loss_workspace_size, 5, 0)
 
 
