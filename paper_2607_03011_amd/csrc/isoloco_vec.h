@@ -66,20 +66,28 @@ __device__ __forceinline__ float value_of(uint64_t key) {
 __device__ __forceinline__ int64_t index_of(uint64_t key) { return (int64_t)(uint32_t)~(uint32_t)key; }
 __device__ __forceinline__ uint64_t max64(uint64_t a, uint64_t b) { return a > b ? a : b; }
 
-// The first `left` values of a row's piece of 16 bytes, zeros after them
-template <typename T>
-__device__ __forceinline__ void load_piece(const T* p, int64_t left, float* x) {
+// The first `left` values of a row's piece of 16 bytes as they are stored, zeros after them.
+// PAST: of data that is read once and larger than the caches.
+template <typename T, bool PAST = false>
+__device__ __forceinline__ u32x4 load_raw(const T* p, int64_t left) {
   if (left >= Vec<T>::N) {
-    unpack<T>(*reinterpret_cast<const u32x4_any*>(p), x);
-  } else {
-#pragma unroll
-    for (int e = 0; e < Vec<T>::N; ++e) x[e] = e < left ? (float)p[e] : 0.f;
+    if constexpr (PAST) return __builtin_nontemporal_load(reinterpret_cast<const u32x4_any*>(p));
+    return *reinterpret_cast<const u32x4_any*>(p);
   }
+  float x[Vec<T>::N];
+#pragma unroll
+  for (int e = 0; e < Vec<T>::N; ++e) x[e] = e < left ? (float)p[e] : 0.f;
+  return pack<T>(x);
 }
 template <typename T>
+__device__ __forceinline__ void load_piece(const T* p, int64_t left, float* x) {
+  unpack<T>(load_raw<T>(p, left), x);
+}
+template <typename T, bool PAST = false>
 __device__ __forceinline__ void store_piece(T* p, int64_t left, const float* x) {
   if (left >= Vec<T>::N) {
-    *reinterpret_cast<u32x4_any*>(p) = pack<T>(x);
+    if constexpr (PAST) __builtin_nontemporal_store(pack<T>(x), reinterpret_cast<u32x4_any*>(p));
+    else *reinterpret_cast<u32x4_any*>(p) = pack<T>(x);
   } else {
 #pragma unroll
     for (int e = 0; e < Vec<T>::N; ++e)
