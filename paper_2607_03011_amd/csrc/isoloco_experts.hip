@@ -51,8 +51,152 @@ size_t experts_bytes(const ExpertShape& s, int64_t ld, int64_t stride) {
   return (size_t)(s.experts - 1) * stride * dtype_bytes(s.dtype) + matrix_bytes(s.cols, s.dim, ld, dtype_bytes(s.dtype));
 }
 
+// ---------------------------------------------------------------------------
+// Few rows an expert
+// ---------------------------------------------------------------------------
+//
+// Products of few rows are bounded by the weights' bytes: a workgroup takes 16 rows of an
+// expert's weights, which go from memory into the registers that the MFMA reads, and its
+// waves split dim so that enough loads are in flight.  Experts without rows are not read.
+// Any alignment, float32 as it is: no copies.
+
+struct FewArgs {
+  Groups groups;
+  Index token;
+  int64_t tokens, dim, cols, ld_x, ld_w, stride_w, ld_out;
+};
+
+constexpr int kFewWaves = 8;
+
+// The values of k that a lane holds of one row, 16 bytes: its MFMA operands.  (Which k a lane's
+// e-th value stands for is the same in both operands.)
+__device__ __forceinline__ floatx4 multiply16(u32x4 a, u32x4 b, floatx4 c, __bf16) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ floatx4 multiply16(u32x4 a, u32x4 b, floatx4 c, float) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[e]), __uint_as_float(b[e]), c, 0, 0, 0);
+  return c;
+}
+
+// Rows `first` .. of the expert, up to 16 NT of them.
+template <typename T, int NT>
+__device__ __forceinline__ void few_rows(const FewArgs& g, const T* x, const T* w, T* out, int64_t first, int64_t end,
+                                         int64_t n0, floatx4 (*sums)[NT][64]) {
+  constexpr int N = Vec<T>::N, kStep = 4 * N;  // k values of one step
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, kl = (lane >> 4) * N;
+  // rows past the matrix and past the expert's are their last ones again: their outputs are not stored
+  const T* pw = w + min(n0 + row, g.cols - 1) * g.ld_w + kl;
+  const T* px[NT];
+  bool none[NT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const int64_t r = min(first + 16 * n + row, end - 1), t = g.token.p ? g.token.get(r) : r;
+    none[n] = t < 0 || t >= g.tokens;  // a row of zeros
+    px[n] = x + (none[n] ? 0 : t * g.ld_x) + kl;
+  }
+  floatx4 s[NT] = {};
+  // kAhead steps' loads are in flight at a time (2, 4, 8, 16 of them: 67.8, 65.7, 63.2, 149 us
+  // for one row each of 64 experts of 1408 x 2048 in bfloat16, 369 MB, and for one row of 8 of
+  // 2048 x 768 6.4, 7.4, 7.5, 11.0; with the weights read past the caches 72.5 and 7.5)
+  constexpr int kAhead = 4;
+  constexpr int64_t kStride = kFewWaves * kStep;
+  int64_t k = (int64_t)wave * kStep;
+  for (; k + (kAhead - 1) * kStride + kStep <= g.dim; k += kAhead * kStride) {
+    u32x4 a[kAhead], c[kAhead][NT];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      a[i] = *reinterpret_cast<const u32x4_any*>(pw + k + i * kStride);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        c[i][n] = (u32x4){};
+        if (!none[n]) c[i][n] = *reinterpret_cast<const u32x4_any*>(px[n] + k + i * kStride);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) s[n] = multiply16(a[i], c[i][n], s[n], T());
+  }
+  for (; k < g.dim; k += kStride) {
+    const int64_t left = g.dim - k - kl;
+    const u32x4 a = load_raw<T>(pw + k, left);
+#pragma unroll
+    for (int n = 0; n < NT; ++n) s[n] = multiply16(a, load_raw<T>(px[n] + k, none[n] ? 0 : left), s[n], T());
+  }
+#pragma unroll
+  for (int n = 0; n < NT; ++n) sums[wave][n][lane] = s[n];
+  __syncthreads();
+  // lane l holds columns n0 + 4 (l / 16) .. + 3 of row l % 16; wave n finishes 16 rows
+  const int64_t r = first + 16 * wave + row;
+  if (wave < NT && r < end) {
+    floatx4 v = {};
+    for (int i = 0; i < kFewWaves; ++i) v += sums[i][wave][lane];
+    const int64_t col = n0 + 4 * (lane >> 4);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (col + e < g.cols) out[r * g.ld_out + col + e] = (T)v[e];
+  }
+  __syncthreads();  // the sums are read
+}
+
+template <typename T, int NT>
+__global__ void __launch_bounds__(64 * kFewWaves, 4) expert_few_kernel(FewArgs g, const T* x, const T* w, T* out, int blocks_n) {
+  __shared__ floatx4 sums[kFewWaves][NT][64];
+  const int e = blockIdx.x / blocks_n;
+  const int64_t n0 = (int64_t)(blockIdx.x - e * blocks_n) * 16;
+  int64_t first, end;
+  g.groups.rows_of(e, first, end);
+  if (e == g.groups.experts) {  // rows of no expert: zeros
+    for (int64_t i = threadIdx.x; i < (end - first) * 16; i += 64 * kFewWaves) {
+      const int64_t col = n0 + (i & 15);
+      if (col < g.cols) out[(first + (i >> 4)) * g.ld_out + col] = (T)0.f;
+    }
+    return;
+  }
+  w += e * g.stride_w;
+  for (; first < end; first += 16 * NT) few_rows<T, NT>(g, x, w, out, first, end, n0, sums);
+}
+
+// Up to this many rows an expert, on average, come here, the others go to the tiles.  Both
+// sides measured, us a call of a graph, here / tiles, for 64 experts of 1408 x 2048 and for 8 of
+// 2048 x 768:
+//   rows an expert   1             4             8             16            32            64            96
+//   bfloat16         65.7 / 78.2   69.5 / 78.1   82.8 / 80.0   109 / 105     142 / 107     263 / 112
+//                    7.4 / 12.1    8.2 / 12.5    8.9 / 12.5    10.9 / 13.8   12.9 / 13.0   22.2 / 13.5
+//   float32          134 / 716     149 / 721     170 / 718     227 / 729     292 / 739     531 / 761     773 / 952
+//                    13.9 / 50.0   14.2 / 49.2   14.5 / 49.5   20.3 / 50.1   23.4 / 51.4   40.8 / 55.0   58.2 / 60.9
+// bfloat16 weights that the tiles would have copied first (150 us of the first kind) are as
+// float32 in this.
+bool few_of(int32_t dtype, int64_t rows, int64_t experts, bool copies) {
+  return rows <= (dtype == ISOLOCO_F32 ? 96 : copies ? 48 : 16) * experts;
+}
+
+template <typename T, int NT>
+void launch_few_rows(const FewArgs& g, const void* x, const void* w, void* out, hipStream_t st) {
+  const int blocks_n = (int)((g.cols + 15) / 16);
+  hipLaunchKernelGGL((expert_few_kernel<T, NT>), dim3((unsigned)((g.groups.experts + 1) * blocks_n)), dim3(64 * kFewWaves), 0,
+                     st, g, static_cast<const T*>(x), static_cast<const T*>(w), static_cast<T*>(out), blocks_n);
+}
+
+// 16 rows at a time, or 32 where an expert has more on average than 8: 16 rows each of 64 experts,
+// as above, 106 / 109 us in bfloat16 and 209 / 227 in float32, 24 rows 186 / 125 and 351 / 258.
+// (64 at a time: 24 rows 181 and 390.)
+template <typename T>
+hipError_t launch_few(const FewArgs& g, const void* x, const void* w, void* out, hipStream_t st) {
+  if (g.groups.rows <= 8 * g.groups.experts) launch_few_rows<T, 1>(g, x, w, out, st);
+  else launch_few_rows<T, 2>(g, x, w, out, st);
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------------------
+// The tile products' operands
+// ---------------------------------------------------------------------------
+
 // What a call hands to the tile products, and where its copies lie in the workspace.
 struct CallPlan {
+  bool few;                     // expert_few_kernel
   bool copy_x, copy_w, copy_d;  // operands that the tiles do not read where they are
   bool gather_x;                // the copy of x has the grouped rows
   size_t x, w, d, partial, bytes;
@@ -67,6 +211,8 @@ bool tile_rows(const void* p, int64_t cols, int64_t ld) {
 CallPlan call_plan(const ExpertShape& s, bool gathered, bool dx, bool dw, bool x_ok, bool w_ok, bool d_ok, int64_t ld_x) {
   CallPlan p = {};
   const bool f32 = s.dtype == ISOLOCO_F32, back = dx || dw;
+  p.few = !back && few_of(s.dtype, s.rows, s.experts, !w_ok);
+  if (p.few) return p;
   const size_t parts = f32 ? kFfnParts : 1;
   const int64_t dim = ffn_pad(s.dim), cols = ffn_pad(s.cols);
   const auto take = [&](size_t bytes) {
@@ -206,6 +352,11 @@ ExpertArgs args_of(const Call& c, const Operands& o, const CallPlan& p, char* ws
 }
 
 hipError_t run_forward(const Call& c, const CallPlan& p, void* out, int64_t ld_out, char* ws, hipStream_t st) {
+  if (p.few) {
+    const FewArgs g = {{c.offsets, c.s.rows, (int)c.s.experts}, c.token, c.s.tokens, c.s.dim, c.s.cols, c.ld_x, c.ld_w,
+                       c.stride_w, ld_out};
+    return c.s.dtype == ISOLOCO_F32 ? launch_few<float>(g, c.x, c.w, out, st) : launch_few<__bf16>(g, c.x, c.w, out, st);
+  }
   const Operands o = copy_operands(c, p, ws, st);
   ExpertArgs g = args_of(c, o, p, ws);
   g.a = o.x;
@@ -277,7 +428,10 @@ isoloco_status isoloco_expert_matmul_workspace_size(int64_t tokens, int64_t rows
   if (flags & ~(ISOLOCO_EXPERTS_BACKWARD | ISOLOCO_EXPERTS_ALIGNED | ISOLOCO_EXPERTS_GATHERED))
     return fail(ISOLOCO_ERR_INVALID_ARG, "flags = %d", flags);
   const bool ok = flags & ISOLOCO_EXPERTS_ALIGNED, back = flags & ISOLOCO_EXPERTS_BACKWARD;
-  *bytes = call_plan(s, flags & ISOLOCO_EXPERTS_GATHERED, back, back, ok, ok, ok, ld_x).bytes;
+  // (without ALIGNED the operands may be either)
+  const bool gathered = flags & ISOLOCO_EXPERTS_GATHERED;
+  *bytes = call_plan(s, gathered, back, back, true, true, true, ld_x).bytes;
+  if (!ok) *bytes = std::max(*bytes, call_plan(s, gathered, back, back, false, false, false, ld_x).bytes);
   return ISOLOCO_OK;
 }
 

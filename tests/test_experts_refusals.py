@@ -68,9 +68,9 @@ EXPERTS = dict(x=A, ld_x=64, tokens=20, token=B, w=C, ld_w=64, stride_w=2048, dt
     (ALIGN, dict(x=A + 1)), (ALIGN, dict(w=C + 1)), (ALIGN, dict(out=E + 1)), (ALIGN, dict(offsets=D + 2)),
     (ALIGN, dict(token=B + 1)), (ALIAS, dict(out=A)), (ALIAS, dict(out=C + 64)), (ALIAS, dict(out=B)),
     (ALIAS, dict(out=D)),
-    # (float32, and rows of 60: copies)
-    (WORKSPACE, dict(dtype=0, workspace=0)), (WORKSPACE, dict(dim=60, ws_bytes=64)),
-    (WORKSPACE, dict(dtype=0, workspace=WS + 8)), (ALIAS, dict(dtype=0, out=WS + 256)),
+    # (float32, and rows of 60: copies, once the rows are many)
+    (WORKSPACE, dict(dtype=0, rows=1000, workspace=0)), (WORKSPACE, dict(dim=60, rows=1000, ws_bytes=64)),
+    (WORKSPACE, dict(dtype=0, rows=1000, workspace=WS + 8)), (ALIAS, dict(dtype=0, rows=1000, out=WS + 256)),
 ])
 def test_expert_matmul_refuses(status, change):
     refused(status, iso.isoloco_expert_matmul, *changed(EXPERTS, **change))
