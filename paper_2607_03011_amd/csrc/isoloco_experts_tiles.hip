@@ -40,32 +40,16 @@ struct Tile {
   int64_t begin, end;  // the group's rows
 };
 
-constexpr int64_t kTileCost = 4;  // slabs that a tile's start and end take
+constexpr int kTileCost = 4;  // slabs that a tile's start and end take
 
-// What a group's tiles are and cost (kDw: slabs of its rows).
-template <ExpertProduct P, class C>
-__device__ __forceinline__ void group_of(const TileArgs& t, int e, int64_t& begin, int64_t& end, int64_t& tiles,
-                                         int64_t& cost) {
-  begin = end = tiles = cost = 0;
-  if (e > t.g.groups.experts || (P == kDw && e == t.g.groups.experts)) return;
-  t.g.groups.rows_of(e, begin, end);
-  if (P == kDw) {
-    tiles = (int64_t)t.tiles_m * t.tiles_n * t.splits;
-    cost = (end - begin + kSlab - 1) / kSlab + kTileCost * t.splits;
-  } else {
-    tiles = (end - begin + C::TM - 1) / C::TM * t.tiles_n * t.splits;
-    cost = 1;
-  }
-  cost *= tiles;
-}
-
-__device__ __forceinline__ int64_t scan64(int64_t v) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
-    const int64_t o = __shfl_up((long long)v, off, 64);
-    if (lane >= off) v += o;
-  }
+// The sum over the lanes up to this one
+__device__ __forceinline__ int scan(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);  // a row of 16: 1, 2, 4, 8 lanes on
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // the last of a row to the next row
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // the last of two rows to the other two
   return v;
 }
 
@@ -75,58 +59,86 @@ __device__ __forceinline__ int64_t lane_of(int64_t v, int at) {
   return (int64_t)((uint64_t)hi << 32 | lo);
 }
 
-// The tile at which the costs of those before reach `cost` (all tiles, if none does); the
-// costs of all tiles.  Every wave by itself.
+// Where the tiles lie, 64 experts at a time, one a lane: every wave by itself.  What an expert
+// counts are its tiles, or (kDw, where all have as many) the slabs of its tiles.
 template <ExpertProduct P, class C>
-__device__ __forceinline__ int64_t tile_at_cost(const TileArgs& t, int64_t cost, int64_t& all) {
-  int64_t tiles_before = 0, found = -1;
-  all = 0;
-  for (int base = 0; base <= t.g.groups.experts; base += 64) {
-    int64_t b, f, tiles, c;
-    group_of<P, C>(t, base + (threadIdx.x & 63), b, f, tiles, c);
-    const int64_t cost_sum = scan64(c), tile_sum = scan64(tiles);
-    const uint64_t past = __ballot(all + cost_sum > cost);
-    if (found < 0 && past) {
-      const int at = __ffsll((unsigned long long)past) - 1;
-      const int64_t own = tiles == 0 ? 0 : (cost - all - (cost_sum - c)) / (c / tiles);
-      found = lane_of(tiles_before + tile_sum - tiles + own, at);
+struct Finder {
+  int64_t begin, end;  // of this lane's expert
+  int own, upto;       // its count, and the counts up to it
+  int base;            // of the 64
+  __device__ __forceinline__ void load(const TileArgs& t, int first) {
+    const int e = first + (threadIdx.x & 63);
+    base = first;
+    begin = end = 0;
+    own = 0;
+    if (e < t.g.groups.experts) {
+      t.g.groups.rows_of(e, begin, end);
+      own = P == kDw ? (int)((end - begin + kSlab - 1) / kSlab) + kTileCost * t.splits
+                     : (int)((end - begin + C::TM - 1) / C::TM) * t.tiles_n * t.splits;
     }
-    all += lane_of(cost_sum, 63);
-    tiles_before += lane_of(tile_sum, 63);
+    upto = scan(own);
   }
-  return found < 0 ? tiles_before : found;
-}
-
-// The index-th tile.  Within a group slices come first, then bands of 8 rows of tiles.
-template <ExpertProduct P, class C>
-__device__ __forceinline__ bool find_tile(const TileArgs& t, int64_t index, Tile& o) {
-  int64_t before = 0;
-  for (int base = 0; base <= t.g.groups.experts; base += 64) {
-    int64_t b, f, tiles, c;
-    group_of<P, C>(t, base + (threadIdx.x & 63), b, f, tiles, c);
-    const int64_t sum = scan64(tiles);
-    const uint64_t past = __ballot(before + sum > index);
-    if (past) {
-      const int at = __ffsll((unsigned long long)past) - 1;
+  // all counts
+  __device__ __forceinline__ int all(const TileArgs& t) {
+    int sum = 0;
+    for (int first = 0; first < t.g.groups.experts; first += 64) {
+      if (first != base) load(t, first);
+      sum += __builtin_amdgcn_readlane(upto, 63);
+    }
+    return sum;
+  }
+  // the lane whose count passes `index`, and what is before the lane's 64; -1: none does
+  __device__ __forceinline__ int pass(const TileArgs& t, int index, int& before) {
+    before = 0;
+    for (int first = 0; first < t.g.groups.experts; first += 64) {
+      if (first != base) load(t, first);
+      const uint64_t past = __ballot(before + upto > index);
+      if (past) return __ffsll((unsigned long long)past) - 1;
+      before += __builtin_amdgcn_readlane(upto, 63);
+    }
+    return -1;
+  }
+  // kDw: the tile that begins where the counts reach `index`
+  __device__ __forceinline__ int64_t tile_at(const TileArgs& t, int index) {
+    const int64_t per = (int64_t)t.tiles_m * t.tiles_n * t.splits;
+    int before;
+    const int at = pass(t, index, before);
+    if (at < 0) return t.g.groups.experts * per;
+    const int count = __builtin_amdgcn_readlane(own, at), past = __builtin_amdgcn_readlane(upto, at) - count;
+    return (base + at) * per + (index - before - past) * per / count;
+  }
+  // The index-th tile.  Within an expert slices come first, then bands of 8 rows of tiles.
+  __device__ __forceinline__ Tile tile(const TileArgs& t, int64_t index) {
+    Tile o;
+    int64_t i;
+    if (P == kDw) {
+      const int64_t per = (int64_t)t.tiles_m * t.tiles_n * t.splits;
+      o.group = (int)(index / per);
+      i = index - o.group * per;
+      if (o.group < base || o.group >= base + 64) load(t, o.group & ~63);
+      const int at = o.group - base;
+      o.begin = lane_of(begin, at);
+      o.end = lane_of(end, at);
+    } else {
+      int before;
+      const int at = pass(t, (int)index, before);
       o.group = base + at;
-      o.begin = lane_of(b, at);
-      o.end = lane_of(f, at);
-      const int64_t i = lane_of(index - before - (sum - tiles), at);
-      const int tiles_m = P == kDw ? t.tiles_m : (int)((o.end - o.begin + C::TM - 1) / C::TM);
-      const int64_t plane = (int64_t)tiles_m * t.tiles_n, band_of = (int64_t)8 * t.tiles_n;
-      o.slice = (int)(i / plane);
-      int64_t in = i - o.slice * plane;
-      const int band = (int)(in / band_of);
-      in -= band * band_of;
-      const int rows = min(8, tiles_m - band * 8);
-      o.tm = band * 8 + (int)(in % rows);
-      o.tn = (int)(in / rows);
-      return true;
+      i = (int)index - before - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(own, at));
+      o.begin = lane_of(begin, at);
+      o.end = lane_of(end, at);
     }
-    before += lane_of(sum, 63);
+    const int tiles_m = P == kDw ? t.tiles_m : (int)((o.end - o.begin + C::TM - 1) / C::TM);
+    const uint32_t plane = (uint32_t)tiles_m * t.tiles_n, band_of = 8u * t.tiles_n;
+    o.slice = (int)((uint32_t)i / plane);
+    uint32_t in = (uint32_t)i - o.slice * plane;
+    const uint32_t band = in / band_of;
+    in -= band * band_of;
+    const uint32_t rows = min(8, tiles_m - (int)band * 8);
+    o.tm = (int)(band * 8 + in % rows);
+    o.tn = (int)(in / rows);
+    return o;
   }
-  return false;
-}
+};
 
 // Bytes from a place to the end of its buffer, as a buffer's size
 __device__ __forceinline__ uint32_t bounded(int64_t bytes) { return (uint32_t)min(max(bytes, (int64_t)0), (int64_t)kMostBytes); }
@@ -152,10 +164,9 @@ __device__ __forceinline__ void multiply_tile(const TileArgs& t, const Tile& til
   const ExpertArgs& g = t.g;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / C::WN, wn = wave % C::WN;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)lds;
-  const bool none = tile.group >= g.groups.experts;  // rows of no expert: zeros
   const int64_t len = tile.end - tile.begin, i0 = (int64_t)tile.tm * C::TM, j0 = (int64_t)tile.tn * C::TN;
   const int64_t m_all = P == kDw ? g.m : len;  // rows of this output
-  const int64_t depth = none ? 0 : P == kDw ? len : g.k;
+  const int64_t depth = P == kDw ? len : g.k;
   const int64_t row_a = 2 * g.ld_a, row_b = 2 * g.ld_b;  // bytes
   const int64_t gathered = 2 * g.tokens * (P == kDw ? g.ld_b : g.ld_a);  // bytes of what token reads
 
@@ -395,14 +406,28 @@ __global__ void __launch_bounds__(C::threads, 2) expert_tile_kernel(TileArgs t) 
   __shared__ __attribute__((aligned(1024))) char lds[TileLds<C>::kBytes];
   // workgroups go round the 8 XCDs in turn
   const int xcd = blockIdx.x & 7, slot = blockIdx.x >> 3, slots = gridDim.x >> 3;
-  int64_t all;
-  tile_at_cost<P, C>(t, 0, all);
-  const int64_t from = tile_at_cost<P, C>(t, all * xcd / 8, all), to = tile_at_cost<P, C>(t, all * (xcd + 1) / 8, all);
+  Finder<P, C> finder;
+  finder.load(t, 0);
+  const int64_t all = finder.all(t);
+  int64_t from = all * xcd / 8, to = all * (xcd + 1) / 8;
+  if (P == kDw) {
+    from = finder.tile_at(t, (int)from);
+    to = finder.tile_at(t, (int)to);
+  }
   for (int64_t i = from + slot; i < to; i += slots) {
-    Tile tile;
-    if (!find_tile<P, C>(t, i, tile)) return;
-    multiply_tile<P, F32, GATHER, C>(t, tile, lds);
+    multiply_tile<P, F32, GATHER, C>(t, finder.tile(t, i), lds);
     __syncthreads();  // the results have left LDS
+  }
+  // rows of no expert
+  if (P != kDw && t.splits == 1) {
+    const ExpertArgs& g = t.g;
+    int64_t begin, end;
+    g.groups.rows_of(g.groups.experts, begin, end);
+    for (int64_t r = begin + blockIdx.x; r < end; r += gridDim.x)
+      for (int64_t c = threadIdx.x; c < g.n; c += C::threads) {
+        if constexpr (F32) static_cast<float*>(g.out)[r * g.ld_out + c] = 0.f;
+        else static_cast<uint16_t*>(g.out)[r * g.ld_out + c] = 0;
+      }
   }
 }
 
@@ -415,8 +440,15 @@ __global__ void __launch_bounds__(256) expert_join_kernel(TileArgs t) {
   const int64_t cols = ffn_pad(g.n), rows = P == kDw ? g.groups.experts * g.m : g.groups.rows;
   const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4, row = i / cols, col = i - row * cols;
   if (row >= rows || col >= g.n) return;
-  floatx4 s = *reinterpret_cast<const floatx4*>(g.partial + i);
-  for (int k = 1; k < t.splits; ++k) s += *reinterpret_cast<const floatx4*>(g.partial + k * rows * cols + i);
+  bool some = true;
+  if (P != kDw) {
+    int64_t begin, end;
+    g.groups.rows_of(g.groups.experts, begin, end);
+    some = row < begin;  // (rows of no expert: zeros)
+  }
+  floatx4 s = {};
+  if (some)
+    for (int k = 0; k < t.splits; ++k) s += *reinterpret_cast<const floatx4*>(g.partial + k * rows * cols + i);
   int64_t at = row * g.ld_out + col;
   if (P == kDw) {
     const int64_t e = row / g.m;
@@ -438,32 +470,33 @@ __global__ void __launch_bounds__(256) expert_join_kernel(TileArgs t) {
 }
 
 template <ExpertProduct P, bool F32, bool GATHER, class C>
-void launch_shape(const ExpertArgs& g, int splits, int per_cu, hipStream_t st) {
+hipError_t launch_shape(const ExpertArgs& g, int splits, int per_cu, hipStream_t st) {
   TileArgs t;
   t.g = g;
   t.splits = splits;
   t.tiles_n = (int)((g.n + C::TN - 1) / C::TN);
   t.tiles_m = P == kDw ? (int)((g.m + C::TM - 1) / C::TM) : 0;
-  // (the most that the experts' sizes can make)
+  // (the most that the experts' sizes can make; tiles are counted in 32 bits)
   const int64_t tiles_m = P == kDw ? (int64_t)g.groups.experts * t.tiles_m
-                                   : g.groups.rows / C::TM + std::min<int64_t>(g.groups.rows, g.groups.experts + 1);
+                                   : g.groups.rows / C::TM + std::min<int64_t>(g.groups.rows, g.groups.experts);
   const int64_t most = tiles_m * t.tiles_n * splits, stay = (int64_t)kCus * per_cu;
+  if (most > INT32_MAX) return hipErrorInvalidConfiguration;
   const unsigned grid = (unsigned)std::min(stay, (most + 7) / 8 * 8);
   hipLaunchKernelGGL((expert_tile_kernel<P, F32, GATHER, C>), dim3(grid), dim3(C::threads), 0, st, t);
   if (splits > 1) {
     const int64_t quads = (P == kDw ? g.groups.experts * g.m : g.groups.rows) * ffn_pad(g.n) / 4;
     hipLaunchKernelGGL((expert_join_kernel<P, F32>), dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, st, t);
   }
+  return hipGetLastError();
 }
 
 template <ExpertProduct P, bool F32, bool GATHER>
 hipError_t launch(const ExpertArgs& g, hipStream_t st) {
   const ExpertPlan p = expert_plan(P, F32, g.groups.rows, g.groups.experts, g.m, g.n, g.k);
   const int per_cu = kShape[p.shape].per_cu;
-  if (p.shape == kLarge) launch_shape<P, F32, GATHER, Large>(g, p.splits, per_cu, st);
-  else if (p.shape == kMiddle) launch_shape<P, F32, GATHER, Middle>(g, p.splits, per_cu, st);
-  else launch_shape<P, F32, GATHER, Small>(g, p.splits, per_cu, st);
-  return hipGetLastError();
+  if (p.shape == kLarge) return launch_shape<P, F32, GATHER, Large>(g, p.splits, per_cu, st);
+  if (p.shape == kMiddle) return launch_shape<P, F32, GATHER, Middle>(g, p.splits, per_cu, st);
+  return launch_shape<P, F32, GATHER, Small>(g, p.splits, per_cu, st);
 }
 
 template <ExpertProduct P, bool F32>
