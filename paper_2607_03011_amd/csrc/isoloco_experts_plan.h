@@ -30,18 +30,31 @@ inline double expert_tiles(const ShapeInfo& h, ExpertProduct p, int64_t rows, in
   return groups * std::max(1.0, even / h.tm + 0.5) * tiles_n;
 }
 
+// The tiles and splits that take the least time by the rounds of the workgroups, as plan_of does
+// it.  dw's tiles are as deep as their experts have rows: the workgroups follow each other
+// there, and an expert of twice the mean is expected (by whole rounds alone 47 where the
+// 128-square tiles take 35.5 us: 4096 rows of 8 experts of 2048 x 768).  Both sides measured, us
+// on 256-square / 192 x 256 / 128-square tiles, uneven experts in bfloat16:
+//   4096 rows, 8 experts of 2048 x 768     out 25.6 / 21.9 / 28.0   dx 46.4 / 39.8 / 31.1   dw 47.4 / 43.3 / 35.5
+//   16384 rows, 8 experts of 1408 x 2048   out 106 / 122 / 107      dx 116 / 97.4 / 115     dw 140 / 154 / 129
+//   32768 rows, 64 experts of 512 x 1024   out 56.0 / 48.6 / 53.1   dx 57.5 / 58.6 / 56.6   dw 60.9 / 66.4 / 61.0
+// and in 1 / 2 / 3 / 6 splits on 128-square ones: dx of 1400 rows, 5 experts of 1637 x 612 in
+// float32 142 / 85 / 70 / 54.
 inline ExpertPlan expert_plan(ExpertProduct p, bool f32, int64_t rows, int64_t experts, int64_t m, int64_t n, int64_t k) {
-  const int64_t depth = p == kDw ? (rows + experts - 1) / experts : k;
-  const int64_t slabs = std::max<int64_t>(1, (depth + kSlab - 1) / kSlab) * (f32 ? 6 : 1);
+  const double parts = f32 ? 6 : 1;
+  const double depth = p == kDw ? std::max(1.0, (double)rows / experts / kSlab) * parts
+                                : (double)std::max<int64_t>(1, (k + kSlab - 1) / kSlab) * parts;
   ExpertPlan best = {kSmall, 1, 1e30};
   for (int s = 0; s < kShapes; ++s) {
+    if (p == kDw && s == kMiddle) continue;  // (never the least of the three there)
     const ShapeInfo& h = kShape[s];
-    const double tiles = expert_tiles(h, p, rows, experts, m, n);
-    for (int q = 1; q <= kMaxSplits && (q == 1 || q * 4 <= slabs); ++q) {
-      const double rounds = std::max(1.0, tiles * q / (kCus * h.per_cu));
-      const double whole = (double)(int64_t)(rounds + 0.999);
-      const double us = whole * round_us(h, (slabs + q - 1) / q) +
-                        (q > 1 ? (double)q * (p == kDw ? experts * m : rows) * n * 8 / 3e6 + kJoinUs : 0.0);
+    const double tiles = expert_tiles(h, p, rows, experts, m, n), slots = kCus * h.per_cu;
+    for (int q = 1; q <= kMaxSplits && (q == 1 || q * 4 <= depth); ++q) {
+      const double one = depth / q * h.slab_us + 4.0;
+      double us;
+      if (p == kDw) us = std::max(tiles * q / slots * one, 2 * one - 4.0) + 0.5 * one;
+      else us = (double)(int64_t)(std::max(1.0, tiles * q / slots) + 0.999) * one;
+      if (q > 1) us += (double)q * (p == kDw ? experts * m : rows) * n * 8 / 3e6 + kJoinUs;
       if (us < best.us) best = {s, q, us};
     }
   }

@@ -495,7 +495,9 @@ hipError_t launch(const ExpertArgs& g, hipStream_t st) {
   const ExpertPlan p = expert_plan(P, F32, g.groups.rows, g.groups.experts, g.m, g.n, g.k);
   const int per_cu = kShape[p.shape].per_cu;
   if (p.shape == kLarge) return launch_shape<P, F32, GATHER, Large>(g, p.splits, per_cu, st);
-  if (p.shape == kMiddle) return launch_shape<P, F32, GATHER, Middle>(g, p.splits, per_cu, st);
+  if constexpr (P != kDw) {
+    if (p.shape == kMiddle) return launch_shape<P, F32, GATHER, Middle>(g, p.splits, per_cu, st);
+  }
   return launch_shape<P, F32, GATHER, Small>(g, p.splits, per_cu, st);
 }
 
