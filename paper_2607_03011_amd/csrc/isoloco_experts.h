@@ -42,7 +42,12 @@ struct ExpertArgs {
   float* partial;
 };
 
-size_t expert_partial_bytes(ExpertProduct product, bool f32, int64_t rows, int64_t experts, int64_t m, int64_t n, int64_t k);
-hipError_t launch_expert_tiles(ExpertProduct product, bool f32, const ExpertArgs& g, hipStream_t st);
+// kOut of rows of k
+size_t expert_out_partial_bytes(bool f32, int64_t rows, int64_t experts, int64_t n, int64_t k);
+hipError_t launch_expert_out(bool f32, const ExpertArgs& g, hipStream_t st);
+
+// kDx and kDw, either of which may be NULL; their `partial` is the same.
+size_t expert_gradients_partial_bytes(bool f32, int64_t rows, int64_t experts, int64_t dim, int64_t cols);
+hipError_t launch_expert_gradients(bool f32, const ExpertArgs* dx, const ExpertArgs* dw, hipStream_t st);
 
 }  // namespace isoloco

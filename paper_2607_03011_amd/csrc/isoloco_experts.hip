@@ -228,11 +228,8 @@ CallPlan call_plan(const ExpertShape& s, bool gathered, bool dx, bool dw, bool x
   if (p.copy_x) p.x = take(2 * parts * (p.gather_x || !gathered ? s.rows : s.tokens) * dim);
   if (p.copy_w) p.w = take(2 * parts * s.experts * s.cols * dim);
   if (p.copy_d) p.d = take(2 * parts * s.rows * cols);
-  size_t partial = 0;
-  if (!back) partial = expert_partial_bytes(kOut, f32, s.rows, s.experts, 0, s.cols, s.dim);
-  if (dx) partial = std::max(partial, expert_partial_bytes(kDx, f32, s.rows, s.experts, 0, s.dim, s.cols));
-  if (dw) partial = std::max(partial, expert_partial_bytes(kDw, f32, s.rows, s.experts, s.cols, s.dim, 0));
-  p.partial = take(partial);
+  p.partial = take(back ? expert_gradients_partial_bytes(f32, s.rows, s.experts, s.dim, s.cols)
+                        : expert_out_partial_bytes(f32, s.rows, s.experts, s.cols, s.dim));
   return p;
 }
 
@@ -370,7 +367,7 @@ hipError_t run_forward(const Call& c, const CallPlan& p, void* out, int64_t ld_o
   g.k = p.copy_x && p.copy_w ? ffn_pad(c.s.dim) : (c.s.dim + 7) / 8 * 8;
   g.out = out;
   g.ld_out = ld_out;
-  return launch_expert_tiles(kOut, c.s.dtype == ISOLOCO_F32, g, st);
+  return launch_expert_out(c.s.dtype == ISOLOCO_F32, g, st);
 }
 
 hipError_t run_backward(const Call& c, const CallPlan& p, void* dx, int64_t ld_dx, void* dw, int64_t ld_dw,
@@ -383,33 +380,26 @@ hipError_t run_backward(const Call& c, const CallPlan& p, void* dx, int64_t ld_d
   g.ld_a = o.ld_d;
   g.part_a = o.part_d;
   g.n = c.s.dim;
-  hipError_t r = hipSuccess;
-  if (dx) {
-    ExpertArgs h = g;
-    h.token = {};
-    h.b = o.w;
-    h.ld_b = o.ld_w;
-    h.part_b = o.part_w;
-    h.stride_b = o.stride_w;
-    h.cols_b = p.copy_w ? dim : c.s.dim;
-    h.k = c.s.cols;
-    h.out = dx;
-    h.ld_out = ld_dx;
-    r = launch_expert_tiles(kDx, f32, h, st);
-  }
-  if (r == hipSuccess && dw) {
-    g.b = o.x;
-    g.ld_b = o.ld_x;
-    g.part_b = o.part_x;
-    g.cols_a = p.copy_d ? cols : c.s.cols;
-    g.cols_b = p.copy_x ? dim : c.s.dim;
-    g.m = c.s.cols;
-    g.out = dw;
-    g.ld_out = ld_dw;
-    g.stride_out = stride_dw;
-    r = launch_expert_tiles(kDw, f32, g, st);
-  }
-  return r;
+  ExpertArgs x = g, w = g;
+  x.token = {};
+  x.b = o.w;
+  x.ld_b = o.ld_w;
+  x.part_b = o.part_w;
+  x.stride_b = o.stride_w;
+  x.cols_b = p.copy_w ? dim : c.s.dim;
+  x.k = c.s.cols;
+  x.out = dx;
+  x.ld_out = ld_dx;
+  w.b = o.x;
+  w.ld_b = o.ld_x;
+  w.part_b = o.part_x;
+  w.cols_a = p.copy_d ? cols : c.s.cols;
+  w.cols_b = p.copy_x ? dim : c.s.dim;
+  w.m = c.s.cols;
+  w.out = dw;
+  w.ld_out = ld_dw;
+  w.stride_out = stride_dw;
+  return launch_expert_gradients(f32, dx ? &x : nullptr, dw ? &w : nullptr, st);
 }
 
 }  // namespace

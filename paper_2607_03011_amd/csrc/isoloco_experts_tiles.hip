@@ -401,44 +401,77 @@ __device__ __forceinline__ void multiply_tile(const TileArgs& t, const Tile& til
   }
 }
 
-template <ExpertProduct P, bool F32, bool GATHER, class C>
-__global__ void __launch_bounds__(C::threads, 2) expert_tile_kernel(TileArgs t) {
-  __shared__ __attribute__((aligned(1024))) char lds[TileLds<C>::kBytes];
-  // workgroups go round the 8 XCDs in turn
-  const int xcd = blockIdx.x & 7, slot = blockIdx.x >> 3, slots = gridDim.x >> 3;
-  Finder<P, C> finder;
+// The run of tiles [from, to) of a workgroup's XCD (workgroups go round the 8 XCDs in turn).
+template <ExpertProduct P, class C>
+__device__ __forceinline__ void run_of(const TileArgs& t, Finder<P, C>& finder, int64_t& from, int64_t& to) {
+  const int xcd = blockIdx.x & 7;
   finder.load(t, 0);
   const int64_t all = finder.all(t);
-  int64_t from = all * xcd / 8, to = all * (xcd + 1) / 8;
+  from = all * xcd / 8;
+  to = all * (xcd + 1) / 8;
   if (P == kDw) {
     from = finder.tile_at(t, (int)from);
     to = finder.tile_at(t, (int)to);
   }
+}
+
+// Rows of no expert: zeros.
+template <bool F32>
+__device__ __forceinline__ void clear_rest(const ExpertArgs& g) {
+  int64_t begin, end;
+  g.groups.rows_of(g.groups.experts, begin, end);
+  for (int64_t r = begin + blockIdx.x; r < end; r += gridDim.x)
+    for (int64_t c = threadIdx.x; c < g.n; c += blockDim.x) {
+      if constexpr (F32) static_cast<float*>(g.out)[r * g.ld_out + c] = 0.f;
+      else static_cast<uint16_t*>(g.out)[r * g.ld_out + c] = 0;
+    }
+}
+
+template <ExpertProduct P, bool F32, bool GATHER, class C>
+__global__ void __launch_bounds__(C::threads, 2) expert_tile_kernel(TileArgs t) {
+  __shared__ __attribute__((aligned(1024))) char lds[TileLds<C>::kBytes];
+  const int slot = blockIdx.x >> 3, slots = gridDim.x >> 3;
+  Finder<P, C> finder;
+  int64_t from, to;
+  run_of(t, finder, from, to);
   for (int64_t i = from + slot; i < to; i += slots) {
     multiply_tile<P, F32, GATHER, C>(t, finder.tile(t, i), lds);
     __syncthreads();  // the results have left LDS
   }
-  // rows of no expert
-  if (P != kDw && t.splits == 1) {
-    const ExpertArgs& g = t.g;
-    int64_t begin, end;
-    g.groups.rows_of(g.groups.experts, begin, end);
-    for (int64_t r = begin + blockIdx.x; r < end; r += gridDim.x)
-      for (int64_t c = threadIdx.x; c < g.n; c += C::threads) {
-        if constexpr (F32) static_cast<float*>(g.out)[r * g.ld_out + c] = 0.f;
-        else static_cast<uint16_t*>(g.out)[r * g.ld_out + c] = 0;
-      }
+  if (P != kDw && t.splits == 1) clear_rest<F32>(t.g);
+}
+
+// Both gradients: neither waits for the other, and where each alone has few tiles, or deep
+// and shallow ones, they fill the card together.
+template <bool F32, bool GATHER, class C>
+__global__ void __launch_bounds__(C::threads, 2) expert_gradients_kernel(TileArgs w, TileArgs x) {
+  __shared__ __attribute__((aligned(1024))) char lds[TileLds<C>::kBytes];
+  const int slot = blockIdx.x >> 3, slots = gridDim.x >> 3;
+  Finder<kDw, C> find_w;
+  Finder<kDx, C> find_x;
+  int64_t from_w, to_w, from_x, to_x;
+  run_of(w, find_w, from_w, to_w);
+  run_of(x, find_x, from_x, to_x);
+  int64_t i = from_w + slot;
+  for (; i < to_w; i += slots) {
+    multiply_tile<kDw, F32, GATHER, C>(w, find_w.tile(w, i), lds);
+    __syncthreads();
   }
+  for (i += from_x - to_w; i < to_x; i += slots) {
+    multiply_tile<kDx, F32, false, C>(x, find_x.tile(x, i), lds);
+    __syncthreads();
+  }
+  if (x.splits == 1) clear_rest<F32>(x.g);
 }
 
 typedef bf16x4 bf16x4_any __attribute__((aligned(2)));
 
 // The splits of a product added in their order.  One thread per quad of columns.
 template <ExpertProduct P, bool F32>
-__global__ void __launch_bounds__(256) expert_join_kernel(TileArgs t) {
+__device__ __forceinline__ void join(const TileArgs& t, int64_t block) {
   const ExpertArgs& g = t.g;
   const int64_t cols = ffn_pad(g.n), rows = P == kDw ? g.groups.experts * g.m : g.groups.rows;
-  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4, row = i / cols, col = i - row * cols;
+  const int64_t i = (block * 256 + threadIdx.x) * 4, row = i / cols, col = i - row * cols;
   if (row >= rows || col >= g.n) return;
   bool some = true;
   if (P != kDw) {
@@ -469,56 +502,122 @@ __global__ void __launch_bounds__(256) expert_join_kernel(TileArgs t) {
   }
 }
 
-template <ExpertProduct P, bool F32, bool GATHER, class C>
-hipError_t launch_shape(const ExpertArgs& g, int splits, int per_cu, hipStream_t st) {
+template <ExpertProduct P, bool F32>
+__global__ void __launch_bounds__(256) expert_join_kernel(TileArgs t) {
+  join<P, F32>(t, blockIdx.x);
+}
+
+template <bool F32>
+__global__ void __launch_bounds__(256) expert_join_gradients_kernel(TileArgs w, TileArgs x, int w_blocks) {
+  const int block = blockIdx.x;
+  if (block < w_blocks) join<kDw, F32>(w, block);
+  else join<kDx, F32>(x, block - w_blocks);
+}
+
+// `most`: the most tiles that the experts' sizes can make.
+template <ExpertProduct P, class C>
+TileArgs tile_args(const ExpertArgs& g, int splits, int64_t& most) {
   TileArgs t;
   t.g = g;
   t.splits = splits;
   t.tiles_n = (int)((g.n + C::TN - 1) / C::TN);
   t.tiles_m = P == kDw ? (int)((g.m + C::TM - 1) / C::TM) : 0;
-  // (the most that the experts' sizes can make; tiles are counted in 32 bits)
   const int64_t tiles_m = P == kDw ? (int64_t)g.groups.experts * t.tiles_m
                                    : g.groups.rows / C::TM + std::min<int64_t>(g.groups.rows, g.groups.experts);
-  const int64_t most = tiles_m * t.tiles_n * splits, stay = (int64_t)kCus * per_cu;
-  if (most > INT32_MAX) return hipErrorInvalidConfiguration;
-  const unsigned grid = (unsigned)std::min(stay, (most + 7) / 8 * 8);
-  hipLaunchKernelGGL((expert_tile_kernel<P, F32, GATHER, C>), dim3(grid), dim3(C::threads), 0, st, t);
-  if (splits > 1) {
-    const int64_t quads = (P == kDw ? g.groups.experts * g.m : g.groups.rows) * ffn_pad(g.n) / 4;
-    hipLaunchKernelGGL((expert_join_kernel<P, F32>), dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, st, t);
-  }
+  most = tiles_m * t.tiles_n * splits;
+  return t;
+}
+
+template <ExpertProduct P>
+unsigned join_blocks(const TileArgs& t) {
+  const int64_t rows = P == kDw ? t.g.groups.experts * t.g.m : t.g.groups.rows;
+  return t.splits > 1 ? (unsigned)((rows * ffn_pad(t.g.n) / 4 + 255) / 256) : 0;
+}
+
+// workgroups that stay: a multiple of 8, one for each XCD
+template <class C>
+unsigned stay(int64_t most) {
+  return (unsigned)std::min<int64_t>((int64_t)kCus * (C::waves == 4 ? 2 : 1), (most + 7) / 8 * 8);
+}
+
+template <ExpertProduct P, bool F32, bool GATHER, class C>
+hipError_t launch_shape(const ExpertArgs& g, int splits, hipStream_t st) {
+  int64_t most;
+  const TileArgs t = tile_args<P, C>(g, splits, most);
+  if (most > INT32_MAX) return hipErrorInvalidConfiguration;  // (tiles are counted in 32 bits)
+  hipLaunchKernelGGL((expert_tile_kernel<P, F32, GATHER, C>), dim3(stay<C>(most)), dim3(C::threads), 0, st, t);
+  if (const unsigned b = join_blocks<P>(t))
+    hipLaunchKernelGGL((expert_join_kernel<P, F32>), dim3(b), dim3(256), 0, st, t);
   return hipGetLastError();
 }
 
 template <ExpertProduct P, bool F32, bool GATHER>
-hipError_t launch(const ExpertArgs& g, hipStream_t st) {
-  const ExpertPlan p = expert_plan(P, F32, g.groups.rows, g.groups.experts, g.m, g.n, g.k);
-  const int per_cu = kShape[p.shape].per_cu;
-  if (p.shape == kLarge) return launch_shape<P, F32, GATHER, Large>(g, p.splits, per_cu, st);
+hipError_t launch_gathered(const ExpertArgs& g, const ExpertPlan& p, hipStream_t st) {
+  if (p.shape == kLarge) return launch_shape<P, F32, GATHER, Large>(g, p.splits, st);
   if constexpr (P != kDw) {
-    if (p.shape == kMiddle) return launch_shape<P, F32, GATHER, Middle>(g, p.splits, per_cu, st);
+    if (p.shape == kMiddle) return launch_shape<P, F32, GATHER, Middle>(g, p.splits, st);
   }
-  return launch_shape<P, F32, GATHER, Small>(g, p.splits, per_cu, st);
+  return launch_shape<P, F32, GATHER, Small>(g, p.splits, st);
 }
 
 template <ExpertProduct P, bool F32>
-hipError_t launch_product(const ExpertArgs& g, hipStream_t st) {
+hipError_t launch_product(const ExpertArgs& g, const ExpertPlan& p, hipStream_t st) {
   if constexpr (P != kDx) {
-    if (g.token.p) return launch<P, F32, true>(g, st);
+    if (g.token.p) return launch_gathered<P, F32, true>(g, p, st);
   }
-  return launch<P, F32, false>(g, st);
+  return launch_gathered<P, F32, false>(g, p, st);
+}
+
+template <bool F32, bool GATHER, class C>
+hipError_t launch_together(const ExpertArgs& dx, const ExpertArgs& dw, const ExpertGradients& p, hipStream_t st) {
+  int64_t most_x, most_w;
+  TileArgs x = tile_args<kDx, C>(dx, p.dx.splits, most_x), w = tile_args<kDw, C>(dw, p.dw.splits, most_w);
+  if (most_x > INT32_MAX || most_w > INT32_MAX) return hipErrorInvalidConfiguration;
+  x.g.partial += expert_partial_bytes(p.dw, kDw, dw.groups.rows, dw.groups.experts, dw.m, dw.n) / sizeof(float);
+  hipLaunchKernelGGL((expert_gradients_kernel<F32, GATHER, C>), dim3(stay<C>(most_x + most_w)), dim3(C::threads), 0, st, w, x);
+  const unsigned jw = join_blocks<kDw>(w), jx = join_blocks<kDx>(x);
+  if (jw + jx) hipLaunchKernelGGL(expert_join_gradients_kernel<F32>, dim3(jw + jx), dim3(256), 0, st, w, x, (int)jw);
+  return hipGetLastError();
+}
+
+// One of them alone goes by the same plan: the same bits.
+template <bool F32>
+hipError_t launch_gradients(const ExpertArgs* dx, const ExpertArgs* dw, hipStream_t st) {
+  if (!dx && !dw) return hipSuccess;
+  const ExpertArgs& any = dx ? *dx : *dw;
+  const ExpertGradients p = expert_plan_gradients(F32, any.groups.rows, any.groups.experts, any.n, dx ? dx->k : dw->m);
+  if (dx && dw && p.together) {
+    const bool gather = dw->token.p;
+    if (p.dw.shape == kLarge)
+      return gather ? launch_together<F32, true, Large>(*dx, *dw, p, st) : launch_together<F32, false, Large>(*dx, *dw, p, st);
+    return gather ? launch_together<F32, true, Small>(*dx, *dw, p, st) : launch_together<F32, false, Small>(*dx, *dw, p, st);
+  }
+  hipError_t e = hipSuccess;
+  if (dx) e = launch_product<kDx, F32>(*dx, p.dx, st);
+  if (e == hipSuccess && dw) e = launch_product<kDw, F32>(*dw, p.dw, st);
+  return e;
 }
 
 }  // namespace
 
-size_t expert_partial_bytes(ExpertProduct product, bool f32, int64_t rows, int64_t experts, int64_t m, int64_t n, int64_t k) {
-  return expert_partial_bytes(expert_plan(product, f32, rows, experts, m, n, k), product, rows, experts, m, n);
+size_t expert_out_partial_bytes(bool f32, int64_t rows, int64_t experts, int64_t n, int64_t k) {
+  return expert_partial_bytes(expert_plan(kOut, f32, rows, experts, 0, n, k), kOut, rows, experts, 0, n);
 }
 
-hipError_t launch_expert_tiles(ExpertProduct product, bool f32, const ExpertArgs& g, hipStream_t st) {
-  if (product == kOut) return f32 ? launch_product<kOut, true>(g, st) : launch_product<kOut, false>(g, st);
-  if (product == kDx) return f32 ? launch_product<kDx, true>(g, st) : launch_product<kDx, false>(g, st);
-  return f32 ? launch_product<kDw, true>(g, st) : launch_product<kDw, false>(g, st);
+size_t expert_gradients_partial_bytes(bool f32, int64_t rows, int64_t experts, int64_t dim, int64_t cols) {
+  const ExpertGradients p = expert_plan_gradients(f32, rows, experts, dim, cols);
+  const size_t x = expert_partial_bytes(p.dx, kDx, rows, experts, 0, dim);
+  const size_t w = expert_partial_bytes(p.dw, kDw, rows, experts, cols, dim);
+  return p.together ? x + w : std::max(x, w);
+}
+
+hipError_t launch_expert_out(bool f32, const ExpertArgs& g, hipStream_t st) {
+  const ExpertPlan p = expert_plan(kOut, f32, g.groups.rows, g.groups.experts, 0, g.n, g.k);
+  return f32 ? launch_product<kOut, true>(g, p, st) : launch_product<kOut, false>(g, p, st);
+}
+
+hipError_t launch_expert_gradients(bool f32, const ExpertArgs* dx, const ExpertArgs* dw, hipStream_t st) {
+  return f32 ? launch_gradients<true>(dx, dw, st) : launch_gradients<false>(dx, dw, st);
 }
 
 }  // namespace isoloco
