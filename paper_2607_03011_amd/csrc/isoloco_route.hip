@@ -12,10 +12,11 @@
 //   gradient, g_j that of weight_j:  normalize  dx_j = w_j (g_j - sum_i w_i g_i), 0 elsewhere
 //                                    otherwise  dx_e = p_e (sum of the g_j at e - sum_i w_i g_i)
 //
-// No atomics decide an order: a workgroup counts its slots by expert, one launch adds the
-// counts up over the workgroups, and each wave then places its slots in their order.
-// Bounded by latency: the scores of 16384 tokens are a few MB; the choosing is top_k rounds
-// of a maximum over a wave.
+// No atomics decide an order: a workgroup counts its slots by expert, and the next launch's
+// workgroup of the same slots adds up the counts before its own and ranks its slots by wave.
+// Bounded by latency: the scores of 16384 tokens are a few MB; the choosing is top_k rounds of a
+// maximum over a wave, which stays in the vector registers (over LDS, and with a launch of its
+// own for the sums of counts, the three launches for 16384 tokens of 64 experts took 65 us).
 #include <hip/hip_runtime.h>
 
 #include <math.h>
@@ -30,150 +31,101 @@
 namespace isoloco {
 namespace {
 
+constexpr int kThreads = 1024, kWaves = kThreads / 64;
+constexpr int kSmallTokens = 64;  // so many are routed by one workgroup
+constexpr int kMostBlocks = 256;  // each adds up the counts of all
+
 struct RouteArgs {
   int64_t ld, tokens;
   int experts, top_k, normalize;
   float* weight;
   int32_t *expert, *row, *token, *offsets;
-  int32_t* counts;  // workgroups x (experts + 1); behind them the experts' totals
-  int32_t* totals;
-  int per_block;  // tokens of a workgroup
+  int32_t* counts;  // workgroups x (experts + 1)
+  int per_block;    // tokens of a workgroup
   int blocks;
 };
 
-constexpr int kSmallTokens = 64;     // so many are routed by one workgroup
-constexpr int kSmallThreads = 1024;
-
-__device__ __forceinline__ uint64_t wave_max(uint64_t v) {
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) v = max64(v, (uint64_t)__shfl_xor((unsigned long long)v, off, 64));
+// Over the lanes up to each: within rows of 16, then a row's last to the next, then two rows'
+// to the other two; lane 63 has all.
+template <typename F>
+__device__ __forceinline__ uint32_t over_lanes(uint32_t v, const F& join) {
+  v = join(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, false));
+  v = join(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, false));
+  v = join(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, false));
+  v = join(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, false));
+  v = join(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, false));
+  v = join(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false));
   return v;
+}
+__device__ __forceinline__ uint32_t max_of(uint32_t v) {
+  return __builtin_amdgcn_readlane(over_lanes(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; }), 63);
+}
+__device__ __forceinline__ float sum_of(float v) {
+  return __uint_as_float(__builtin_amdgcn_readlane(
+      over_lanes(__float_as_uint(v), [](uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }),
+      63));
+}
+__device__ __forceinline__ int scan_of(int v) {
+  return (int)over_lanes((uint32_t)v, [](uint32_t a, uint32_t b) { return a + b; });
 }
 
 // One wave chooses a token's experts: lane j gets the j-th (-1: none), and its weight.
 template <typename T, int EL>
 __device__ __forceinline__ void choose(const T* scores, const RouteArgs& g, int& expert, float& weight) {
   const int lane = threadIdx.x & 63;
-  uint64_t key[EL];
+  uint32_t key[EL];  // the order of the values; 0: chosen, or no expert
   float x[EL];
 #pragma unroll
   for (int i = 0; i < EL; ++i) {
     const int e = 64 * i + lane;
     x[i] = e < g.experts ? (float)scores[e] : -INFINITY;
-    key[i] = e < g.experts ? key_of(x[i], (uint32_t)e) : 0;
+    key[i] = e < g.experts ? order_of(x[i]) : 0;
   }
-  uint64_t mine = 0;
+  uint32_t mine = 0;
+  expert = -1;
   for (int j = 0; j < g.top_k; ++j) {
-    uint64_t best = key[0];
+    uint32_t best = key[0];
 #pragma unroll
-    for (int i = 1; i < EL; ++i) best = max64(best, key[i]);
-    best = wave_max(best);
-    if (lane == j) mine = best;
+    for (int i = 1; i < EL; ++i) best = key[i] > best ? key[i] : best;
+    best = max_of(best);
+    // the lowest expert that has it
+    bool found = false;
 #pragma unroll
-    for (int i = 0; i < EL; ++i)
-      if (key[i] == best) key[i] = 0;
+    for (int i = 0; i < EL; ++i) {
+      const uint64_t at = __ballot(key[i] == best);
+      if (!found && at) {
+        found = true;
+        const int winner = __ffsll((unsigned long long)at) - 1;
+        if (lane == winner) key[i] = 0;
+        if (lane == j) {
+          mine = best;
+          expert = 64 * i + winner;
+        }
+      }
+    }
   }
-  const float value = lane < g.top_k ? value_of(mine) : -INFINITY;
-  const float m = __shfl(value, 0, 64);
-  expert = value == -INFINITY ? -1 : (int)index_of(mine);
-  float e = value == -INFINITY ? 0.f : expf(value - m), s = e;
+  const float value = lane < g.top_k ? value_of((uint64_t)mine << 32) : -INFINITY;
+  const float m = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(value), 0));
+  if (value == -INFINITY) expert = -1;
+  const float e = value == -INFINITY ? 0.f : expf(value - m);
+  float s = e;
   if (!g.normalize) {
     s = 0.f;
 #pragma unroll
     for (int i = 0; i < EL; ++i) s += x[i] == -INFINITY ? 0.f : expf(x[i] - m);
   }
-  s = wave_sum(s);
+  s = sum_of(s);
   weight = expert < 0 ? 0.f : e / s;
 }
 
-// Where the experts' slots begin: the scan of `total` (experts + 1 groups) into `begin`, by one wave.
-__device__ __forceinline__ void scan_groups(const int32_t* total, int groups, int32_t* begin) {
-  const int lane = threadIdx.x & 63;
-  int carry = 0;
-  for (int base = 0; base < groups; base += 64) {
-    const int i = base + lane, n = i < groups ? total[i] : 0;
-    int sum = n;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-      const int o = __shfl_up(sum, off, 64);
-      if (lane >= off) sum += o;
-    }
-    if (i < groups) begin[i] = carry + sum - n;
-    carry += __shfl(sum, 63, 64);
-  }
-}
-
-// One wave places the slots from `first` to `end` in their order; next[g] is the place of
-// group g's next slot.  group_of(slot): its group.
-template <typename GroupOf>
-__device__ __forceinline__ void place(const RouteArgs& g, int64_t first, int64_t end, int32_t* next,
-                                      const GroupOf& group_of) {
-  const int lane = threadIdx.x & 63;
-  int bits = 0;
-  while ((1 << bits) <= g.experts) ++bits;  // groups are 0 .. experts
-  for (int64_t base = first; base < end; base += 64) {
-    const int64_t slot = base + lane;
-    const bool live = slot < end;
-    const int group = live ? group_of(slot) : 0;
-    // the lanes of the same group
-    uint64_t same = __ballot(live);
-    for (int b = 0; b < bits; ++b) {
-      const uint64_t set = __ballot(group >> b & 1);
-      same &= group >> b & 1 ? set : ~set;
-    }
-    const int before = __popcll(same & ((1ull << lane) - 1));
-    if (live) {
-      const int at = next[group] + before;
-      g.row[slot] = at;
-      g.token[at] = (int32_t)(slot / g.top_k);
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    // (the group's last lane moves its place on)
-    if (live && (same >> lane) == 1) next[group] += before + 1;
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-  }
-}
-
-// Everything, by one workgroup.
+// The workgroup's tokens: their experts and weights, and the slots' counts by group (of which
+// the last is no expert).
 template <typename T, int EL>
-__global__ void __launch_bounds__(kSmallThreads) route_small_kernel(const T* scores, RouteArgs g) {
-  __shared__ int32_t count[ISOLOCO_MAX_EXPERTS + 1], begin[ISOLOCO_MAX_EXPERTS + 1];
-  __shared__ int16_t group[kSmallTokens * ISOLOCO_MAX_TOP];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, groups = g.experts + 1;
-  for (int i = threadIdx.x; i < groups; i += kSmallThreads) count[i] = 0;
+__device__ __forceinline__ void choose_all(const T* scores, const RouteArgs& g, int64_t first, int64_t end, int32_t* count) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for (int i = threadIdx.x; i <= g.experts; i += kThreads) count[i] = 0;
   __syncthreads();
-  for (int t = wave; t < (int)g.tokens; t += kSmallThreads / 64) {
-    int expert;
-    float weight;
-    choose<T, EL>(scores + t * g.ld, g, expert, weight);
-    if (lane < g.top_k) {
-      const int slot = t * g.top_k + lane;
-      g.weight[slot] = weight;
-      g.expert[slot] = expert;
-      group[slot] = (int16_t)(expert < 0 ? g.experts : expert);
-      atomicAdd(&count[group[slot]], 1);
-    }
-  }
-  __syncthreads();
-  if (wave > 0) return;
-  scan_groups(count, groups, begin);
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  for (int i = lane; i < groups; i += 64) g.offsets[i] = begin[i];
-  place(g, 0, g.tokens * g.top_k, begin, [&](int64_t slot) { return (int)group[slot]; });
-}
-
-// The choice of a workgroup's tokens, and its slots' counts by expert.
-template <typename T, int EL>
-__global__ void __launch_bounds__(256) route_choose_kernel(const T* scores, RouteArgs g) {
-  __shared__ int32_t count[ISOLOCO_MAX_EXPERTS + 1];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, groups = g.experts + 1;
-  for (int i = threadIdx.x; i < groups; i += 256) count[i] = 0;
-  __syncthreads();
-  const int64_t first = (int64_t)blockIdx.x * g.per_block, end = min(g.tokens, first + g.per_block);
-  for (int64_t t = first + wave; t < end; t += 4) {
+  for (int64_t t = first + wave; t < end; t += kWaves) {
     int expert;
     float weight;
     choose<T, EL>(scores + t * g.ld, g, expert, weight);
@@ -185,56 +137,120 @@ __global__ void __launch_bounds__(256) route_choose_kernel(const T* scores, Rout
     }
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < groups; i += 256) g.counts[(int64_t)blockIdx.x * groups + i] = count[i];
 }
 
-// The counts of the workgroups before each, and the totals: 64 groups per workgroup, its
-// waves a run of the workgroups' counts each.
-constexpr int kScanWaves = 16;
-__global__ void __launch_bounds__(64 * kScanWaves) route_scan_kernel(RouteArgs g) {
-  __shared__ int32_t sums[kScanWaves][64];
+// The scan of `total` over the groups, in place, by one wave.
+__device__ __forceinline__ void scan_groups(int32_t* total, int groups) {
+  const int lane = threadIdx.x & 63;
+  int carry = 0;
+  for (int base = 0; base < groups; base += 64) {
+    const int i = base + lane, n = i < groups ? total[i] : 0, upto = scan_of(n);
+    if (i < groups) total[i] = carry + upto - n;
+    carry += __builtin_amdgcn_readlane(upto, 63);
+  }
+}
+
+// The workgroup places its slots in their order; next[i] is the place of group i's next one.
+__device__ __forceinline__ void place(const RouteArgs& g, int64_t first, int64_t end, int32_t* next,
+                                      uint8_t (*of_wave)[ISOLOCO_MAX_EXPERTS + 4]) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, groups = g.experts + 1;
-  const int group = blockIdx.x * 64 + lane, per = (g.blocks + kScanWaves - 1) / kScanWaves;
-  const int first = min(wave * per, g.blocks), end = min(first + per, g.blocks);
-  const bool live = group < groups;
-  int sum = 0;
-  if (live)
-    for (int b = first; b < end; ++b) sum += g.counts[(int64_t)b * groups + group];
-  sums[wave][lane] = sum;
-  __syncthreads();
-  if (!live) return;
-  int before = 0, total = 0;
-  for (int w = 0; w < kScanWaves; ++w) {
-    before += w < wave ? sums[w][lane] : 0;
-    total += sums[w][lane];
+  int bits = 0;
+  while ((1 << bits) < groups) ++bits;
+  for (int64_t base = first; base < end; base += kThreads) {
+    for (int i = threadIdx.x; i < kWaves * (ISOLOCO_MAX_EXPERTS + 4) / 4; i += kThreads)
+      reinterpret_cast<uint32_t*>(of_wave)[i] = 0;
+    __syncthreads();
+    const int64_t slot = base + threadIdx.x;
+    const bool live = slot < end;
+    int group = live ? g.expert[slot] : 0;
+    if (group < 0) group = g.experts;
+    // the wave's lanes of the same group
+    uint64_t same = __ballot(live);
+    for (int b = 0; b < bits; ++b) {
+      const uint64_t set = __ballot(group >> b & 1);
+      same &= group >> b & 1 ? set : ~set;
+    }
+    const int before = __popcll(same & ((1ull << lane) - 1));
+    if (live && (same >> lane) == 1) of_wave[wave][group] = (uint8_t)(before + 1);
+    __syncthreads();
+    if (live) {
+      int at = next[group] + before;
+      for (int w = 0; w < wave; ++w) at += of_wave[w][group];
+      g.row[slot] = at;
+      g.token[at] = (int32_t)(slot / g.top_k);
+    }
+    if (base + kThreads >= end) return;
+    __syncthreads();
+    for (int i = threadIdx.x; i < groups; i += kThreads) {
+      int sum = 0;
+      for (int w = 0; w < kWaves; ++w) sum += of_wave[w][i];
+      next[i] += sum;
+    }
+    __syncthreads();
   }
-  for (int b = first; b < end; ++b) {
-    int32_t* c = g.counts + (int64_t)b * groups + group;
-    const int n = *c;
-    *c = before;
-    before += n;
-  }
-  if (wave == 0) g.totals[group] = total;
 }
 
-// One wave per workgroup of the choice.
-__global__ void __launch_bounds__(64) route_place_kernel(RouteArgs g) {
+// Everything, by one workgroup.
+template <typename T, int EL>
+__global__ void __launch_bounds__(kThreads) route_small_kernel(const T* scores, RouteArgs g) {
   __shared__ int32_t next[ISOLOCO_MAX_EXPERTS + 1];
-  const int lane = threadIdx.x, groups = g.experts + 1;
-  scan_groups(g.totals, groups, next);
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  for (int i = lane; i < groups; i += 64) {
-    if (blockIdx.x == 0) g.offsets[i] = next[i];
-    next[i] += g.counts[(int64_t)blockIdx.x * groups + i];
-  }
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
+  __shared__ __attribute__((aligned(4))) uint8_t of_wave[kWaves][ISOLOCO_MAX_EXPERTS + 4];
+  choose_all<T, EL>(scores, g, 0, g.tokens, next);
+  if (threadIdx.x < 64) scan_groups(next, g.experts + 1);
+  __syncthreads();  // (the experts that were stored are read again, too)
+  for (int i = threadIdx.x; i <= g.experts; i += kThreads) g.offsets[i] = next[i];
+  place(g, 0, g.tokens * g.top_k, next, of_wave);
+}
+
+// The choice of a workgroup's tokens, and its slots' counts.
+template <typename T, int EL>
+__global__ void __launch_bounds__(kThreads) route_choose_kernel(const T* scores, RouteArgs g) {
+  __shared__ int32_t count[ISOLOCO_MAX_EXPERTS + 1];
   const int64_t first = (int64_t)blockIdx.x * g.per_block, end = min(g.tokens, first + g.per_block);
-  place(g, first * g.top_k, end * g.top_k, next, [&](int64_t slot) {
-    const int e = g.expert[slot];
-    return e < 0 ? g.experts : e;
-  });
+  choose_all<T, EL>(scores, g, first, end, count);
+  int32_t* out = g.counts + (int64_t)blockIdx.x * (g.experts + 1);
+  for (int i = threadIdx.x; i <= g.experts; i += kThreads) out[i] = count[i];
+}
+
+// The places of the same workgroup's slots: 64 groups at a time, each wave adds up some of the
+// workgroups' counts, those before this one apart.
+__global__ void __launch_bounds__(kThreads) route_place_kernel(RouteArgs g) {
+  __shared__ int32_t next[ISOLOCO_MAX_EXPERTS + 1], earlier[ISOLOCO_MAX_EXPERTS + 1];
+  __shared__ int32_t sum[kWaves][64], sum_before[kWaves][64];
+  __shared__ __attribute__((aligned(4))) uint8_t of_wave[kWaves][ISOLOCO_MAX_EXPERTS + 4];
+  constexpr int kPer = kMostBlocks / kWaves;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, groups = g.experts + 1;
+  for (int base = 0; base < groups; base += 64) {
+    int n[kPer], all = 0, before = 0;
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) {
+      const int b = wave * kPer + u;
+      n[u] = b < g.blocks && base + lane < groups ? g.counts[(int64_t)b * groups + base + lane] : 0;
+    }
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) {
+      all += n[u];
+      before += wave * kPer + u < (int)blockIdx.x ? n[u] : 0;
+    }
+    sum[wave][lane] = all;
+    sum_before[wave][lane] = before;
+    __syncthreads();
+    if (wave < 2 && base + lane < groups) {
+      int s = 0;
+      for (int w = 0; w < kWaves; ++w) s += wave ? sum_before[w][lane] : sum[w][lane];
+      (wave ? earlier : next)[base + lane] = s;
+    }
+    __syncthreads();
+  }
+  if (wave == 0) scan_groups(next, groups);
+  __syncthreads();
+  for (int i = threadIdx.x; i < groups; i += kThreads) {
+    if (blockIdx.x == 0) g.offsets[i] = next[i];
+    next[i] += earlier[i];
+  }
+  __syncthreads();
+  const int64_t first = (int64_t)blockIdx.x * g.per_block, end = min(g.tokens, first + g.per_block);
+  place(g, first * g.top_k, end * g.top_k, next, of_wave);
 }
 
 struct RouteGradArgs {
@@ -268,8 +284,7 @@ __global__ void __launch_bounds__(256) route_grad_kernel(const T* scores, T* dsc
 #pragma unroll
     for (int i = 0; i < EL; ++i) m = fmaxf(m, x[i]);
   }
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
+  m = value_of((uint64_t)max_of(order_of(m)) << 32);
   const float from = m == -INFINITY ? 0.f : m;
   float p[EL], s = 0.f, w = expert < 0 ? 0.f : expf(chosen - from);
   if (g.normalize) {
@@ -281,10 +296,10 @@ __global__ void __launch_bounds__(256) route_grad_kernel(const T* scores, T* dsc
       s += p[i];
     }
   }
-  s = wave_sum(s);
+  s = sum_of(s);
   const float inv = s == 0.f ? 0.f : 1.f / s;
   w *= inv;
-  const float inner = wave_sum(w * grad);
+  const float inner = sum_of(w * grad);
   float d[EL];
 #pragma unroll
   for (int i = 0; i < EL; ++i) d[i] = g.normalize ? 0.f : -(p[i] * inv) * inner;
@@ -315,29 +330,26 @@ isoloco_status check_shape(int64_t tokens, int64_t experts, int32_t top_k, int32
   return ISOLOCO_OK;
 }
 
-// Tokens of a workgroup: 64, or more where that makes too many workgroups' counts.
-int per_block_of(int64_t tokens) {
-  int64_t n = 64;
-  while ((tokens + n - 1) / n > 4096) n *= 2;
-  return (int)n;
+// Tokens of a workgroup: 64, or more where that makes too many workgroups.
+int64_t per_block_of(int64_t tokens) {
+  return std::max<int64_t>(64, (tokens + kMostBlocks - 1) / kMostBlocks);
 }
 
 size_t route_workspace(int64_t tokens, int64_t experts) {
   if (tokens <= kSmallTokens) return 0;
   const int64_t per = per_block_of(tokens);
-  return (size_t)((tokens + per - 1) / per + 1) * (size_t)(experts + 1) * 4;
+  return (size_t)((tokens + per - 1) / per) * (size_t)(experts + 1) * 4;
 }
 
 template <typename T, int EL>
 void run_forward(const void* scores, const RouteArgs& g, hipStream_t st) {
   const T* s = static_cast<const T*>(scores);
   if (g.tokens <= kSmallTokens) {
-    hipLaunchKernelGGL((route_small_kernel<T, EL>), dim3(1), dim3(kSmallThreads), 0, st, s, g);
+    hipLaunchKernelGGL((route_small_kernel<T, EL>), dim3(1), dim3(kThreads), 0, st, s, g);
     return;
   }
-  hipLaunchKernelGGL((route_choose_kernel<T, EL>), dim3(g.blocks), dim3(256), 0, st, s, g);
-  hipLaunchKernelGGL(route_scan_kernel, dim3(g.experts / 64 + 1), dim3(64 * kScanWaves), 0, st, g);
-  hipLaunchKernelGGL(route_place_kernel, dim3(g.blocks), dim3(64), 0, st, g);
+  hipLaunchKernelGGL((route_choose_kernel<T, EL>), dim3(g.blocks), dim3(kThreads), 0, st, s, g);
+  hipLaunchKernelGGL(route_place_kernel, dim3(g.blocks), dim3(kThreads), 0, st, g);
 }
 
 template <typename T, int EL>
@@ -392,10 +404,9 @@ isoloco_status isoloco_route_tokens(const void* scores, int64_t ld_scores, int32
   g.row = row;
   g.token = token;
   g.offsets = offsets;
-  g.per_block = per_block_of(tokens);
+  g.per_block = (int)per_block_of(tokens);
   g.blocks = (int)((tokens + g.per_block - 1) / g.per_block);
   g.counts = static_cast<int32_t*>(workspace);
-  g.totals = g.counts + (int64_t)g.blocks * (experts + 1);
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
   if (dtype == ISOLOCO_F32) BY_EXPERTS(run_forward, float, scores, g, st);
   else BY_EXPERTS(run_forward, __bf16, scores, g, st);
