@@ -32,6 +32,7 @@ namespace {
 constexpr int kMaxSplits = 64;
 constexpr int kHeld = 64;               // logits that a thread holds in registers
 constexpr int64_t kMostSpan = 1 << 17;  // columns of a workgroup with a bitmap: 16 KiB of it
+constexpr int kHalfTurns = 2;          // of 256 threads, see threads_of
 constexpr int kPerLane = (ISOLOCO_MAX_TEACHER + 63) / 64;
 
 // Sums of e^((x - m) scale) over some of a row's logits ({-infinity, 0} of nothing).
@@ -76,10 +77,23 @@ __device__ __forceinline__ bool first_of_its_column(const int32_t* column, int i
   return first;
 }
 
+// Lane by lane whether no entry before names its column (entry 64 u + lane)
+struct Firsts {
+  bool of[kPerLane];
+  __device__ __forceinline__ void find(const int32_t* column, int top_k) {
+#pragma unroll
+    for (int u = 0; u < kPerLane; ++u) {
+      const int i = 64 * u + (threadIdx.x & 63);
+      of[u] = i < top_k && first_of_its_column(column, i);
+    }
+  }
+};
+
 // The row's loss, by one wave: `a` is the sum over all of its columns, or (bucket) over
 // those that are not listed.  `column`: the entries' columns, -1 where there is none.
 template <typename T, bool BUCKET>
-__device__ void put_loss(const LossArgs& g, const T* row, const int32_t* column, int64_t r, const Sum& a) {
+__device__ void put_loss(const LossArgs& g, const T* row, const int32_t* column, const Firsts& firsts,
+                         int64_t r, const Sum& a) {
   const int lane = threadIdx.x & 63;
   const double scale = g.scale;
   double t[kPerLane], x[kPerLane];
@@ -88,9 +102,10 @@ __device__ void put_loss(const LossArgs& g, const T* row, const int32_t* column,
 #pragma unroll
   for (int u = 0; u < kPerLane; ++u) {
     const int i = 64 * u + lane;
-    given[u] = i < g.top_k && column[i] >= 0;
+    const int32_t c = i < g.top_k ? column[i] : -1;
+    given[u] = c >= 0;
     t[u] = given[u] ? (double)g.top[r * g.top_k + i] : -INFINITY;
-    x[u] = given[u] ? (double)(float)row[column[i]] : -INFINITY;
+    x[u] = given[u] ? (double)(float)row[c] : -INFINITY;
     tm = fmax(tm, t[u]);
     xm = fmax(xm, x[u]);
   }
@@ -106,11 +121,13 @@ __device__ void put_loss(const LossArgs& g, const T* row, const int32_t* column,
   const bool none = tm == -INFINITY;
 #pragma unroll
   for (int u = 0; u < kPerLane; ++u) {
-    const int i = 64 * u + lane;
+    p[u] = 0.0;
+    if (64 * u >= g.top_k) continue;
     p[u] = given[u] && !none ? exp(t[u] - tm) : 0.0;
     p_sum += p[u];
-    if (BUCKET && given[u] && (x[u] > -INFINITY || x[u] != x[u]) && first_of_its_column(column, i))
-      s += exp((x[u] - xm) * scale);
+    if constexpr (BUCKET) {
+      if (given[u] && (x[u] > -INFINITY || x[u] != x[u]) && firsts.of[u]) s += exp((x[u] - xm) * scale);
+    }
   }
   p_sum = wave_sum(p_sum);
   const double others = a.m == -INFINITY ? (double)a.s : (double)a.s * exp(((double)a.m - xm) * scale);
@@ -119,6 +136,7 @@ __device__ void put_loss(const LossArgs& g, const T* row, const int32_t* column,
   double loss = 0.0, weight = 0.0;
 #pragma unroll
   for (int u = 0; u < kPerLane; ++u) {
+    if (64 * u >= g.top_k) continue;
     const double mass = none ? 0.0 : p[u] * inv_p;
     weight += mass;
     if (given[u] && mass != 0.0) {
@@ -184,7 +202,7 @@ __global__ void __launch_bounds__(64 * WAVES, sizeof(T) == 2 ? 8 : 4)
     distill_kernel(const T* logits, const ID* index, LossArgs g) {
   constexpr int N = Vec<T>::N, kThreads = 64 * WAVES, kVecs = kHeld / N;
   constexpr int turn = kThreads * kVecs;  // vectors that the workgroup holds
-  constexpr int kWords = !BUCKET ? 1 : (WAVES == 8 ? (int)kMostSpan : turn * N) / 32;
+  constexpr int kWords = !BUCKET ? 1 : (WAVES == 8 ? (int)kMostSpan : WAVES == 4 ? kHalfTurns * turn * N : turn * N) / 32;
   __shared__ Sum part[WAVES];
   __shared__ int32_t column[ISOLOCO_MAX_TEACHER];
   __shared__ uint32_t marks[kWords];
@@ -225,8 +243,14 @@ __global__ void __launch_bounds__(64 * WAVES, sizeof(T) == 2 ? 8 : 4)
   }
 
   Sum a = {-INFINITY, 0.f};
+  load(0);
+  // (while the first of them come)
+  Firsts firsts;
+  if constexpr (BUCKET) {
+    if (wave == 0) firsts.find(column, g.top_k);
+  }
   for (int base = 0; base == 0 || base < whole; base += turn) {
-    load(base);
+    if (base) load(base);
     if constexpr (BUCKET) {
 #pragma unroll
       for (int c = 0; c < kVecs; ++c) {
@@ -293,7 +317,7 @@ __global__ void __launch_bounds__(64 * WAVES, sizeof(T) == 2 ? 8 : 4)
   if (g.splits > 1) {
     if (lane == 0) g.part[blockIdx.x] = a;
   } else {
-    put_loss<T, BUCKET>(g, row, column, r, a);
+    put_loss<T, BUCKET>(g, row, column, firsts, r, a);
   }
 }
 
@@ -306,7 +330,9 @@ __global__ void __launch_bounds__(64) distill_join_kernel(const T* logits, const
   const Sum* part = g.part + r * g.splits;
   Sum a = part[0];
   for (int i = 1; i < g.splits; ++i) a.join(part[i], g.rate);
-  put_loss<T, BUCKET>(g, logits + r * g.ld, column, r, a);
+  Firsts firsts;
+  if constexpr (BUCKET) firsts.find(column, g.top_k);
+  put_loss<T, BUCKET>(g, logits + r * g.ld, column, firsts, r, a);
 }
 
 struct GradArgs {
@@ -433,8 +459,11 @@ size_t distill_workspace(int64_t rows, int64_t vocab) {
   return s > 1 ? (size_t)rows * s * sizeof(Sum) : 0;
 }
 
-// the fewest that hold a row (or split) at once, if any do
-int threads_of(int64_t span) { return span <= 64 * kHeld ? 64 : span <= 256 * kHeld ? 256 : 512; }
+// One wave if it holds the row (or split) at once, 256 threads if they do in two turns.  (8192
+// rows of 32000, us, in 512 threads' one turn / 256 threads' two: 115 / 98.9 in bfloat16, 137 /
+// 117 with the rest; 192 / 193 and 226 / 192 in float32.  4096 rows of 128000 in four / eight: 198
+// / 214 in bfloat16 with the rest, 366 / 375 in float32.)
+int threads_of(int64_t span) { return span <= 64 * kHeld ? 64 : span <= kHalfTurns * 256 * kHeld ? 256 : 512; }
 
 template <typename T, typename ID, bool BUCKET>
 void run_loss(const T* l, const ID* index, int64_t rows, const LossArgs& g, hipStream_t st) {
