@@ -588,7 +588,7 @@ isoloco_status isoloco_combine_tokens_backward(const void* dout, int64_t ld_dout
  * loss: rows floats.  stats: rows x ISOLOCO_DISTILL_STATS floats for the gradient,
  * of which [6] is the row's log-sum-exp of z.  top_k <= ISOLOCO_MAX_TEACHER. */
 #define ISOLOCO_MAX_TEACHER 128
-#define ISOLOCO_DISTILL_STATS 8
+#define ISOLOCO_DISTILL_STATS 10
 
 typedef enum { ISOLOCO_REST_DROP = 0, ISOLOCO_REST_BUCKET = 1 } isoloco_rest;
 

@@ -80,7 +80,7 @@ ISOLOCO_EXPERTS_BACKWARD = 1
 ISOLOCO_EXPERTS_ALIGNED = 2
 ISOLOCO_EXPERTS_GATHERED = 4
 ISOLOCO_MAX_TEACHER = 128
-ISOLOCO_DISTILL_STATS = 8
+ISOLOCO_DISTILL_STATS = 10
 ISOLOCO_REST_DROP = 0
 ISOLOCO_REST_BUCKET = 1
 

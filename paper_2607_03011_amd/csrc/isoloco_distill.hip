@@ -15,12 +15,17 @@
 // the others (which leaves nothing of a small one): the listed columns are marked in a
 // bitmap in LDS, and the pass over the row takes a marked column for -infinity.
 //
+// float32 logits take that path without q_r too: the listed columns, which are most of the sum
+// once the student agrees, are then summed in 64 bits.
+//
 // Bounded by memory: the loss reads the logits once, the gradient reads them again and
 // writes as much.
 #include <hip/hip_runtime.h>
 
 #include <math.h>
 #include <stdint.h>
+
+#include <type_traits>
 
 #include "isoloco_device.h"
 #include "isoloco_error.h"
@@ -35,15 +40,41 @@ constexpr int64_t kMostSpan = 1 << 17;  // columns of a workgroup with a bitmap:
 constexpr int kHalfTurns = 2;          // of 256 threads, see threads_of
 constexpr int kPerLane = (ISOLOCO_MAX_TEACHER + 63) / 64;
 
-// Sums of e^((x - m) scale) over some of a row's logits ({-infinity, 0} of nothing).
+// scale log2 e in two floats, and the distance from which on its power of 2 is 0.
+struct Rate {
+  float hi, lo, least;
+};
+Rate rate_parts(float scale) {
+  const float hi = rate_of(scale);
+  const double lo = (double)scale * 1.4426950408889634074 - hi;
+  return {hi, hi == FLT_MAX ? 0.f : (float)lo, -200.f / hi};
+}
+
+// e^(d scale), d <= 0.  EXACT: to float32's last bits, for float32 logits (the rounding of the
+// product alone moves the plain one by |d scale| of them); bfloat16 ones do not need it.
+template <bool EXACT>
+__device__ __forceinline__ float power(float d, const Rate& r) {
+  if constexpr (!EXACT) return __builtin_amdgcn_exp2f(d * r.hi);
+  d = d < r.least ? r.least : d;  // (a NaN stays)
+  const float n = __builtin_rintf(d * r.hi);
+  return ldexpf(__builtin_amdgcn_exp2f(fmaf(d, r.lo, fmaf(d, r.hi, -n))), (int)n);
+}
+
+// Whether the pass over the row leaves the listed columns out
+template <typename T, bool BUCKET>
+constexpr bool kApart = BUCKET || sizeof(T) == 4;
+
+// Sums of e^((x - m) scale) over some of a row's logits ({-infinity, 0} of nothing): a
+// thread's in 32 bits, joined in 64.
 struct Sum {
-  float m, s;
-  __device__ __forceinline__ void raise(float to, float rate) {
+  float m;
+  double s;
+  __device__ __forceinline__ void raise(float to, const Rate& rate) {
     if (to == m) return;
-    s = m == -INFINITY ? s : s * __builtin_amdgcn_exp2f((m - to) * rate);
+    s = m == -INFINITY ? s : s * power<true>(m - to, rate);
     m = to;
   }
-  __device__ __forceinline__ void join(Sum o, float rate) {
+  __device__ __forceinline__ void join(Sum o, const Rate& rate) {
     const float to = fmaxf(m, o.m);
     raise(to, rate);
     o.raise(to, rate);
@@ -55,7 +86,8 @@ struct LossArgs {
   int64_t ld, vocab;
   const float* top;
   int top_k;
-  float scale, rate;
+  float scale;
+  Rate rate;
   int splits;    // workgroups per row
   int64_t span;  // a split's columns (a multiple of a vector's)
   Sum* part;     // splits > 1: each one's sum
@@ -89,12 +121,13 @@ struct Firsts {
   }
 };
 
-// The row's loss, by one wave: `a` is the sum over all of its columns, or (bucket) over
-// those that are not listed.  `column`: the entries' columns, -1 where there is none.
+// The row's loss, by one wave: `a` is the sum over all of its columns, or (kApart) over those
+// that are not listed.  `column`: the entries' columns, -1 where there is none.
 template <typename T, bool BUCKET>
 __device__ void put_loss(const LossArgs& g, const T* row, const int32_t* column, const Firsts& firsts,
                          int64_t r, const Sum& a) {
   const int lane = threadIdx.x & 63;
+  constexpr bool APART = kApart<T, BUCKET>;
   const double scale = g.scale;
   double t[kPerLane], x[kPerLane];
   bool given[kPerLane];
@@ -110,13 +143,13 @@ __device__ void put_loss(const LossArgs& g, const T* row, const int32_t* column,
     xm = fmax(xm, x[u]);
   }
   tm = BUCKET ? 0.0 : wave_max(tm);
-  xm = BUCKET ? wave_max(xm) : (double)a.m;
+  xm = APART ? wave_max(xm) : (double)a.m;
   // (a maximum passes over NaN: with 0 in its place the sum does not)
   bool odd = false;
 #pragma unroll
   for (int u = 0; u < kPerLane; ++u) odd |= given[u] && t[u] != t[u];
   if (__any(odd)) tm = 0.0;
-  // sums against xm: the listed columns' (bucket: each column once), and those of the rest
+  // sums against xm: the listed columns' (each column once), and those of the rest
   double s = 0.0, p_sum = 0.0, p[kPerLane];
   const bool none = tm == -INFINITY;
 #pragma unroll
@@ -125,13 +158,13 @@ __device__ void put_loss(const LossArgs& g, const T* row, const int32_t* column,
     if (64 * u >= g.top_k) continue;
     p[u] = given[u] && !none ? exp(t[u] - tm) : 0.0;
     p_sum += p[u];
-    if constexpr (BUCKET) {
+    if constexpr (APART) {
       if (given[u] && (x[u] > -INFINITY || x[u] != x[u]) && firsts.of[u]) s += exp((x[u] - xm) * scale);
     }
   }
   p_sum = wave_sum(p_sum);
-  const double others = a.m == -INFINITY ? (double)a.s : (double)a.s * exp(((double)a.m - xm) * scale);
-  s = BUCKET ? wave_sum(s) + others : (double)a.s;
+  const double others = a.m == -INFINITY ? a.s : a.s * exp(((double)a.m - xm) * scale);
+  s = APART ? wave_sum(s) + others : a.s;
   const double log_s = log(s), inv_p = BUCKET ? 1.0 : 1.0 / p_sum, log_p = BUCKET ? 0.0 : tm + log(p_sum);
   double loss = 0.0, weight = 0.0;
 #pragma unroll
@@ -162,17 +195,19 @@ __device__ void put_loss(const LossArgs& g, const T* row, const int32_t* column,
   }
   if (lane == 0) {
     g.loss[r] = (float)loss;
-    // what the gradient takes: q_j = stats[1] e^((x_j - stats[0]) scale), the factors of q
-    // at listed and other columns, and p_i = stats[5] e^(t_i - stats[4])
+    // what the gradient takes: q_j = (stats[1] + [7]) e^((x_j - [0]) scale), the factors of q at
+    // listed and other columns, and p_i = ([5] + [8]) e^(t_i - [4])
     float* o = g.stats + r * ISOLOCO_DISTILL_STATS;
     o[0] = s != s ? NAN : (float)xm;
     o[1] = (float)(1.0 / s);
+    o[7] = s > 0.0 ? (float)(1.0 / s - (double)o[1]) : 0.f;
     o[2] = (float)weight;
     o[3] = (float)rest_factor;
     o[4] = none ? 0.f : (float)tm;
     o[5] = none ? 0.f : (float)inv_p;
+    o[8] = none ? 0.f : (float)(inv_p - (double)o[5]);
     o[6] = s == 0.0 ? -INFINITY : (float)(xm * scale + log_s);
-    o[7] = 0.f;
+    o[9] = 0.f;
   }
 }
 
@@ -202,7 +237,8 @@ __global__ void __launch_bounds__(64 * WAVES, sizeof(T) == 2 ? 8 : 4)
     distill_kernel(const T* logits, const ID* index, LossArgs g) {
   constexpr int N = Vec<T>::N, kThreads = 64 * WAVES, kVecs = kHeld / N;
   constexpr int turn = kThreads * kVecs;  // vectors that the workgroup holds
-  constexpr int kWords = !BUCKET ? 1 : (WAVES == 8 ? (int)kMostSpan : WAVES == 4 ? kHalfTurns * turn * N : turn * N) / 32;
+  constexpr bool APART = kApart<T, BUCKET>;
+  constexpr int kWords = !APART ? 1 : (WAVES == 8 ? (int)kMostSpan : WAVES == 4 ? kHalfTurns * turn * N : turn * N) / 32;
   __shared__ Sum part[WAVES];
   __shared__ int32_t column[ISOLOCO_MAX_TEACHER];
   __shared__ uint32_t marks[kWords];
@@ -226,7 +262,7 @@ __global__ void __launch_bounds__(64 * WAVES, sizeof(T) == 2 ? 8 : 4)
     const int at = whole * N + (int)threadIdx.x;
     last = base == 0 && at < count ? (float)p[at] : -INFINITY;
   };
-  if constexpr (BUCKET) {
+  if constexpr (APART) {
     for (int i = threadIdx.x; i < (count + 31) / 32; i += kThreads) marks[i] = 0;
   }
   const bool any = load_columns(index, r, g.top_k, g.vocab, column);
@@ -234,7 +270,7 @@ __global__ void __launch_bounds__(64 * WAVES, sizeof(T) == 2 ? 8 : 4)
     if (split == 0 && threadIdx.x == 0) put_none(g, r);
     return;
   }
-  if constexpr (BUCKET) {
+  if constexpr (APART) {
     for (int i = threadIdx.x; i < g.top_k; i += kThreads) {
       const int64_t c = column[i] - begin;
       if (column[i] >= 0 && c >= 0 && c < count) atomicOr(&marks[c >> 5], 1u << (c & 31));
@@ -242,16 +278,18 @@ __global__ void __launch_bounds__(64 * WAVES, sizeof(T) == 2 ? 8 : 4)
     __syncthreads();
   }
 
-  Sum a = {-INFINITY, 0.f};
+  struct {
+    float m, s;
+  } own = {-INFINITY, 0.f};
   load(0);
   // (while the first of them come)
   Firsts firsts;
-  if constexpr (BUCKET) {
+  if constexpr (APART) {
     if (wave == 0) firsts.find(column, g.top_k);
   }
   for (int base = 0; base == 0 || base < whole; base += turn) {
     if (base) load(base);
-    if constexpr (BUCKET) {
+    if constexpr (APART) {
 #pragma unroll
       for (int c = 0; c < kVecs; ++c) {
         const int i = base + c * kThreads + (int)threadIdx.x;
@@ -288,18 +326,21 @@ __global__ void __launch_bounds__(64 * WAVES, sizeof(T) == 2 ? 8 : 4)
 #pragma unroll
       for (int c = 0; c < kVecs; ++c) asm("" : "+v"(v[c]));
     }
-    a.raise(fmaxf(a.m, most), g.rate);
-    const float m = a.m == -INFINITY ? 0.f : a.m;
+    most = fmaxf(own.m, most);
+    if (most != own.m && own.m != -INFINITY) own.s *= power<true>(own.m - most, g.rate);
+    own.m = most;
+    const float m = most == -INFINITY ? 0.f : most;
 #pragma unroll
     for (int c = 0; c < kVecs; ++c)
       if (base + c * kThreads < whole) {
         float x[N];
         unpack<T>(v[c], x);
 #pragma unroll
-        for (int e = 0; e < N; ++e) a.s += __builtin_amdgcn_exp2f((x[e] - m) * g.rate);
+        for (int e = 0; e < N; ++e) own.s += power<sizeof(T) == 4>(x[e] - m, g.rate);
       }
-    if (base == 0) a.s += __builtin_amdgcn_exp2f((last - m) * g.rate);
+    if (base == 0) own.s += power<sizeof(T) == 4>(last - m, g.rate);
   }
+  Sum a = {own.m, own.s};
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) {
     Sum o;
@@ -331,7 +372,7 @@ __global__ void __launch_bounds__(64) distill_join_kernel(const T* logits, const
   Sum a = part[0];
   for (int i = 1; i < g.splits; ++i) a.join(part[i], g.rate);
   Firsts firsts;
-  if constexpr (BUCKET) firsts.find(column, g.top_k);
+  if constexpr (kApart<T, BUCKET>) firsts.find(column, g.top_k);
   put_loss<T, BUCKET>(g, logits + r * g.ld, column, firsts, r, a);
 }
 
@@ -339,7 +380,8 @@ struct GradArgs {
   int64_t ld, rows, vocab, ld_d;
   const float* top;
   int top_k;
-  float scale, rate;
+  float scale;
+  Rate rate;
   const float* stats;
   const float* dloss;
   int spans;
@@ -356,7 +398,10 @@ __global__ void __launch_bounds__(kGradThreads) distill_grad_kernel(const T* log
                                                                     GradArgs g) {
   constexpr int N = Vec<T>::N;
   __shared__ int32_t column[ISOLOCO_MAX_TEACHER];
-  __shared__ float mass[ISOLOCO_MAX_TEACHER];
+  // q and p are near each other once the student has learnt: float32 results take their
+  // difference in 64 bits
+  typedef typename std::conditional<sizeof(T) == 4, double, float>::type Fine;
+  __shared__ Fine mass[ISOLOCO_MAX_TEACHER];
   static_assert(ISOLOCO_MAX_TEACHER <= kGradThreads, "one entry a thread");
   // (the last rows first: the forward pass read them last, some are still in a cache)
   const int64_t r = g.rows - 1 - blockIdx.x / g.spans;
@@ -389,14 +434,17 @@ __global__ void __launch_bounds__(kGradThreads) distill_grad_kernel(const T* log
     c = index[r * g.top_k + i];
     const bool in = c >= 0 && c < g.vocab;
     column[i] = in ? (int32_t)c : -1;
-    mass[i] = in ? inv_p * exp2f((g.top[r * g.top_k + i] - tm) * kLog2e) : 0.f;
+    if constexpr (sizeof(T) == 4)
+      mass[i] = in ? ((double)inv_p + (double)st[8]) * exp((double)g.top[r * g.top_k + i] - (double)tm) : 0.0;
+    else
+      mass[i] = in ? inv_p * expf(g.top[r * g.top_k + i] - tm) : 0.f;
     const int64_t vec = c / N;
     mine = in && (vec >= whole ? span == 0 : vec >= first && vec < first + kGradThreads * kGradVecs);
     if (mine) x_top = (float)row[c];
   }
   __syncthreads();
   const float other = none ? 0.f : inv_s * rest_factor * dl;
-  const auto grad = [&](float x) { return none ? 0.f : __builtin_amdgcn_exp2f((x - from) * g.rate) * other; };
+  const auto grad = [&](float x) { return none ? 0.f : power<sizeof(T) == 4>(x - from, g.rate) * other; };
 #pragma unroll
   for (int u = 0; u < kGradVecs; ++u) {
     const int64_t j = first + u * kGradThreads + threadIdx.x;
@@ -417,10 +465,13 @@ __global__ void __launch_bounds__(kGradThreads) distill_grad_kernel(const T* log
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   if (!mine || !first_of_its_column(column, i)) return;
-  float p = 0.f;
-  for (int j = i; j < g.top_k; ++j) p += column[j] == (int32_t)c ? mass[j] : 0.f;
-  const float q = __builtin_amdgcn_exp2f((x_top - from) * g.rate) * inv_s;
-  out[c] = (T)((q * factor - p) * dl);
+  Fine p = 0, q;
+  for (int j = i; j < g.top_k; ++j) p += column[j] == (int32_t)c ? mass[j] : (Fine)0;
+  if constexpr (sizeof(T) == 4)
+    q = exp(((double)x_top - (double)from) * (double)g.scale) * ((double)inv_s + (double)st[7]);
+  else
+    q = power<true>(x_top - from, g.rate) * inv_s;
+  out[c] = (T)(float)((q * factor - p) * dl);
 }
 
 struct DistillShape {
@@ -540,7 +591,7 @@ isoloco_status isoloco_distill_loss(const void* logits, int64_t ld_logits, int32
   g.top = top_logprob;
   g.top_k = top_k;
   g.scale = scale;
-  g.rate = rate_of(scale);
+  g.rate = rate_parts(scale);
   g.splits = splits_of(rows, vocab);
   g.span = ((vocab + g.splits - 1) / g.splits + 7) / 8 * 8;
   g.splits = (int)((vocab + g.span - 1) / g.span);
@@ -585,7 +636,7 @@ isoloco_status isoloco_distill_loss_backward(const void* logits, int64_t ld_logi
   g.top = top_logprob;
   g.top_k = top_k;
   g.scale = scale;
-  g.rate = rate_of(scale);
+  g.rate = rate_parts(scale);
   g.stats = stats;
   g.dloss = dloss;
   g.spans = (int)spans;

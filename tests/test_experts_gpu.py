@@ -718,7 +718,7 @@ def test_distill_shapes(iso):
     z = torch.randn(2, 3, 50, device="cuda")
     teacher = iso.token_logprobs(torch.randn(2, 3, 50, device="cuda"), top_k=4)
     r = iso.distill_loss(z, teacher.top_logprob, teacher.top_index)
-    assert r.loss.shape == (2, 3) and r.stats.shape == (2, 3, 8)
+    assert r.loss.shape == (2, 3) and r.stats.shape == (2, 3, iso.ISOLOCO_DISTILL_STATS)
     e = iso.distill_loss(z[:0], teacher.top_logprob[:0], teacher.top_index[:0])
     assert e.loss.shape == (0, 3)
     with pytest.raises(ValueError):
