@@ -517,7 +517,8 @@ isoloco_status isoloco_route_tokens_backward(const void* scores, int64_t ld_scor
  * values are not known to the host, and nothing outside the tensors is touched
  * whatever they are.  Rows from offsets[experts] on are zeros, and a token
  * outside 0 .. tokens - 1 stands for a row of zeros.  An expert may have no rows.
- * float32 products are formed as in isoloco_gated_ffn.
+ * float32 products are formed as in isoloco_gated_ffn (forward, in float32 where the
+ * experts have up to 96 rows on average).
  *
  * The workspace's size goes by the call: ISOLOCO_EXPERTS_BACKWARD for the
  * gradient, ISOLOCO_EXPERTS_GATHERED where token is given, and

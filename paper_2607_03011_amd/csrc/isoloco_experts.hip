@@ -36,6 +36,12 @@ isoloco_status check_shape(const ExpertShape& s) {
   if (s.experts < 1 || s.experts > ISOLOCO_MAX_EXPERTS)
     return fail(ISOLOCO_ERR_INVALID_ARG, "%lld experts, of 1 to %d", (long long)s.experts, ISOLOCO_MAX_EXPERTS);
   if (!is_dtype(s.dtype)) return fail(ISOLOCO_ERR_INVALID_ARG, "dtype %d", s.dtype);
+  // tiles are counted in 32 bits (splits are of few tiles)
+  const int64_t dims = (s.dim + 127) / 128, cols = (s.cols + 127) / 128;
+  if ((s.rows / 128 + std::min(s.rows, s.experts)) * std::max(dims, cols) > INT32_MAX / 2 ||
+      s.experts * dims * cols > INT32_MAX / 2)
+    return fail(ISOLOCO_ERR_UNSUPPORTED, "too many tiles: %lld rows, %lld experts of %lld x %lld", (long long)s.rows,
+                (long long)s.experts, (long long)s.cols, (long long)s.dim);
   return ISOLOCO_OK;
 }
 
@@ -169,8 +175,9 @@ __global__ void __launch_bounds__(64 * kFewWaves, 4) expert_few_kernel(FewArgs g
 //                    13.9 / 50.0   14.2 / 49.2   14.5 / 49.5   20.3 / 50.1   23.4 / 51.4   40.8 / 55.0   58.2 / 60.9
 // bfloat16 weights that the tiles would have copied first (150 us of the first kind) are as
 // float32 in this.
-bool few_of(int32_t dtype, int64_t rows, int64_t experts, bool copies) {
-  return rows <= (dtype == ISOLOCO_F32 ? 96 : copies ? 48 : 16) * experts;
+bool few_of(int32_t dtype, int64_t rows, int64_t experts, int64_t cols, bool copies) {
+  return rows <= (dtype == ISOLOCO_F32 ? 96 : copies ? 48 : 16) * experts &&
+         launchable((experts + 1) * ((cols + 15) / 16), 64 * kFewWaves);
 }
 
 template <typename T, int NT>
@@ -211,7 +218,7 @@ bool tile_rows(const void* p, int64_t cols, int64_t ld) {
 CallPlan call_plan(const ExpertShape& s, bool gathered, bool dx, bool dw, bool x_ok, bool w_ok, bool d_ok, int64_t ld_x) {
   CallPlan p = {};
   const bool f32 = s.dtype == ISOLOCO_F32, back = dx || dw;
-  p.few = !back && few_of(s.dtype, s.rows, s.experts, !w_ok);
+  p.few = !back && few_of(s.dtype, s.rows, s.experts, s.cols, !w_ok);
   if (p.few) return p;
   const size_t parts = f32 ? kFfnParts : 1;
   const int64_t dim = ffn_pad(s.dim), cols = ffn_pad(s.cols);

@@ -544,7 +544,6 @@ template <ExpertProduct P, bool F32, bool GATHER, class C>
 hipError_t launch_shape(const ExpertArgs& g, int splits, hipStream_t st) {
   int64_t most;
   const TileArgs t = tile_args<P, C>(g, splits, most);
-  if (most > INT32_MAX) return hipErrorInvalidConfiguration;  // (tiles are counted in 32 bits)
   hipLaunchKernelGGL((expert_tile_kernel<P, F32, GATHER, C>), dim3(stay<C>(most)), dim3(C::threads), 0, st, t);
   if (const unsigned b = join_blocks<P>(t))
     hipLaunchKernelGGL((expert_join_kernel<P, F32>), dim3(b), dim3(256), 0, st, t);
@@ -572,7 +571,6 @@ template <bool F32, bool GATHER, class C>
 hipError_t launch_together(const ExpertArgs& dx, const ExpertArgs& dw, const ExpertGradients& p, hipStream_t st) {
   int64_t most_x, most_w;
   TileArgs x = tile_args<kDx, C>(dx, p.dx.splits, most_x), w = tile_args<kDw, C>(dw, p.dw.splits, most_w);
-  if (most_x > INT32_MAX || most_w > INT32_MAX) return hipErrorInvalidConfiguration;
   x.g.partial += expert_partial_bytes(p.dw, kDw, dw.groups.rows, dw.groups.experts, dw.m, dw.n) / sizeof(float);
   hipLaunchKernelGGL((expert_gradients_kernel<F32, GATHER, C>), dim3(stay<C>(most_x + most_w)), dim3(C::threads), 0, st, w, x);
   const unsigned jw = join_blocks<kDw>(w), jx = join_blocks<kDx>(x);

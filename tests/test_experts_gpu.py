@@ -10,6 +10,8 @@ import math
 
 import pytest
 
+from _expert_cases import CASES
+
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
@@ -979,3 +981,62 @@ def test_combine_past_32_bits(iso):
     small = iso.combine_tokens_backward(out[pick], y[row[pick].long().flatten()], torch.arange(6, device="cuda").view(3, 2),
                                         w[pick])
     assert torch.equal(dy[row[pick].long().flatten()], small[0]) and torch.equal(dweight[pick], small[1])
+
+
+# --------------------------------------------------------------------------
+# Every instance of the products
+# --------------------------------------------------------------------------
+
+@pytest.mark.parametrize("case", range(len(CASES)))
+def test_expert_products(iso, case):
+    """Larger products against torch's in 64 bits on the GPU: uneven experts, one without rows,
+    some rows behind the last one's, rows as they lie and gathered."""
+    kind, experts, rows, dim, cols, _ = CASES[case]
+    dtype = BF16 if kind == "bf16" else F32
+    g = torch.Generator(device="cuda")
+    g.manual_seed(case)
+
+    def randn(*shape, std=1.0):
+        return (torch.randn(*shape, generator=g, device="cuda") * std).to(dtype)
+
+    want = torch.rand(experts, generator=g, device="cuda") + 0.2
+    want[experts // 2] = 0.0
+    sizes = torch.multinomial(want, rows - 37, replacement=True, generator=g).bincount(minlength=experts)
+    offsets = torch.zeros(experts + 1, dtype=I64, device="cuda")
+    offsets[1:] = sizes.cumsum(0)
+    tokens, last = rows // 2 + 1, rows - 37
+    x, token = randn(tokens, dim), torch.randint(0, tokens, (rows,), generator=g, device="cuda")
+    w, d = randn(experts, cols, dim, std=dim ** -0.5), randn(rows, cols)
+    flat = x[token].contiguous()
+    out = iso.expert_matmul(flat, w, offsets)
+    assert torch.equal(iso.expert_matmul(x, w, offsets, token=token), out)
+    dx, dw = iso.expert_matmul_backward(flat, w, offsets, d)
+    assert torch.equal(iso.expert_matmul_backward(x, w, offsets, d, token=token, need_dx=False)[1], dw)
+    assert torch.equal(iso.expert_matmul_backward(flat, w, offsets, d, need_dw=False)[0], dx)
+    row = torch.full((tokens, 1), -1, dtype=I64, device="cuda")
+    assert torch.equal(iso.expert_matmul_backward(x, w, offsets, d, token=token, row=row)[1], dw)
+    assert not out[last:].any() and not dx[last:].any()
+    for e in range(experts):
+        a, b = int(offsets[e]), int(offsets[e + 1])
+        X, W, D = flat[a:b].double(), w[e].double(), d[a:b].double()
+        for got, want, size, n in ((out[a:b], X @ W.T, X.abs() @ W.abs().T, dim), (dx[a:b], D @ W, D.abs() @ W.abs(), cols),
+                                   (dw[e], D.T @ X, D.abs().T @ X.abs(), b - a)):
+            # (float32: the 6 products of parts are as many sums)
+            bound = ((6 if dtype == F32 else 1) * n + 8) * U32 * size + ROUND[dtype] * want.abs() + 1e-37
+            assert ((got.double() - want).abs() <= bound).all()
+
+
+def test_expert_matmul_wide_experts(iso):
+    """More experts than a wave has lanes, on the tiles: experts are found 64 at a time."""
+    g = gen(12)
+    experts, rows = 300, 9000
+    offsets, token, row = grouped(g, rows, experts, 1)
+    x, w, d = randn(g, rows, 64, dtype=BF16), randn(g, experts, 72, 64, std=0.125, dtype=BF16), randn(g, rows, 72, dtype=BF16)
+    want, size = expert_reference(x[token], w, offsets)
+    o, t, r = (v.int().cuda() for v in (offsets, token, row))
+    within(iso.expert_matmul(x.cuda(), w.cuda(), o, token=t), want, 72 * U32 * size + ROUND[BF16] * want.abs())
+    dx, dxs, dw, dws = expert_reference(x[token], w, offsets, d)
+    got = iso.expert_matmul_backward(x[token].cuda(), w.cuda(), o, d.cuda())
+    within(got[0], dx, 80 * U32 * dxs + ROUND[BF16] * dx.abs())
+    n = torch.diff(offsets).double()[:, None, None]
+    within(got[1], dw, (n + 8) * U32 * dws + ROUND[BF16] * dw.abs() + 1e-37)

@@ -6,6 +6,8 @@ import subprocess
 
 import pytest
 
+from _expert_cases import CASES
+
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 PROGRAM = r"""
@@ -53,3 +55,45 @@ def test_plans(tmp_path):
     out = subprocess.run([str(exe)], capture_output=True, text=True)
     assert out.returncode == 0, "case %d" % out.returncode
     assert int(out.stdout) == 7 * 4 * 100 * 2
+
+
+def test_cases_take_what_they_say(tmp_path):
+    cxx = shutil.which("g++") or shutil.which("clang++")
+    if cxx is None:
+        pytest.skip("no C++ compiler")
+    calls = "\n".join("  show(%d, %d, %d, %d, %d);" % (kind == "f32", e, r, d, c) for kind, e, r, d, c, _ in CASES)
+    src, exe = tmp_path / "cases.cpp", tmp_path / "cases"
+    src.write_text(r"""
+#include "isoloco_experts_plan.h"
+#include <stdio.h>
+using namespace isoloco;
+static void one(const ExpertPlan& p) { printf("%c%d", "LMS"[p.shape], p.splits); }
+static void show(bool f32, long experts, long rows, long dim, long cols) {
+  const ExpertGradients g = expert_plan_gradients(f32, rows, experts, dim, cols);
+  one(expert_plan(kOut, f32, rows, experts, 0, cols, dim));
+  printf(" ");
+  one(g.dx);
+  printf(g.together ? "+" : " ");
+  one(g.dw);
+  printf("\n");
+}
+int main() {
+""" + calls + "\n}\n")
+    subprocess.run([cxx, "-std=c++17", "-I", os.path.join(ROOT, "paper_2607_03011_amd", "csrc"), str(src), "-o", str(exe)],
+                   check=True)
+    got = subprocess.run([str(exe)], capture_output=True, text=True, check=True).stdout.splitlines()
+    seen = set()
+    for line, (kind, _, _, _, _, plan) in zip(got, CASES, strict=True):
+        if plan.startswith("few"):
+            line = "few " + line.split(" ", 1)[1]
+        assert line == plan
+        out, back = plan.split(" ", 1)
+        dx, dw = back.replace("+", " ").split()
+        seen |= {(kind, "out", out[0]), (kind, "dx", dx[0]), (kind, "dw", dw[0])}
+        if "+" in back:
+            seen.add((kind, "both", dx[0]))
+    for kind in ("bf16", "f32"):
+        for tile in "LMS":
+            assert {(kind, "out", tile), (kind, "dx", tile)} <= seen
+        for tile in "LS":
+            assert {(kind, "dw", tile), (kind, "both", tile)} <= seen
