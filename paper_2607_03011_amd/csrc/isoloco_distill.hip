@@ -514,12 +514,17 @@ size_t distill_workspace(int64_t rows, int64_t vocab) {
 // rows of 32000, us, in 512 threads' one turn / 256 threads' two: 115 / 98.9 in bfloat16, 137 /
 // 117 with the rest; 192 / 193 and 226 / 192 in float32.  4096 rows of 128000 in four / eight: 198
 // / 214 in bfloat16 with the rest, 366 / 375 in float32.)
-int threads_of(int64_t span) { return span <= 64 * kHeld ? 64 : span <= kHalfTurns * 256 * kHeld ? 256 : 512; }
+int threads_of(int64_t span, int64_t blocks) {
+  if (span <= 64 * kHeld) return 64;
+  // (up to two workgroups a CU: the shorter way for each; 16 rows of 32000 in 256 / 512 threads
+  // 12.2 / 11.1 us in bfloat16, 15.2 / 13.4 in float32)
+  return span <= 256 * kHeld || (span <= kHalfTurns * 256 * kHeld && blocks > 512) ? 256 : 512;
+}
 
 template <typename T, typename ID, bool BUCKET>
 void run_loss(const T* l, const ID* index, int64_t rows, const LossArgs& g, hipStream_t st) {
   const dim3 grid((unsigned)(rows * g.splits));
-  const int threads = threads_of(g.span);
+  const int threads = threads_of(g.span, rows * g.splits);
   if (threads == 64) hipLaunchKernelGGL((distill_kernel<T, ID, 1, BUCKET>), grid, dim3(64), 0, st, l, index, g);
   else if (threads == 256) hipLaunchKernelGGL((distill_kernel<T, ID, 4, BUCKET>), grid, dim3(256), 0, st, l, index, g);
   else hipLaunchKernelGGL((distill_kernel<T, ID, 8, BUCKET>), grid, dim3(512), 0, st, l, index, g);
@@ -598,7 +603,7 @@ isoloco_status isoloco_distill_loss(const void* logits, int64_t ld_logits, int32
   g.part = static_cast<Sum*>(workspace);
   g.loss = loss;
   g.stats = stats;
-  if (!launchable(rows * g.splits, threads_of(g.span)))
+  if (!launchable(rows * g.splits, threads_of(g.span, rows * g.splits)))
     return fail(ISOLOCO_ERR_UNSUPPORTED, "too many rows for one launch");
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
   BY_TYPES(run_forward, logits, top_index, rows, rest, g, st);
