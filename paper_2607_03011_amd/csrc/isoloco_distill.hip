@@ -493,11 +493,16 @@ isoloco_status check_shape(const DistillShape& s) {
   return ISOLOCO_OK;
 }
 
-// Workgroups per row: one, unless the rows are few and long, or longer than a bitmap.
+// Workgroups per row: one, unless the rows are few and long, or longer than a bitmap.  Both sides
+// measured, us a call of a graph with the rest in bfloat16, 1 / 2 / 4 / 8 / 16 splits:
+//            1 row                              127 rows                           256 rows
+//    32000   9.5 / 11.8 / 11.1 / 11.7 / 12.6    10.1 / 12.4 / 12.5 / 12.8 / 14.4   10.4 / 13.5 / 14.4 / 14.0 / 16.4
+//    50257   11.3 / 11.8 / 11.6 / 11.7 / 13.1   13.2 / 13.5 / 13.6 / 14.8 / 15.5   13.6 / 17.1 / 17.2 / 19.8 / 18.8
+//   128000   16.7 / 14.7 / 12.3 / 12.2 / 13.2   18.3 / 17.1 / 17.3 / 17.7 / 21.3   20.9 / 23.7 / 23.3 / 24.3 / 29.7
 int splits_of(int64_t rows, int64_t vocab) {
   int64_t s = 1;
-  if (rows < 128 && vocab > 40000) {
-    const int64_t most = vocab / 8192, wanted = 512 / (rows ? rows : 1);
+  if (rows < 128 && vocab > 80000) {
+    const int64_t most = vocab / 24576, wanted = 512 / (rows ? rows : 1);
     s = most < wanted ? most : wanted;
     s = s < 1 ? 1 : s > kMaxSplits ? kMaxSplits : s;
   }

@@ -580,7 +580,8 @@ def distill_inputs(rows, vocab, top, dtype, scale, seed, odd=False):
 
 
 DISTILLS = [(1, 1, 1), (1, 3, 2), (3, 40, 40), (5, 100, 8), (9, 128, 128), (4, 511, 5), (16, 4096, 32), (7, 4097, 64),
-            (5, 16385, 8), (3, 32000, 128), (130, 1000, 20), (2, 70000, 32), (1, 140001, 8), (3, 33000, 1)]
+            (5, 16385, 8), (3, 32000, 128), (130, 1000, 20), (2, 70000, 32), (1, 140001, 8), (3, 33000, 1), (3, 100003, 128), (600, 5001, 8),
+            (130, 131080, 4)]
 
 
 @pytest.mark.parametrize("rows,vocab,top", DISTILLS)

@@ -131,10 +131,10 @@ DISTILL = dict(logits=A, ld=1000, dtype=1, rows=3, vocab=1000, top_logprob=B, to
     (INVALID, dict(scale=math.inf)), (ALIGN, dict(logits=A + 1)), (ALIGN, dict(top_logprob=B + 2)),
     (ALIGN, dict(top_index=C + 4)), (ALIGN, dict(stats=E + 2)), (ALIAS, dict(loss=A)), (ALIAS, dict(stats=B)),
     (ALIAS, dict(loss=C)), (ALIAS, dict(stats=D - 8)),
-    # (two rows of 50000: split, so that a workspace is needed)
-    (WORKSPACE, dict(rows=2, vocab=50000, ld=50000, workspace=0)),
-    (WORKSPACE, dict(rows=2, vocab=50000, ld=50000, ws_bytes=8)),
-    (ALIAS, dict(rows=2, vocab=50000, ld=50000, loss=WS)),
+    # (two rows of 100000: split, so that a workspace is needed)
+    (WORKSPACE, dict(rows=2, vocab=100000, ld=100000, workspace=0)),
+    (WORKSPACE, dict(rows=2, vocab=100000, ld=100000, ws_bytes=8)),
+    (ALIAS, dict(rows=2, vocab=100000, ld=100000, loss=WS)),
 ])
 def test_distill_refuses(status, change):
     refused(status, iso.isoloco_distill_loss, *changed(DISTILL, **change))
