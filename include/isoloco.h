@@ -563,12 +563,15 @@ isoloco_status isoloco_combine_tokens(const void* y, int64_t ld_y, int32_t dtype
  *
  *   dy[row[t, j]] = weight[t, j] dout[t]          dweight[t, j] = <dout[t], y[row[t, j]]>
  *
- * No two entries of row may be the same; rows of dy that none names are left as
- * they were.  dweight is 0 where the entry is outside.  y is read for dweight only. */
+ * No two entries of row may be the same; rows of dy that none names are zeros.
+ * dweight is 0 where the entry is outside.  y is read for dweight only, and the
+ * workspace serves dy only. */
+isoloco_status isoloco_combine_tokens_backward_workspace_size(int64_t tokens, int32_t top_k, size_t* bytes);
 isoloco_status isoloco_combine_tokens_backward(const void* dout, int64_t ld_dout, const void* y, int64_t ld_y,
                                                int32_t dtype, int64_t rows, int64_t dim, const void* row,
                                                int32_t index_type, const float* weight, int64_t tokens, int32_t top_k,
-                                               void* dy, int64_t ld_dy, float* dweight, void* hip_stream);
+                                               void* dy, int64_t ld_dy, float* dweight, void* workspace,
+                                               size_t workspace_bytes, void* hip_stream);
 
 /* Distillation from a teacher's most likely tokens.  With z = scale * logits of a
  * row (scale > 0), q their softmax, and the row's top_k entries t_i = top_logprob

@@ -35,7 +35,7 @@ __all__ = [
     "combine_tokens", "combine_tokens_backward", "distill_loss", "distill_loss_backward", "DistillLoss",
     "isoloco_route_tokens_workspace_size", "isoloco_route_tokens", "isoloco_route_tokens_backward",
     "isoloco_expert_matmul_workspace_size", "isoloco_expert_matmul", "isoloco_expert_matmul_backward",
-    "isoloco_combine_tokens", "isoloco_combine_tokens_backward",
+    "isoloco_combine_tokens", "isoloco_combine_tokens_backward_workspace_size", "isoloco_combine_tokens_backward",
     "isoloco_distill_loss_workspace_size", "isoloco_distill_loss", "isoloco_distill_loss_backward",
     "ISOLOCO_MAX_EXPERTS", "ISOLOCO_EXPERTS_BACKWARD", "ISOLOCO_EXPERTS_ALIGNED", "ISOLOCO_EXPERTS_GATHERED",
     "ISOLOCO_MAX_TEACHER", "ISOLOCO_DISTILL_STATS", "ISOLOCO_REST_DROP", "ISOLOCO_REST_BUCKET",
@@ -95,7 +95,7 @@ EXPORTED_SYMBOLS = (
     "isoloco_gated_ffn_workspace_size", "isoloco_gated_ffn", "isoloco_gated_ffn_backward",
     "isoloco_route_tokens_workspace_size", "isoloco_route_tokens", "isoloco_route_tokens_backward",
     "isoloco_expert_matmul_workspace_size", "isoloco_expert_matmul", "isoloco_expert_matmul_backward",
-    "isoloco_combine_tokens", "isoloco_combine_tokens_backward",
+    "isoloco_combine_tokens", "isoloco_combine_tokens_backward_workspace_size", "isoloco_combine_tokens_backward",
     "isoloco_distill_loss_workspace_size", "isoloco_distill_loss", "isoloco_distill_loss_backward",
 )
 
@@ -197,7 +197,8 @@ _sig = {
                                                       _I64, _I64, _P, _I64, _P, _I64, _P, _I64, _I64, _P, _SIZE, _P]),
     "isoloco_combine_tokens": (ctypes.c_int, [_P, _I64, _I32, _I64, _I64, _P, _I32, _P, _I64, _I32, _P, _I64, _P]),
     "isoloco_combine_tokens_backward": (ctypes.c_int, [_P, _I64, _P, _I64, _I32, _I64, _I64, _P, _I32, _P, _I64, _I32,
-                                                       _P, _I64, _P, _P]),
+                                                       _P, _I64, _P, _P, _SIZE, _P]),
+    "isoloco_combine_tokens_backward_workspace_size": (ctypes.c_int, [_I64, _I32, ctypes.POINTER(_SIZE)]),
     "isoloco_distill_loss_workspace_size": (ctypes.c_int, [_I64, _I64, ctypes.POINTER(_SIZE)]),
     "isoloco_distill_loss": (ctypes.c_int, [_P, _I64, _I32, _I64, _I64, _P, _P, _I32, _I32, _F, _I32, _P, _P, _P, _SIZE,
                                             _P]),
@@ -434,6 +435,7 @@ from .operators import (  # noqa: E402,F401
 from .experts import (  # noqa: E402,F401
     DistillLoss, TokenRoutes, combine_tokens, combine_tokens_backward, distill_loss, distill_loss_backward,
     expert_matmul, expert_matmul_backward, isoloco_combine_tokens, isoloco_combine_tokens_backward,
+    isoloco_combine_tokens_backward_workspace_size,
     isoloco_distill_loss, isoloco_distill_loss_backward, isoloco_distill_loss_workspace_size, isoloco_expert_matmul,
     isoloco_expert_matmul_backward, isoloco_expert_matmul_workspace_size, isoloco_route_tokens,
     isoloco_route_tokens_backward, isoloco_route_tokens_workspace_size, route_tokens, route_tokens_backward)

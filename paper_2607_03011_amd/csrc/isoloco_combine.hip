@@ -2,6 +2,7 @@
 //
 //   out[t] = sum_j weight[t, j] y[row[t, j]]
 //   dy[row[t, j]] = weight[t, j] dout[t],   dweight[t, j] = <dout[t], y[row[t, j]]>
+//   (zeros in rows that no slot names)
 //
 // The terms of a sum are added in the order of j; no two slots name one row, so that
 // nothing is added across tokens.  Bounded by memory: every row is read once (backward:
@@ -58,6 +59,52 @@ __global__ void __launch_bounds__(256) combine_kernel(const T* y, T* out, Combin
     }
   }
   store_piece<T>(out + t * g.ld_out + col, left, sum);
+}
+
+// Rows of dy that no slot names have no gradient.  As no two slots name one, there are such rows
+// exactly where fewer slots than rows name one: the slots that do are counted, and only then
+// all of dy is cleared before the named rows are written (which costs 105 us of 344 for 537 MB
+// where it is not needed; the counting 5).
+constexpr int kCounts = 256;
+constexpr int64_t kCountedAtOnce = 8192;  // so many slots each workgroup that clears counts itself
+
+__device__ __forceinline__ int count_named(const Index& row, int64_t rows, int64_t first, int64_t step, int64_t slots) {
+  int n = 0;
+  for (int64_t i = first; i < slots; i += step) {
+    const int64_t r = row.get(i);
+    n += r >= 0 && r < rows;
+  }
+  return n;
+}
+
+// The sum of a workgroup's values, in every thread.
+__device__ __forceinline__ int64_t sum_of(int v) {
+  __shared__ int part[4];
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+  __syncthreads();
+  return (int64_t)part[0] + part[1] + part[2] + part[3];
+}
+
+__global__ void __launch_bounds__(256) combine_count_kernel(Index row, int64_t rows, int64_t slots, int32_t* counts) {
+  const int64_t n = sum_of(count_named(row, rows, (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256, slots));
+  if (threadIdx.x == 0) counts[blockIdx.x] = (int32_t)n;
+}
+
+// `counts`: kCounts of them, or NULL: the slots are few.
+template <typename T>
+__global__ void __launch_bounds__(256) combine_clear_kernel(Index row, int64_t rows, int64_t slots, const int32_t* counts,
+                                                            T* dy, int64_t ld, int64_t dim) {
+  const int64_t named = sum_of(counts ? counts[threadIdx.x] : count_named(row, rows, threadIdx.x, 256, slots));
+  if (named >= rows) return;
+  constexpr int N = Vec<T>::N;
+  const int64_t pieces = (dim + N - 1) / N;
+  const float zeros[N] = {};
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * pieces; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / pieces, col = (i - r * pieces) * N;
+    store_piece<T>(dy + r * ld + col, dim - col, zeros);
+  }
 }
 
 struct CombineGradArgs {
@@ -162,8 +209,21 @@ void run_forward(const void* y, void* out, const CombineArgs& g, int pieces, int
                      static_cast<T*>(out), g, pieces);
 }
 
+size_t combine_grad_workspace(int64_t tokens, int32_t top_k) {
+  return tokens * top_k > kCountedAtOnce ? kCounts * sizeof(int32_t) : 0;
+}
+
 template <typename T, bool PAST>
-void run_grad(const void* dout, const void* y, void* dy, const CombineGradArgs& g, int64_t blocks, hipStream_t st) {
+void run_grad(const void* dout, const void* y, void* dy, const CombineGradArgs& g, int64_t blocks, int32_t* counts,
+              hipStream_t st) {
+  if (dy && g.rows) {
+    const int64_t slots = g.tokens * g.top_k;
+    const bool few = slots <= kCountedAtOnce;
+    if (!few) hipLaunchKernelGGL(combine_count_kernel, dim3(kCounts), dim3(256), 0, st, g.row, g.rows, slots, counts);
+    hipLaunchKernelGGL(combine_clear_kernel<T>, dim3((unsigned)std::min<int64_t>(1024, g.rows)), dim3(256), 0, st, g.row,
+                       g.rows, slots, few ? nullptr : counts, static_cast<T*>(dy), g.ld_dy, g.dim);
+  }
+  if (blocks == 0) return;
   const dim3 grid((unsigned)blocks);
   const T *d = static_cast<const T*>(dout), *x = static_cast<const T*>(y);
   T* o = static_cast<T*>(dy);
@@ -213,14 +273,23 @@ isoloco_status isoloco_combine_tokens(const void* y, int64_t ld_y, int32_t dtype
   return err == hipSuccess ? ISOLOCO_OK : hip_fail(err, "combination of tokens");
 }
 
+isoloco_status isoloco_combine_tokens_backward_workspace_size(int64_t tokens, int32_t top_k, size_t* bytes) {
+  if (!bytes) return fail(ISOLOCO_ERR_INVALID_ARG, "bytes is NULL");
+  ISOLOCO_TRY(check_shape(ISOLOCO_F32, tokens, 0, 1, ISOLOCO_I32, top_k));
+  *bytes = combine_grad_workspace(tokens, top_k);
+  return ISOLOCO_OK;
+}
+
 isoloco_status isoloco_combine_tokens_backward(const void* dout, int64_t ld_dout, const void* y, int64_t ld_y,
                                                int32_t dtype, int64_t rows, int64_t dim, const void* row,
                                                int32_t index_type, const float* weight, int64_t tokens, int32_t top_k,
-                                               void* dy, int64_t ld_dy, float* dweight, void* hip_stream) {
+                                               void* dy, int64_t ld_dy, float* dweight, void* workspace,
+                                               size_t workspace_bytes, void* hip_stream) {
   ISOLOCO_TRY(check_shape(dtype, tokens, rows, dim, index_type, top_k));
   if (dweight && !weight) return fail(ISOLOCO_ERR_INVALID_ARG, "dweight needs weight");
-  if (tokens == 0 || (!dy && !dweight)) return ISOLOCO_OK;
+  if (!dy && !dweight) return ISOLOCO_OK;
   const size_t e = dtype_bytes(dtype), ib = index_bytes(index_type), n = (size_t)tokens * top_k;
+  const size_t need = dy ? combine_grad_workspace(tokens, top_k) : 0;
   ISOLOCO_TRY(check_matrix("dout", dout, tokens, dim, ld_dout, e));
   if (dweight) ISOLOCO_TRY(check_matrix("y", y, rows, dim, ld_y, e));
   if (dy) ISOLOCO_TRY(check_matrix("dy", dy, rows, dim, ld_dy, e));
@@ -229,19 +298,22 @@ isoloco_status isoloco_combine_tokens_backward(const void* dout, int64_t ld_dout
                          {"row", row, n * ib, ib},
                          {"weight", weight, weight ? n * 4 : 0, 4}};
   const Operand outs[] = {{"dy", dy, dy ? matrix_bytes(rows, dim, ld_dy, e) : 0, e},
-                          {"dweight", dweight, dweight ? n * 4 : 0, 4}};
-  ISOLOCO_TRY(check_operands(outs, 2, ins, 4));
+                          {"dweight", dweight, dweight ? n * 4 : 0, 4},
+                          {"the workspace", workspace, need, 1}};
+  ISOLOCO_TRY(check_workspace(workspace, workspace_bytes, need));
+  ISOLOCO_TRY(check_operands(outs, 3, ins, 4));
   CombineGradArgs g = {{row, index_type == ISOLOCO_I64}, weight, tokens, rows, dim, ld_dout, ld_y, ld_dy, top_k, dweight, 3};
   const int64_t per = 16 / (int64_t)e;
   while (g.lanes_log2 < kMostLanesLog2 && (per << g.lanes_log2) < dim) ++g.lanes_log2;
   const int64_t blocks = (tokens + (256 >> g.lanes_log2) - 1) >> (8 - g.lanes_log2);
   if (!launchable(blocks, 256)) return fail(ISOLOCO_ERR_UNSUPPORTED, "too many tokens for one launch");
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  int32_t* counts = static_cast<int32_t*>(workspace);
   // Both sides measured, past the caches / through them, us of both passes over 537 MB of rows:
   // 468 / 622 (the stores alone past them 602, the loads alone 610).
   const bool past = rows * dim * (int64_t)e > kCacheBytes;
-  if (dtype == ISOLOCO_F32) (past ? run_grad<float, true> : run_grad<float, false>)(dout, y, dy, g, blocks, st);
-  else (past ? run_grad<__bf16, true> : run_grad<__bf16, false>)(dout, y, dy, g, blocks, st);
+  if (dtype == ISOLOCO_F32) (past ? run_grad<float, true> : run_grad<float, false>)(dout, y, dy, g, blocks, counts, st);
+  else (past ? run_grad<__bf16, true> : run_grad<__bf16, false>)(dout, y, dy, g, blocks, counts, st);
   const hipError_t err = hipGetLastError();
   return err == hipSuccess ? ISOLOCO_OK : hip_fail(err, "gradient of the combination of tokens");
 }

@@ -425,10 +425,11 @@ isoloco_status isoloco_expert_matmul_workspace_size(int64_t tokens, int64_t rows
   if (flags & ~(ISOLOCO_EXPERTS_BACKWARD | ISOLOCO_EXPERTS_ALIGNED | ISOLOCO_EXPERTS_GATHERED))
     return fail(ISOLOCO_ERR_INVALID_ARG, "flags = %d", flags);
   const bool ok = flags & ISOLOCO_EXPERTS_ALIGNED, back = flags & ISOLOCO_EXPERTS_BACKWARD;
-  // (without ALIGNED the operands may be either)
+  // (without ALIGNED each operand may be either)
   const bool gathered = flags & ISOLOCO_EXPERTS_GATHERED;
-  *bytes = call_plan(s, gathered, back, back, true, true, true, ld_x).bytes;
-  if (!ok) *bytes = std::max(*bytes, call_plan(s, gathered, back, back, false, false, false, ld_x).bytes);
+  *bytes = 0;
+  for (int i = ok ? 7 : 0; i < 8; ++i)
+    *bytes = std::max(*bytes, call_plan(s, gathered, back, back, i & 1, i & 2, i & 4, ld_x).bytes);
   return ISOLOCO_OK;
 }
 

@@ -77,10 +77,14 @@ def isoloco_combine_tokens(y, ld_y, dtype, rows, dim, row, index_type, weight, t
                                        stream), "isoloco_combine_tokens")
 
 
+def isoloco_combine_tokens_backward_workspace_size(tokens, top_k):
+    return _size_of("isoloco_combine_tokens_backward_workspace_size", tokens, top_k)
+
+
 def isoloco_combine_tokens_backward(dout, ld_dout, y, ld_y, dtype, rows, dim, row, index_type, weight, tokens, top_k,
-                                    dy, ld_dy, dweight, stream=0):
+                                    dy, ld_dy, dweight, workspace, workspace_bytes, stream=0):
     _check(_lib.isoloco_combine_tokens_backward(dout, ld_dout, y, ld_y, dtype, rows, dim, row, index_type, weight,
-                                                tokens, top_k, dy, ld_dy, dweight, stream),
+                                                tokens, top_k, dy, ld_dy, dweight, workspace, workspace_bytes, stream),
            "isoloco_combine_tokens_backward")
 
 
@@ -334,27 +338,28 @@ def combine_tokens(y, row, weight=None, out=None):
 
 
 @_with_stream
-def combine_tokens_backward(dout, y, row, weight=None, need_dy=True, need_dweight=True):
+def combine_tokens_backward(dout, y, row, weight=None, need_dy=True, need_dweight=True, workspace=None):
     """(dy, dweight) from ``dout`` [tokens, dim]; None for what is not needed (dweight
-    without weight).  No two entries of ``row`` may be the same; where y has as many rows
-    as row has entries, row is taken for a permutation of them, otherwise rows of y that
-    none names have a zero gradient."""
+    without weight).  No two entries of ``row`` may be the same; rows of y that none names
+    have a zero gradient."""
     index, dtype, rows, dim, ld_y, tokens, top_k, index_type, weight_at = _combine_operands(y, row, weight)
     _same_device(index, dout)
     if dout.dtype != y.dtype or tuple(dout.shape) != (tokens, dim):
         raise ValueError("dout must be %s of %s" % (y.dtype, (tokens, dim)))
-    ld_dout = _rows("dout", dout)[1]
-    dy = dweight = dy_at = dweight_at = None
+    ld_dout, device = _rows("dout", dout)[1], y.device
+    dy = dweight = dy_at = dweight_at = keep = ws = None
+    ws_bytes = 0
     if need_dy:
-        make = _empty if rows == row.numel() else torch.zeros
-        dy = make(rows, dim, dtype=y.dtype, device=y.device)
+        dy = _empty(rows, dim, dtype=y.dtype, device=device)
         dy_at = dy.data_ptr()
+        keep, ws, ws_bytes = _workspace(workspace, isoloco_combine_tokens_backward_workspace_size(tokens, top_k), device)
     if need_dweight and weight is not None:
-        dweight = _empty(tokens, top_k, dtype=_F32, device=y.device)
+        dweight = _empty(tokens, top_k, dtype=_F32, device=device)
         dweight_at = dweight.data_ptr()
     _check(_lib.isoloco_combine_tokens_backward(dout.data_ptr(), ld_dout, y.data_ptr(), ld_y, dtype, rows, dim,
                                                 row.data_ptr(), index_type, weight_at, tokens, top_k, dy_at, dim,
-                                                dweight_at, _raw_stream(index)), "isoloco_combine_tokens_backward")
+                                                dweight_at, ws, ws_bytes, _raw_stream(index)),
+           "isoloco_combine_tokens_backward")
     return dy, dweight
 
 

@@ -477,15 +477,35 @@ def test_combine(iso, tokens, top, dim, dtype, more):
     assert torch.isnan(out.as_strided((tokens, 5), (dim + 5, 1), dim)[:-1]).all()
 
 
-def test_combine_gradient_leaves_other_rows(iso):
-    """The C call writes the rows that are named, and no others."""
-    row = torch.tensor([[4, -1], [9, 2]], dtype=I32, device="cuda")
-    dout, dy = torch.randn(2, 40, device="cuda"), torch.full((12, 40), 7.0, device="cuda")
-    iso.isoloco_combine_tokens_backward(dout.data_ptr(), 40, None, 40, iso.ISOLOCO_F32, 12, 40, row.data_ptr(),
-                                        iso.ISOLOCO_I32, None, 2, 2, dy.data_ptr(), 40, None,
-                                        torch.cuda.current_stream().cuda_stream)
-    assert torch.equal(dy[[4, 9, 2]], dout[[0, 1, 1]])
-    assert (dy[[0, 1, 3, 5, 6, 7, 8, 10, 11]] == 7).all()
+@pytest.mark.parametrize("tokens", [3, 700, 5000])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_combine_gradient_of_rows_without_a_token(iso, tokens, dtype):
+    """Slots that are dropped leave rows that no slot names: their gradient is zero, also where
+    there are as many rows as slots and dy's memory held something."""
+    g = gen(tokens)
+    y, dout, w = randn(g, tokens * 2, 96, dtype=dtype), randn(g, tokens, 96, dtype=dtype), randn(g, tokens, 2)
+    row = torch.randperm(tokens * 2, generator=g).view(tokens, 2)
+    row[torch.rand(tokens, 2, generator=g) < 0.3] = -1
+    row[0, 0], row[-1, 1] = 2 ** 31 - 1, -1
+    want = torch.zeros(tokens * 2, 96, dtype=torch.float64)
+    ok = (row >= 0) & (row < tokens * 2)
+    want[row[ok]] = (w.double()[:, :, None] * dout.double()[:, None, :])[ok]
+    filler = [torch.full_like(y, math.nan, device="cuda") for _ in range(8)]
+    del filler
+    r = row.int().cuda()
+    got = iso.combine_tokens_backward(dout.cuda(), y.cuda(), r, w.cuda())[0]
+    within(got, want, ROUND[dtype] * want.abs() + 1e-37)
+    dy = torch.full((tokens * 2, 96), 7.0, device="cuda", dtype=dtype)
+    ws = torch.empty(4096, dtype=torch.uint8, device="cuda")
+    at = (ws.data_ptr() + 255) // 256 * 256
+    d, wd = dout.cuda(), w.cuda()
+    iso.isoloco_combine_tokens_backward(d.data_ptr(), 96, None, 96, iso.ISOLOCO_F32 if dtype == F32 else iso.ISOLOCO_BF16,
+                                        tokens * 2, 96, r.data_ptr(), iso.ISOLOCO_I32, wd.data_ptr(), tokens, 2,
+                                        dy.data_ptr(), 96, None, at, 2048, torch.cuda.current_stream().cuda_stream)
+    assert torch.equal(dy, got)
+    a = wanted(y.cuda())
+    iso.combine_tokens(a, r, wd).backward(d)
+    assert torch.equal(a.grad, got)
 
 
 def test_combine_of_nothing(iso):

@@ -107,13 +107,16 @@ def test_combine_refuses(status, change):
 
 
 COMBINE_GRAD = dict(dout=A, ld_dout=64, y=B, ld_y=64, dtype=1, rows=40, dim=64, row=C, index_type=1, weight=D, tokens=20,
-                    top_k=2, dy=E, ld_dy=64, dweight=F)
+                    top_k=2, dy=E, ld_dy=64, dweight=F, workspace=WS, ws_bytes=BIG)
 
 
 @pytest.mark.parametrize("status,change", [
     (INVALID, dict(dout=0)), (INVALID, dict(y=0)), (INVALID, dict(row=0)), (INVALID, dict(weight=0)),
     (INVALID, dict(ld_dy=10)), (INVALID, dict(ld_dout=10)), (ALIGN, dict(dy=E + 1)), (ALIGN, dict(dweight=F + 1)),
     (ALIGN, dict(row=C + 4)), (ALIAS, dict(dy=A)), (ALIAS, dict(dy=B)), (ALIAS, dict(dweight=D)), (ALIAS, dict(dweight=E)),
+    # (slots that are counted apart)
+    (WORKSPACE, dict(tokens=5000, workspace=0)), (WORKSPACE, dict(tokens=5000, ws_bytes=512)),
+    (WORKSPACE, dict(tokens=5000, workspace=WS + 8)), (ALIAS, dict(tokens=5000, dweight=WS + 256)),
 ])
 def test_combine_backward_refuses(status, change):
     refused(status, iso.isoloco_combine_tokens_backward, *changed(COMBINE_GRAD, **change))
@@ -161,13 +164,26 @@ def test_workspace_sizes_refuse():
     refused(INVALID, iso.isoloco_expert_matmul_workspace_size, 5, 5, 0, 8, 8, 8, 0, 0)
     refused(INVALID, iso.isoloco_expert_matmul_workspace_size, 5, 5, 1, 8, 8, 8, 0, 8)
     refused(INVALID, iso.isoloco_distill_loss_workspace_size, 5, 0)
+    refused(INVALID, iso.isoloco_combine_tokens_backward_workspace_size, -1, 2)
+    refused(INVALID, iso.isoloco_combine_tokens_backward_workspace_size, 5, 0)
+
+
+def test_workspace_of_experts_covers_every_alignment():
+    """Without the flag the size is enough whichever operands are aligned: one row of x far
+    from the next, so that gathered rows are copied, and weights that are too."""
+    need = iso.isoloco_expert_matmul_workspace_size
+    tokens, rows, far = 1000, 8000, 1 << 22
+    whole = need(tokens, rows, 8, 64, 64, far, 1, 4)
+    # the gathered rows, the weights' copy
+    assert whole >= rows * 64 * 2 + 8 * 64 * 64 * 2
+    assert need(tokens, rows, 8, 64, 64, 64, 1, 4 | 2) < whole
 
 
 def test_nothing_is_nothing():
     """Calls without rows end before any launch."""
     iso.isoloco_expert_matmul(*changed(EXPERTS, rows=0))
     iso.isoloco_combine_tokens(*changed(COMBINE, tokens=0))
-    iso.isoloco_combine_tokens_backward(*changed(COMBINE_GRAD, dy=0, dweight=0))
+    iso.isoloco_combine_tokens_backward(*changed(COMBINE_GRAD, dy=0, dweight=0, workspace=0))
     iso.isoloco_distill_loss(*changed(DISTILL, rows=0))
     iso.isoloco_route_tokens_backward(*changed(ROUTE_GRAD, tokens=0))
 
