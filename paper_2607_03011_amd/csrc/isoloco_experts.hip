@@ -36,10 +36,10 @@ isoloco_status check_shape(const ExpertShape& s) {
   if (s.experts < 1 || s.experts > ISOLOCO_MAX_EXPERTS)
     return fail(ISOLOCO_ERR_INVALID_ARG, "%lld experts, of 1 to %d", (long long)s.experts, ISOLOCO_MAX_EXPERTS);
   if (!is_dtype(s.dtype)) return fail(ISOLOCO_ERR_INVALID_ARG, "dtype %d", s.dtype);
-  // tiles are counted in 32 bits (splits are of few tiles)
+  // 64 experts' tiles are counted in 32 bits (splits are of few tiles)
   const int64_t dims = (s.dim + 127) / 128, cols = (s.cols + 127) / 128;
-  if ((s.rows / 128 + std::min(s.rows, s.experts)) * std::max(dims, cols) > INT32_MAX / 2 ||
-      s.experts * dims * cols > INT32_MAX / 2)
+  if ((s.rows / 128 + std::min(s.rows, s.experts)) * std::max(dims, cols) > 1 << 24 ||
+      dims * cols > 1 << 24)
     return fail(ISOLOCO_ERR_UNSUPPORTED, "too many tiles: %lld rows, %lld experts of %lld x %lld", (long long)s.rows,
                 (long long)s.experts, (long long)s.cols, (long long)s.dim);
   return ISOLOCO_OK;

@@ -60,7 +60,9 @@ __device__ __forceinline__ int64_t lane_of(int64_t v, int at) {
 }
 
 // Where the tiles lie, 64 experts at a time, one a lane: every wave by itself.  What an expert
-// counts are its tiles, or (kDw, where all have as many) the slabs of its tiles.
+// counts are its tiles, or (kDw, where all have as many) the slabs of its tiles (in 128s where
+// the rows are many).  64 experts' counts fit 32 bits also where offsets fall and every expert
+// has all rows: whatever they are, a tile lies inside the tensors.
 template <ExpertProduct P, class C>
 struct Finder {
   int64_t begin, end;  // of this lane's expert
@@ -73,14 +75,15 @@ struct Finder {
     own = 0;
     if (e < t.g.groups.experts) {
       t.g.groups.rows_of(e, begin, end);
-      own = P == kDw ? (int)((end - begin + kSlab - 1) / kSlab) + kTileCost * t.splits
+      const int many = t.g.groups.rows >> 24 ? 7 : 0;
+      own = P == kDw ? (int)((end - begin + kSlab - 1) / kSlab >> many) + kTileCost * t.splits
                      : (int)((end - begin + C::TM - 1) / C::TM) * t.tiles_n * t.splits;
     }
     upto = scan(own);
   }
   // all counts
-  __device__ __forceinline__ int all(const TileArgs& t) {
-    int sum = 0;
+  __device__ __forceinline__ int64_t all(const TileArgs& t) {
+    int64_t sum = 0;
     for (int first = 0; first < t.g.groups.experts; first += 64) {
       if (first != base) load(t, first);
       sum += __builtin_amdgcn_readlane(upto, 63);
@@ -88,7 +91,7 @@ struct Finder {
     return sum;
   }
   // the lane whose count passes `index`, and what is before the lane's 64; -1: none does
-  __device__ __forceinline__ int pass(const TileArgs& t, int index, int& before) {
+  __device__ __forceinline__ int pass(const TileArgs& t, int64_t index, int64_t& before) {
     before = 0;
     for (int first = 0; first < t.g.groups.experts; first += 64) {
       if (first != base) load(t, first);
@@ -99,9 +102,9 @@ struct Finder {
     return -1;
   }
   // kDw: the tile that begins where the counts reach `index`
-  __device__ __forceinline__ int64_t tile_at(const TileArgs& t, int index) {
+  __device__ __forceinline__ int64_t tile_at(const TileArgs& t, int64_t index) {
     const int64_t per = (int64_t)t.tiles_m * t.tiles_n * t.splits;
-    int before;
+    int64_t before;
     const int at = pass(t, index, before);
     if (at < 0) return t.g.groups.experts * per;
     const int count = __builtin_amdgcn_readlane(own, at), past = __builtin_amdgcn_readlane(upto, at) - count;
@@ -120,10 +123,10 @@ struct Finder {
       o.begin = lane_of(begin, at);
       o.end = lane_of(end, at);
     } else {
-      int before;
-      const int at = pass(t, (int)index, before);
+      int64_t before;
+      const int at = pass(t, index, before);
       o.group = base + at;
-      i = (int)index - before - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(own, at));
+      i = index - before - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(own, at));
       o.begin = lane_of(begin, at);
       o.end = lane_of(end, at);
     }
@@ -410,8 +413,8 @@ __device__ __forceinline__ void run_of(const TileArgs& t, Finder<P, C>& finder, 
   from = all * xcd / 8;
   to = all * (xcd + 1) / 8;
   if (P == kDw) {
-    from = finder.tile_at(t, (int)from);
-    to = finder.tile_at(t, (int)to);
+    from = finder.tile_at(t, from);
+    to = finder.tile_at(t, to);
   }
 }
 

@@ -411,6 +411,26 @@ def test_expert_matmul_offsets_outside(iso):
             assert torch.equal(p, q)
 
 
+@pytest.mark.parametrize("experts,rows", [(3, 40), (70, 900), (5, 3000)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_expert_matmul_offsets_of_any_kind(iso, experts, rows, dtype):
+    """Offsets that fall and lie anywhere: what is around the results stays as it was."""
+    g = gen(experts)
+    offsets = torch.randint(-rows, 2 * rows, (experts + 1,), generator=g).cuda()
+    token = torch.randint(-5, 60, (rows,), generator=g).cuda()
+    x, w = randn(g, 50, 72, dtype=dtype).cuda(), randn(g, experts, 136, 72, dtype=dtype).cuda()
+    around = torch.full((rows + 20, 136 + 16), 7.0, dtype=dtype, device="cuda")
+    out = around[10:rows + 10, 8:144]
+    out.zero_()
+    iso.expert_matmul(x, w, offsets, token=token, out=out)
+    assert torch.isfinite(out).all()
+    out.fill_(7.0)
+    assert (around == 7.0).all()
+    dx, dw = iso.expert_matmul_backward(x[token.clamp(0, 49)], w, offsets, randn(g, rows, 136, dtype=dtype).cuda())
+    # (dw is each expert's own; rows that two experts claim are one's, those that none does are any)
+    assert dx.shape == (rows, 72) and torch.isfinite(dw).all()
+
+
 def test_expert_matmul_against_differences(iso):
     """The products are linear in each operand: a difference of any step is the slope."""
     offsets, token, row, x, w, d = expert_inputs(60, 5, 2, 48, 56, F32, 4)

@@ -200,7 +200,7 @@ def test_tiles_past_32_bits_are_refused():
     far = dict(x=1 << 60, w=1 << 58, out=1 << 59, offsets=64, token=1 << 44)
     refused(UNSUPPORTED, iso.isoloco_expert_matmul, *changed(
         EXPERTS, **far, rows=1 << 30, cols=1 << 20, ld_out=1 << 20, stride_w=1 << 26, dim=64))
-    refused(UNSUPPORTED, iso.isoloco_expert_matmul_workspace_size, 5, 5, 1024, 4000000, 4000000, 4000000, 1, 0)
+    refused(UNSUPPORTED, iso.isoloco_expert_matmul_workspace_size, 5, 5, 1, 4000000, 4000000, 4000000, 1, 0)
 
 
 def test_tensors_on_the_host_are_refused():
