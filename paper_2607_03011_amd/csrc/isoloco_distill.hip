@@ -47,7 +47,8 @@ struct Rate {
 Rate rate_parts(float scale) {
   const float hi = rate_of(scale);
   const double lo = (double)scale * 1.4426950408889634074 - hi;
-  return {hi, hi == FLT_MAX ? 0.f : (float)lo, -200.f / hi};
+  // (finite: a masked logit is at -infinity, however small the scale)
+  return {hi, hi == FLT_MAX ? 0.f : (float)lo, fmaxf(-200.f / hi, -FLT_MAX)};
 }
 
 // e^(d scale), d <= 0.  EXACT: to float32's last bits, for float32 logits (the rounding of the
@@ -55,9 +56,8 @@ Rate rate_parts(float scale) {
 template <bool EXACT>
 __device__ __forceinline__ float power(float d, const Rate& r) {
   if constexpr (!EXACT) return __builtin_amdgcn_exp2f(d * r.hi);
-  d = d < r.least ? r.least : d;  // (a NaN stays)
-  const float n = __builtin_rintf(d * r.hi);
-  return ldexpf(__builtin_amdgcn_exp2f(fmaf(d, r.lo, fmaf(d, r.hi, -n))), (int)n);
+  const float n = __builtin_rintf(d * r.hi), e = ldexpf(__builtin_amdgcn_exp2f(fmaf(d, r.lo, fmaf(d, r.hi, -n))), (int)n);
+  return d < r.least ? 0.f : e;  // (a NaN stays)
 }
 
 // Whether the pass over the row leaves the listed columns out

@@ -706,6 +706,22 @@ def test_distill_large_finite_masks(iso, dtype, value):
             assert torch.equal(da, db)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rest", ["drop", "bucket"])
+def test_distill_small_scale(iso, dtype, rest):
+    """Masked columns weigh nothing at a scale that leaves nothing of the others' differences."""
+    scale, up = 2.0 ** -123, 2.0 ** 100
+    x, t, index = distill_inputs(6, 500, 8, dtype, 1.0, 8)
+    t = torch.log_softmax(torch.arange(8.0).expand(6, 8), 1) - 0.5  # their sum is e^-0.5
+    dloss = torch.full((6,), up)
+    want, bound, _ = distill_reference(x, t, index, scale, rest)
+    r = iso.distill_loss(x.cuda(), t.cuda(), index.cuda(), scale=scale, rest=rest)
+    within(r.loss, want, bound)
+    grad, size = distill_reference(x, t, index, scale, rest, dloss)
+    d = iso.distill_loss_backward(x.cuda(), t.cuda(), index.cuda(), r.stats, dloss.cuda(), scale=scale, rest=rest)
+    within(d, grad, size + ROUND[dtype] * grad.abs() + 1e-37)
+
+
 def test_distill_small_rest(iso):
     """A rest of 1e-12 of the student's probability is as exact as any."""
     x = torch.full((1, 1000), -30.0)
