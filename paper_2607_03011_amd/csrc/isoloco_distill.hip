@@ -9,6 +9,14 @@
 //   W = sum_i p_i (+ p_r);  dz_j = q_j W - sum of the p_i with c_i = j, less p_r q_j / q_r
 //   where j is not listed
 //
+// With M the maximum over the columns that are not listed, A the sum of their e^((x_j - M) scale)
+// and S that of all against the row's maximum m, those columns' gradient is
+//
+//   dz_j = c e^((x_j - M) scale),   c = W e^((M - m) scale) / S - p_r / A
+//
+// one exponential against their own maximum: against the row's it is 0 in float32 once they lie
+// 87 / scale below it, where p_r / q_r is past float32 and the product is still their share of p_r.
+//
 // The loss is the difference of nearly equal numbers once the student has learnt, so what
 // is formed once a row is formed in 64 bits; the sums over the vocabulary are of float32
 // exponentials.  q_r is summed from the columns that are not listed, not taken as one less
@@ -179,7 +187,9 @@ __device__ void put_loss(const LossArgs& g, const T* row, const int32_t* column,
   }
   loss = wave_sum(loss);
   weight = wave_sum(weight);
-  double rest_factor = weight;
+  // the gradient's factor of the columns that are not listed, against a.m
+  const double beside = a.m == -INFINITY ? 0.0 : exp(((double)a.m - xm) * scale) / s;
+  double rest_factor = weight * beside;
   if (BUCKET) {
     // (columns that are all masked, or none, are no bucket: what the rounding of the
     // teacher's values leaves of one less their sum would make the loss infinite)
@@ -187,7 +197,7 @@ __device__ void put_loss(const LossArgs& g, const T* row, const int32_t* column,
     if (p_r > 0.0 && others > 0.0) {
       const double log_r = log(others) - log_s;
       loss += p_r * (log(p_r) - log_r);
-      rest_factor = 1.0 - p_r * exp(-log_r);
+      rest_factor = beside - p_r / a.s;
       weight = 1.0;
     } else if (others != others) {
       loss = others;
@@ -195,8 +205,8 @@ __device__ void put_loss(const LossArgs& g, const T* row, const int32_t* column,
   }
   if (lane == 0) {
     g.loss[r] = (float)loss;
-    // what the gradient takes: q_j = (stats[1] + [7]) e^((x_j - [0]) scale), the factors of q at
-    // listed and other columns, and p_i = ([5] + [8]) e^(t_i - [4])
+    // what the gradient takes: at listed columns q_j = (stats[1] + [7]) e^((x_j - [0]) scale) with
+    // the factor [2] and p_i = ([5] + [8]) e^(t_i - [4]), at others [3] e^((x_j - [9]) scale)
     float* o = g.stats + r * ISOLOCO_DISTILL_STATS;
     o[0] = s != s ? NAN : (float)xm;
     o[1] = (float)(1.0 / s);
@@ -207,7 +217,8 @@ __device__ void put_loss(const LossArgs& g, const T* row, const int32_t* column,
     o[5] = none ? 0.f : (float)inv_p;
     o[8] = none ? 0.f : (float)(inv_p - (double)o[5]);
     o[6] = s == 0.0 ? -INFINITY : (float)(xm * scale + log_s);
-    o[9] = 0.f;
+    // (columns that are all masked: 0 times what -infinity gives)
+    o[9] = s != s ? NAN : a.m == -INFINITY ? 0.f : a.m;
   }
 }
 
@@ -410,11 +421,11 @@ __global__ void __launch_bounds__(kGradThreads) distill_grad_kernel(const T* log
   const T* row = logits + r * g.ld;
   T* out = dlogits + r * g.ld_d;
   const float* st = g.stats + r * ISOLOCO_DISTILL_STATS;
-  const float m = st[0], inv_s = st[1], factor = st[2], rest_factor = st[3], tm = st[4], inv_p = st[5];
+  const float m = st[0], inv_s = st[1], factor = st[2], tm = st[4], inv_p = st[5];
   const float dl = g.dloss[r] * g.scale;
   // nothing to hand back: no loss wanted, no teacher, no student
   const bool none = dl == 0.f || inv_p == 0.f || m == -INFINITY;
-  const float from = none ? 0.f : m;
+  const float from = none ? 0.f : m, from_other = st[9];
   u32x4 v[kGradVecs];
 #pragma unroll
   for (int u = 0; u < kGradVecs; ++u) {
@@ -443,8 +454,8 @@ __global__ void __launch_bounds__(kGradThreads) distill_grad_kernel(const T* log
     if (mine) x_top = (float)row[c];
   }
   __syncthreads();
-  const float other = none ? 0.f : inv_s * rest_factor * dl;
-  const auto grad = [&](float x) { return none ? 0.f : power<sizeof(T) == 4>(x - from, g.rate) * other; };
+  const float other = none ? 0.f : st[3] * dl;
+  const auto grad = [&](float x) { return none ? 0.f : power<sizeof(T) == 4>(x - from_other, g.rate) * other; };
 #pragma unroll
   for (int u = 0; u < kGradVecs; ++u) {
     const int64_t j = first + u * kGradThreads + threadIdx.x;
