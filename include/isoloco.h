@@ -584,7 +584,8 @@ isoloco_status isoloco_combine_tokens_backward(const void* dout, int64_t ld_dout
  *
  * where q_r is the sum of q over the columns that are not listed: what the teacher
  * gives to all others is compared as one (left out where the student has no such
- * column, or only masked ones).  An entry outside the vocabulary is none; a row
+ * column, or only masked ones: logits of -infinity.  Columns that are all at a large
+ * finite value, -1e30 say, are a bucket as any, and log q_r is as large).  An entry outside the vocabulary is none; a row
  * without entries has no loss and no gradient.  t_i = -infinity adds nothing; a
  * column that is listed twice counts as often.  Logits of -infinity are masked: q =
  * 0, and the loss is infinite where p_i > 0 there.  A NaN or +infinity among a row's

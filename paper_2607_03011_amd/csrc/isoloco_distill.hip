@@ -192,10 +192,11 @@ __device__ void put_loss(const LossArgs& g, const T* row, const int32_t* column,
   double rest_factor = weight * beside;
   if (BUCKET) {
     // (columns that are all masked, or none, are no bucket: what the rounding of the
-    // teacher's values leaves of one less their sum would make the loss infinite)
+    // teacher's values leaves of one less their sum would make the loss infinite.  Any that
+    // is not masked makes one: q_r is taken by its logarithm, as it may be past a double.)
     const double p_r = 1.0 - weight;
-    if (p_r > 0.0 && others > 0.0) {
-      const double log_r = log(others) - log_s;
+    if (p_r > 0.0 && a.m > -INFINITY && a.s > 0.0) {
+      const double log_r = ((double)a.m - xm) * scale + log(a.s) - log_s;
       loss += p_r * (log(p_r) - log_r);
       rest_factor = beside - p_r / a.s;
       weight = 1.0;

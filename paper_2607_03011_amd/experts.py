@@ -411,7 +411,9 @@ def distill_loss(logits, top_logprob, top_index, scale=1.0, rest="drop", workspa
     most likely tokens, ``top_index`` (int32 or int64; entries outside the vocabulary
     are none) with ``top_logprob`` (float32), [..., top_k] each, as ``token_logprobs``
     gives them.  ``rest``: "drop" compares the listed tokens alone, the teacher's
-    probabilities over their sum; "bucket" compares all others' sum as one more."""
+    probabilities over their sum; "bucket" compares all others' sum as one more.  Mask
+    logits with -infinity: where every other column has a large finite one, the bucket is
+    as far from the teacher's as that says."""
     if logits.requires_grad and _recorded(None):
         if top_logprob.requires_grad:
             raise ValueError("the teacher's log probabilities carry no gradient: detach them")

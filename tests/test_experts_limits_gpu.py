@@ -77,3 +77,27 @@ def test_distill_gradient_of_a_far_rest(iso, dtype, scale, vocab):
         a = wanted(dev)
         iso.distill_loss(a, td, ix, scale=scale, rest="bucket").loss.sum().backward()
         assert torch.equal(a.grad, d)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("margin", [740.0, 750.0, 800.0, 5000.0, 1e30, 3e38])
+@pytest.mark.parametrize("vocab", [300, 100003])
+def test_distill_of_a_rest_past_any_exponential(iso, dtype, margin, vocab):
+    """The rest's term is p_r (log p_r - log q_r) also where no double holds q_r; only
+    -infinity masks a column."""
+    x, t, index = far_inputs(margin, dtype, 1.0, vocab)
+    loss, bound, grad, size = far_reference(x, t, index, 1.0)
+    dev, td, ix = x.cuda(), t.cuda(), index.cuda()
+    r = iso.distill_loss(dev, td, ix, rest="bucket")
+    within(r.loss, loss, bound)
+    d = iso.distill_loss_backward(dev, td, ix, r.stats, torch.ones(5, device="cuda"), rest="bucket")
+    within(d, grad, size + HALF[dtype] * (grad.abs() + size) + 1e-37)
+    # masked: no such columns
+    listed = torch.zeros(5, vocab, dtype=torch.bool).scatter_(1, index, True)
+    masked = x.masked_fill(~listed, -math.inf).cuda()
+    r = iso.distill_loss(masked, td, ix, rest="bucket")
+    log_q = torch.log_softmax(x.double().gather(1, index), 1)
+    want = (t.double().exp() * (t.double() - log_q)).sum(1)
+    within(r.loss, want, 2 * 264 * U32 + 2 * U32 * want.abs())
+    d = iso.distill_loss_backward(masked, td, ix, r.stats, torch.ones(5, device="cuda"), rest="bucket")
+    assert torch.isfinite(d).all() and not d.cpu()[~listed].any()
