@@ -543,14 +543,32 @@ isoloco_status isoloco_expert_matmul(const void* x, int64_t ld_x, int64_t tokens
  *   dx[r] = dout[r] w[e] (rows x dim: of the grouped rows; rows of no expert: zeros)
  *   dw[e] = sum over the rows of e of dout[r]^T x_r (zeros without any)
  *
- * With token given, the gradient of x is the sum of dx over a token's rows: what
- * isoloco_combine_tokens without weight forms. */
+ * With token given, the gradient of x is the sum of dx over a token's rows, which
+ * isoloco_expert_matmul_backward_tokens forms. */
 isoloco_status isoloco_expert_matmul_backward(const void* x, int64_t ld_x, int64_t tokens, const void* token,
                                               const void* w, int64_t ld_w, int64_t stride_w, int32_t dtype,
                                               const void* offsets, int32_t index_type, int64_t experts, int64_t rows,
                                               int64_t dim, int64_t cols, const void* dout, int64_t ld_dout, void* dx,
                                               int64_t ld_dx, void* dw, int64_t ld_dw, int64_t stride_dw,
                                               void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* The same where token is given, with the gradient of x itself:
+ *
+ *   dx[t] = sum_j of row row[t, j] of the above's dx (tokens x dim)
+ *
+ * row (tokens x top_k, of row_type; isoloco_route_tokens' row): the rows whose token is t,
+ * entries outside 0 .. rows - 1 add nothing.  The rows are held in float32, in dx_rows (rows x dim:
+ * scratch), and a sum is rounded once.  dx is formed always, dw unless it is NULL, and
+ * the workspace's size is the one for the gradient with token given.  top_k <=
+ * ISOLOCO_MAX_TOP. */
+isoloco_status isoloco_expert_matmul_backward_tokens(const void* x, int64_t ld_x, int64_t tokens, const void* token,
+                                                     const void* row, int32_t row_type, int32_t top_k, const void* w,
+                                                     int64_t ld_w, int64_t stride_w, int32_t dtype, const void* offsets,
+                                                     int32_t index_type, int64_t experts, int64_t rows, int64_t dim,
+                                                     int64_t cols, const void* dout, int64_t ld_dout, void* dx,
+                                                     int64_t ld_dx, float* dx_rows, void* dw, int64_t ld_dw,
+                                                     int64_t stride_dw, void* workspace, size_t workspace_bytes,
+                                                     void* hip_stream);
 
 /* out[t] = sum_j weight[t, j] y[row[t, j]]; y: rows x dim, row and weight: tokens x
  * top_k (weight NULL: ones), out: tokens x dim.  Entries of row outside 0 .. rows

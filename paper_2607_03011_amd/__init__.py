@@ -35,6 +35,7 @@ __all__ = [
     "combine_tokens", "combine_tokens_backward", "distill_loss", "distill_loss_backward", "DistillLoss",
     "isoloco_route_tokens_workspace_size", "isoloco_route_tokens", "isoloco_route_tokens_backward",
     "isoloco_expert_matmul_workspace_size", "isoloco_expert_matmul", "isoloco_expert_matmul_backward",
+    "isoloco_expert_matmul_backward_tokens",
     "isoloco_combine_tokens", "isoloco_combine_tokens_backward_workspace_size", "isoloco_combine_tokens_backward",
     "isoloco_distill_loss_workspace_size", "isoloco_distill_loss", "isoloco_distill_loss_backward",
     "ISOLOCO_MAX_EXPERTS", "ISOLOCO_EXPERTS_BACKWARD", "ISOLOCO_EXPERTS_ALIGNED", "ISOLOCO_EXPERTS_GATHERED",
@@ -95,6 +96,7 @@ EXPORTED_SYMBOLS = (
     "isoloco_gated_ffn_workspace_size", "isoloco_gated_ffn", "isoloco_gated_ffn_backward",
     "isoloco_route_tokens_workspace_size", "isoloco_route_tokens", "isoloco_route_tokens_backward",
     "isoloco_expert_matmul_workspace_size", "isoloco_expert_matmul", "isoloco_expert_matmul_backward",
+    "isoloco_expert_matmul_backward_tokens",
     "isoloco_combine_tokens", "isoloco_combine_tokens_backward_workspace_size", "isoloco_combine_tokens_backward",
     "isoloco_distill_loss_workspace_size", "isoloco_distill_loss", "isoloco_distill_loss_backward",
 )
@@ -195,6 +197,9 @@ _sig = {
                                              _P, _I64, _P, _SIZE, _P]),
     "isoloco_expert_matmul_backward": (ctypes.c_int, [_P, _I64, _I64, _P, _P, _I64, _I64, _I32, _P, _I32, _I64, _I64,
                                                       _I64, _I64, _P, _I64, _P, _I64, _P, _I64, _I64, _P, _SIZE, _P]),
+    "isoloco_expert_matmul_backward_tokens": (ctypes.c_int, [
+        _P, _I64, _I64, _P, _P, _I32, _I32, _P, _I64, _I64, _I32, _P, _I32, _I64, _I64, _I64, _I64, _P, _I64, _P, _I64, _P,
+        _P, _I64, _I64, _P, _SIZE, _P]),
     "isoloco_combine_tokens": (ctypes.c_int, [_P, _I64, _I32, _I64, _I64, _P, _I32, _P, _I64, _I32, _P, _I64, _P]),
     "isoloco_combine_tokens_backward": (ctypes.c_int, [_P, _I64, _P, _I64, _I32, _I64, _I64, _P, _I32, _P, _I64, _I32,
                                                        _P, _I64, _P, _P, _SIZE, _P]),
@@ -437,5 +442,6 @@ from .experts import (  # noqa: E402,F401
     expert_matmul, expert_matmul_backward, isoloco_combine_tokens, isoloco_combine_tokens_backward,
     isoloco_combine_tokens_backward_workspace_size,
     isoloco_distill_loss, isoloco_distill_loss_backward, isoloco_distill_loss_workspace_size, isoloco_expert_matmul,
-    isoloco_expert_matmul_backward, isoloco_expert_matmul_workspace_size, isoloco_route_tokens,
+    isoloco_expert_matmul_backward, isoloco_expert_matmul_backward_tokens, isoloco_expert_matmul_workspace_size,
+    isoloco_route_tokens,
     isoloco_route_tokens_backward, isoloco_route_tokens_workspace_size, route_tokens, route_tokens_backward)

@@ -15,6 +15,7 @@
 
 #include "isoloco_device.h"
 #include "isoloco_error.h"
+#include "isoloco_experts.h"
 #include "isoloco_vec.h"
 
 namespace isoloco {
@@ -29,10 +30,11 @@ struct CombineArgs {
 
 constexpr int kAtOnce = 8;  // rows whose pieces a thread has in flight
 
-// One thread per piece of 16 bytes of the result (16384 tokens of 8 rows of 2048 in bfloat16:
-// 120 us, 5.0 TB/s; with the rows read past the caches 27 us more).
-template <typename T>
-__global__ void __launch_bounds__(256) combine_kernel(const T* y, T* out, CombineArgs g, int pieces) {
+// One thread per piece of 16 bytes of y's rows (16384 tokens of 8 rows of 2048 in bfloat16:
+// 120 us, 5.0 TB/s; with the rows read past the caches 27 us more).  PAST: of rows that were
+// stored past the caches.
+template <typename T, typename O, bool PAST>
+__global__ void __launch_bounds__(256) combine_kernel(const T* y, O* out, CombineArgs g, int pieces) {
   constexpr int N = Vec<T>::N;
   const int64_t item = (int64_t)blockIdx.x * 256 + threadIdx.x, t = item / pieces;
   if (t >= g.tokens) return;
@@ -48,7 +50,7 @@ __global__ void __launch_bounds__(256) combine_kernel(const T* y, T* out, Combin
       const bool in = r >= 0 && r < g.rows;
       w[u] = in ? (g.weight ? g.weight[t * g.top_k + j] : 1.f) : 0.f;
       v[u] = (u32x4){};
-      if (in) v[u] = load_raw<T>(y + r * g.ld_y + col, left);
+      if (in) v[u] = load_raw<T, PAST>(y + r * g.ld_y + col, left);
     }
 #pragma unroll
     for (int u = 0; u < kAtOnce; ++u) {
@@ -58,7 +60,17 @@ __global__ void __launch_bounds__(256) combine_kernel(const T* y, T* out, Combin
       for (int e = 0; e < N; ++e) sum[e] = fmaf(w[u], x[e], sum[e]);
     }
   }
-  store_piece<T>(out + t * g.ld_out + col, left, sum);
+  O* to = out + t * g.ld_out + col;
+  if constexpr (sizeof(O) == sizeof(T)) {
+    store_piece<O>(to, left, sum);
+  } else if (left >= N) {
+    // (half a piece)
+    *reinterpret_cast<u32x2_any*>(to) = pack4(sum);
+  } else {
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (e < left) to[e] = (O)sum[e];
+  }
 }
 
 // Rows of dy that no slot names have no gradient.  As no two slots name one, there are such rows
@@ -203,10 +215,10 @@ __global__ void __launch_bounds__(256) combine_grad_kernel(const T* dout, const 
   }
 }
 
-template <typename T>
+template <typename T, typename O = T, bool PAST = false>
 void run_forward(const void* y, void* out, const CombineArgs& g, int pieces, int64_t blocks, hipStream_t st) {
-  hipLaunchKernelGGL(combine_kernel<T>, dim3((unsigned)blocks), dim3(256), 0, st, static_cast<const T*>(y),
-                     static_cast<T*>(out), g, pieces);
+  hipLaunchKernelGGL((combine_kernel<T, O, PAST>), dim3((unsigned)blocks), dim3(256), 0, st, static_cast<const T*>(y),
+                     static_cast<O*>(out), g, pieces);
 }
 
 size_t combine_grad_workspace(int64_t tokens, int32_t top_k) {
@@ -244,6 +256,20 @@ isoloco_status check_shape(int32_t dtype, int64_t tokens, int64_t rows, int64_t 
 }
 
 }  // namespace
+
+bool rows_sum_launchable(int64_t tokens, int64_t dim) { return launchable((tokens * ((dim + 3) / 4) + 255) / 256, 256); }
+
+hipError_t launch_rows_sum(const float* y, int64_t rows, int64_t dim, Index row, int64_t tokens, int top_k, bool f32,
+                           bool past, void* out, int64_t ld_out, hipStream_t st) {
+  const CombineArgs g = {row, nullptr, tokens, rows, dim, dim, ld_out, top_k};
+  const int64_t pieces = (dim + 3) / 4, blocks = (tokens * pieces + 255) / 256;
+  if (blocks == 0) return hipSuccess;
+  if (f32) run_forward<float>(y, out, g, (int)pieces, blocks, st);
+  else if (past) run_forward<float, __bf16, true>(y, out, g, (int)pieces, blocks, st);
+  else run_forward<float, __bf16>(y, out, g, (int)pieces, blocks, st);
+  return hipGetLastError();
+}
+
 }  // namespace isoloco
 
 using namespace isoloco;

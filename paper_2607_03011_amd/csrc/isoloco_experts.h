@@ -28,6 +28,7 @@ struct Groups {
 // their columns multiples of 8.
 //   kOut  a: rows (or, with token, tokens) of k, b: n rows of k per expert;  out: rows x n
 //   kDx   a: rows of k, b: k rows of n per expert;                           out: rows x n
+//         (wide_out: of float32, whatever the operands are; past: those past the caches)
 //   kDw   a: rows of m, b: rows (or, with token, tokens) of n;               out: m x n per expert
 struct ExpertArgs {
   Groups groups;
@@ -39,6 +40,7 @@ struct ExpertArgs {
   int64_t cols_a, cols_b;  // columns of the operands whose rows are k values: multiples of 8, at least m and n
   void* out;
   int64_t ld_out, stride_out;
+  bool wide_out, past;
   float* partial;
 };
 
@@ -49,5 +51,11 @@ hipError_t launch_expert_out(bool f32, const ExpertArgs& g, hipStream_t st);
 // kDx and kDw, either of which may be NULL; their `partial` is the same.
 size_t expert_gradients_partial_bytes(bool f32, int64_t rows, int64_t experts, int64_t dim, int64_t cols);
 hipError_t launch_expert_gradients(bool f32, const ExpertArgs* dx, const ExpertArgs* dw, hipStream_t st);
+
+// out[t] = sum_j y[row[t, j]] of float32 rows of dim, rounded once to out's type (past: the rows lie
+// past the caches), where the elements are not too many for a launch
+bool rows_sum_launchable(int64_t tokens, int64_t dim);
+hipError_t launch_rows_sum(const float* y, int64_t rows, int64_t dim, Index row, int64_t tokens, int top_k, bool f32,
+                           bool past, void* out, int64_t ld_out, hipStream_t st);
 
 }  // namespace isoloco

@@ -377,7 +377,8 @@ hipError_t run_forward(const Call& c, const CallPlan& p, void* out, int64_t ld_o
   return launch_expert_out(c.s.dtype == ISOLOCO_F32, g, st);
 }
 
-hipError_t run_backward(const Call& c, const CallPlan& p, void* dx, int64_t ld_dx, void* dw, int64_t ld_dw,
+// wide_dx: dx of float32, past: and past the caches
+hipError_t run_backward(const Call& c, const CallPlan& p, void* dx, int64_t ld_dx, bool wide_dx, bool past, void* dw, int64_t ld_dw,
                         int64_t stride_dw, char* ws, hipStream_t st) {
   const bool f32 = c.s.dtype == ISOLOCO_F32;
   const int64_t dim = ffn_pad(c.s.dim), cols = ffn_pad(c.s.cols);
@@ -397,6 +398,8 @@ hipError_t run_backward(const Call& c, const CallPlan& p, void* dx, int64_t ld_d
   x.k = c.s.cols;
   x.out = dx;
   x.ld_out = ld_dx;
+  x.wide_out = wide_dx;
+  x.past = past;
   w.b = o.x;
   w.ld_b = o.ld_x;
   w.part_b = o.part_x;
@@ -407,6 +410,73 @@ hipError_t run_backward(const Call& c, const CallPlan& p, void* dx, int64_t ld_d
   w.ld_out = ld_dw;
   w.stride_out = stride_dw;
   return launch_expert_gradients(f32, dx ? &x : nullptr, dw ? &w : nullptr, st);
+}
+
+// What a call of the gradients is given.
+struct Gradients {
+  ExpertShape s;
+  const void *x, *token, *w, *offsets, *dout;
+  int64_t ld_x, ld_w, stride_w, ld_dout;
+  int32_t index_type;
+  void *dx, *dw;
+  int64_t ld_dx, ld_dw, stride_dw;
+  // dx of the tokens: the sums of float32 rows, which are formed in dx_rows
+  const void* row;
+  int32_t row_type, top_k;
+  float* dx_rows;
+  bool sum;
+};
+
+isoloco_status gradients(Gradients g, void* workspace, size_t workspace_bytes, hipStream_t st) {
+  const ExpertShape& s = g.s;
+  ISOLOCO_TRY(check_shape(s));
+  if (!is_index_type(g.index_type)) return fail(ISOLOCO_ERR_INVALID_ARG, "index type %d", g.index_type);
+  if (!g.token && !g.sum && s.tokens != s.rows)
+    return fail(ISOLOCO_ERR_INVALID_ARG, "%lld rows of x, %lld wanted", (long long)s.tokens, (long long)s.rows);
+  const size_t e = dtype_bytes(s.dtype), ib = index_bytes(g.index_type);
+  if (g.sum) {
+    if (!is_index_type(g.row_type)) return fail(ISOLOCO_ERR_INVALID_ARG, "index type of row %d", g.row_type);
+    if (g.top_k < 1 || g.top_k > ISOLOCO_MAX_TOP)
+      return fail(ISOLOCO_ERR_INVALID_ARG, "top_k = %d, of 1 to %d", g.top_k, ISOLOCO_MAX_TOP);
+    if (!rows_sum_launchable(s.tokens, s.dim)) return fail(ISOLOCO_ERR_UNSUPPORTED, "too many elements for one launch");
+  }
+  const int64_t dx_rows = g.sum ? s.tokens : s.rows;
+  const bool dx = g.dx || g.sum;
+  if (g.dw) {
+    ISOLOCO_TRY(check_matrix("x", g.x, s.tokens, s.dim, g.ld_x, e));
+    ISOLOCO_TRY(check_experts("dw", g.dw, s, g.ld_dw, g.stride_dw));
+  }
+  if (dx && s.rows) ISOLOCO_TRY(check_experts("w", g.w, s, g.ld_w, g.stride_w));
+  if (dx) ISOLOCO_TRY(check_matrix("dx", g.dx, dx_rows, s.dim, g.ld_dx, e));
+  ISOLOCO_TRY(check_matrix("dout", g.dout, s.rows, s.cols, g.ld_dout, e));
+  void* rows_out = s.rows == 0 ? nullptr : g.sum ? static_cast<void*>(g.dx_rows) : g.dx;
+  const CallPlan p = call_plan(s, g.token, rows_out, g.dw, tile_rows(g.x, s.dim, g.ld_x),
+                               tile_rows(g.w, s.dim, g.ld_w) && (s.experts == 1 || (g.stride_w & 7) == 0),
+                               tile_rows(g.dout, s.cols, g.ld_dout), g.ld_x);
+  const size_t need = p.bytes;
+  ISOLOCO_TRY(check_workspace(workspace, workspace_bytes, need));
+  const size_t row_bytes = g.sum ? (size_t)s.tokens * g.top_k * index_bytes(g.row_type) : 0;
+  const Operand ins[] = {{"x", g.x, g.dw ? matrix_bytes(s.tokens, s.dim, g.ld_x, e) : 0, e},
+                         {"w", g.w, dx && s.rows ? experts_bytes(s, g.ld_w, g.stride_w) : 0, e},
+                         {"dout", g.dout, matrix_bytes(s.rows, s.cols, g.ld_dout, e), e},
+                         {"offsets", g.offsets, (size_t)(s.experts + 1) * ib, ib},
+                         {"token", g.token, g.sum || (g.token && g.dw) ? (size_t)s.rows * ib : 0, ib},
+                         {"row", g.row, row_bytes, g.sum ? index_bytes(g.row_type) : 1}};
+  const Operand outs[] = {{"dx", g.dx, dx ? matrix_bytes(dx_rows, s.dim, g.ld_dx, e) : 0, e},
+                          {"dw", g.dw, g.dw ? experts_bytes(s, g.ld_dw, g.stride_dw) : 0, e},
+                          {"the workspace", workspace, need, 1},
+                          {"dx_rows", g.dx_rows, g.sum ? (size_t)s.rows * s.dim * 4 : 0, 4}};
+  ISOLOCO_TRY(check_operands(outs, 4, ins, 6));
+  const bool wide = g.index_type == ISOLOCO_I64;
+  const Call c = {s, g.x, g.w, g.dout, g.ld_x, g.ld_w, g.stride_w, g.ld_dout, {g.offsets, wide}, {g.token, wide}};
+  // (both passes over 131072 rows of 2048 of them, past the caches / through them: 1034 / 1090 us)
+  const bool past = g.sum && s.dtype == ISOLOCO_BF16 && s.rows * s.dim * 4 > kCacheBytes;
+  hipError_t r = run_backward(c, p, rows_out, g.sum ? s.dim : g.ld_dx, g.sum, past, g.dw, g.ld_dw, g.stride_dw,
+                              static_cast<char*>(workspace), st);
+  if (r == hipSuccess && g.sum)
+    r = launch_rows_sum(g.dx_rows, s.rows, s.dim, {g.row, g.row_type == ISOLOCO_I64}, s.tokens, g.top_k,
+                        s.dtype == ISOLOCO_F32, past, g.dx, g.ld_dx, st);
+  return r == hipSuccess ? ISOLOCO_OK : hip_fail(r, "gradient of products grouped by expert");
 }
 
 }  // namespace
@@ -469,39 +539,35 @@ isoloco_status isoloco_expert_matmul_backward(const void* x, int64_t ld_x, int64
                                               int64_t dim, int64_t cols, const void* dout, int64_t ld_dout, void* dx,
                                               int64_t ld_dx, void* dw, int64_t ld_dw, int64_t stride_dw,
                                               void* workspace, size_t workspace_bytes, void* hip_stream) {
-  const ExpertShape s = {tokens, rows, experts, dim, cols, dtype};
-  ISOLOCO_TRY(check_shape(s));
-  if (!is_index_type(index_type)) return fail(ISOLOCO_ERR_INVALID_ARG, "index type %d", index_type);
-  if (!token && tokens != rows) return fail(ISOLOCO_ERR_INVALID_ARG, "%lld rows of x, %lld wanted", (long long)tokens, (long long)rows);
-  const size_t e = dtype_bytes(dtype), ib = index_bytes(index_type);
-  if (dw) {
-    ISOLOCO_TRY(check_matrix("x", x, tokens, dim, ld_x, e));
-    ISOLOCO_TRY(check_experts("dw", dw, s, ld_dw, stride_dw));
-  }
-  if (dx && rows) {
-    ISOLOCO_TRY(check_experts("w", w, s, ld_w, stride_w));
-    ISOLOCO_TRY(check_matrix("dx", dx, rows, dim, ld_dx, e));
-  }
-  ISOLOCO_TRY(check_matrix("dout", dout, rows, cols, ld_dout, e));
-  if (rows == 0) dx = nullptr;
-  const CallPlan p = call_plan(s, token, dx, dw, tile_rows(x, dim, ld_x),
-                         tile_rows(w, dim, ld_w) && (experts == 1 || (stride_w & 7) == 0), tile_rows(dout, cols, ld_dout), ld_x);
-  const size_t need = p.bytes;
-  ISOLOCO_TRY(check_workspace(workspace, workspace_bytes, need));
-  const Operand ins[] = {{"x", x, dw ? matrix_bytes(tokens, dim, ld_x, e) : 0, e},
-                         {"w", w, dx && rows ? experts_bytes(s, ld_w, stride_w) : 0, e},
-                         {"dout", dout, matrix_bytes(rows, cols, ld_dout, e), e},
-                         {"offsets", offsets, (size_t)(experts + 1) * ib, ib},
-                         {"token", token, token && dw ? (size_t)rows * ib : 0, ib}};
-  const Operand outs[] = {{"dx", dx, dx ? matrix_bytes(rows, dim, ld_dx, e) : 0, e},
-                          {"dw", dw, dw ? experts_bytes(s, ld_dw, stride_dw) : 0, e},
-                          {"the workspace", workspace, need, 1}};
-  ISOLOCO_TRY(check_operands(outs, 3, ins, 5));
-  const bool wide = index_type == ISOLOCO_I64;
-  const Call c = {s, x, w, dout, ld_x, ld_w, stride_w, ld_dout, {offsets, wide}, {token, wide}};
-  const hipError_t r = run_backward(c, p, dx, ld_dx, dw, ld_dw, stride_dw, static_cast<char*>(workspace),
-                                    static_cast<hipStream_t>(hip_stream));
-  return r == hipSuccess ? ISOLOCO_OK : hip_fail(r, "gradient of products grouped by expert");
+  Gradients g = {};
+  g.s = {tokens, rows, experts, dim, cols, dtype};
+  g.x = x, g.token = token, g.w = w, g.offsets = offsets, g.dout = dout;
+  g.ld_x = ld_x, g.ld_w = ld_w, g.stride_w = stride_w, g.ld_dout = ld_dout;
+  g.index_type = index_type;
+  g.dx = dx, g.dw = dw;
+  g.ld_dx = ld_dx, g.ld_dw = ld_dw, g.stride_dw = stride_dw;
+  return gradients(g, workspace, workspace_bytes, static_cast<hipStream_t>(hip_stream));
+}
+
+isoloco_status isoloco_expert_matmul_backward_tokens(const void* x, int64_t ld_x, int64_t tokens, const void* token,
+                                                     const void* row, int32_t row_type, int32_t top_k, const void* w,
+                                                     int64_t ld_w, int64_t stride_w, int32_t dtype, const void* offsets,
+                                                     int32_t index_type, int64_t experts, int64_t rows, int64_t dim,
+                                                     int64_t cols, const void* dout, int64_t ld_dout, void* dx,
+                                                     int64_t ld_dx, float* dx_rows, void* dw, int64_t ld_dw,
+                                                     int64_t stride_dw, void* workspace, size_t workspace_bytes,
+                                                     void* hip_stream) {
+  Gradients g = {};
+  g.s = {tokens, rows, experts, dim, cols, dtype};
+  g.x = x, g.token = token, g.w = w, g.offsets = offsets, g.dout = dout;
+  g.ld_x = ld_x, g.ld_w = ld_w, g.stride_w = stride_w, g.ld_dout = ld_dout;
+  g.index_type = index_type;
+  g.dx = dx, g.dw = dw;
+  g.ld_dx = ld_dx, g.ld_dw = ld_dw, g.stride_dw = stride_dw;
+  g.row = row, g.row_type = row_type, g.top_k = top_k;
+  g.dx_rows = dx_rows;
+  g.sum = true;
+  return gradients(g, workspace, workspace_bytes, static_cast<hipStream_t>(hip_stream));
 }
 
 }  // extern "C"

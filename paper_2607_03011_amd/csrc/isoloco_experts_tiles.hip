@@ -389,6 +389,36 @@ __device__ __forceinline__ void multiply_tile(const TileArgs& t, const Tile& til
     }
   } else {
     char* ws = lds + wave * TileLds<C>::kWs;
+    if (P == kDx && g.wide_out) {
+      // half of the columns at a time (131072 rows of 2048 from 1408, 1074 MB: 835 us, 815 past the
+      // caches; 911 with the quads going out as they are, 32 bytes of 32 rows at once)
+      constexpr int kHalf = C::NB / 2, kLanes = kHalf * 8, kRows_ = 64 / kLanes;
+      float* out = static_cast<float*>(g.out) + out_at;
+#pragma unroll
+      for (int x = 0; x < C::NA; ++x)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+          for (int y = 0; y < kHalf; ++y)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              *reinterpret_cast<floatx4*>(Patch_::quad(ws, 2 * (32 * y + 8 * q + 4 * (lane >> 5)))) =
+                  quad_of(x, h * kHalf + y, q);
+          wave_fence();
+#pragma unroll
+          for (int u = 0; u < 32 / kRows_; ++u) {
+            const int r = u * kRows_ + lane / kLanes, c4 = lane % kLanes;
+            const int64_t row = i0 + (wm * C::NA + x) * 32 + r, col = col0 + 32 * h * kHalf + 4 * c4;
+            const floatx4 v = *reinterpret_cast<const floatx4*>(ws + r * Patch_::kPitch + c4 * 16);
+            if (row >= m_all || col >= g.n) continue;
+            float* to = out + row * g.ld_out + col;
+            if (g.past && col + 4 <= g.n) __builtin_nontemporal_store(v, reinterpret_cast<floatx4_any*>(to));
+            else store4(to, v, g.n - col);
+          }
+          wave_fence();
+        }
+      return;
+    }
     uint16_t* out = static_cast<uint16_t*>(g.out) + out_at;
 #pragma unroll
     for (int x = 0; x < C::NA; ++x) {
@@ -425,7 +455,7 @@ __device__ __forceinline__ void clear_rest(const ExpertArgs& g) {
   g.groups.rows_of(g.groups.experts, begin, end);
   for (int64_t r = begin + blockIdx.x; r < end; r += gridDim.x)
     for (int64_t c = threadIdx.x; c < g.n; c += blockDim.x) {
-      if constexpr (F32) static_cast<float*>(g.out)[r * g.ld_out + c] = 0.f;
+      if (F32 || g.wide_out) static_cast<float*>(g.out)[r * g.ld_out + c] = 0.f;
       else static_cast<uint16_t*>(g.out)[r * g.ld_out + c] = 0;
     }
 }
@@ -490,7 +520,7 @@ __device__ __forceinline__ void join(const TileArgs& t, int64_t block) {
     const int64_t e = row / g.m;
     at = e * g.stride_out + (row - e * g.m) * g.ld_out + col;
   }
-  if constexpr (F32) {
+  if (F32 || (P == kDx && g.wide_out)) {
     store4(static_cast<float*>(g.out) + at, s, g.n - col);
   } else {
     uint16_t* out = static_cast<uint16_t*>(g.out) + at;

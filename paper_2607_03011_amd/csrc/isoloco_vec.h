@@ -50,6 +50,14 @@ __device__ __forceinline__ u32x4 pack(const float* x) {
   return v;
 }
 
+// 4 values as bfloat16
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+__device__ __forceinline__ u32x2_any pack4(const float* x) {
+  typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+  typedef float floatx4_t __attribute__((ext_vector_type(4)));
+  return __builtin_bit_cast(u32x2_any, __builtin_convertvector((floatx4_t){x[0], x[1], x[2], x[3]}, bf16x4_t));
+}
+
 // The order of the values: of equal ones (-0 and 0 among them) the lower index is
 // the larger key; NaN is above all.
 __device__ __forceinline__ uint32_t order_of(float x) {

@@ -72,6 +72,15 @@ def isoloco_expert_matmul_backward(x, ld_x, tokens, token, w, ld_w, stride_w, dt
            "isoloco_expert_matmul_backward")
 
 
+def isoloco_expert_matmul_backward_tokens(x, ld_x, tokens, token, row, row_type, top_k, w, ld_w, stride_w, dtype, offsets,
+                                          index_type, experts, rows, dim, cols, dout, ld_dout, dx, ld_dx, dx_rows, dw,
+                                          ld_dw, stride_dw, workspace, workspace_bytes, stream=0):
+    _check(_lib.isoloco_expert_matmul_backward_tokens(x, ld_x, tokens, token, row, row_type, top_k, w, ld_w, stride_w,
+                                                      dtype, offsets, index_type, experts, rows, dim, cols, dout,
+                                                      ld_dout, dx, ld_dx, dx_rows, dw, ld_dw, stride_dw, workspace,
+                                                      workspace_bytes, stream), "isoloco_expert_matmul_backward_tokens")
+
+
 def isoloco_combine_tokens(y, ld_y, dtype, rows, dim, row, index_type, weight, tokens, top_k, out, ld_out, stream=0):
     _check(_lib.isoloco_combine_tokens(y, ld_y, dtype, rows, dim, row, index_type, weight, tokens, top_k, out, ld_out,
                                        stream), "isoloco_combine_tokens")
@@ -250,8 +259,8 @@ def expert_matmul(x, w, offsets, token=None, row=None, out=None, workspace=None)
 @_with_stream
 def expert_matmul_backward(x, w, offsets, dout, token=None, row=None, need_dx=True, need_dw=True, workspace=None):
     """(dx, dw) from ``dout`` [rows, cols]; None for what is not needed.  With ``token``, dx
-    is the sum over a token's rows, which ``row`` [tokens, top_k] names (in bfloat16 of
-    the rows' gradients as they are rounded)."""
+    is the sum over a token's rows, which ``row`` [tokens, top_k] names, of float32 and
+    rounded once."""
     index, dtype, tokens, rows, experts, dim, cols, ld_x, ld_w, stride_w, index_type, token_at, at, flags = \
         _expert_operands(x, w, offsets, token)
     _same_device(index, dout, row)
@@ -264,20 +273,27 @@ def expert_matmul_backward(x, w, offsets, dout, token=None, row=None, need_dx=Tr
     if d_at & 15 or ld_dout & 7 or ld_dout > _LD:
         flags &= ~ISOLOCO_EXPERTS_ALIGNED
     dx = dw = dx_at = dw_at = None
+    sums = need_dx and token is not None
     if need_dx:
-        dx = _empty(rows, dim, dtype=x.dtype, device=device)
+        dx = _empty(tokens if sums else rows, dim, dtype=x.dtype, device=device)
         dx_at = dx.data_ptr()
     if need_dw:
         dw = _empty(experts, cols, dim, dtype=x.dtype, device=device)
         dw_at = dw.data_ptr()
     keep, ws, ws_bytes = _workspace(workspace, isoloco_expert_matmul_workspace_size(
         tokens, rows, experts, dim, cols, ld_x, dtype, flags | ISOLOCO_EXPERTS_BACKWARD), device)
+    if sums:
+        dx_rows = _empty(rows, dim, dtype=_F32, device=device)
+        _check(_lib.isoloco_expert_matmul_backward_tokens(
+            at[0], ld_x, tokens, token_at, row.data_ptr(), _ids("row", row, row.numel()), row.shape[1], at[1], ld_w,
+            stride_w, dtype, offsets.data_ptr(), index_type, experts, rows, dim, cols, d_at, ld_dout, dx_at, dim,
+            dx_rows.data_ptr(), dw_at, dim, cols * dim, ws, ws_bytes, _raw_stream(index)),
+            "isoloco_expert_matmul_backward_tokens")
+        return dx, dw
     _check(_lib.isoloco_expert_matmul_backward(at[0], ld_x, tokens, token_at, at[1], ld_w, stride_w, dtype,
                                                offsets.data_ptr(), index_type, experts, rows, dim, cols, d_at, ld_dout,
                                                dx_at, dim, dw_at, dim, cols * dim, ws, ws_bytes, _raw_stream(index)),
            "isoloco_expert_matmul_backward")
-    if need_dx and token is not None:
-        dx = combine_tokens(dx, row)
     return dx, dw
 
 

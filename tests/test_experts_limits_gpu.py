@@ -1,10 +1,11 @@
 """The operators of a block of experts and of distillation where their ranges end: margins
-between logits that no float32 exponential spans."""
+between logits that no float32 exponential spans, sums that cancel."""
 import math
 
 import pytest
 
-from test_experts_gpu import BF16, F32, U32, gen, iso, randn, wanted, within  # noqa: F401
+from _expert_cases import CASES
+from test_experts_gpu import BF16, F32, I32, I64, U32, gen, iso, randn, wanted, within  # noqa: F401
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
@@ -101,3 +102,76 @@ def test_distill_of_a_rest_past_any_exponential(iso, dtype, margin, vocab):
     within(r.loss, want, 2 * 264 * U32 + 2 * U32 * want.abs())
     d = iso.distill_loss_backward(masked, td, ix, r.stats, torch.ones(5, device="cuda"), rest="bucket")
     assert torch.isfinite(d).all() and not d.cpu()[~listed].any()
+
+
+# --------------------------------------------------------------------------
+# Products grouped by expert
+# --------------------------------------------------------------------------
+
+@pytest.mark.parametrize("tokens,dim,cols", [(5, 64, 32), (300, 136, 72), (700, 2048, 264), (3000, 200, 1032)])
+def test_expert_gradient_of_a_token_is_rounded_once(iso, tokens, dim, cols):
+    """A token's rows in bfloat16: two experts whose weights differ little but for the sign, so
+    that the sum is small against its terms."""
+    g = gen(dim)
+    top = 3
+    w = randn(g, top, cols, dim, std=cols ** -0.5, dtype=BF16)
+    w[1] = (-w[0].double() * (1 + 2.0 ** -6 * torch.rand(cols, dim, generator=g))).to(BF16)
+    w[2] *= 2.0 ** -6
+    x, d = randn(g, tokens, dim, dtype=BF16), randn(g, tokens, cols, dtype=BF16)
+    # expert e has row t of every token t but the last, which expert 2 has not
+    keep = [tokens, tokens, tokens - 1]
+    offsets = torch.tensor([0, *keep], dtype=I64).cumsum(0)
+    token = torch.cat([torch.arange(n) for n in keep])
+    row = torch.stack([offsets[e] + torch.arange(tokens) for e in range(top)], 1)
+    row[-1, 2] = -1
+    dout = d[token].contiguous()
+    want, size = torch.zeros(tokens, dim, dtype=torch.float64), torch.zeros(tokens, dim, dtype=torch.float64)
+    for e in range(top):
+        n = keep[e]
+        want[:n] += d[:n].double() @ w[e].double()
+        size[:n] += d[:n].double().abs() @ w[e].double().abs()
+    # float32 sums of cols terms and of a token's rows, and one rounding to bfloat16
+    off = (cols + 8 + top) * U32 * size
+    bound = off + HALF[BF16] * (want.abs() + off) + 1e-37
+    for kind in (I32, I64):
+        o, t, r = (v.to(kind).cuda() for v in (offsets, token, row))
+        dx, dw = iso.expert_matmul_backward(x.cuda(), w.cuda(), o, dout.cuda(), token=t, row=r)
+        within(dx, want, bound)
+        only = iso.expert_matmul_backward(x.cuda(), w.cuda(), o, dout.cuda(), token=t, row=r, need_dw=False)
+        assert torch.equal(only[0], dx)
+        alone = iso.expert_matmul_backward(x.cuda(), w.cuda(), o, dout.cuda(), token=t, need_dx=False)
+        assert torch.equal(alone[1], dw)
+    a = wanted(x.cuda())
+    iso.expert_matmul(a, w.cuda(), o, token=t, row=r).backward(dout.cuda())
+    assert torch.equal(a.grad, dx)
+
+
+@pytest.mark.parametrize("experts,rows,dim,cols", [c[1:5] for c in CASES if c[0] == "bf16"] + [
+    (3, 70001, 1024, 40), (3, 70001, 1021, 40)])
+def test_expert_gradient_of_a_token_by_every_instance(iso, experts, rows, dim, cols):
+    """The same by each tile, in splits and beside the weights' gradient, and of rows that are larger
+    than the caches: uneven experts, one without rows, rows behind the last one's."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(rows + dim)
+    share = torch.rand(experts, generator=g, device="cuda") + 0.2
+    share[experts // 2] = 0.0
+    last, tokens = rows - 37, rows // 2
+    sizes = torch.multinomial(share, last, replacement=True, generator=g).bincount(minlength=experts)
+    offsets = torch.zeros(experts + 1, dtype=I64, device="cuda")
+    offsets[1:] = sizes.cumsum(0)
+    row = torch.randperm(rows, generator=g, device="cuda")[:2 * tokens].view(tokens, 2)
+    token = torch.zeros(rows, dtype=I64, device="cuda")
+    token[row.flatten()] = torch.arange(tokens, device="cuda").repeat_interleave(2)
+    x = torch.randn(tokens, dim, generator=g, device="cuda").to(BF16)
+    w = (torch.randn(experts, cols, dim, generator=g, device="cuda") * cols ** -0.5).to(BF16)
+    d = torch.randn(rows, cols, generator=g, device="cuda").to(BF16)
+    dx, dw = iso.expert_matmul_backward(x, w, offsets, d, token=token, row=row)
+    terms, sizes = (torch.zeros(rows, dim, dtype=torch.float64, device="cuda") for _ in range(2))
+    for e in range(experts):
+        a, b = int(offsets[e]), int(offsets[e + 1])
+        terms[a:b], sizes[a:b] = d[a:b].double() @ w[e].double(), d[a:b].double().abs() @ w[e].double().abs()
+    want = terms[row[:, 0]] + terms[row[:, 1]]
+    off = (cols + 10) * U32 * (sizes[row[:, 0]] + sizes[row[:, 1]])
+    assert ((dx.double() - want).abs() <= off + HALF[BF16] * (want.abs() + off) + 1e-37).all()
+    assert torch.equal(iso.expert_matmul_backward(x, w, offsets, d, token=token, row=row.int(), need_dw=False)[0], dx)
+    assert torch.equal(iso.expert_matmul_backward(x, w, offsets, d, token=token, need_dx=False)[1], dw)
