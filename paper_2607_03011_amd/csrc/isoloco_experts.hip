@@ -441,7 +441,8 @@ isoloco_status gradients(Gradients g, void* workspace, size_t workspace_bytes, h
     if (!rows_sum_launchable(s.tokens, s.dim)) return fail(ISOLOCO_ERR_UNSUPPORTED, "too many elements for one launch");
   }
   const int64_t dx_rows = g.sum ? s.tokens : s.rows;
-  const bool dx = g.dx || g.sum;
+  const bool dx = (g.dx || g.sum) && dx_rows;
+  if (!dx && !g.dw) return ISOLOCO_OK;
   if (g.dw) {
     ISOLOCO_TRY(check_matrix("x", g.x, s.tokens, s.dim, g.ld_x, e));
     ISOLOCO_TRY(check_experts("dw", g.dw, s, g.ld_dw, g.stride_dw));
@@ -449,10 +450,14 @@ isoloco_status gradients(Gradients g, void* workspace, size_t workspace_bytes, h
   if (dx && s.rows) ISOLOCO_TRY(check_experts("w", g.w, s, g.ld_w, g.stride_w));
   if (dx) ISOLOCO_TRY(check_matrix("dx", g.dx, dx_rows, s.dim, g.ld_dx, e));
   ISOLOCO_TRY(check_matrix("dout", g.dout, s.rows, s.cols, g.ld_dout, e));
-  void* rows_out = s.rows == 0 ? nullptr : g.sum ? static_cast<void*>(g.dx_rows) : g.dx;
-  const CallPlan p = call_plan(s, g.token, rows_out, g.dw, tile_rows(g.x, s.dim, g.ld_x),
-                               tile_rows(g.w, s.dim, g.ld_w) && (s.experts == 1 || (g.stride_w & 7) == 0),
-                               tile_rows(g.dout, s.cols, g.ld_dout), g.ld_x);
+  void* rows_out = !dx || s.rows == 0 ? nullptr : g.sum ? static_cast<void*>(g.dx_rows) : g.dx;
+  // (no rows and no dw: nothing to multiply, and dx of the tokens is zeros)
+  const bool products = rows_out || g.dw;
+  CallPlan p = {};
+  if (products)
+    p = call_plan(s, g.token, rows_out, g.dw, tile_rows(g.x, s.dim, g.ld_x),
+                  tile_rows(g.w, s.dim, g.ld_w) && (s.experts == 1 || (g.stride_w & 7) == 0),
+                  tile_rows(g.dout, s.cols, g.ld_dout), g.ld_x);
   const size_t need = p.bytes;
   ISOLOCO_TRY(check_workspace(workspace, workspace_bytes, need));
   const size_t row_bytes = g.sum ? (size_t)s.tokens * g.top_k * index_bytes(g.row_type) : 0;
@@ -471,8 +476,10 @@ isoloco_status gradients(Gradients g, void* workspace, size_t workspace_bytes, h
   const Call c = {s, g.x, g.w, g.dout, g.ld_x, g.ld_w, g.stride_w, g.ld_dout, {g.offsets, wide}, {g.token, wide}};
   // (both passes over 131072 rows of 2048 of them, past the caches / through them: 1034 / 1090 us)
   const bool past = g.sum && s.dtype == ISOLOCO_BF16 && s.rows * s.dim * 4 > kCacheBytes;
-  hipError_t r = run_backward(c, p, rows_out, g.sum ? s.dim : g.ld_dx, g.sum, past, g.dw, g.ld_dw, g.stride_dw,
-                              static_cast<char*>(workspace), st);
+  hipError_t r = hipSuccess;
+  if (products)
+    r = run_backward(c, p, rows_out, g.sum ? s.dim : g.ld_dx, g.sum, past, g.dw, g.ld_dw, g.stride_dw,
+                     static_cast<char*>(workspace), st);
   if (r == hipSuccess && g.sum)
     r = launch_rows_sum(g.dx_rows, s.rows, s.dim, {g.row, g.row_type == ISOLOCO_I64}, s.tokens, g.top_k,
                         s.dtype == ISOLOCO_F32, past, g.dx, g.ld_dx, st);

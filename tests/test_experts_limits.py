@@ -2,8 +2,8 @@
 calls end before anything is enqueued, and the addresses are never read)."""
 import pytest
 
-from test_experts_refusals import (ALIAS, ALIGN, BIG, INVALID, WORKSPACE, WS, A, B, C, D, E, F, changed, iso,  # noqa: F401
-                                   refused)
+from test_experts_refusals import (ALIAS, ALIGN, BIG, EXPERTS_GRAD, INVALID, WORKSPACE, WS, A, B, C, D, E, F,  # noqa: F401
+                                   changed, iso, refused)
 
 G, H = 0x90000000, 0xa0000000
 
@@ -25,3 +25,11 @@ TOKENS_GRAD = dict(x=A, ld_x=64, tokens=20, token=B, row=G, row_type=0, top_k=2,
 ])
 def test_expert_matmul_backward_tokens_refuses(status, change):
     refused(status, iso.isoloco_expert_matmul_backward_tokens, *changed(TOKENS_GRAD, **change))
+
+
+def test_expert_gradients_of_neither_operand_read_nothing():
+    """Neither dx nor dw wanted: no operand is read and no workspace needed, whatever the sizes."""
+    for rows in (40, 1000, 100000):
+        iso.isoloco_expert_matmul_backward(*changed(EXPERTS_GRAD, rows=rows, x=0, w=0, dx=0, dw=0, workspace=0))
+    # and a gradient of no token is none
+    iso.isoloco_expert_matmul_backward_tokens(*changed(TOKENS_GRAD, rows=1000, tokens=0, x=0, dx=0, row=0, dw=0, workspace=0))
