@@ -431,7 +431,7 @@ isoloco_status gradients(Gradients g, void* workspace, size_t workspace_bytes, h
   const ExpertShape& s = g.s;
   ISOLOCO_TRY(check_shape(s));
   if (!is_index_type(g.index_type)) return fail(ISOLOCO_ERR_INVALID_ARG, "index type %d", g.index_type);
-  if (!g.token && !g.sum && s.tokens != s.rows)
+  if (!g.token && !g.sum && s.rows && s.tokens != s.rows)
     return fail(ISOLOCO_ERR_INVALID_ARG, "%lld rows of x, %lld wanted", (long long)s.tokens, (long long)s.rows);
   const size_t e = dtype_bytes(s.dtype), ib = index_bytes(g.index_type);
   if (g.sum) {
@@ -518,7 +518,7 @@ isoloco_status isoloco_expert_matmul(const void* x, int64_t ld_x, int64_t tokens
   const ExpertShape s = {tokens, rows, experts, dim, cols, dtype};
   ISOLOCO_TRY(check_shape(s));
   if (!is_index_type(index_type)) return fail(ISOLOCO_ERR_INVALID_ARG, "index type %d", index_type);
-  if (!token && tokens != rows) return fail(ISOLOCO_ERR_INVALID_ARG, "%lld rows of x, %lld wanted", (long long)tokens, (long long)rows);
+  if (!token && rows && tokens != rows) return fail(ISOLOCO_ERR_INVALID_ARG, "%lld rows of x, %lld wanted", (long long)tokens, (long long)rows);
   if (rows == 0) return ISOLOCO_OK;
   const size_t e = dtype_bytes(dtype), ib = index_bytes(index_type);
   ISOLOCO_TRY(check_matrix("x", x, tokens, dim, ld_x, e));

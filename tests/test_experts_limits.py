@@ -2,8 +2,8 @@
 calls end before anything is enqueued, and the addresses are never read)."""
 import pytest
 
-from test_experts_refusals import (ALIAS, ALIGN, BIG, EXPERTS_GRAD, INVALID, WORKSPACE, WS, A, B, C, D, E, F,  # noqa: F401
-                                   changed, iso, refused)
+from test_experts_refusals import (ALIAS, ALIGN, BIG, EXPERTS, EXPERTS_GRAD, INVALID, WORKSPACE, WS, A, B, C, D, E,  # noqa: F401
+                                   F, changed, iso, refused)
 
 G, H = 0x90000000, 0xa0000000
 
@@ -33,3 +33,9 @@ def test_expert_gradients_of_neither_operand_read_nothing():
         iso.isoloco_expert_matmul_backward(*changed(EXPERTS_GRAD, rows=rows, x=0, w=0, dx=0, dw=0, workspace=0))
     # and a gradient of no token is none
     iso.isoloco_expert_matmul_backward_tokens(*changed(TOKENS_GRAD, rows=1000, tokens=0, x=0, dx=0, row=0, dw=0, workspace=0))
+
+
+def test_no_rows_of_some_tokens_are_nothing():
+    """No place of the grouped order names any token: an empty tensor has no address."""
+    iso.isoloco_expert_matmul(*changed(EXPERTS, rows=0, token=0, out=0))
+    iso.isoloco_expert_matmul_backward(*changed(EXPERTS_GRAD, rows=0, token=0, dout=0, dx=0, dw=0, workspace=0))

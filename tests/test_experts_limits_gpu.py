@@ -175,3 +175,19 @@ def test_expert_gradient_of_a_token_by_every_instance(iso, experts, rows, dim, c
     assert ((dx.double() - want).abs() <= off + HALF[BF16] * (want.abs() + off) + 1e-37).all()
     assert torch.equal(iso.expert_matmul_backward(x, w, offsets, d, token=token, row=row.int(), need_dw=False)[0], dx)
     assert torch.equal(iso.expert_matmul_backward(x, w, offsets, d, token=token, need_dx=False)[1], dw)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_experts_without_any_token(iso, dtype):
+    """Tokens of which none is routed here: no rows, and gradients of zeros."""
+    x, w = wanted(torch.randn(5, 64, device="cuda").to(dtype)), wanted(torch.randn(3, 32, 64, device="cuda").to(dtype))
+    o, token = torch.zeros(4, dtype=I32, device="cuda"), torch.empty(0, dtype=I32, device="cuda")
+    row = torch.full((5, 2), -1, dtype=I32, device="cuda")
+    h = iso.expert_matmul(x, w, o, token=token, row=row)
+    y = wanted(torch.empty(0, 64, device="cuda", dtype=dtype))
+    out = iso.combine_tokens(y, row)
+    assert h.shape == (0, 32) and out.shape == (5, 64) and not out.any()
+    (h.sum() + out.sum()).backward()
+    assert x.grad.shape == x.shape and not x.grad.any() and not w.grad.any() and y.grad.shape == y.shape
+    dx, dw = iso.expert_matmul_backward(x.detach(), w.detach(), o, h.detach(), token=token, row=row, need_dw=False)
+    assert not dx.any() and dw is None
