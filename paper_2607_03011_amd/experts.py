@@ -24,7 +24,7 @@ import torch
 from torch.autograd.function import once_differentiable
 
 from . import (ISOLOCO_EXPERTS_ALIGNED, ISOLOCO_EXPERTS_BACKWARD, ISOLOCO_EXPERTS_GATHERED, ISOLOCO_DISTILL_STATS,
-               ISOLOCO_REST_BUCKET, ISOLOCO_REST_DROP, _check, _lib)
+               ISOLOCO_MAX_TOP, ISOLOCO_REST_BUCKET, ISOLOCO_REST_DROP, _check, _lib)
 from .operators import (_empty, _F32, _ids, _output, _place, _raw_stream, _recorded, _rows, _same_device, _size_of,
                         _type, _vector, _with_stream, _workspace, _written)
 
@@ -227,6 +227,16 @@ def _expert_operands(x, w, offsets, token):
     return index, dtype, tokens, rows, experts, dim, cols, ld_x, ld_w, stride_w, index_type, token_at, at, flags
 
 
+def _row_of(index, row, tokens):
+    """Where row [tokens, top_k], the rows of each token, lies, and its type."""
+    if row is None:
+        raise ValueError("the gradient of x needs row beside token")
+    _same_device(index, row)
+    if row.dim() != 2 or row.shape[0] != tokens or not 1 <= row.shape[1] <= ISOLOCO_MAX_TOP:
+        raise ValueError("row must be [%d, 1 to %d], not %s" % (tokens, ISOLOCO_MAX_TOP, tuple(row.shape)))
+    return row.data_ptr(), _ids("row", row, row.numel())
+
+
 @_with_stream
 def expert_matmul(x, w, offsets, token=None, row=None, out=None, workspace=None):
     """``x_r w[e]^T`` for the rows r = offsets[e] .. offsets[e + 1] - 1 of each expert e, w
@@ -235,8 +245,8 @@ def expert_matmul(x, w, offsets, token=None, row=None, out=None, workspace=None)
     and are not read by the host.  ``row`` (``route_tokens``' inverse of token, [tokens,
     top_k]) is needed with ``token`` for the gradient of x."""
     if (x.requires_grad or w.requires_grad) and _recorded(out):
-        if token is not None and x.requires_grad and row is None:
-            raise ValueError("the gradient of x needs row beside token")
+        if token is not None and x.requires_grad:
+            _row_of(_place(x), row, x.shape[0])  # (now: it is read by the gradient alone)
         return _ExpertMatmul.apply(x, w, offsets, token, row, workspace)
     index, dtype, tokens, rows, experts, dim, cols, ld_x, ld_w, stride_w, index_type, token_at, at, flags = \
         _expert_operands(x, w, offsets, token)
@@ -263,17 +273,17 @@ def expert_matmul_backward(x, w, offsets, dout, token=None, row=None, need_dx=Tr
     rounded once."""
     index, dtype, tokens, rows, experts, dim, cols, ld_x, ld_w, stride_w, index_type, token_at, at, flags = \
         _expert_operands(x, w, offsets, token)
-    _same_device(index, dout, row)
+    _same_device(index, dout)
     if dout.dtype != x.dtype or tuple(dout.shape) != (rows, cols):
         raise ValueError("dout must be %s of %s" % (x.dtype, (rows, cols)))
-    if need_dx and token is not None and (row is None or row.dim() != 2 or row.shape[0] != tokens):
-        raise ValueError("dx needs row of [tokens, top_k] beside token")
     ld_dout, device = _rows("dout", dout)[1], x.device
     d_at = dout.data_ptr()
     if d_at & 15 or ld_dout & 7 or ld_dout > _LD:
         flags &= ~ISOLOCO_EXPERTS_ALIGNED
     dx = dw = dx_at = dw_at = None
     sums = need_dx and token is not None
+    if sums:
+        row_at, row_type = _row_of(index, row, tokens)
     if need_dx:
         dx = _empty(tokens if sums else rows, dim, dtype=x.dtype, device=device)
         dx_at = dx.data_ptr()
@@ -285,7 +295,7 @@ def expert_matmul_backward(x, w, offsets, dout, token=None, row=None, need_dx=Tr
     if sums:
         dx_rows = _empty(rows, dim, dtype=_F32, device=device)
         _check(_lib.isoloco_expert_matmul_backward_tokens(
-            at[0], ld_x, tokens, token_at, row.data_ptr(), _ids("row", row, row.numel()), row.shape[1], at[1], ld_w,
+            at[0], ld_x, tokens, token_at, row_at, row_type, row.shape[1], at[1], ld_w,
             stride_w, dtype, offsets.data_ptr(), index_type, experts, rows, dim, cols, d_at, ld_dout, dx_at, dim,
             dx_rows.data_ptr(), dw_at, dim, cols * dim, ws, ws_bytes, _raw_stream(index)),
             "isoloco_expert_matmul_backward_tokens")

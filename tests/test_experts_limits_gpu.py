@@ -191,3 +191,15 @@ def test_experts_without_any_token(iso, dtype):
     assert x.grad.shape == x.shape and not x.grad.any() and not w.grad.any() and y.grad.shape == y.shape
     dx, dw = iso.expert_matmul_backward(x.detach(), w.detach(), o, h.detach(), token=token, row=row, need_dw=False)
     assert not dx.any() and dw is None
+
+
+def test_expert_matmul_finds_a_wrong_row_at_once(iso):
+    x, w = wanted(torch.randn(10, 8, device="cuda")), torch.randn(3, 5, 8, device="cuda")
+    o = torch.tensor([0, 5, 15, 20], dtype=I32, device="cuda")
+    t = torch.arange(20, dtype=I32, device="cuda") // 2
+    row = torch.arange(20, dtype=I32, device="cuda").view(10, 2)
+    for wrong in (row.flatten(), row[:9], row.float(), row.view(5, 4), row.t(), row.cpu(),
+                  torch.zeros(10, 33, dtype=I32, device="cuda"), row[:, :0]):
+        with pytest.raises(ValueError):
+            iso.expert_matmul(x, w, o, token=t, row=wrong)
+    iso.expert_matmul(x, w, o, token=t, row=row).sum().backward()
