@@ -581,7 +581,8 @@ isoloco_status isoloco_combine_tokens(const void* y, int64_t ld_y, int32_t dtype
  *
  *   dy[row[t, j]] = weight[t, j] dout[t]          dweight[t, j] = <dout[t], y[row[t, j]]>
  *
- * No two entries of row may be the same; rows of dy that none names are zeros.
+ * No two entries of row may be the same (the row's gradient is then from any of
+ * them); rows of dy that none names are zeros.
  * dweight is 0 where the entry is outside.  y is read for dweight only, and the
  * workspace serves dy only. */
 isoloco_status isoloco_combine_tokens_backward_workspace_size(int64_t tokens, int32_t top_k, size_t* bytes);

@@ -12,6 +12,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "isoloco_device.h"
 #include "isoloco_error.h"
@@ -73,49 +74,79 @@ __global__ void __launch_bounds__(256) combine_kernel(const T* y, O* out, Combin
   }
 }
 
-// Rows of dy that no slot names have no gradient.  As no two slots name one, there are such rows
-// exactly where fewer slots than rows name one: the slots that do are counted, and only then
-// all of dy is cleared before the named rows are written (which costs 105 us of 344 for 537 MB
-// where it is not needed; the counting 5).
-constexpr int kCounts = 256;
-constexpr int64_t kCountedAtOnce = 8192;  // so many slots each workgroup that clears counts itself
+// Rows of dy that no slot names have no gradient, and are cleared before the named rows are written
+// (clearing all of them costs 105 us of 344 for 537 MB).  Where there are as many slots as rows or
+// more, the rows that slots name are marked, a bit each: by every workgroup that clears, if the
+// slots are few, otherwise ahead of it, where each workgroup finds the slots of its rows among all
+// (131072 slots: 9.6 us, 11.7 with a load a slot, and the clearing that finds none to clear 4.5).
+// Counting the slots takes half of it, but tells nothing where two name one row and leave another
+// without any.
+constexpr int64_t kFewSlots = 8192;
+constexpr int kMarkThreads = 1024;
+constexpr int64_t kMostMarked = (int64_t)1 << 18;  // rows of a workgroup that marks: 32 KiB of bits
 
-__device__ __forceinline__ int count_named(const Index& row, int64_t rows, int64_t first, int64_t step, int64_t slots) {
-  int n = 0;
-  for (int64_t i = first; i < slots; i += step) {
-    const int64_t r = row.get(i);
-    n += r >= 0 && r < rows;
-  }
-  return n;
-}
-
-// The sum of a workgroup's values, in every thread.
-__device__ __forceinline__ int64_t sum_of(int v) {
-  __shared__ int part[4];
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+// The bits of rows first .. first + count - 1, in `bits`, by the workgroup.
+template <typename ID, int THREADS>
+__device__ __forceinline__ void mark_rows(const ID* row, int64_t slots, int64_t first, int64_t count, uint32_t* bits) {
+  typedef typename std::make_unsigned<ID>::type U;
+  for (int64_t i = threadIdx.x; i < (count + 31) / 32; i += THREADS) bits[i] = 0;
   __syncthreads();
-  return (int64_t)part[0] + part[1] + part[2] + part[3];
+  const U from = (U)first, many = (U)count;
+  const auto mark = [&](ID at) {
+    const U r = (U)at - from;
+    if (r < many) atomicOr(&bits[(uint32_t)r >> 5], 1u << ((uint32_t)r & 31));
+  };
+  // 16 bytes of slots a load, and so many loads in flight
+  constexpr int kPer = 16 / sizeof(ID), kAhead = 8;
+  int64_t base = 0;
+  for (; base + kPer * kAhead * THREADS <= slots; base += kPer * kAhead * THREADS) {
+    const u32x4_any* p = reinterpret_cast<const u32x4_any*>(row + base);
+    u32x4 v[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) v[u] = p[u * THREADS + (int)threadIdx.x];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      ID r[kPer];
+      __builtin_memcpy(r, &v[u], 16);
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) mark(r[e]);
+    }
+  }
+  for (int64_t i = base + threadIdx.x; i < slots; i += THREADS) mark(row[i]);
+  __syncthreads();
+}
+template <int THREADS>
+__device__ __forceinline__ void mark_rows(const Index& row, int64_t slots, int64_t first, int64_t count, uint32_t* bits) {
+  if (row.wide) mark_rows<int64_t, THREADS>(static_cast<const int64_t*>(row.p), slots, first, count, bits);
+  else mark_rows<int32_t, THREADS>(static_cast<const int32_t*>(row.p), slots, first, count, bits);
 }
 
-__global__ void __launch_bounds__(256) combine_count_kernel(Index row, int64_t rows, int64_t slots, int32_t* counts) {
-  const int64_t n = sum_of(count_named(row, rows, (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256, slots));
-  if (threadIdx.x == 0) counts[blockIdx.x] = (int32_t)n;
+// per: rows of a workgroup, a multiple of 32
+__global__ void __launch_bounds__(kMarkThreads) combine_mark_kernel(Index row, int64_t rows, int64_t slots, int64_t per,
+                                                                    uint32_t* marks) {
+  __shared__ uint32_t bits[kMostMarked / 32];
+  const int64_t first = blockIdx.x * per, count = min(per, rows - first);
+  mark_rows<kMarkThreads>(row, slots, first, count, bits);
+  for (int64_t i = threadIdx.x; i < (count + 31) / 32; i += kMarkThreads) marks[first / 32 + i] = bits[i];
 }
 
-// `counts`: kCounts of them, or NULL: the slots are few.
-template <typename T>
-__global__ void __launch_bounds__(256) combine_clear_kernel(Index row, int64_t rows, int64_t slots, const int32_t* counts,
+// MARKED: the rows' bits are in `marks`, FEW: they are formed here, ALL: no row is marked.
+enum Clearing { kMarked, kFew, kAll };
+template <typename T, Clearing HOW>
+__global__ void __launch_bounds__(256) combine_clear_kernel(Index row, int64_t rows, int64_t slots, const uint32_t* marks,
                                                             T* dy, int64_t ld, int64_t dim) {
-  const int64_t named = sum_of(counts ? counts[threadIdx.x] : count_named(row, rows, threadIdx.x, 256, slots));
-  if (named >= rows) return;
+  __shared__ uint32_t bits[HOW == kFew ? kFewSlots / 32 : 1];
+  if constexpr (HOW == kFew) mark_rows<256>(row, slots, 0, rows, bits);
   constexpr int N = Vec<T>::N;
-  const int64_t pieces = (dim + N - 1) / N;
   const float zeros[N] = {};
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * pieces; i += (int64_t)gridDim.x * 256) {
-    const int64_t r = i / pieces, col = (i - r * pieces) * N;
-    store_piece<T>(dy + r * ld + col, dim - col, zeros);
+  const int64_t words = (rows + 31) / 32, from = words * blockIdx.x / gridDim.x, to = words * (blockIdx.x + 1) / gridDim.x;
+  for (int64_t w = from; w < to; ++w) {
+    uint32_t none = ~(HOW == kAll ? 0u : HOW == kFew ? bits[w] : marks[w]);
+    if (rows - 32 * w < 32) none &= (1u << (rows - 32 * w)) - 1;
+    for (; none; none &= none - 1) {
+      T* to_row = dy + (32 * w + __ffs(none) - 1) * ld;
+      for (int64_t col = (int64_t)threadIdx.x * N; col < dim; col += 256 * N) store_piece<T>(to_row + col, dim - col, zeros);
+    }
   }
 }
 
@@ -221,20 +252,34 @@ void run_forward(const void* y, void* out, const CombineArgs& g, int pieces, int
                      static_cast<O*>(out), g, pieces);
 }
 
+// the marks of as many rows as slots
 size_t combine_grad_workspace(int64_t tokens, int32_t top_k) {
-  return tokens * top_k > kCountedAtOnce ? kCounts * sizeof(int32_t) : 0;
+  const int64_t slots = tokens * top_k;
+  return slots > kFewSlots ? (size_t)(slots + 31) / 32 * sizeof(uint32_t) : 0;
+}
+
+template <typename T>
+void clear_rows(const CombineGradArgs& g, T* dy, uint32_t* marks, hipStream_t st) {
+  const int64_t slots = g.tokens * g.top_k, rows = g.rows;
+  const dim3 grid((unsigned)std::min<int64_t>(1024, (rows + 31) / 32));
+  if (rows > slots) {
+    hipLaunchKernelGGL((combine_clear_kernel<T, kAll>), grid, dim3(256), 0, st, g.row, rows, slots, marks, dy, g.ld_dy, g.dim);
+  } else if (slots <= kFewSlots) {
+    hipLaunchKernelGGL((combine_clear_kernel<T, kFew>), grid, dim3(256), 0, st, g.row, rows, slots, marks, dy, g.ld_dy, g.dim);
+  } else {
+    // about a workgroup a CU
+    const int64_t per = std::min(kMostMarked, (rows / 256 / 32 + 1) * 32);
+    hipLaunchKernelGGL(combine_mark_kernel, dim3((unsigned)((rows + per - 1) / per)), dim3(kMarkThreads), 0, st, g.row, rows,
+                       slots, per, marks);
+    hipLaunchKernelGGL((combine_clear_kernel<T, kMarked>), grid, dim3(256), 0, st, g.row, rows, slots, marks, dy, g.ld_dy,
+                       g.dim);
+  }
 }
 
 template <typename T, bool PAST>
-void run_grad(const void* dout, const void* y, void* dy, const CombineGradArgs& g, int64_t blocks, int32_t* counts,
+void run_grad(const void* dout, const void* y, void* dy, const CombineGradArgs& g, int64_t blocks, uint32_t* marks,
               hipStream_t st) {
-  if (dy && g.rows) {
-    const int64_t slots = g.tokens * g.top_k;
-    const bool few = slots <= kCountedAtOnce;
-    if (!few) hipLaunchKernelGGL(combine_count_kernel, dim3(kCounts), dim3(256), 0, st, g.row, g.rows, slots, counts);
-    hipLaunchKernelGGL(combine_clear_kernel<T>, dim3((unsigned)std::min<int64_t>(1024, g.rows)), dim3(256), 0, st, g.row,
-                       g.rows, slots, few ? nullptr : counts, static_cast<T*>(dy), g.ld_dy, g.dim);
-  }
+  if (dy && g.rows) clear_rows(g, static_cast<T*>(dy), marks, st);
   if (blocks == 0) return;
   const dim3 grid((unsigned)blocks);
   const T *d = static_cast<const T*>(dout), *x = static_cast<const T*>(y);
@@ -334,12 +379,12 @@ isoloco_status isoloco_combine_tokens_backward(const void* dout, int64_t ld_dout
   const int64_t blocks = (tokens + (256 >> g.lanes_log2) - 1) >> (8 - g.lanes_log2);
   if (!launchable(blocks, 256)) return fail(ISOLOCO_ERR_UNSUPPORTED, "too many tokens for one launch");
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  int32_t* counts = static_cast<int32_t*>(workspace);
+  uint32_t* marks = static_cast<uint32_t*>(workspace);
   // Both sides measured, past the caches / through them, us of both passes over 537 MB of rows:
   // 468 / 622 (the stores alone past them 602, the loads alone 610).
   const bool past = rows * dim * (int64_t)e > kCacheBytes;
-  if (dtype == ISOLOCO_F32) (past ? run_grad<float, true> : run_grad<float, false>)(dout, y, dy, g, blocks, counts, st);
-  else (past ? run_grad<__bf16, true> : run_grad<__bf16, false>)(dout, y, dy, g, blocks, counts, st);
+  if (dtype == ISOLOCO_F32) (past ? run_grad<float, true> : run_grad<float, false>)(dout, y, dy, g, blocks, marks, st);
+  else (past ? run_grad<__bf16, true> : run_grad<__bf16, false>)(dout, y, dy, g, blocks, marks, st);
   const hipError_t err = hipGetLastError();
   return err == hipSuccess ? ISOLOCO_OK : hip_fail(err, "gradient of the combination of tokens");
 }

@@ -366,8 +366,8 @@ def combine_tokens(y, row, weight=None, out=None):
 @_with_stream
 def combine_tokens_backward(dout, y, row, weight=None, need_dy=True, need_dweight=True, workspace=None):
     """(dy, dweight) from ``dout`` [tokens, dim]; None for what is not needed (dweight
-    without weight).  No two entries of ``row`` may be the same; rows of y that none names
-    have a zero gradient."""
+    without weight).  No two entries of ``row`` may be the same (the row's gradient is then
+    from any of them); rows of y that none names have a zero gradient."""
     index, dtype, rows, dim, ld_y, tokens, top_k, index_type, weight_at = _combine_operands(y, row, weight)
     _same_device(index, dout)
     if dout.dtype != y.dtype or tuple(dout.shape) != (tokens, dim):

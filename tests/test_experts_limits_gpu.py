@@ -1,5 +1,6 @@
 """The operators of a block of experts and of distillation where their ranges end: margins
-between logits that no float32 exponential spans, sums that cancel."""
+between logits that no float32 exponential spans, sums that cancel,
+entries that repeat."""
 import math
 
 import pytest
@@ -203,3 +204,55 @@ def test_expert_matmul_finds_a_wrong_row_at_once(iso):
         with pytest.raises(ValueError):
             iso.expert_matmul(x, w, o, token=t, row=wrong)
     iso.expert_matmul(x, w, o, token=t, row=row).sum().backward()
+
+
+# --------------------------------------------------------------------------
+# Combination
+# --------------------------------------------------------------------------
+
+@pytest.mark.parametrize("tokens", [3, 700, 5000])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("kind", [I32, I64])
+def test_combine_gradient_where_entries_repeat(iso, tokens, dtype, kind):
+    """A row that two entries name leaves another without any, though there are as many entries as
+    rows: that one's gradient is zero, whatever dy's memory held, and those named once have theirs."""
+    g = gen(tokens)
+    rows = tokens * 2
+    y, dout, w = randn(g, rows, 96, dtype=dtype), randn(g, tokens, 96, dtype=dtype), randn(g, tokens, 2)
+    row = torch.randperm(rows, generator=g).view(tokens, 2)
+    row[::3, 1] = row[::3, 0]
+    row[-1, 0] = row[0, 0]
+    named = torch.bincount(row.flatten(), minlength=rows)
+    assert (named == 0).any() and (named > 1).any()
+    want = torch.zeros(rows, 96, dtype=torch.float64)
+    want[row.flatten()] = (w.double()[:, :, None] * dout.double()[:, None, :]).flatten(0, 1)
+    dy = torch.full((rows, 96), math.nan, device="cuda", dtype=dtype)
+    size = iso.isoloco_combine_tokens_backward_workspace_size(tokens, 2)
+    ws = torch.full((size + 256,), 255, dtype=torch.uint8, device="cuda")
+    at = (ws.data_ptr() + 255) // 256 * 256
+    d, wd, r = dout.cuda(), w.cuda(), row.to(kind).cuda()
+    for _ in range(2):
+        iso.isoloco_combine_tokens_backward(
+            d.data_ptr(), 96, None, 96, iso.ISOLOCO_F32 if dtype == F32 else iso.ISOLOCO_BF16, rows, 96, r.data_ptr(),
+            iso.ISOLOCO_I32 if kind == I32 else iso.ISOLOCO_I64, wd.data_ptr(), tokens, 2, dy.data_ptr(), 96, None, at, size,
+            torch.cuda.current_stream().cuda_stream)
+        got = dy.cpu()
+        assert not got[named == 0].any()
+        within(got[named == 1], want[named == 1], HALF[dtype] * want[named == 1].abs() + 1e-37)
+        assert torch.isfinite(got).all()
+
+
+def test_combine_gradient_of_many_rows(iso):
+    """More rows than the workgroups that mark them take at once on a card's 256 units."""
+    rows = (1 << 26) + (1 << 18) + 5
+    row = torch.arange(rows - 1, -1, -1, dtype=I32, device="cuda")
+    row[12345] = row[rows - 7]
+    dout, dy = torch.ones(rows, 1, dtype=BF16, device="cuda"), torch.full((rows, 1), math.nan, dtype=BF16, device="cuda")
+    size = iso.isoloco_combine_tokens_backward_workspace_size(rows, 1)
+    ws = torch.full((size + 256,), 255, dtype=torch.uint8, device="cuda")
+    iso.isoloco_combine_tokens_backward(
+        dout.data_ptr(), 1, None, 1, iso.ISOLOCO_BF16, rows, 1, row.data_ptr(), iso.ISOLOCO_I32, None, rows, 1,
+        dy.data_ptr(), 1, None, (ws.data_ptr() + 255) // 256 * 256, size, torch.cuda.current_stream().cuda_stream)
+    assert dy[rows - 1 - 12345] == 0
+    dy[rows - 1 - 12345] = 1
+    assert (dy == 1).all()
