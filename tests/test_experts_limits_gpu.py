@@ -1,6 +1,6 @@
 """The operators of a block of experts and of distillation where their ranges end: margins
 between logits that no float32 exponential spans, sums that cancel,
-entries that repeat."""
+entries that repeat, each part of a float32 operand."""
 import math
 
 import pytest
@@ -206,6 +206,55 @@ def test_expert_matmul_finds_a_wrong_row_at_once(iso):
     iso.expert_matmul(x, w, o, token=t, row=row).sum().backward()
 
 
+@pytest.mark.parametrize("case", [i for i, c in enumerate(CASES) if c[0] == "f32"])
+def test_expert_products_of_every_part(iso, case):
+    """float32 products with one term each, or few: an operand has one value that is not zero in a
+    row, of 24 bits, the other is full, so that the bound is the rounding of a product and a part
+    of an operand that is lost, doubled or taken for another shows.
+
+    The parts of a and b are off by nothing, what their six products leave out is at most 2^-23
+    of a b, and their sum is rounded six times, once more a split."""
+    _, experts, rows, dim, cols, _ = CASES[case]
+    g = torch.Generator(device="cuda")
+    g.manual_seed(case)
+
+    def full(*shape):
+        return (1.0 + torch.rand(*shape, generator=g, device="cuda")) * torch.where(
+            torch.rand(*shape, generator=g, device="cuda") < 0.5, -1.0, 1.0)
+
+    def single(n, width):
+        """[n, width] with one value a row, at any column, and where."""
+        at = torch.randint(0, width, (n,), generator=g, device="cuda")
+        out = torch.zeros(n, width, device="cuda")
+        out.scatter_(1, at[:, None], full(n, 1))
+        return out, at
+
+    sizes = torch.multinomial(torch.rand(experts, generator=g, device="cuda") + 0.2, rows, replacement=True,
+                              generator=g).bincount(minlength=experts)
+    offsets = torch.zeros(experts + 1, dtype=I64, device="cuda")
+    offsets[1:] = sizes.cumsum(0)
+    expert = torch.repeat_interleave(torch.arange(experts, device="cuda"), sizes)
+    w = full(experts, cols, dim)
+    x, at = single(rows, dim)
+    d, to = single(rows, cols)
+    value = x.gather(1, at[:, None]).double()
+    want = value * w[expert, :, at].double()
+    got = iso.expert_matmul(x, w, offsets)
+    assert ((got.double() - want).abs() <= 24 * U32 * want.abs()).all()
+    want = d.gather(1, to[:, None]).double() * w[expert, to].double()
+    dx = iso.expert_matmul_backward(x, w, offsets, d, need_dw=False)[0]
+    assert ((dx.double() - want).abs() <= 24 * U32 * want.abs()).all()
+    # a row of x adds to one column of its expert's gradient: as many terms as rows have the column
+    dense = full(rows, cols)
+    dw = iso.expert_matmul_backward(x, w, offsets, dense, need_dx=False)[1].double()
+    for e in range(experts):
+        a, b = int(offsets[e]), int(offsets[e + 1])
+        X, D = x[a:b].double(), dense[a:b].double()
+        n = (X != 0).sum(0)[None, :]
+        size = D.abs().T @ X.abs()
+        assert ((dw[e] - D.T @ X).abs() <= (24 + 6 * n) * U32 * size).all()
+
+
 # --------------------------------------------------------------------------
 # Combination
 # --------------------------------------------------------------------------
@@ -256,3 +305,31 @@ def test_combine_gradient_of_many_rows(iso):
     assert dy[rows - 1 - 12345] == 0
     dy[rows - 1 - 12345] = 1
     assert (dy == 1).all()
+
+
+# --------------------------------------------------------------------------
+# Routing
+# --------------------------------------------------------------------------
+
+@pytest.mark.parametrize("tokens", [5, 200])
+@pytest.mark.parametrize("normalize", [True, False])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_route_of_nan_and_infinity(iso, tokens, normalize, dtype):
+    """Each makes all of its token's weights NaN, and the gradient of the scores that they depend
+    on; other tokens' stay as they are."""
+    g = gen(1)
+    s, dw = randn(g, tokens, 40, dtype=dtype), randn(g, tokens, 4)
+    clean = iso.route_tokens(s.cuda(), 4, normalize=normalize)
+    s[1, 7] = math.nan
+    s[3, 9] = math.inf
+    r = iso.route_tokens(s.cuda(), 4, normalize=normalize)
+    odd, fine = [1, 3], [t for t in range(tokens) if t not in (1, 3)]
+    assert torch.isnan(r.weight[odd]).all()
+    assert torch.equal(r.weight[fine], clean.weight[fine]) and torch.equal(r.expert[fine], clean.expert[fine])
+    d = iso.route_tokens_backward(s.cuda(), r.expert, dw.cuda(), normalize=normalize)
+    want = iso.route_tokens_backward(s[fine].cuda(), r.expert[fine].contiguous(), dw[fine].cuda(), normalize=normalize)
+    assert torch.equal(d[fine], want)
+    if normalize:
+        assert torch.isnan(d[odd].gather(1, r.expert[odd].long())).all()
+    else:
+        assert torch.isnan(d[odd]).all()
