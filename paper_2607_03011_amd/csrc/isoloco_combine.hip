@@ -161,8 +161,8 @@ struct CombineGradArgs {
 
 // 2^lanes_log2 threads per token, which go through its columns kAtOnce slots at a time.  The
 // pieces stay as they are stored until they are used, and the stores go ahead of the products:
-// 16384 tokens of 8 rows of 2048 in bfloat16 take 216 us (1141 MB, 5.3 TB/s) where unpacked
-// ones took 326.  64 / 128 / 256 threads a token: both passes 351 / 342 / 352 us.
+// 16384 tokens of 8 rows of 2048 in bfloat16 take 222 us (1141 MB, 5.1 TB/s) where unpacked
+// ones took 326.  64 / 128 / 256 threads a token: both passes 363 / 357 / 364 us.
 constexpr int kMostLanesLog2 = 7;
 
 // PAST: y and its gradient go past the caches.
@@ -381,7 +381,7 @@ isoloco_status isoloco_combine_tokens_backward(const void* dout, int64_t ld_dout
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
   uint32_t* marks = static_cast<uint32_t*>(workspace);
   // Both sides measured, past the caches / through them, us of both passes over 537 MB of rows:
-  // 468 / 622 (the stores alone past them 602, the loads alone 610).
+  // 357 / 379.
   const bool past = rows * dim * (int64_t)e > kCacheBytes;
   if (dtype == ISOLOCO_F32) (past ? run_grad<float, true> : run_grad<float, false>)(dout, y, dy, g, blocks, marks, st);
   else (past ? run_grad<__bf16, true> : run_grad<__bf16, false>)(dout, y, dy, g, blocks, marks, st);

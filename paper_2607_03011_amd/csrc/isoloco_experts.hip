@@ -174,7 +174,9 @@ __global__ void __launch_bounds__(64 * kFewWaves, 4) expert_few_kernel(FewArgs g
 //   float32          134 / 716     149 / 721     170 / 718     227 / 729     292 / 739     531 / 761     773 / 952
 //                    13.9 / 50.0   14.2 / 49.2   14.5 / 49.5   20.3 / 50.1   23.4 / 51.4   40.8 / 55.0   58.2 / 60.9
 // bfloat16 weights that the tiles would have copied first (150 us of the first kind) are as
-// float32 in this.
+// float32 in this.  The host knows the mean alone, and the rows above are spread as evenly as they
+// can be: an expert that has most of them is walked by the workgroups of its columns, 16 or 32
+// rows at a time, on a fraction of the card.
 bool few_of(int32_t dtype, int64_t rows, int64_t experts, int64_t cols, bool copies) {
   return rows <= (dtype == ISOLOCO_F32 ? 96 : copies ? 48 : 16) * experts &&
          launchable((experts + 1) * ((cols + 15) / 16), 64 * kFewWaves);
