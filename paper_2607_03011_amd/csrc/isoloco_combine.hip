@@ -139,13 +139,14 @@ __global__ void __launch_bounds__(256) combine_clear_kernel(Index row, int64_t r
   if constexpr (HOW == kFew) mark_rows<256>(row, slots, 0, rows, bits);
   constexpr int N = Vec<T>::N;
   const float zeros[N] = {};
-  const int64_t words = (rows + 31) / 32, from = words * blockIdx.x / gridDim.x, to = words * (blockIdx.x + 1) / gridDim.x;
+  const int64_t pieces = (dim + N - 1) / N, words = (rows + 31) / 32, from = words * blockIdx.x / gridDim.x, to = words * (blockIdx.x + 1) / gridDim.x;
   for (int64_t w = from; w < to; ++w) {
     uint32_t none = ~(HOW == kAll ? 0u : HOW == kFew ? bits[w] : marks[w]);
     if (rows - 32 * w < 32) none &= (1u << (rows - 32 * w)) - 1;
-    for (; none; none &= none - 1) {
-      T* to_row = dy + (32 * w + __ffs(none) - 1) * ld;
-      for (int64_t col = (int64_t)threadIdx.x * N; col < dim; col += 256 * N) store_piece<T>(to_row + col, dim - col, zeros);
+    if (none == 0) continue;
+    for (int64_t i = (int64_t)blockIdx.y * 256 + threadIdx.x; i < 32 * pieces; i += (int64_t)gridDim.y * 256) {
+      const int64_t r = i / pieces, col = (i - r * pieces) * N;
+      if (none >> r & 1u) store_piece<T>(dy + (32 * w + r) * ld + col, dim - col, zeros);
     }
   }
 }
@@ -261,7 +262,10 @@ size_t combine_grad_workspace(int64_t tokens, int32_t top_k) {
 template <typename T>
 void clear_rows(const CombineGradArgs& g, T* dy, uint32_t* marks, hipStream_t st) {
   const int64_t slots = g.tokens * g.top_k, rows = g.rows;
-  const dim3 grid((unsigned)std::min<int64_t>(1024, (rows + 31) / 32));
+  // about 1024 workgroups; where the rows are fewer than those take, some share 32 rows
+  const int64_t words = (rows + 31) / 32, pieces = (g.dim + Vec<T>::N - 1) / Vec<T>::N;
+  const dim3 grid((unsigned)std::min<int64_t>(1024, words),
+                  (unsigned)std::min(std::max<int64_t>(1, 1024 / words), (pieces + 31) / 32));
   if (rows > slots) {
     hipLaunchKernelGGL((combine_clear_kernel<T, kAll>), grid, dim3(256), 0, st, g.row, rows, slots, marks, dy, g.ld_dy, g.dim);
   } else if (slots <= kFewSlots) {
