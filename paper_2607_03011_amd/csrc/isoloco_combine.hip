@@ -306,16 +306,20 @@ isoloco_status check_shape(int32_t dtype, int64_t tokens, int64_t rows, int64_t 
 
 }  // namespace
 
-bool rows_sum_launchable(int64_t tokens, int64_t dim) { return launchable((tokens * ((dim + 3) / 4) + 255) / 256, 256); }
-
 hipError_t launch_rows_sum(const float* y, int64_t rows, int64_t dim, Index row, int64_t tokens, int top_k, bool f32,
                            bool past, void* out, int64_t ld_out, hipStream_t st) {
-  const CombineArgs g = {row, nullptr, tokens, rows, dim, dim, ld_out, top_k};
-  const int64_t pieces = (dim + 3) / 4, blocks = (tokens * pieces + 255) / 256;
-  if (blocks == 0) return hipSuccess;
-  if (f32) run_forward<float>(y, out, g, (int)pieces, blocks, st);
-  else if (past) run_forward<float, __bf16, true>(y, out, g, (int)pieces, blocks, st);
-  else run_forward<float, __bf16>(y, out, g, (int)pieces, blocks, st);
+  // so many tokens as one launch has threads for
+  const int64_t pieces = (dim + 3) / 4, most = ((int64_t)1 << 31) / pieces;
+  const int64_t row_bytes = (int64_t)top_k * (row.wide ? 8 : 4), out_bytes = ld_out * (f32 ? 4 : 2);
+  for (int64_t t = 0; t < tokens; t += most) {
+    const CombineArgs g = {{static_cast<const char*>(row.p) + t * row_bytes, row.wide}, nullptr, std::min(most, tokens - t), rows,
+                           dim, dim, ld_out, top_k};
+    const int64_t blocks = (g.tokens * pieces + 255) / 256;
+    void* to = static_cast<char*>(out) + t * out_bytes;
+    if (f32) run_forward<float>(y, to, g, (int)pieces, blocks, st);
+    else if (past) run_forward<float, __bf16, true>(y, to, g, (int)pieces, blocks, st);
+    else run_forward<float, __bf16>(y, to, g, (int)pieces, blocks, st);
+  }
   return hipGetLastError();
 }
 

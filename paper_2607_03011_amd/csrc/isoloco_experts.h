@@ -53,8 +53,7 @@ size_t expert_gradients_partial_bytes(bool f32, int64_t rows, int64_t experts, i
 hipError_t launch_expert_gradients(bool f32, const ExpertArgs* dx, const ExpertArgs* dw, hipStream_t st);
 
 // out[t] = sum_j y[row[t, j]] of float32 rows of dim, rounded once to out's type (past: the rows lie
-// past the caches), where the elements are not too many for a launch
-bool rows_sum_launchable(int64_t tokens, int64_t dim);
+// past the caches)
 hipError_t launch_rows_sum(const float* y, int64_t rows, int64_t dim, Index row, int64_t tokens, int top_k, bool f32,
                            bool past, void* out, int64_t ld_out, hipStream_t st);
 

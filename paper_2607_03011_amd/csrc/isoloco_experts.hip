@@ -440,7 +440,6 @@ isoloco_status gradients(Gradients g, void* workspace, size_t workspace_bytes, h
     if (!is_index_type(g.row_type)) return fail(ISOLOCO_ERR_INVALID_ARG, "index type of row %d", g.row_type);
     if (g.top_k < 1 || g.top_k > ISOLOCO_MAX_TOP)
       return fail(ISOLOCO_ERR_INVALID_ARG, "top_k = %d, of 1 to %d", g.top_k, ISOLOCO_MAX_TOP);
-    if (!rows_sum_launchable(s.tokens, s.dim)) return fail(ISOLOCO_ERR_UNSUPPORTED, "too many elements for one launch");
   }
   const int64_t dx_rows = g.sum ? s.tokens : s.rows;
   const bool dx = (g.dx || g.sum) && dx_rows;
