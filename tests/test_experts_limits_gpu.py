@@ -333,3 +333,31 @@ def test_route_of_nan_and_infinity(iso, tokens, normalize, dtype):
         assert torch.isnan(d[odd].gather(1, r.expert[odd].long())).all()
     else:
         assert torch.isnan(d[odd]).all()
+
+
+def test_combine_gradient_in_a_graph_follows_its_rows(iso):
+    """Many slots, marked and cleared anew at each replay."""
+    g = gen(4)
+    tokens, rows = 6000, 12000
+    dout, w = randn(g, tokens, 72, dtype=BF16).cuda(), randn(g, tokens, 2).cuda()
+    y = randn(g, rows, 72, dtype=BF16).cuda()
+    kinds = []
+    for drop in (0.0, 0.3, 1.0, 0.0):
+        r = torch.randperm(rows, generator=g).view(tokens, 2)
+        r[torch.rand(tokens, 2, generator=g) < drop] = -1
+        kinds.append(r.int().cuda())
+    row = kinds[0].clone()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        iso.combine_tokens_backward(dout, y, row, w)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        dy, dweight = iso.combine_tokens_backward(dout, y, row, w)
+    for r in kinds * 2:
+        row.copy_(r)
+        dy.fill_(math.nan)
+        graph.replay()
+        torch.cuda.synchronize()
+        want = iso.combine_tokens_backward(dout, y, r, w)
+        assert torch.equal(dy, want[0]) and torch.equal(dweight, want[1])
